@@ -164,7 +164,7 @@ hexgen_status_t hexgen_kv_cache_commit(hexgen_kv_cache_t *kv, const int32_t *seq
 /* dst[i] += src[i] for n fp32 device elements (fixed-order rank sum of the validation driver). */
 hexgen_status_t hexgen_accumulate_f32(void *dst, const void *src, int64_t n, void *stream);
 
-/* Read back / install cache rows as HOST fp32 [n, hkv_local, head_dim] (K after rotation).
+/* Read back / install cache rows as HOST fp32 [n, hkv_local, head_dim] (K after rotation); fill takes device memory as well.
  * Both synchronise.  fill: sets positions 0..n-1 of `seq` in `layer`; when every layer of every
  * sequence of a batch has been filled, call hexgen_kv_cache_set_lengths to declare the context
  * (this also marks the cache "prefilled" and restarts the decode step count at 0).
@@ -175,6 +175,57 @@ hexgen_status_t hexgen_kv_cache_fill(hexgen_kv_cache_t *kv, int layer, int seq, 
                                      const float *k, const float *v);
 hexgen_status_t hexgen_kv_cache_set_lengths(hexgen_kv_cache_t *kv, const int32_t *lens, int batch);
 hexgen_status_t hexgen_kv_cache_get_lengths(hexgen_kv_cache_t *kv, int32_t *lens_out, int batch);
+
+/* ---- drafted trees (speculative decoding) --------------------------------------------------------------------
+ * A step of speculative decoding takes, per sequence, a tree of drafted tokens through the model at once and keeps the path that the
+ * model agrees with.  Node 0 of a sequence's tree is its root -- the token that is certain already, but not in the cache yet -- and
+ * every other node continues its parent.  With len_i the committed length of sequence i, node x of depth d(x) (root: 0) stands at
+ * position len_i + d(x) (its rotary angle), its keys and values go to cache slot len_i + x, uncommitted, and it attends the context,
+ * its ancestors and itself.  A sequence whose tree has no node sits the step out; one node is an ordinary decode step.
+ *
+ *   hexgen_tree_create: room for trees of up to max_batch sequences and max_rows nodes in all.  Allocates no device memory.
+ *   hexgen_tree_set: HOST counts[batch], 0 .. HEXGEN_TREE_MAX_NODES nodes per sequence, and HOST parents[sum of counts], packed
+ *     sequence by sequence: -1 for a tree's node 0, else a smaller index of the same tree (HEXGEN_ERR_SHAPE otherwise, or when there is no
+ *     node at all; HEXGEN_ERR_CAPACITY beyond max_batch, max_rows or HEXGEN_TREE_MAX_NODES; the former trees stay then).  The arrays may
+ *     be changed when it returns.  The copy to the device runs on `stream`, calls that use the trees on other streams have to be
+ *     put behind it by the caller; it cannot be recorded into a graph (HEXGEN_ERR_DEVICE).
+ *   hexgen_tree_accept: greedy acceptance.  draft, chosen: device int32 [rows], the drafted token of every node and the token the model
+ *     chooses behind it (hexgen_head_greedy's token_out over the rows of hexgen_stage_decode_tree).  From the root on, a child whose
+ *     drafted token is its parent's chosen one is taken, the first of several.  Device int32 outputs: kept[batch] = length of the path (0
+ *     without nodes), path[rows] = its nodes and tokens[rows] = their chosen tokens, each sequence's at the place of its rows and
+ *     filled up with -1.  tokens are the sequence's kept[i] new tokens, the last of which is the next tree's root.
+ *     Enqueues on `stream`; HEXGEN_ERR_STATE before hexgen_tree_set.
+ */
+#define HEXGEN_TREE_MAX_NODES 256
+typedef struct hexgen_tree hexgen_tree_t;          /* opaque, library-owned */
+hexgen_status_t hexgen_tree_create(int max_batch, int max_rows, hexgen_tree_t **out);
+void            hexgen_tree_destroy(hexgen_tree_t *tr);
+hexgen_status_t hexgen_tree_set(hexgen_tree_t *tr, const int32_t *counts, const int32_t *parents, int batch, void *stream);
+hexgen_status_t hexgen_tree_accept(const hexgen_tree_t *tr, const int32_t *draft, const int32_t *chosen, int32_t *kept,
+                                   int32_t *path, int32_t *tokens, void *stream);
+
+/* hexgen_stage_decode_tree: the trees' rows through every layer of the stage.  hidden_in, out_partial, out_resid as for prefill, one
+ * row per node.  The committed lengths and the decode steps' count do not change, so the call may be repeated.
+ * hexgen_kv_tree_attention: one layer's attention alone, for callers with projections of their own.  Device pointers, dtype, one row per
+ * node: q [rows, hq_local, d] and k [rows, hkv_local, d] rotated at the nodes' positions, v [rows, hkv_local, d]; rows are ldq, ldk and ldv
+ * elements apart (multiples of 8 for 16-bit types, of 4 for fp32, and 16-byte aligned pointers: HEXGEN_ERR_INVALID_ARG otherwise), so
+ * that they may be parts of one fused projection.  out [rows, hq_local, d], dense, 16-byte aligned, apart from the inputs.  k and v join `layer`'s
+ * cache as above.  What a node does not attend has no influence on its row, infinities and NaN included.
+ * hexgen_kv_cache_keep: HOST kept[batch] and HOST path[rows] as hexgen_tree_accept lays them out, from that call or from another rule of
+ * acceptance: the rows of every path (root first, each node a child of the one before it: HEXGEN_ERR_SHAPE otherwise; kept[i] = 0
+ * drops the whole tree) move to the slots behind the context, in every layer, and the committed lengths grow by kept[i].  The
+ * arrays may be changed when it returns; it enqueues on `stream` and cannot be recorded into a graph (HEXGEN_ERR_DEVICE).
+ * All three: HEXGEN_ERR_STATE unless the cache holds a batch (prefill, set_lengths, commit) and the trees are set for just as many
+ * sequences; HEXGEN_ERR_CAPACITY when a context and its tree exceed max_seq.  hexgen_stage_decode_tree and
+ * hexgen_kv_tree_attention can be recorded once a call of that size has run outside a graph; they read lengths and
+ * trees from the device when replayed.
+ */
+hexgen_status_t hexgen_stage_decode_tree(hexgen_stage_t *st, hexgen_kv_cache_t *kv, const hexgen_tree_t *tr, const void *hidden_in,
+                                         void *out_partial, void *out_resid, void *stream);
+hexgen_status_t hexgen_kv_tree_attention(hexgen_kv_cache_t *kv, int layer, const hexgen_tree_t *tr, const void *q, int64_t ldq,
+                                         const void *k, int64_t ldk, const void *v, int64_t ldv, void *out, void *stream);
+hexgen_status_t hexgen_kv_cache_keep(hexgen_kv_cache_t *kv, hexgen_tree_t *tr, const int32_t *kept, const int32_t *path,
+                                     void *stream);
 
 /* Debug tap: at the entry of `layer` during prefill / decode, the fp32 residual stream
  * [rows, hidden] is copied to `h_dump` (device).  NULL removes the tap.

@@ -45,6 +45,13 @@ SIGNATURES = {
     "hexgen_kv_cache_set_lengths": (_i, [_vp, _ip, _i]),
     "hexgen_kv_cache_get_lengths": (_i, [_vp, _ip, _i]),
     "hexgen_stage_set_tap": (_i, [_vp, _i, _vp]),
+    "hexgen_tree_create": (_i, [_i, _i, C.POINTER(_vp)]),
+    "hexgen_tree_destroy": (None, [_vp]),
+    "hexgen_tree_set": (_i, [_vp, _ip, _ip, _i, _vp]),
+    "hexgen_tree_accept": (_i, [_vp] * 7),
+    "hexgen_stage_decode_tree": (_i, [_vp] * 7),
+    "hexgen_kv_tree_attention": (_i, [_vp, _i, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]),
+    "hexgen_kv_cache_keep": (_i, [_vp, _vp, _ip, _ip, _vp]),
     "hexgen_stage_weight_bytes": (_i64, [_vp]),
     "hexgen_stream_copy": (_i, [_vp, _vp, _i64, _i, _vp]),
     "hexgen_stream_read": (_i, [_vp, _vp, _i64, _i, _vp]),
@@ -125,6 +132,37 @@ def _stream_handle(stream: Optional[torch.cuda.Stream]) -> Optional[int]:
     return s.cuda_stream or None
 
 
+def _empty(shape, dtype, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """A result of a call on `stream`, taken from that stream's memory."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device="cuda")
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device="cuda")
+
+
+def _device_tensor(t: torch.Tensor, name: str, shape, dtype) -> torch.Tensor:
+    """A tensor that is handed on as a dense device pointer: checked here, where its shape, type and place are known."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {tuple(shape)} tensor of {dtype} is wanted, got {tuple(t.shape)} of {t.dtype}, strides {tuple(t.stride())}")
+    return _on_device(t, name)
+
+
+def _on_device(t: torch.Tensor, name: str) -> torch.Tensor:
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, not on the current GPU")
+    return t
+
+
+def _rows_of_heads(t: torch.Tensor, name: str, rows: int, heads: int, d: int, dtype) -> int:
+    """Elements between the rows of a [rows, heads, d] or [rows, heads * d] tensor whose rows are dense."""
+    if tuple(t.shape) not in ((rows, heads, d), (rows, heads * d)) or t.dtype != dtype:
+        raise ValueError(f"{name}: a ({rows}, {heads}, {d}) tensor of {dtype} is wanted, got {tuple(t.shape)} of {t.dtype}")
+    if t.stride(-1) != 1 or (t.dim() == 3 and heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{name}: the elements of a row have to be dense, got strides {tuple(t.stride())}")
+    _on_device(t, name)
+    return t.stride(0) if rows > 1 else heads * d
+
+
 def _torch_dtype(dtype: int):
     return {HEXGEN_F32: torch.float32, HEXGEN_BF16: torch.bfloat16, HEXGEN_F16: torch.float16}[dtype]
 
@@ -149,7 +187,7 @@ class Stage:
         self.handle = h
         self.hidden, self.n_layers = hidden, n_layers
         self.head_dim = hidden // n_heads
-        self.hkv_l = n_kv_heads // tp_degree
+        self.hq_l, self.hkv_l = n_heads // tp_degree, n_kv_heads // tp_degree
         _check(lib.hexgen_stage_set_params(self.handle, rms_eps, rope_theta), "hexgen_stage_set_params")
         self._taps = {}
 
@@ -187,6 +225,16 @@ class Stage:
         """hexgen_stage_decode_static: the decode step for callers that cannot allocate."""
         _check(lib.hexgen_stage_decode_static(self.handle, kv.handle, step, _ptr(hidden_in), _ptr(out_partial),
                                               _ptr(out_resid), _stream_handle(stream)), "hexgen_stage_decode_static")
+
+    def decode_tree(self, kv: "KVCache", tree: "Tree", hidden_in: torch.Tensor, out_partial: torch.Tensor,
+                    out_resid: Optional[torch.Tensor] = None, stream=None):
+        """hexgen_stage_decode_tree: the drafted trees' rows through every layer; the committed lengths stay."""
+        shape, td = (tree.rows, self.hidden), _torch_dtype(self.dtype)
+        for name, t in (("hidden_in", hidden_in), ("out_partial", out_partial), ("out_resid", out_resid)):
+            if t is not None:
+                _device_tensor(t, name, shape, td)
+        _check(lib.hexgen_stage_decode_tree(self.handle, kv.handle, tree.handle, _ptr(hidden_in), _ptr(out_partial),
+                                            _ptr(out_resid), _stream_handle(stream)), "hexgen_stage_decode_tree")
 
     def decode_static_bytes(self, batch: int) -> int:
         return int(lib.hexgen_stage_decode_static_bytes(self.handle, batch))
@@ -256,9 +304,9 @@ class KVCache:
         return list(out)
 
     def fill(self, layer: int, seq: int, k: torch.Tensor, v: torch.Tensor):
-        """k, v: host fp32 [n, hkv_local, head_dim]."""
-        k = k.to(torch.float32).contiguous().cpu()
-        v = v.to(torch.float32).contiguous().cpu()
+        """k, v: [n, hkv_local, head_dim], host or device, taken as fp32."""
+        k = k.to(torch.float32).contiguous()
+        v = v.to(torch.float32).contiguous()
         _check(lib.hexgen_kv_cache_fill(self.handle, layer, seq, k.shape[0],
                                         C.cast(k.data_ptr(), _fp), C.cast(v.data_ptr(), _fp)), "hexgen_kv_cache_fill")
 
@@ -269,6 +317,65 @@ class KVCache:
         _check(lib.hexgen_kv_cache_read(self.handle, layer, seq, pos0, n, C.cast(k.data_ptr(), _fp),
                                         C.cast(v.data_ptr(), _fp)), "hexgen_kv_cache_read")
         return k, v
+
+
+    def tree_attention(self, layer: int, tree: "Tree", q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                       out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """hexgen_kv_tree_attention: q [rows, hq_local, head_dim], k, v [rows, hkv_local, head_dim] of the trees' nodes, rotated; rows may
+        be apart (parts of a fused projection).  Returns [rows, hq_local, head_dim]."""
+        st, rows, td = self.stage, tree.rows, _torch_dtype(self.stage.dtype)
+        ldq = _rows_of_heads(q, "q", rows, st.hq_l, st.head_dim, td)
+        ldk = _rows_of_heads(k, "k", rows, st.hkv_l, st.head_dim, td)
+        ldv = _rows_of_heads(v, "v", rows, st.hkv_l, st.head_dim, td)
+        if out is None:
+            out = _empty((rows, st.hq_l, st.head_dim), td, stream)
+        else:
+            _device_tensor(out, "out", (rows, st.hq_l, st.head_dim), td)
+        _check(lib.hexgen_kv_tree_attention(self.handle, layer, tree.handle, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
+                                            out.data_ptr(), _stream_handle(stream)), "hexgen_kv_tree_attention")
+        return out
+
+    def keep(self, tree: "Tree", kept: Sequence[int], path: Sequence[int], stream=None):
+        """hexgen_kv_cache_keep: HOST kept[batch] and path[rows], e.g. the lists of what Tree.accept returned."""
+        kept, path = [int(x) for x in kept], [int(x) for x in path]
+        if len(kept) != tree.batch or len(path) != tree.rows:
+            raise ValueError(f"keep: {tree.batch} counts and {tree.rows} path entries are wanted, got {len(kept)} and {len(path)}")
+        _check(lib.hexgen_kv_cache_keep(self.handle, tree.handle, _i32(kept), _i32(path), _stream_handle(stream)), "hexgen_kv_cache_keep")
+
+
+class Tree:
+    """Owns a hexgen_tree_t: the drafted trees of a batch, up to max_rows nodes in all."""
+
+    def __init__(self, max_batch: int, max_rows: int):
+        h = C.c_void_p()
+        _check(lib.hexgen_tree_create(max_batch, max_rows, C.byref(h)), "hexgen_tree_create")
+        self.handle, self.batch, self.rows = h, 0, 0
+
+    def close(self, _lib=lib):
+        if getattr(self, "handle", None):
+            _lib.hexgen_tree_destroy(self.handle)
+            self.handle = None
+
+    __del__ = close
+
+    def set(self, counts: Sequence[int], parents: Sequence[int], stream=None):
+        """counts[batch] nodes per sequence; parents of all nodes, packed: -1 for a tree's node 0, else a smaller index of that tree."""
+        counts, parents = [int(x) for x in counts], [int(x) for x in parents]
+        if any(x >= 0 for x in counts) and sum(x for x in counts if x > 0) != len(parents):
+            raise ValueError(f"set: {len(parents)} parents for trees of {sum(counts)} nodes")
+        # (one entry too many: an empty list has no address of its own)
+        _check(lib.hexgen_tree_set(self.handle, _i32(counts + [0]), _i32(parents + [0]), len(counts),
+                                   _stream_handle(stream) if torch.cuda.is_available() else None), "hexgen_tree_set")
+        self.batch, self.rows = len(counts), len(parents)
+
+    def accept(self, draft: torch.Tensor, chosen: torch.Tensor, stream=None):
+        """hexgen_tree_accept: draft, chosen int32 [rows] -> (kept [batch], path [rows], tokens [rows]), int32 on the device."""
+        for name, t in (("draft", draft), ("chosen", chosen)):
+            _device_tensor(t, name, (self.rows,), torch.int32)
+        kept, path, tokens = (_empty((n,), torch.int32, stream) for n in (self.batch, self.rows, self.rows))
+        _check(lib.hexgen_tree_accept(self.handle, _ptr(draft), _ptr(chosen), _ptr(kept), _ptr(path), _ptr(tokens), _stream_handle(stream)),
+               "hexgen_tree_accept")
+        return kept, path, tokens
 
 
 def stream_copy(dst: torch.Tensor, src: torch.Tensor, blocks: int = 4096, stream=None):

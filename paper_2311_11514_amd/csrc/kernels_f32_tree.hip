@@ -1,0 +1,331 @@
+// Attention of drafted trees over the cache, fp32 stages (cache [seq][kv head][smax][d]), and what does not depend on the type: acceptance.
+#include "kernels.h"
+
+#define NEG_INF (-INFINITY)
+
+namespace {
+
+__device__ __forceinline__ floatx4 mfma_f32(float a, float b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
+// rows of a user's projection -> cache slots len + index, four elements of one head of K and of V per thread
+__global__ __launch_bounds__(256) void f32_tree_append_kernel(const float *__restrict__ k, int64_t ldk, const float *__restrict__ v, int64_t ldv,
+                                                              float *__restrict__ kc, float *__restrict__ vc, KvGeom kg, TreeView tv,
+                                                              const int32_t *__restrict__ lens) {
+    const int per_row = kg.hkv_l * kg.d / 4, idx = blockIdx.x * 256 + threadIdx.x;
+    if (idx >= tv.rows * per_row) return;
+    const int t = idx / per_row, e = (idx - t * per_row) * 4, c = e / kg.d, dd = e - c * kg.d;
+    const TreeRow row = tv.row[t];
+    const int slot = lens[row.seq] + row.index;
+    if (slot >= kg.smax) return;
+    const size_t at = (size_t)row.seq * kg.seq_stride + ((size_t)c * kg.smax + slot) * kg.d + dd;
+    *reinterpret_cast<floatx4 *>(kc + at) = *reinterpret_cast<const floatx4 *>(k + (size_t)t * ldk + e);
+    *reinterpret_cast<floatx4 *>(vc + at) = *reinterpret_cast<const floatx4 *>(v + (size_t)t * ldv + e);
+}
+
+// raw projection [rows][(hq + 2 hkv) d] -> rotary embedding at len + depth, q as plain rows, k and v into the cache; a rotary pair per thread
+__global__ __launch_bounds__(256) void f32_tree_rope_append_kernel(const float *__restrict__ qkv, int hq_l, KvGeom kg, TreeView tv,
+                                                                   const int32_t *__restrict__ lens, const float *__restrict__ cos_tab,
+                                                                   const float *__restrict__ sin_tab, float *__restrict__ q,
+                                                                   float *__restrict__ kc, float *__restrict__ vc) {
+    const int d = kg.d, half = d >> 1, heads = hq_l + 2 * kg.hkv_l, idx = blockIdx.x * 256 + threadIdx.x;
+    if (idx >= tv.rows * heads * half) return;
+    const int t = idx / (heads * half), rem = idx - t * heads * half, head = rem / half, i = rem - head * half;
+    const TreeRow row = tv.row[t];
+    const int len = lens[row.seq], slot = len + row.index;
+    if (slot >= kg.smax) return;
+    const float *src = qkv + (size_t)t * heads * d + (size_t)head * d + i;
+    float lo = src[0], hi = src[half];
+    if (head < hq_l + kg.hkv_l) {
+        const size_t at = (size_t)(len + row.depth) * half + i;
+        const float c = cos_tab[at], sn = sin_tab[at], l = lo * c - hi * sn;
+        hi = hi * c + lo * sn;
+        lo = l;
+    }
+    const size_t slab = (size_t)row.seq * kg.seq_stride;
+    float *dst = head < hq_l ? q + ((size_t)t * hq_l + head) * d
+                 : head < hq_l + kg.hkv_l ? kc + slab + ((size_t)(head - hq_l) * kg.smax + slot) * d
+                                          : vc + slab + ((size_t)(head - hq_l - kg.hkv_l) * kg.smax + slot) * d;
+    dst[i] = lo;
+    dst[half + i] = hi;
+}
+
+// A block takes 16 query columns of one (sequence, kv head) -- column j: node j / G, head j % G -- and a run of 16-position tiles, over
+// which its W waves interleave; the products and register layouts are those of the stage's fp32 attention (v_mfma_f32_16x16x4_f32, a
+// lane owns column l % 16 and positions 4 (l / 16) + r, P stays in registers).  Masks, runs and the way of values that are not finite as in
+// the 16-bit kernel.  Bound by the fp32 matrix instructions, 32 cycles for 4 KB of K or V, and by the one round trip per tile and wave.
+template <int D, int W>
+__global__ __launch_bounds__(64 * W) void f32_tree_attn_kernel(const float *__restrict__ q, int64_t ldq, const float *__restrict__ kc,
+                                                               const float *__restrict__ vc, KvGeom kg, int hq_l, int G, int nrb, TreeView tv,
+                                                               const int32_t *__restrict__ lens, TreeSplit sp, float *__restrict__ o) {
+    constexpr int KT = D / 16, VH = D / 64;
+    __shared__ float s_m[W][16], s_l[W][16];
+    __shared__ __align__(16) float s_o[W][16][D];
+    const int slot = blockIdx.x >> 3, rb = slot % nrb;
+    int combo = (slot / nrb) * 8 + (blockIdx.x & 7);
+    if (combo >= tv.batch * kg.hkv_l * sp.nsplit) return;
+    const int split = combo % sp.nsplit;
+    combo /= sp.nsplit;
+    const int c = combo % kg.hkv_l, seq = combo / kg.hkv_l;
+    const int row0 = tv.cu[seq], n = tv.cu[seq + 1] - row0, R = n * G;
+    if (rb * 16 >= R) return;
+    const int len = lens[seq], last = min(len + n, kg.smax) - 1, nt = (last + 32) >> 5;      // runs count 32 positions, as for 16 bits
+    const int per = max(sp.chunk, (nt + sp.nsplit - 1) / sp.nsplit), t0 = split * per;
+    if (t0 >= nt) return;
+    const int t1 = min(2 * (t0 + per), (last >> 4) + 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    const int rr = min(rb * 16 + i, R - 1), node = rr / G, head = c * G + (rr - node * G);
+    const uint32_t *mask = tv.mask + (size_t)(row0 + node) * tv.mask_words;
+    const size_t slab = (size_t)seq * kg.seq_stride + (size_t)c * kg.smax * D;
+    const float *K = kc + slab, *V = vc + slab;
+    floatx4 qf[KT];
+#pragma unroll
+    for (int k = 0; k < KT; ++k) qf[k] = *reinterpret_cast<const floatx4 *>(q + (size_t)(row0 + node) * ldq + (size_t)head * D + 16 * k + 4 * g);
+    const float scale = 1.0f / sqrtf((float)D);
+    floatx4 oacc[VH][4];
+#pragma unroll
+    for (int h = 0; h < VH; ++h)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) oacc[h][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+    float m = NEG_INF, lsum = 0.f;
+    for (int t = 2 * t0 + wave; t < t1; t += W) {
+        floatx4 kf[KT], vf[4][VH];
+#pragma unroll
+        for (int k = 0; k < KT; ++k) kf[k] = *reinterpret_cast<const floatx4 *>(K + (size_t)min(16 * t + i, last) * D + 16 * k + 4 * g);
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int h = 0; h < VH; ++h) vf[x][h] = *reinterpret_cast<const floatx4 *>(V + (size_t)min(16 * t + 4 * g + x, last) * D + 64 * h + 4 * i);
+        floatx4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) s = mfma_f32(kf[k][x], qf[k][x], s);
+        const bool masked = 16 * t + 15 >= len;
+        uint32_t sees = 0xffffu;                              // of the tile's 16 positions
+        if (masked) {
+            const int rel = 16 * t - len;
+            if (rel < 0) {
+                sees = (mask[0] << -rel) | ((1u << -rel) - 1);
+            } else {
+                const int w = rel >> 5, sh = rel & 31;
+                const uint32_t a = w < tv.mask_words ? mask[w] : 0u, b = w + 1 < tv.mask_words ? mask[w + 1] : 0u;
+                sees = sh == 0 ? a : (a >> sh) | (b << (32 - sh));
+            }
+        }
+        float mx = NEG_INF;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            s[r] = (sees >> (4 * g + r)) & 1u ? s[r] * scale : NEG_INF;
+            mx = fmaxf(mx, s[r]);
+        }
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float m_new = fmaxf(m, mx), base = m_new == NEG_INF ? 0.f : m_new, alpha = expf(m - base);
+        m = m_new;
+        float ps = 0.f, pr[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            pr[r] = expf(s[r] - base);
+            ps += pr[r];
+        }
+        lsum = lsum * alpha + ps;
+#pragma unroll
+        for (int h = 0; h < VH; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) oacc[h][e] *= alpha;
+        bool odd = false;
+        if (masked) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int h = 0; h < VH; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) odd = odd || !(fabsf(vf[x][h][e]) < INFINITY);
+        }
+        if (__builtin_amdgcn_ballot_w64(odd) == 0) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int h = 0; h < VH; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) oacc[h][e] = mfma_f32(vf[x][h][e], pr[x], oacc[h][e]);
+        } else {
+            for (int pp = 0; pp < 16; ++pp) {
+                const int src = i + 16 * (pp >> 2);
+                const float w0 = __shfl(pr[0], src, 64), w1 = __shfl(pr[1], src, 64), w2 = __shfl(pr[2], src, 64), w3 = __shfl(pr[3], src, 64);
+                const float w = (pp & 3) == 0 ? w0 : (pp & 3) == 1 ? w1 : (pp & 3) == 2 ? w2 : w3;
+                if (!((sees >> pp) & 1u)) continue;
+#pragma unroll
+                for (int h = 0; h < VH; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            oacc[h][e][r] = fmaf(w, V[(size_t)min(16 * t + pp, last) * D + 64 * h + 4 * (4 * g + r) + e], oacc[h][e][r]);
+            }
+        }
+    }
+    lsum += __shfl_xor(lsum, 16, 64);
+    lsum += __shfl_xor(lsum, 32, 64);
+    if (g == 0) { s_m[wave][i] = m; s_l[wave][i] = lsum; }
+    // register r of oacc[h][e]: head element 64 h + 4 (4 g + r) + e of column i
+#pragma unroll
+    for (int h = 0; h < VH; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            *reinterpret_cast<floatx4 *>(&s_o[wave][i][64 * h + 16 * g + 4 * r]) = floatx4{oacc[h][0][r], oacc[h][1][r], oacc[h][2][r], oacc[h][3][r]};
+    __syncthreads();
+    const int nb = (nt + per - 1) / per;
+    const size_t part_row = (size_t)tv.rows * hq_l;
+    for (int idx = threadIdx.x * 4; idx < 16 * D; idx += 64 * W * 4) {
+        const int j = idx / D, dd = idx % D, at = rb * 16 + j;
+        if (at >= R) break;
+        float M = NEG_INF, L = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) M = fmaxf(M, s_m[w][j]);
+        const float b = M == NEG_INF ? 0.f : M;
+        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float wt = expf(s_m[w][j] - b);
+            L += s_l[w][j] * wt;
+            acc += *reinterpret_cast<const floatx4 *>(&s_o[w][j][dd]) * wt;
+        }
+        const size_t e = (size_t)(row0 + at / G) * hq_l + c * G + at % G;
+        if (nb == 1) {
+            *reinterpret_cast<floatx4 *>(o + e * D + dd) = acc / L;
+        } else {
+            *reinterpret_cast<floatx4 *>(sp.part_o + (split * part_row + e) * D + dd) = acc;
+            if (dd == 0) *reinterpret_cast<float2 *>(sp.part_ml + 2 * (split * part_row + e)) = float2{M, L};
+        }
+    }
+}
+
+// joins the runs of every (row, head), D / 4 threads each
+template <int D>
+__global__ __launch_bounds__(256) void f32_tree_merge_kernel(KvGeom kg, int hq_l, TreeView tv, const int32_t *__restrict__ lens, TreeSplit sp,
+                                                             float *__restrict__ o) {
+    constexpr int TP = D / 4;
+    const int e = blockIdx.x * (256 / TP) + threadIdx.x / TP, dd = 4 * (threadIdx.x % TP);
+    if (e >= tv.rows * hq_l) return;
+    const int t = e / hq_l, seq = tv.row[t].seq, n = tv.cu[seq + 1] - tv.cu[seq];
+    const int nt = (min(lens[seq] + n, kg.smax) + 31) >> 5, per = max(sp.chunk, (nt + sp.nsplit - 1) / sp.nsplit), nb = (nt + per - 1) / per;
+    if (nb <= 1) return;
+    const size_t part_row = (size_t)tv.rows * hq_l;
+    float M = NEG_INF, L = 0.f;
+    for (int u = 0; u < nb; ++u) M = fmaxf(M, sp.part_ml[2 * (u * part_row + e)]);
+    const float b = M == NEG_INF ? 0.f : M;
+    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < nb; ++u) {
+        const float2 ml = *reinterpret_cast<const float2 *>(sp.part_ml + 2 * (u * part_row + e));
+        const float wt = expf(ml.x - b);
+        L += ml.y * wt;
+        acc += *reinterpret_cast<const floatx4 *>(sp.part_o + (u * part_row + e) * D + dd) * wt;
+    }
+    *reinterpret_cast<floatx4 *>(o + (size_t)e * D + dd) = acc / L;
+}
+
+// slot len + path[j] -> len + j in every layer, one element of K and V per thread (see the 16-bit kernel for the order)
+__global__ __launch_bounds__(256) void f32_tree_keep_kernel(float *__restrict__ kc, float *__restrict__ vc, int64_t layer_stride, KvGeom kg,
+                                                            const int32_t *__restrict__ lens, const int32_t *__restrict__ cu,
+                                                            const int32_t *__restrict__ kept, const int32_t *__restrict__ path) {
+    const int seq = blockIdx.y, dd = (blockIdx.x * 256 + threadIdx.x) % kg.d, c = (blockIdx.x * 256 + threadIdx.x) / kg.d;
+    const int n = kept[seq], len = lens[seq], row0 = cu[seq];
+    if (c >= kg.hkv_l || len + n > kg.smax) return;
+    const size_t slab = (size_t)blockIdx.z * layer_stride + (size_t)seq * kg.seq_stride + (size_t)c * kg.smax * kg.d + dd;
+    float *ks = kc + slab, *vs = vc + slab;
+    for (int j0 = 1; j0 < n; j0 += 8) {
+        float a[8], b[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const size_t src = (size_t)(len + path[row0 + min(j0 + i, n - 1)]) * kg.d;
+            a[i] = ks[src];
+            b[i] = vs[src];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (j0 + i < n) {
+                ks[(size_t)(len + j0 + i) * kg.d] = a[i];
+                vs[(size_t)(len + j0 + i) * kg.d] = b[i];
+            }
+    }
+}
+
+__global__ void tree_advance_kernel(int32_t *__restrict__ lens, const int32_t *__restrict__ kept, int batch) {
+    const int i = blockIdx.x * 64 + threadIdx.x;
+    if (i < batch) lens[i] += kept[i];
+}
+
+// One wave per sequence walks its tree: the 64 lanes look at four nodes each for the first child of the current node whose drafted
+// token is the chosen one.  Bound by latency: a step is a ballot and two reads of LDS.
+__global__ __launch_bounds__(64) void tree_accept_kernel(TreeView tv, const int32_t *__restrict__ draft, const int32_t *__restrict__ chosen,
+                                                         int32_t *__restrict__ kept, int32_t *__restrict__ path, int32_t *__restrict__ tokens) {
+    constexpr int PL = kTreeMaxNodes / 64;
+    __shared__ int32_t s_chosen[kTreeMaxNodes];
+    const int seq = blockIdx.x, lane = threadIdx.x, row0 = tv.cu[seq], n = tv.cu[seq + 1] - row0;
+    int parent[PL], token[PL];
+#pragma unroll
+    for (int i = 0; i < PL; ++i) {
+        const int x = 64 * i + lane;
+        parent[i] = -2;                                       // no node: nobody's child
+        token[i] = 0;
+        if (x < n) {
+            parent[i] = tv.row[row0 + x].parent;
+            token[i] = draft[row0 + x];
+            s_chosen[x] = chosen[row0 + x];
+        }
+    }
+    __syncthreads();
+    int count = 0, at = n > 0 ? 0 : -1;
+    while (at >= 0) {
+        const int want = s_chosen[at];
+        if (lane == 0) { path[row0 + count] = at; tokens[row0 + count] = want; }
+        ++count;
+        int next = -1;
+#pragma unroll
+        for (int i = 0; i < PL; ++i) {
+            if (64 * i >= n) break;
+            const unsigned long long hit = __builtin_amdgcn_ballot_w64(parent[i] == at && token[i] == want);
+            if (next < 0 && hit != 0) next = 64 * i + __builtin_ctzll(hit);
+        }
+        at = next;                                            // children have larger indexes than their parents: the walk ends
+    }
+    for (int x = count + lane; x < n; x += 64) { path[row0 + x] = -1; tokens[row0 + x] = -1; }
+    if (lane == 0) kept[seq] = count;
+}
+
+}  // namespace
+
+void launch_tree_accept(const TreeView &tv, const int32_t *draft, const int32_t *chosen, int32_t *kept, int32_t *path, int32_t *tokens, hipStream_t s) {
+    hipLaunchKernelGGL(tree_accept_kernel, dim3(tv.batch), dim3(64), 0, s, tv, draft, chosen, kept, path, tokens);
+}
+void launch_tree_advance(int32_t *lens, const int32_t *kept, int batch, hipStream_t s) {
+    hipLaunchKernelGGL(tree_advance_kernel, dim3((batch + 63) / 64), dim3(64), 0, s, lens, kept, batch);
+}
+void f32_launch_tree_append(const float *k, int64_t ldk, const float *v, int64_t ldv, float *kc, float *vc, KvGeom kg, const TreeView &tv,
+                            const int32_t *lens, hipStream_t s) {
+    const int n = tv.rows * (kg.hkv_l * kg.d / 4);
+    hipLaunchKernelGGL(f32_tree_append_kernel, dim3((n + 255) / 256), dim3(256), 0, s, k, ldk, v, ldv, kc, vc, kg, tv, lens);
+}
+void f32_launch_tree_rope_append(const float *qkv, int hq_l, KvGeom kg, const TreeView &tv, const int32_t *lens, const float *cos_tab,
+                                 const float *sin_tab, float *q, float *kc, float *vc, hipStream_t s) {
+    const int n = tv.rows * (hq_l + 2 * kg.hkv_l) * (kg.d / 2);
+    hipLaunchKernelGGL(f32_tree_rope_append_kernel, dim3((n + 255) / 256), dim3(256), 0, s, qkv, hq_l, kg, tv, lens, cos_tab, sin_tab, q, kc, vc);
+}
+void f32_launch_tree_attn(const float *q, int64_t ldq, const float *kc, const float *vc, KvGeom kg, int hq_l, const TreeView &tv,
+                          const int32_t *lens, const TreeSplit &sp, float *o, hipStream_t s) {
+    const int G = hq_l / kg.hkv_l, nrb = (tv.max_n * G + 15) / 16;
+    const dim3 grid((unsigned)nrb * (unsigned)((tv.batch * kg.hkv_l * sp.nsplit + 7) / 8 * 8));
+    if (kg.d == 128) hipLaunchKernelGGL((f32_tree_attn_kernel<128, 4>), grid, dim3(256), 0, s, q, ldq, kc, vc, kg, hq_l, G, nrb, tv, lens, sp, o);
+    else hipLaunchKernelGGL((f32_tree_attn_kernel<64, 4>), grid, dim3(256), 0, s, q, ldq, kc, vc, kg, hq_l, G, nrb, tv, lens, sp, o);
+    if (sp.nsplit <= 1) return;
+    if (kg.d == 128) hipLaunchKernelGGL(f32_tree_merge_kernel<128>, dim3((tv.rows * hq_l + 7) / 8), dim3(256), 0, s, kg, hq_l, tv, lens, sp, o);
+    else hipLaunchKernelGGL(f32_tree_merge_kernel<64>, dim3((tv.rows * hq_l + 15) / 16), dim3(256), 0, s, kg, hq_l, tv, lens, sp, o);
+}
+void f32_launch_tree_keep(float *kc, float *vc, int64_t layer_stride, int layers, KvGeom kg, int batch, const int32_t *lens, const int32_t *cu,
+                          const int32_t *kept, const int32_t *path, hipStream_t s) {
+    for (int l0 = 0; l0 < layers; l0 += 65535) {
+        const dim3 grid((kg.hkv_l * kg.d + 255) / 256, batch, layers - l0 < 65535 ? layers - l0 : 65535);
+        hipLaunchKernelGGL(f32_tree_keep_kernel, grid, dim3(256), 0, s, kc + l0 * layer_stride, vc + l0 * layer_stride, layer_stride, kg, lens, cu, kept, path);
+    }
+}

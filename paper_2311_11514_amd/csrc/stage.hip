@@ -85,6 +85,7 @@ struct Workspace {
     float *ssq_pf = nullptr;                    // prefill: 2 x [H/128][T] sums of squares
     // fp32 path: raw QKV projection, normalised rows (more than 32 rows only), rotated q, attention output, SwiGLU output
     float *qkv32 = nullptr, *n32 = nullptr, *q32 = nullptr, *o32 = nullptr, *u32 = nullptr;
+    float *tree_qkv = nullptr;       // 16 bits, from the first decode_tree on: the trees' raw QKV projection, cap_rows rows
     // row bookkeeping
     int32_t *rowmap = nullptr;       // one block: row_seq | row_pos | cu_rows | pos0, packed by the sizes of the call
     int32_t *row_seq = nullptr, *row_pos = nullptr, *cu_rows = nullptr, *pos0 = nullptr;   // views into rowmap
@@ -112,6 +113,7 @@ struct hexgen_stage {
     size_t dec_part_row = 0;         // 16 bits: most floats per row of the split decode projections' partial sums (dec_part_floats)
     int last_decode_rows = 0;        // rows of the last decode call that ran on the weight-streaming kernels
     int ws_batch_cap = 0;
+    float *tree_part = nullptr;      // from the first tree call on: partial results of contexts cut into runs, kTreePartFloats
     int64_t weight_bytes = 0;
     Profiler prof;
 };
@@ -130,7 +132,28 @@ struct hexgen_kv_cache {
     int steps = 0;
 };
 
+struct hexgen_tree {
+    int max_batch, max_rows;
+    int batch = 0, rows = 0, max_n = 0, mask_words = 1;      // of the trees that are set; batch 0: none yet
+    std::vector<int32_t> cu, parents;                         // host copy
+    // device: cu | rows (TreeRow) | masks | kept | path, from the first set on; pinned staging in turn, as in Workspace
+    int32_t *dev = nullptr, *host_stage = nullptr;
+    size_t stage_words = 0;
+    int stage_next = 0;
+    hipEvent_t stage_ev[kStageSlots] = {};
+    size_t rows_at() const { return ((size_t)max_batch + 1 + 3) / 4 * 4; }
+    size_t masks_at() const { return rows_at() + (size_t)max_rows * (sizeof(TreeRow) / 4); }
+    size_t kept_at() const { return masks_at() + (size_t)max_rows * (kTreeMaxNodes / 32); }
+    size_t path_at() const { return kept_at() + max_batch; }
+    size_t words() const { return path_at() + max_rows; }
+    TreeView view() const {
+        return TreeView{dev, reinterpret_cast<const TreeRow *>(dev + rows_at()), reinterpret_cast<const uint32_t *>(dev + masks_at()), mask_words, rows, batch, max_n};
+    }
+};
+
 namespace {
+
+constexpr size_t kTreePartFloats = (size_t)16 << 20;        // 64 MB
 
 size_t esize(hexgen_dtype_t dt) { return dt == HEXGEN_F32 ? 4 : 2; }
 bool is_h16(hexgen_dtype_t dt) { return dt == HEXGEN_BF16 || dt == HEXGEN_F16; }
@@ -151,7 +174,7 @@ size_t dec_part_floats(const hexgen_stage *st, int rows) {
 
 void free_ws(Workspace &w) {
     void *ptrs[] = {w.dec_part, w.gemm_part, w.gemm_arrived, w.h, w.n, w.o, w.u, w.q, w.xa_n, w.xa_o, w.xa_u, w.q_lo, w.ssq, w.ssq_pf, w.att_o, w.att_ml, w.att_arrived, w.qkv32, w.n32, w.q32, w.o32, w.u32,
-                    w.rowmap};
+                    w.tree_qkv, w.rowmap};
     for (void *p : ptrs)
         if (p) (void)hipFree(p);
     if (w.host_stage) (void)hipHostFree(w.host_stage);
@@ -237,6 +260,7 @@ struct Rows {
     bool decode = false;          // on the decode kernels
     bool dev_rows = false;        // one new row per sequence: the prologue takes sequences and positions from the committed lengths
     RowMap rm{};
+    const hexgen_tree *tree = nullptr;      // the rows are the nodes of drafted trees
 };
 
 // Work that takes host-side state of this moment along (row maps, staged copies) cannot be recorded for replay.
@@ -338,6 +362,46 @@ KvGeom geom(const hexgen_stage *st, const hexgen_kv_cache *kv) {
     return g;
 }
 
+// ---- drafted trees: the attention of every path ----------------------------------------------------------------
+// How many runs the contexts are cut into: enough blocks for the chip, runs of eight tiles at least.
+TreeSplit pick_tree_split(const hexgen_stage *st, const hexgen_kv_cache *kv, const hexgen_tree *tr) {
+    const int G = st->hq_l / st->hkv_l;
+    const int block_rows = is_h16(st->dtype) ? 32 * tree_row_groups(tr->max_n, G) : 16;
+    long work = 0;
+    int longest = 1;
+    for (int i = 0; i < tr->batch; ++i) {
+        const int n = tr->cu[i + 1] - tr->cu[i], nt = (kv->lens[i] + n + 31) / 32;
+        if (n == 0) continue;
+        work += (long)((n * G + block_rows - 1) / block_rows) * nt;
+        longest = std::max(longest, nt);
+    }
+    work *= st->hkv_l;
+    TreeSplit sp;
+    sp.chunk = (int)std::max(8L, (work + 511) / 512);
+    sp.nsplit = std::min((longest + sp.chunk - 1) / sp.chunk, kTreeMaxSplit);
+    sp.nsplit = (int)std::max((size_t)1, std::min((size_t)sp.nsplit, kTreePartFloats / ((size_t)tr->rows * st->hq_l * (st->d + 2))));
+    sp.part_o = st->tree_part;
+    sp.part_ml = st->tree_part + (size_t)sp.nsplit * tr->rows * st->hq_l * st->d;
+    return sp;
+}
+
+// The raw QKV projection of the trees' rows (16 bits: ws.tree_qkv, packed columns; fp32: ws.qkv32) -> rotated q, cache rows, attention
+void attn_tree(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const Rows &r, const TreeOut &out, hipStream_t s) {
+    Workspace &w = st->ws;
+    const KvGeom kg = geom(st, kv);
+    const TreeView tv = r.tree->view();
+    const TreeSplit sp = pick_tree_split(st, kv, r.tree);
+    if (is_h16(st->dtype)) {
+        h16_t *kc = static_cast<h16_t *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<h16_t *>(kv->v) + (size_t)layer * kv->layer_stride;
+        HX_K(st->dtype, launch_tree_rope_append, w.tree_qkv, st->hq_l, kg, tv, kv->d_lens, kv->cos_tab, kv->sin_tab, w.q, kc, vc, s);
+        HX_K(st->dtype, launch_tree_attn, w.q, st->qw, kc, vc, kg, st->hq_l, tv, kv->d_lens, sp, out, s);
+    } else {
+        float *kc = static_cast<float *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<float *>(kv->v) + (size_t)layer * kv->layer_stride;
+        f32_launch_tree_rope_append(w.qkv32, st->hq_l, kg, tv, kv->d_lens, kv->cos_tab, kv->sin_tab, w.q32, kc, vc, s);
+        f32_launch_tree_attn(w.q32, st->qw, kc, vc, kg, st->hq_l, tv, kv->d_lens, sp, static_cast<float *>(out.o), s);
+    }
+}
+
 // ---- bf16 prefill flow: five kernels per layer; RoPE / cache append, residual + next-norm operand and SwiGLU
 // run in the GEMM epilogues, RMSNorm enters as a per-token scale after the contraction ---------------------
 GemmEpi gemm_epi_base(hexgen_stage *st, int mode) {
@@ -362,6 +426,16 @@ void attn_prefill_h16(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const Ro
                        hipStream_t s) {
     Workspace &w = st->ws;
     const Layer &ly = st->layers[layer];
+    if (r.tree != nullptr) {
+        GemmEpi raw = gemm_epi_base(st, DEC_RAW);
+        raw.ssq_in = ssq_in;
+        raw.raw_out = w.tree_qkv;
+        gemm_h16(st, r, ly.wqkv, w.n, st->nqkv, st->H, raw, PROF_QKV, s);
+        st->prof.mark(PROF_ATTN, s);
+        attn_tree(st, kv, layer, r, TreeOut{TREE_OUT_FRAG, r.T, st->qw, w.o}, s);
+        st->prof.mark(PROF_ATTN, s);
+        return;
+    }
     const KvGeom kg = geom(st, kv);
     h16_t *kc = static_cast<h16_t *>(kv->k) + (size_t)layer * kv->layer_stride;
     h16_t *vc = static_cast<h16_t *>(kv->v) + (size_t)layer * kv->layer_stride;
@@ -501,6 +575,16 @@ void attn_decode_h16(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const Row
                       hipStream_t s) {
     Workspace &w = *st->cur;
     const Layer &ly = st->layers[layer];
+    if (r.tree != nullptr) {
+        DecodeEpi raw = epi_base(st, DEC_RAW);
+        raw.ssq_in = ssq_in;
+        raw.raw_out = w.tree_qkv;
+        decode_proj(st, r, ly.wqkv, w.xa_n, st->nqkv, st->H, raw, PROF_QKV, s);
+        st->prof.mark(PROF_ATTN, s);
+        attn_tree(st, kv, layer, r, TreeOut{TREE_OUT_ACT, r.T, st->qw, w.xa_o}, s);
+        st->prof.mark(PROF_ATTN, s);
+        return;
+    }
     const KvGeom kg = geom(st, kv);
     h16_t *kc = static_cast<h16_t *>(kv->k) + (size_t)layer * kv->layer_stride;
     h16_t *vc = static_cast<h16_t *>(kv->v) + (size_t)layer * kv->layer_stride;
@@ -525,8 +609,8 @@ hexgen_status_t forward_decode_h16(hexgen_stage *st, hexgen_kv_cache *kv, const 
                                     void *out_partial, void *out_resid, hipStream_t s) {
     Workspace &w = *st->cur;
     float *ssq_a = w.ssq, *ssq_f = w.ssq + (size_t)(st->H / 16) * kDecodeMaxRows;
-    HX_K(st->dtype, launch_decode_prologue, hidden_in, nullptr, 1, w.h, st->layers[0].g_attn, w.xa_n, ssq_a, r.T, st->H, kv->d_lens,
-                           w.row_pos, 1, s);
+    HX_K(st->dtype, launch_decode_prologue, hidden_in, nullptr, 1, w.h, st->layers[0].g_attn, w.xa_n, ssq_a, r.T, st->H,
+                           r.tree != nullptr ? nullptr : kv->d_lens, w.row_pos, 1, s);
     for (int l = 0; l < st->L; ++l) {
         const Layer &ly = st->layers[l];
         const bool last = l + 1 == st->L;
@@ -594,7 +678,7 @@ void proj_f32(hexgen_stage *st, int mode, const F32Proj &p, hipStream_t s) {
 // Does a step take attention and W_O in one launch?  By the longest context; a step that is being recorded may be replayed at any length of its
 // cache, which the host does not see, and goes by the cache's capacity.
 bool takes_attn_wo(const hexgen_stage *st, const hexgen_kv_cache *kv, const Rows &r, hipStream_t s) {
-    if (!r.decode) return false;
+    if (!r.decode || r.tree != nullptr) return false;
     int positions = 0;
     for (int i = 0; i < r.batch; ++i) positions = std::max(positions, kv->lens[i] + 1);
     if (!f32_attn_wo_fits(r.T, st->hq_l, st->hkv_l, st->d, st->H, positions)) return false;
@@ -614,6 +698,10 @@ void attn_f32(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const Rows &r, c
     proj_f32(st, F32_PLAIN, f32_proj(st, h, ly.g_attn, ly.wqkv, r.T, st->H, st->nqkv, st->nqkv, w.qkv32), s);
     if (wo != nullptr) {
         f32_launch_attn_wo(w.qkv32, kc, vc, st->hq_l, st->hkv_l, st->d, kv->smax, kv->d_lens, kv->cos_tab, kv->sin_tab, *wo, s);
+        return;
+    }
+    if (r.tree != nullptr) {
+        attn_tree(st, kv, layer, r, TreeOut{TREE_OUT_ROWS, r.T, st->qw, w.o32}, s);
         return;
     }
     if (r.max_new == 1) {          // row = sequence
@@ -682,6 +770,40 @@ void free_layer(Layer &l) {
     l = Layer();
 }
 
+
+// ---- drafted trees: storage and checks ----------------------------------------------------------------------------
+constexpr int kTreeMaxBatch = 1 << 15, kTreeMaxRows = 1 << 16;      // what the grids and 32-bit indexes of the tree kernels take
+static_assert(kTreeMaxNodes == HEXGEN_TREE_MAX_NODES, "one limit");
+
+hexgen_status_t tree_storage(hexgen_tree *tr) {
+    if (tr->dev == nullptr) HX_TRY(dmalloc(&tr->dev, tr->words()));
+    if (tr->host_stage == nullptr) {
+        tr->stage_words = tr->words();
+        HX_HIP(hipHostMalloc(reinterpret_cast<void **>(&tr->host_stage), kStageSlots * tr->stage_words * sizeof(int32_t), hipHostMallocDefault));
+    }
+    for (hipEvent_t &e : tr->stage_ev)
+        if (e == nullptr) HX_HIP(hipEventCreateWithFlags(&e, hipEventDisableTiming));
+    return HEXGEN_OK;
+}
+// the next piece of pinned staging, free once the copies that last read it are through
+hexgen_status_t tree_stage(hexgen_tree *tr, int32_t **words, int *slot) {
+    *slot = tr->stage_next;
+    tr->stage_next = (tr->stage_next + 1) % kStageSlots;
+    HX_HIP(hipEventSynchronize(tr->stage_ev[*slot]));
+    *words = tr->host_stage + (size_t)*slot * tr->stage_words;
+    return HEXGEN_OK;
+}
+hexgen_status_t ensure_tree_part(hexgen_stage *st, hipStream_t s) {
+    if (st->tree_part != nullptr) return HEXGEN_OK;
+    HX_TRY(refuse_capture(s));
+    return dmalloc(&st->tree_part, kTreePartFloats);
+}
+hexgen_status_t check_tree(const hexgen_kv_cache *kv, const hexgen_tree *tr) {
+    if (!kv->prefilled || tr->batch == 0 || tr->batch != kv->batch) return HEXGEN_ERR_STATE;
+    for (int i = 0; i < tr->batch; ++i)
+        if ((long)kv->lens[i] + (tr->cu[i + 1] - tr->cu[i]) > kv->max_seq) return HEXGEN_ERR_CAPACITY;
+    return HEXGEN_OK;
+}
 
 // ---- the allocation-free decode step: its whole workspace lives in one file-scope device array ------------------
 constexpr size_t kStaticScratchBytes = (size_t)HEXGEN_STATIC_SCRATCH_BYTES;
@@ -813,6 +935,7 @@ void hexgen_stage_destroy(hexgen_stage_t *st) {
     (void)hipDeviceSynchronize();
     for (Layer &l : st->layers) free_layer(l);
     free_ws(st->ws);
+    if (st->tree_part) (void)hipFree(st->tree_part);
     st->prof.clear();
     delete st;
 }
@@ -1038,8 +1161,8 @@ static hexgen_status_t kv_io(hexgen_kv_cache_t *kv, int layer, int seq, int pos0
     if (rc != HEXGEN_OK) { (void)hipFree(dk); return rc; }
     hipError_t e = hipSuccess;
     if (to_cache) {
-        e = hipMemcpy(dk, k, cnt * sizeof(float), hipMemcpyHostToDevice);
-        if (e == hipSuccess) e = hipMemcpy(dv, v, cnt * sizeof(float), hipMemcpyHostToDevice);
+        e = hipMemcpy(dk, k, cnt * sizeof(float), hipMemcpyDefault);
+        if (e == hipSuccess) e = hipMemcpy(dv, v, cnt * sizeof(float), hipMemcpyDefault);
     }
     if (e == hipSuccess) {
         if (is_h16(st->dtype)) {
@@ -1186,6 +1309,183 @@ hexgen_status_t hexgen_stage_decode_static(hexgen_stage_t *st, hexgen_kv_cache_t
 int64_t hexgen_stage_decode_static_bytes(const hexgen_stage_t *st, int batch) {
     if (!st || batch <= 0 || !is_h16(st->dtype)) return -1;
     return (int64_t)carve_decode_workspace(st, batch, nullptr, nullptr);
+}
+
+// ---- drafted trees ---------------------------------------------------------------------------------
+hexgen_status_t hexgen_tree_create(int max_batch, int max_rows, hexgen_tree_t **out) {
+    if (!out || max_batch <= 0 || max_rows <= 0) return HEXGEN_ERR_INVALID_ARG;
+    if (max_batch > kTreeMaxBatch || max_rows > kTreeMaxRows) return HEXGEN_ERR_CAPACITY;
+    hexgen_tree *tr = new (std::nothrow) hexgen_tree();
+    if (!tr) return HEXGEN_ERR_OOM;
+    tr->max_batch = max_batch;
+    tr->max_rows = max_rows;
+    *out = tr;
+    return HEXGEN_OK;
+}
+
+void hexgen_tree_destroy(hexgen_tree_t *tr) {
+    if (!tr) return;
+    if (tr->dev != nullptr || tr->host_stage != nullptr) (void)hipDeviceSynchronize();
+    if (tr->dev) (void)hipFree(tr->dev);
+    if (tr->host_stage) (void)hipHostFree(tr->host_stage);
+    for (hipEvent_t e : tr->stage_ev)
+        if (e) (void)hipEventDestroy(e);
+    delete tr;
+}
+
+hexgen_status_t hexgen_tree_set(hexgen_tree_t *tr, const int32_t *counts, const int32_t *parents, int batch, void *stream) {
+    if (!tr || !counts || !parents || batch <= 0) return HEXGEN_ERR_INVALID_ARG;
+    if (batch > tr->max_batch) return HEXGEN_ERR_CAPACITY;
+    long total = 0;
+    int max_n = 0;
+    for (int i = 0; i < batch; ++i) {
+        if (counts[i] < 0) return HEXGEN_ERR_INVALID_ARG;
+        if (counts[i] > kTreeMaxNodes) return HEXGEN_ERR_CAPACITY;
+        total += counts[i];
+        max_n = std::max(max_n, (int)counts[i]);
+    }
+    if (total > tr->max_rows) return HEXGEN_ERR_CAPACITY;
+    if (total == 0) return HEXGEN_ERR_SHAPE;
+    for (long i = 0, row = 0; i < batch; row += counts[i], ++i)
+        for (int x = 0; x < counts[i]; ++x)
+            if (x == 0 ? parents[row] != -1 : (parents[row + x] < 0 || parents[row + x] >= x)) return HEXGEN_ERR_SHAPE;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    HX_TRY(refuse_capture(s));
+    HX_TRY(tree_storage(tr));
+    std::vector<int32_t> cu, par;
+    try {       // no exception crosses the C boundary
+        cu.assign((size_t)batch + 1, 0);
+        par.assign(parents, parents + total);
+    } catch (...) {
+        return HEXGEN_ERR_OOM;
+    }
+    int32_t *hs = nullptr;
+    int slot = 0;
+    HX_TRY(tree_stage(tr, &hs, &slot));
+    const int mw = (max_n + 31) / 32;
+    TreeRow *rows = reinterpret_cast<TreeRow *>(hs + tr->rows_at());
+    uint32_t *masks = reinterpret_cast<uint32_t *>(hs + tr->masks_at());
+    for (int i = 0, row = 0; i < batch; ++i) {
+        for (int x = 0; x < counts[i]; ++x) {
+            const int p = parents[row + x];
+            rows[row + x] = TreeRow{i, x, x == 0 ? 0 : rows[row + p].depth + 1, p};
+            uint32_t *m = masks + (size_t)(row + x) * mw;
+            for (int w = 0; w < mw; ++w) m[w] = x == 0 ? 0u : masks[(size_t)(row + p) * mw + w];
+            m[x >> 5] |= 1u << (x & 31);
+        }
+        row += counts[i];
+        cu[i + 1] = row;
+    }
+    std::copy(cu.begin(), cu.end(), hs);
+    tr->batch = 0;                // not valid should a copy fail
+    HX_HIP(hipMemcpyAsync(tr->dev, hs, (tr->rows_at() + (size_t)total * (sizeof(TreeRow) / 4)) * sizeof(int32_t), hipMemcpyHostToDevice, s));
+    HX_HIP(hipMemcpyAsync(tr->dev + tr->masks_at(), masks, (size_t)total * mw * sizeof(uint32_t), hipMemcpyHostToDevice, s));
+    HX_HIP(hipEventRecord(tr->stage_ev[slot], s));
+    tr->cu.swap(cu);
+    tr->parents.swap(par);
+    tr->rows = (int)total;
+    tr->max_n = max_n;
+    tr->mask_words = mw;
+    tr->batch = batch;
+    return HEXGEN_OK;
+}
+
+hexgen_status_t hexgen_tree_accept(const hexgen_tree_t *tr, const int32_t *draft, const int32_t *chosen, int32_t *kept, int32_t *path,
+                                   int32_t *tokens, void *stream) {
+    if (!tr || !draft || !chosen || !kept || !path || !tokens) return HEXGEN_ERR_INVALID_ARG;
+    if (tr->batch == 0) return HEXGEN_ERR_STATE;
+    launch_tree_accept(tr->view(), draft, chosen, kept, path, tokens, static_cast<hipStream_t>(stream));
+    HX_HIP(hipGetLastError());
+    return HEXGEN_OK;
+}
+
+hexgen_status_t hexgen_kv_tree_attention(hexgen_kv_cache_t *kv, int layer, const hexgen_tree_t *tr, const void *q, int64_t ldq,
+                                         const void *k, int64_t ldk, const void *v, int64_t ldv, void *out, void *stream) {
+    if (!kv || !tr || !q || !k || !v || !out || layer < 0 || layer >= kv->st->L) return HEXGEN_ERR_INVALID_ARG;
+    hexgen_stage *st = kv->st;
+    const int64_t kw = (int64_t)st->hkv_l * st->d;
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(out);
+    if (bits % 16 || (ldq | ldk | ldv) % (16 / (int)esize(st->dtype)) || ldq < st->qw || ldk < kw || ldv < kw) return HEXGEN_ERR_INVALID_ARG;
+    HX_TRY(check_tree(kv, tr));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    HX_TRY(ensure_tree_part(st, s));
+    const KvGeom kg = geom(st, kv);
+    const TreeView tv = tr->view();
+    const TreeSplit sp = pick_tree_split(st, kv, tr);
+    if (is_h16(st->dtype)) {
+        h16_t *kc = static_cast<h16_t *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<h16_t *>(kv->v) + (size_t)layer * kv->layer_stride;
+        HX_K(st->dtype, launch_tree_append, static_cast<const h16_t *>(k), ldk, static_cast<const h16_t *>(v), ldv, kc, vc, kg, tv, kv->d_lens, s);
+        HX_K(st->dtype, launch_tree_attn, static_cast<const h16_t *>(q), ldq, kc, vc, kg, st->hq_l, tv, kv->d_lens, sp, TreeOut{TREE_OUT_ROWS, tr->rows, st->qw, out}, s);
+    } else {
+        float *kc = static_cast<float *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<float *>(kv->v) + (size_t)layer * kv->layer_stride;
+        f32_launch_tree_append(static_cast<const float *>(k), ldk, static_cast<const float *>(v), ldv, kc, vc, kg, tv, kv->d_lens, s);
+        f32_launch_tree_attn(static_cast<const float *>(q), ldq, kc, vc, kg, st->hq_l, tv, kv->d_lens, sp, static_cast<float *>(out), s);
+    }
+    HX_HIP(hipGetLastError());
+    return HEXGEN_OK;
+}
+
+hexgen_status_t hexgen_stage_decode_tree(hexgen_stage_t *st, hexgen_kv_cache_t *kv, const hexgen_tree_t *tr, const void *hidden_in,
+                                         void *out_partial, void *out_resid, void *stream) {
+    if (!st || !kv || !tr || !hidden_in || !out_partial || kv->st != st) return HEXGEN_ERR_INVALID_ARG;
+    HX_TRY(check_loaded(st));
+    HX_TRY(check_tree(kv, tr));
+    HX_TRY(check_rope(st, kv));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Rows r;
+    r.T = tr->rows;
+    r.batch = tr->batch;
+    r.max_new = tr->max_n;
+    r.tree = tr;
+    r.decode = r.T <= (is_h16(st->dtype) ? kDecodeMaxRows : kF32StreamRows);
+    if (r.T > st->ws.cap_rows || r.batch > st->ws_batch_cap) HX_TRY(refuse_capture(s));
+    HX_TRY(ensure_workspace(st, r.T, r.batch));
+    HX_TRY(ensure_tree_part(st, s));
+    if (is_h16(st->dtype) && st->ws.tree_qkv == nullptr) {
+        HX_TRY(refuse_capture(s));
+        HX_TRY(dmalloc(&st->ws.tree_qkv, (size_t)st->ws.cap_rows * st->nqkv));
+    }
+    st->prof.mark(PROF_CALL, s);
+    if (is_h16(st->dtype)) HX_TRY(forward_h16(st, kv, r, hidden_in, out_partial, out_resid, s));
+    else HX_TRY(forward_f32(st, kv, r, hidden_in, out_partial, out_resid, nullptr, s));
+    if (r.decode && is_h16(st->dtype)) st->last_decode_rows = r.T;
+    st->prof.mark(PROF_CALL, s);
+    HX_HIP(hipGetLastError());
+    return HEXGEN_OK;
+}
+
+hexgen_status_t hexgen_kv_cache_keep(hexgen_kv_cache_t *kv, hexgen_tree_t *tr, const int32_t *kept, const int32_t *path, void *stream) {
+    if (!kv || !tr || !kept || !path) return HEXGEN_ERR_INVALID_ARG;
+    HX_TRY(check_tree(kv, tr));
+    for (int i = 0; i < tr->batch; ++i) {
+        const int row = tr->cu[i], n = tr->cu[i + 1] - row;
+        if (kept[i] < 0 || kept[i] > n) return HEXGEN_ERR_SHAPE;
+        for (int j = 0; j < kept[i]; ++j) {
+            const int x = path[row + j];
+            if (x < 0 || x >= n || tr->parents[row + x] != (j == 0 ? -1 : path[row + j - 1])) return HEXGEN_ERR_SHAPE;
+        }
+    }
+    hexgen_stage *st = kv->st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    HX_TRY(refuse_capture(s));
+    int32_t *hs = nullptr;
+    int slot = 0;
+    HX_TRY(tree_stage(tr, &hs, &slot));
+    std::copy(kept, kept + tr->batch, hs);
+    std::copy(path, path + tr->rows, hs + tr->max_batch);
+    int32_t *d_kept = tr->dev + tr->kept_at(), *d_path = tr->dev + tr->path_at();
+    HX_HIP(hipMemcpyAsync(d_kept, hs, ((size_t)tr->max_batch + tr->rows) * sizeof(int32_t), hipMemcpyHostToDevice, s));
+    HX_HIP(hipEventRecord(tr->stage_ev[slot], s));
+    const KvGeom kg = geom(st, kv);
+    if (is_h16(st->dtype))
+        HX_K(st->dtype, launch_tree_keep, static_cast<h16_t *>(kv->k), static_cast<h16_t *>(kv->v), kv->layer_stride, st->L, kg, tr->batch, kv->d_lens, tr->dev, d_kept,
+             d_path, s);
+    else
+        f32_launch_tree_keep(static_cast<float *>(kv->k), static_cast<float *>(kv->v), kv->layer_stride, st->L, kg, tr->batch, kv->d_lens, tr->dev, d_kept, d_path, s);
+    launch_tree_advance(kv->d_lens, d_kept, tr->batch, s);
+    HX_HIP(hipGetLastError());
+    for (int i = 0; i < tr->batch; ++i) kv->lens[i] += kept[i];
+    return HEXGEN_OK;
 }
 
 // ---- validation surface ----------------------------------------------------------------------------
