@@ -65,6 +65,11 @@ SIGNATURES = {
     "hexgen_head_load": (_i, [_vp, _vp, _vp]),
     "hexgen_head_greedy": (_i, [_vp, _vp, _vp, _i, _vp, _vp, _vp]),
     "hexgen_head_destroy": (None, [_vp]),
+    "hexgen_head_load_q4": (_i, [_vp, _vp, _vp, _vp, _vp, _i]),
+    "hexgen_q4_create": (_i, [_i, _i, _i, _i, C.POINTER(_vp)]),
+    "hexgen_q4_destroy": (None, [_vp]),
+    "hexgen_q4_load": (_i, [_vp, _vp, _vp, _vp]),
+    "hexgen_q4_project": (_i, [_vp, _vp, _i64, _i, _vp, _vp]),
     "hexgen_cost_comp": (C.c_double, [_i, C.c_double, _i, _i, _i, _i, _i, _i, _vp, _vp]),
     "hexgen_cost_comp_prefill": (C.c_double, [_i, C.c_double, _i, _i, _i, _i, _i, _i, _vp, _vp]),
     "hexgen_cost_comp_decode": (C.c_double, [_i, C.c_double, _i, _i, _i, _i, _i, _i, _vp, _vp]),
@@ -388,6 +393,52 @@ def stream_read(src: torch.Tensor, sink: torch.Tensor, blocks: int = 4096, strea
     _check(lib.hexgen_stream_read(_ptr(src), _ptr(sink), nbytes, blocks, _stream_handle(stream)), "hexgen_stream_read")
 
 
+def _q4_tensors(w4, scales, zeros, n_in: int, n_out: int, group: int, td):
+    """The three arrays of a 4-bit matrix, checked against its shape."""
+    groups = -(-n_in // group) if group > 0 else 0
+    for name, t, shape, ok in (("w4", w4, (n_in, n_out // 2), torch.uint8), ("scales", scales, (groups, n_out), None), ("zeros", zeros, (groups, n_out // 2), torch.uint8)):
+        if t is not None and (tuple(t.shape) != shape or (ok is not None and t.dtype != ok)):
+            raise ValueError(f"{name}: a {shape} tensor{'' if ok is None else ' of ' + str(ok)} is wanted, got {tuple(t.shape)} of {t.dtype}")
+    return w4.contiguous(), scales.to(td).contiguous(), None if zeros is None else zeros.contiguous()
+
+
+class Q4Matrix:
+    """Owns a hexgen_q4_t: a matrix of 4-bit weights with a scale, and possibly a zero point, per group of input features."""
+
+    def __init__(self, n_in: int, n_out: int, group: int, dtype):
+        self.dtype = _dtype_code(dtype)
+        h = C.c_void_p()
+        _check(lib.hexgen_q4_create(n_in, n_out, group, self.dtype, C.byref(h)), "hexgen_q4_create")
+        self.handle, self.n_in, self.n_out, self.group = h, n_in, n_out, group
+
+    def close(self, _lib=lib):
+        if getattr(self, "handle", None):
+            _lib.hexgen_q4_destroy(self.handle)
+            self.handle = None
+
+    __del__ = close
+
+    def load(self, w4: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor] = None):
+        """w4 uint8 [n_in, n_out / 2], column 2 i in the low nibble of byte i; scales [ceil(n_in / group), n_out]; zeros uint8
+        [ceil(n_in / group), n_out / 2] or None (8 everywhere).  Host or device."""
+        w, s, z = _q4_tensors(w4, scales, zeros, self.n_in, self.n_out, self.group, _torch_dtype(self.dtype))
+        _check(lib.hexgen_q4_load(self.handle, w.data_ptr(), s.data_ptr(), None if z is None else z.data_ptr()), "hexgen_q4_load")
+
+    def project(self, x: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """x [rows, n_in] (rows may be apart) times the matrix: [rows, n_out]."""
+        td, rows = _torch_dtype(self.dtype), x.shape[0] if x.dim() == 2 else 0
+        if x.dim() != 2 or x.shape[1] != self.n_in or rows < 1 or x.dtype != td or (self.n_in > 1 and x.stride(1) != 1):
+            raise ValueError(f"x: a (rows, {self.n_in}) tensor of {td} with dense rows is wanted, got {tuple(x.shape)} of {x.dtype}, strides {tuple(x.stride())}")
+        _on_device(x, "x")
+        if out is None:
+            out = _empty((rows, self.n_out), td, stream)
+        else:
+            _device_tensor(out, "out", (rows, self.n_out), td)
+        _check(lib.hexgen_q4_project(self.handle, x.data_ptr(), x.stride(0) if rows > 1 else self.n_in, rows, out.data_ptr(), _stream_handle(stream)),
+               "hexgen_q4_project")
+        return out
+
+
 class Head:
     """Final RMSNorm + vocabulary-parallel LM head + greedy arg-max of one rank (hexgen_head_*)."""
 
@@ -410,6 +461,16 @@ class Head:
         g, w = g_final.to(td).contiguous(), w_lm.to(td).contiguous()
         assert tuple(w.shape) == (self.hidden, self.vocab) and g.numel() == self.hidden
         _check(lib.hexgen_head_load(self.handle, _ptr(g), _ptr(w)), "hexgen_head_load")
+
+    def load_q4(self, g_final: torch.Tensor, w4: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor] = None, group: int = 128):
+        """hexgen_head_load_q4: w4 uint8 [hidden, vocab / 2], scales [ceil(hidden / group), vocab], zeros uint8 or None (8), as in Q4Matrix.load."""
+        td = _torch_dtype(self.dtype)
+        g = g_final.to(td).contiguous()
+        if g.numel() != self.hidden:
+            raise ValueError(f"g_final: {self.hidden} elements are wanted, got {g.numel()}")
+        w, s, z = _q4_tensors(w4, scales, zeros, self.hidden, self.vocab, group, td)
+        _check(lib.hexgen_head_load_q4(self.handle, g.data_ptr(), w.data_ptr(), s.data_ptr(), None if z is None else z.data_ptr(), group),
+               "hexgen_head_load_q4")
 
     def splits(self, rows: int) -> int:
         """How a pass over that many rows runs the projection: 0 in one kernel, else the splits of its contraction."""

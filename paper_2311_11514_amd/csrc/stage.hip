@@ -13,21 +13,9 @@
 
 #include "../../include/hexgen.h"
 #include "../../include/hexgen_bench.h"
+#include "host.h"
 #include "kernels.h"
-
-#define HX_HIP(expr)                                                          \
-    do {                                                                      \
-        hipError_t e_ = (expr);                                               \
-        if (e_ != hipSuccess) {                                               \
-            (void)hipGetLastError();                                          \
-            return e_ == hipErrorOutOfMemory ? HEXGEN_ERR_OOM : HEXGEN_ERR_DEVICE; \
-        }                                                                     \
-    } while (0)
-#define HX_TRY(expr)                              \
-    do {                                          \
-        hexgen_status_t s_ = (expr);              \
-        if (s_ != HEXGEN_OK) return s_;           \
-    } while (0)
+#include "q4.h"
 
 namespace {
 
@@ -1623,15 +1611,48 @@ struct hexgen_head {
     int32_t *best_id = nullptr;
     float *scratch = nullptr;     // split partial sums of the batched projection
     size_t scratch_floats = 0;
+    // a 4-bit matrix instead of w: candidates of the arg-max for kQ4PartRows rows
+    Q4Store q4;
+    float *q4_val = nullptr;
+    int32_t *q4_id = nullptr;
 };
 
 namespace {
 // rows of one pass over the head's weights: what the projections of either type take at a time
 int head_chunk_rows(const hexgen_head *hd) { return is_h16(hd->dtype) ? kHeadRows : kF32StreamRows; }
 void free_head(hexgen_head *hd) {
-    void *ptrs[] = {hd->w, hd->g, hd->xa, hd->ssq, hd->logits, hd->best_val, hd->best_id, hd->scratch};
+    void *ptrs[] = {hd->w, hd->g, hd->xa, hd->ssq, hd->logits, hd->best_val, hd->best_id, hd->scratch, hd->q4_val, hd->q4_id};
     for (void *p : ptrs)
         if (p) (void)hipFree(p);
+    q4_free(&hd->q4);
+}
+// the matrix of an earlier load, of either kind
+void drop_head_matrix(hexgen_head *hd) {
+    void *ptrs[] = {hd->w, hd->q4_val, hd->q4_id};
+    for (void *p : ptrs)
+        if (p) (void)hipFree(p);
+    hd->w = nullptr;
+    hd->q4_val = nullptr;
+    hd->q4_id = nullptr;
+    q4_free(&hd->q4);
+    hd->loaded = false;
+}
+// the final norm's gain -> fp32
+hexgen_status_t load_gain(hexgen_head *hd, const void *g_final) {
+    if (!is_h16(hd->dtype)) {
+        HX_HIP(hipMemcpy(hd->g, g_final, sizeof(float) * hd->H, hipMemcpyDefault));
+        return HEXGEN_OK;
+    }
+    h16_t *tmp = nullptr;
+    HX_TRY(dmalloc(&tmp, (size_t)hd->H));
+    hipError_t e = hipMemcpy(tmp, g_final, sizeof(h16_t) * hd->H, hipMemcpyDefault);
+    if (e == hipSuccess) {
+        HX_K(hd->dtype, launch_cvt_h16_to_f32, tmp, hd->g, hd->H, nullptr);
+        e = hipDeviceSynchronize();
+    }
+    (void)hipFree(tmp);
+    HX_HIP(e);
+    return HEXGEN_OK;
 }
 }  // namespace
 
@@ -1678,8 +1699,7 @@ hexgen_status_t hexgen_head_load(hexgen_head_t *hd, const void *g_final, const v
     HX_HIP(hipDeviceSynchronize());
     const int H = hd->H, c0 = hd->r * hd->Vl;
     const size_t es = esize(hd->dtype);
-    if (hd->w) { (void)hipFree(hd->w); hd->w = nullptr; }
-    hd->loaded = false;
+    drop_head_matrix(hd);
     if (hd->dtype == HEXGEN_F32) {
         HX_HIP(hipMemcpy(hd->g, g_final, sizeof(float) * H, hipMemcpyDefault));
         const size_t bytes = (size_t)round_up(H, 32) * hd->Vpad * es;
@@ -1710,6 +1730,26 @@ hexgen_status_t hexgen_head_load(hexgen_head_t *hd, const void *g_final, const v
     return HEXGEN_OK;
 }
 
+hexgen_status_t hexgen_head_load_q4(hexgen_head_t *hd, const void *g_final, const void *w4, const void *scales, const void *zeros, int group) {
+    if (!hd || !g_final || !w4 || !scales || group <= 0) return HEXGEN_ERR_INVALID_ARG;
+    if (hd->V % 2 || !q4_group_ok(group)) return HEXGEN_ERR_SHAPE;
+    HX_HIP(hipDeviceSynchronize());
+    drop_head_matrix(hd);
+    HX_TRY(load_gain(hd, g_final));
+    hexgen_status_t rc = q4_load(&hd->q4, hd->dtype, hd->H, hd->V, hd->r * hd->Vl, hd->Vl, group, w4, scales, zeros);
+    size_t cands = 0;
+    if (rc == HEXGEN_OK)
+        for (int t = 1; t <= kQ4PartRows; ++t) cands = std::max(cands, (size_t)t * q4_best_units(hd->q4.v, t));
+    if (rc == HEXGEN_OK) rc = dmalloc(&hd->q4_val, cands);
+    if (rc == HEXGEN_OK) rc = dmalloc(&hd->q4_id, cands);
+    if (rc != HEXGEN_OK) {
+        drop_head_matrix(hd);
+        return rc;
+    }
+    hd->loaded = true;
+    return HEXGEN_OK;
+}
+
 hexgen_status_t hexgen_head_greedy(hexgen_head_t *hd, const void *hidden_a, const void *hidden_b, int n_rows,
                                    int32_t *token_out, float *logit_out, void *stream) {
     if (!hd || !hidden_a || !token_out || n_rows <= 0) return HEXGEN_ERR_INVALID_ARG;
@@ -1717,12 +1757,18 @@ hexgen_status_t hexgen_head_greedy(hexgen_head_t *hd, const void *hidden_a, cons
     hipStream_t s = static_cast<hipStream_t>(stream);
     const size_t es = esize(hd->dtype);
     const int H = hd->H;
-    const int chunk = head_chunk_rows(hd);
+    const bool q4 = hd->q4.v.w != nullptr;
+    const int chunk = q4 ? kQ4PartRows : head_chunk_rows(hd);
     for (int r0 = 0; r0 < n_rows; r0 += chunk) {
         const int n = std::min(chunk, n_rows - r0);
         const char *a = static_cast<const char *>(hidden_a) + (size_t)r0 * H * es;
         const char *b = hidden_b ? static_cast<const char *>(hidden_b) + (size_t)r0 * H * es : nullptr;
-        if (is_h16(hd->dtype)) {
+        if (q4) {
+            // normalised rows in full precision, as three-part operand; the arg-max over the blocks' best columns
+            launch_q4_parts((int)hd->dtype, a, b, H, hd->g, hd->eps, H, hd->q4.padded(), n, hd->q4.planes, s);
+            launch_q4(hd->q4.v, true, hd->q4.planes, hd->q4.padded(), n, Q4Out{nullptr, 0, hd->q4_val, hd->q4_id}, hd->q4.part, s);
+            launch_row_best(hd->q4_val, hd->q4_id, q4_best_units(hd->q4.v, n), n, hd->r * hd->Vl, token_out + r0, logit_out ? logit_out + r0 : nullptr, s);
+        } else if (is_h16(hd->dtype)) {
             // same kernels as a decode projection: prologue (x = a + b, x * g as hi/lo operand, sums of squares),
             // weight-streaming projection with 1 / rms applied after the contraction; its epilogue keeps the best column of
             // every unit, so that no logits are written and read back
@@ -1759,7 +1805,7 @@ hexgen_status_t hexgen_head_greedy(hexgen_head_t *hd, const void *hidden_a, cons
 }
 
 int hexgen_head_splits(const hexgen_head_t *hd, int rows) {
-    if (!hd || !is_h16(hd->dtype) || rows < 1 || rows > kHeadRows) return -1;
+    if (!hd || !is_h16(hd->dtype) || hd->q4.v.w != nullptr || rows < 1 || rows > kHeadRows) return -1;
     return bf16::decode_splits(DEC_BEST, hd->Vpad, hd->H, rows, hd->scratch_floats);
 }
 
