@@ -6,12 +6,14 @@
 // the sum X over x alone (the same operand against ones: it arrives in the lanes that need it) give s * (S - (16 + z) X); products of
 // 5-bit and 8- or 11-bit numbers are exact in fp32, and 16 is the smallest offset that needs no arithmetic on the weights, so that S
 // and its sum with X lose little of what the group's sum has.
-// fp32 rows are cut into three bf16 parts of 8 bits each, exactly, that take three columns of the operand; their products are added
-// up per part and joined at the end.
+// fp32 rows are cut into two fp16 parts, x 2^e = hi + lo with e such that the row's largest value fits the type (22 bits of a value, 2^-39 of the
+// row's largest), that take two columns of the operand; their products are added up per part and joined, and scaled back, at the end.
 //
 // Layout: blocks of 16 columns x 128 input features, 1 KB, [k / 128][n / 16][lane][4 words]: word i of lane l holds features
-// 128 kq + 32 i + 8 (l / 16) + 0 .. 7 of column 16 tile + l % 16, feature 2 p + h in bits 16 h + 4 p: what one lane of
-// v_mfma_f32_16x16x32 contributes to four steps, in one 16-byte request.
+// 128 kq + 32 i + 8 (l / 16) + 0 .. 7 of column 16 tile + l % 16, what one lane of v_mfma_f32_16x16x32 contributes to four steps, in one
+// 16-byte request.  Feature 2 p + h sits in bits 16 h + 4 p of the word turned left by 3 (bf16) or 6 (fp16), so that pair 0 is in place
+// and the others are a shift or turn of 4, 8 and 12 away.
+// Scales have a row for every group, or for every 128 features where groups are larger; zero points are bytes 16 + z, or one row of 24s.
 #include <algorithm>
 #include <type_traits>
 
@@ -48,16 +50,22 @@ __device__ __forceinline__ floatx4 mfma(u32x4 a, u32x4 b, floatx4 c) {
     if constexpr (F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, a), __builtin_bit_cast(b16x8, b), c, 0, 0, 0);
 }
-// eight nibbles -> eight times 16 + q
-template <bool F16>
-__device__ __forceinline__ u32x4 widen(uint32_t w) {
-    if constexpr (F16)
-        return u32x4{((w << 6) & 0x03c003c0u) | 0x4c004c00u, ((w << 2) & 0x03c003c0u) | 0x4c004c00u, ((w >> 2) & 0x03c003c0u) | 0x4c004c00u,
-                     ((w >> 6) & 0x03c003c0u) | 0x4c004c00u};
-    else
-        return u32x4{((w << 3) & 0x00780078u) | 0x41804180u, ((w >> 1) & 0x00780078u) | 0x41804180u, ((w >> 5) & 0x00780078u) | 0x41804180u,
-                     ((w >> 9) & 0x00780078u) | 0x41804180u};
-}
+// Eight nibbles -> eight times 16 + q.  The constants are kept in registers out of the compiler's sight: an and-or takes no literals on this
+// processor, and with constants that it knows the compiler makes two operations of it.
+struct Widen {
+    uint32_t mask, sixteen;
+    template <bool F16>
+    __device__ __forceinline__ static Widen make() {
+        Widen w;
+        asm("s_mov_b32 %0, %1" : "=s"(w.mask) : "i"(F16 ? 0x03c003c0 : 0x00780078));
+        asm("v_mov_b32 %0, %1" : "=v"(w.sixteen) : "i"(F16 ? 0x4c004c00 : 0x41804180));
+        return w;
+    }
+    __device__ __forceinline__ u32x4 operator()(uint32_t w) const {
+        return u32x4{(w & mask) | sixteen, (__builtin_amdgcn_alignbit(w, w, 4) & mask) | sixteen, (__builtin_amdgcn_alignbit(w, w, 8) & mask) | sixteen,
+                     (__builtin_amdgcn_alignbit(w, w, 12) & mask) | sixteen};
+    }
+};
 
 // four neighbouring columns' scales, as they are loaded and as fp32
 template <int ST> using scale_raw = std::conditional_t<ST == HX_T_F32, floatx4, uint2>;
@@ -68,46 +76,44 @@ __device__ __forceinline__ floatx4 scale4(const scale_raw<ST> &v) {
     else return floatx4{f16_f32(v.x & 0xffffu), f16_f32(v.x >> 16), f16_f32(v.y & 0xffffu), f16_f32(v.y >> 16)};
 }
 
-// x columns of one 32-feature step (fragments of the second operand) for a 128-feature block of UT weight tiles: acc += this block's share
-template <bool F16, int ST, int NB, int UT, int FL, typename XF>
-__device__ __forceinline__ void contract_block(const u32x4 (&w)[UT], const scale_raw<ST> (&s)[UT][4 / FL], const uint32_t (&z)[UT][4 / FL], bool zeros, XF x,
+// acc += a 128-feature block's share: UT weight tiles against NB operand tiles, x(step, tile) the operand of 32 features, sums(f, tile)
+// the sum of its columns over the features of group f
+template <bool F16, int ST, int NB, int UT, int FL, typename XF, typename SF>
+__device__ __forceinline__ void contract_block(const Widen &widen, const u32x4 (&w)[UT], const scale_raw<ST> (&s)[UT][4 / FL], const uint32_t (&z)[UT][4 / FL], XF x, SF sums,
                                                floatx4 (&acc)[UT][NB]) {
-    const uint32_t one = F16 ? 0x3c003c00u : 0x3f803f80u;
-    const u32x4 ones = {one, one, one, one};
 #pragma unroll
     for (int f = 0; f < 4 / FL; ++f) {
-        floatx4 X[NB], S[UT][NB];
+        floatx4 S[UT][NB];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            X[b] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int u = 0; u < UT; ++u) S[u][b] = floatx4{0.f, 0.f, 0.f, 0.f};
-        }
 #pragma unroll
         for (int st = f * FL; st < f * FL + FL; ++st) {
             u32x4 a[UT];
 #pragma unroll
-            for (int u = 0; u < UT; ++u) a[u] = widen<F16>(w[u][st]);
+            for (int u = 0; u < UT; ++u) a[u] = widen(w[u][st]);
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 const u32x4 xb = x(st, b);
-                X[b] = mfma<F16>(ones, xb, X[b]);
 #pragma unroll
                 for (int u = 0; u < UT; ++u) S[u][b] = mfma<F16>(a[u], xb, S[u][b]);
             }
         }
+        floatx4 s4[UT], z4[UT];
 #pragma unroll
         for (int u = 0; u < UT; ++u) {
-            const floatx4 s4 = scale4<ST>(s[u][f]);
-            floatx4 z4 = {24.f, 24.f, 24.f, 24.f};
-            if (zeros) {
+            s4[u] = scale4<ST>(s[u][f]);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) z4[r] = 16.f + (float)((z[u][f] >> (8 * r)) & 255u);
-            }
+            for (int r = 0; r < 4; ++r) z4[u][r] = (float)((z[u][f] >> (8 * r)) & 255u);
+        }
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < NB; ++b) {
+            const floatx4 X = sums(f, b);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[u][b][r] = fmaf(s4[r], fmaf(-z4[r], X[b][r], S[u][b][r]), acc[u][b][r]);
+            for (int u = 0; u < UT; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[u][b][r] = fmaf(s4[u][r], fmaf(-z4[u][r], X[r], S[u][b][r]), acc[u][b][r]);
         }
         if (FL < 4) {                                           // one group's sums at a time: side by side they do not fit the registers
 #pragma unroll
@@ -118,20 +124,30 @@ __device__ __forceinline__ void contract_block(const u32x4 (&w)[UT], const scale
         }
     }
 }
-// the scales (and zero points) of a 128-feature block for four columns from `col` on
+// the scales and zero points of a 128-feature block for four columns from `col` on
 template <int ST, int NF>
-__device__ __forceinline__ void load_scales(const Q4View &m, int kq, int col, scale_raw<ST> (&s)[NF], uint32_t (&z)[NF]) {
+__device__ __forceinline__ void load_scales(const Q4View &m, int kq, uint32_t col, scale_raw<ST> (&s)[NF], uint32_t (&z)[NF]) {
 #pragma unroll
     for (int f = 0; f < NF; ++f) {
-        const size_t at = (size_t)((kq * 128 + f * (128 / NF)) / m.group) * (m.n_tiles * 16) + col;
-        s[f] = *reinterpret_cast<const scale_raw<ST> *>(static_cast<const unsigned char *>(m.scales) + at * (ST == HX_T_F32 ? 4 : 2));
-        if (m.zeros != nullptr) z[f] = *reinterpret_cast<const uint32_t *>(m.zeros + at);
+        const size_t row = kq * NF + f;                         // the same in every lane
+        s[f] = *reinterpret_cast<const scale_raw<ST> *>(static_cast<const unsigned char *>(m.scales) + row * (m.n_tiles * 16) * (ST == HX_T_F32 ? 4 : 2) + col * (ST == HX_T_F32 ? 4u : 2u));
+        z[f] = *reinterpret_cast<const uint32_t *>(m.zeros + row * m.zeros_row + col);
     }
+}
+__device__ __forceinline__ u32x4 load_weights(const Q4View &m, int kq, uint32_t off) {
+    return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(static_cast<const unsigned char *>(m.w) + (size_t)kq * m.n_tiles * 1024 + off));
 }
 __device__ __forceinline__ void store_pair(const Q4Out &out, size_t at, float a, float b) {
     if (out.type == HX_T_F32) *reinterpret_cast<float2 *>(static_cast<float *>(out.y) + at) = float2{a, b};
     else if (out.type == HX_T_BF16) *reinterpret_cast<uint32_t *>(static_cast<h16_t *>(out.y) + at) = to_bf16(a) | (uint32_t)to_bf16(b) << 16;
     else *reinterpret_cast<uint32_t *>(static_cast<h16_t *>(out.y) + at) = to_f16(a) | (uint32_t)to_f16(b) << 16;
+}
+// the power of two that a row's parts were made with
+__device__ __forceinline__ void scale_back(const Q4Out &out, int t, floatx4 &v) {
+    if (out.exps == nullptr) return;
+    const int e = out.exps[t];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = ldexpf(v[r], -e);
 }
 // four columns from n0 on of row t (n_valid is even, so that columns come in pairs)
 __device__ __forceinline__ void store_columns(const Q4View &m, const Q4Out &out, int t, int n0, floatx4 v) {
@@ -154,50 +170,90 @@ __device__ __forceinline__ void best_of_lanes(float &bv, int &bi) {
     }
 }
 
-// Up to 16 operand columns (rows times parts; columns beyond C repeat the last one and are not stored).  A block of eight waves owns UT
+// Up to 16 operand columns (rows times parts; columns beyond C repeat the last one and are not stored).  A block of W waves owns UT
 // tiles of 16 columns over the whole contraction; its waves take the 128-feature blocks in turn and are summed through LDS in wave order, so
-// that no partial result leaves the block.  A wave holds R blocks with their operands and scales in registers, requested that far ahead.
+// that no partial result leaves the block.  A wave holds R blocks with their scales in registers, requested that far ahead; every request is
+// unconditional (past the end it repeats the last block's), so that the compiler can count what is in flight and waits for the oldest
+// alone.  XLDS: the operand is staged in LDS once, else a wave requests its pieces one block ahead, from L2.
 // Bound by HBM on wide matrices, on small ones by the launch and one round trip.
 // FL: 32-feature steps of a scale's group inside a 128-feature block (4: groups of 128 and more).
-template <bool F16, int ST, int UT, int FL>
-__global__ __launch_bounds__(512) void q4_few_kernel(Q4View m, const h16_t *__restrict__ x, int64_t ldx, int C, int T, Q4Out out) {
-    constexpr int W = 8, NF = 4 / FL, R = FL == 4 ? 4 : 2;
+template <bool F16, int ST, int UT, int FL, int W, int R, bool XLDS>
+__global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) void q4_few_kernel(Q4View m, const h16_t *__restrict__ x, int64_t ldx, int C, int T, Q4Out out) {
+    constexpr int NF = 4 / FL;
+    static_assert(R % 2 == 0, "the operand's two slots alternate");
     __shared__ floatx4 red[W][UT][64];
+    extern __shared__ __align__(16) u32x4 xs[];                 // XLDS: [k / 8][column]
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     const int tile0 = blockIdx.x * UT;
-    const u32x4 *wp[UT];
-    int col[UT];
+    uint32_t off[UT], col[UT];
 #pragma unroll
     for (int u = 0; u < UT; ++u) {
-        const int t = min(tile0 + u, m.n_tiles - 1);           // a last tile of its own: the block's second repeats it, not stored
-        wp[u] = static_cast<const u32x4 *>(m.w) + (size_t)t * 64 + lane;
-        col[u] = t * 16 + 4 * g;
+        const uint32_t t = min(tile0 + u, m.n_tiles - 1);      // a last tile of its own: the block's second repeats it, not stored
+        off[u] = t * 1024u + lane * 16u;
+        col[u] = t * 16u + 4u * g;
     }
     const h16_t *xp = x + (size_t)min(j, C - 1) * ldx + 8 * g;
+    const Widen widen = Widen::make<F16>();
+    const uint32_t one = F16 ? 0x3c003c00u : 0x3f803f80u;
+    const u32x4 ones = {one, one, one, one};
     floatx4 acc[UT][1];
 #pragma unroll
     for (int u = 0; u < UT; ++u) acc[u][0] = floatx4{0.f, 0.f, 0.f, 0.f};
-    u32x4 wr[R][UT], xr[R][4];
+    u32x4 wr[R][UT], xr[XLDS ? 1 : 2][4];
     scale_raw<ST> sr[R][UT][NF];
     uint32_t zr[R][UT][NF];
-    const size_t kstride = (size_t)m.n_tiles * 64;
     auto request = [&](int i, int kq) {
 #pragma unroll
-        for (int u = 0; u < UT; ++u) wr[i][u] = __builtin_nontemporal_load(wp[u] + (size_t)kq * kstride);
+        for (int u = 0; u < UT; ++u) wr[i][u] = load_weights(m, kq, off[u]);
 #pragma unroll
         for (int u = 0; u < UT; ++u) load_scales<ST, NF>(m, kq, col[u], sr[i][u], zr[i][u]);
+    };
+    auto fetch = [&](int i, int kq) {
 #pragma unroll
         for (int s = 0; s < 4; ++s) xr[i][s] = *reinterpret_cast<const u32x4 *>(xp + kq * 128 + s * 32);
     };
-    // ring slot i holds block wave + i W of the round; past the last block a slot re-reads it and is not used
-    const int last = m.k_blocks - 1;
+    // ring slot i holds block wave + i W of the round
+    const int last = m.k_blocks - 1, mine = (last - wave + W) / W, full = mine / R;
 #pragma unroll
     for (int i = 0; i < R; ++i) request(i, min(wave + i * W, last));
-    for (int k0 = wave; k0 <= last; k0 += R * W) {
+    if constexpr (XLDS) {
+        const int pieces = m.k_blocks * 16;
+        for (int c = 0; c < C; ++c)
+            for (int p = threadIdx.x; p < pieces; p += 64 * W) xs[p * C + c] = *reinterpret_cast<const u32x4 *>(x + (size_t)c * ldx + 8 * p);
+        HX_LDS_BARRIER();
+    } else {
+        fetch(0, min(wave, last));
+        fetch(1, min(wave + W, last));
+    }
+    const u32x4 *xl = xs + g * C + min(j, C - 1);
+    auto contract = [&](int i, int kq) {
+        u32x4 xb[4];
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            if (k0 + i * W <= last) contract_block<F16, ST, 1, UT, FL>(wr[i], sr[i], zr[i], m.zeros != nullptr, [&](int s, int) { return xr[i][s]; }, acc);
-            request(i, min(k0 + (i + R) * W, last));
+        for (int s = 0; s < 4; ++s) xb[s] = XLDS ? xl[(kq * 4 + s) * 4 * C] : xr[XLDS ? 0 : i & 1][s];
+        // the columns' sums: the same operand against ones, which leaves them in the lanes that need them
+        auto sums = [&](int f, int) {
+            floatx4 X = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = f * FL; s < f * FL + FL; ++s) X = mfma<F16>(ones, xb[s], X);
+            return X;
+        };
+        contract_block<F16, ST, 1, UT, FL>(widen, wr[i], sr[i], zr[i], [&](int s, int) { return xb[s]; }, sums, acc);
+    };
+    int kq = wave;
+    for (int rd = 0; rd < full; ++rd) {
+#pragma unroll
+        for (int i = 0; i < R; ++i, kq += W) {
+            contract(i, kq);
+            request(i, min(kq + R * W, last));
+            if constexpr (!XLDS) fetch(i & 1, min(kq + 2 * W, last));
+            __builtin_amdgcn_sched_barrier(0);                  // each refill right behind its slot's use
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        if (i < mine - full * R) {                              // uniform over the wave
+            contract(i, kq + i * W);
+            if constexpr (!XLDS) fetch(i & 1, min(kq + (i + 2) * W, last));
         }
     }
 #pragma unroll
@@ -215,6 +271,7 @@ __global__ __launch_bounds__(512) void q4_few_kernel(Q4View m, const h16_t *__re
         v += a;
     }
     const int n0 = (tile0 + u) * 16 + 4 * gg;
+    scale_back(out, t, v);
     if (out.best_val == nullptr) {
         store_columns(m, out, t, n0, v);
         return;
@@ -229,73 +286,127 @@ __global__ __launch_bounds__(512) void q4_few_kernel(Q4View m, const h16_t *__re
     }
 }
 
-// More operand columns: the operand outweighs the weights that a tile of 16 columns has, so the eight waves of a block own eight times UT
-// neighbouring tiles and walk the same 128-feature blocks, whose operand they share through LDS (two buffers, one barrier a step).  The contraction
-// is split over blockIdx.y where the matrix has too few columns for the chip.  Results that need no more adding up (one split, one
-// part) are stored from here; everything else goes to `part` [split][column of the operand][16 n_tiles] and q4_finish_kernel.
-// Bound by HBM up to some 40 columns, beyond by the matrix instructions and the work on the weights beside them.
+// the sum of eight elements
+template <bool F16>
+__device__ __forceinline__ float sum8(u32x4 v) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (F16) {
+            typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+            s = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, (uint32_t)v[i]), f16x2{(_Float16)1.f, (_Float16)1.f}, s, false);
+        } else {
+            typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
+            s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b16x2, (uint32_t)v[i]), b16x2{(__bf16)1.f, (__bf16)1.f}, s, false);
+        }
+    }
+    return s;
+}
+
+// the sum over the four rows of 16 lanes, in every lane: each swap leaves the even rows in one register and the odd ones in the other
+__device__ __forceinline__ float sum_rows(float v) {
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+// More operand columns: the operand outweighs the weights that a tile of 16 columns has, so the waves of a block (eight to sixteen) own UT
+// neighbouring tiles each and walk the same 128-feature blocks, whose operand they share through LDS (two buffers, one barrier a step), the
+// columns' sums with it.  The contraction is split over blockIdx.y where the matrix has too few columns for the chip.  Results that need no more
+// adding up (one split, one part) are stored from here; everything else goes to `part` [split][column of the operand][16 n_tiles] and
+// q4_finish_kernel.
+// Bound by HBM, with many rows by LDS: a wave reads NB KB of operand for every UT KB of weights a quarter as often.
 template <bool F16, int ST, int NB, int UT, int FL>
-__global__ __launch_bounds__(512) void q4_shared_kernel(Q4View m, const h16_t *__restrict__ x, int64_t ldx, int C, int T, Q4Out out, int per, float *__restrict__ part) {
-    constexpr int NF = 4 / FL, R = 2, XL = NB / 2;              // XL: operand pieces a wave fetches per step, of 4 NB
-    static_assert(NB % 2 == 0, "pieces divide over the waves");
+__global__ __launch_bounds__(UT == 1 ? 1024 : 512, UT == 1 ? 4 : 2) void q4_shared_kernel(Q4View m, const h16_t *__restrict__ x, int64_t ldx, int C, int T, Q4Out out, int per, float *__restrict__ part) {
+    constexpr int NF = 4 / FL, R = 2, XL = (4 * NB + 7) / 8;    // XL: operand pieces a wave fetches per step, of 4 NB (the last ones more than once)
+    static_assert(R % 2 == 0, "the operand's two buffers alternate");
     __shared__ u32x4 xs[2][4 * NB][64];
+    __shared__ floatx4 xsum[2][NB][16];                         // [operand tile][column][32-feature step]
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
-    const int tile0 = (blockIdx.x * 8 + wave) * UT;
+    const int waves = blockDim.x >> 6, tile0 = (blockIdx.x * waves + wave) * UT;
     const int k0 = blockIdx.y * per, k1 = min(k0 + per, m.k_blocks);
-    const u32x4 *wp[UT];
-    int col[UT];
+    uint32_t off[UT], col[UT];
 #pragma unroll
     for (int u = 0; u < UT; ++u) {
-        const int t = min(tile0 + u, m.n_tiles - 1);
-        wp[u] = static_cast<const u32x4 *>(m.w) + (size_t)t * 64 + lane;
-        col[u] = t * 16 + 4 * g;
+        const uint32_t t = min(tile0 + u, m.n_tiles - 1);
+        off[u] = t * 1024u + lane * 16u;
+        col[u] = t * 16u + 4u * g;
     }
     const h16_t *xp[XL];
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
-        const int f = wave + 8 * i, b = f % NB, s = f / NB;
+        const int f = min(wave + waves * i, 4 * NB - 1), b = f % NB, s = f / NB;
         xp[i] = x + (size_t)min(16 * b + j, C - 1) * ldx + s * 32 + 8 * g;
     }
+    const Widen widen = Widen::make<F16>();
     floatx4 acc[UT][NB];
 #pragma unroll
     for (int u = 0; u < UT; ++u)
 #pragma unroll
         for (int b = 0; b < NB; ++b) acc[u][b] = floatx4{0.f, 0.f, 0.f, 0.f};
-    u32x4 wr[R][UT], xg[XL];
+    u32x4 wr[R][UT], xg[R][XL];
     scale_raw<ST> sr[R][UT][NF];
     uint32_t zr[R][UT][NF];
-    const size_t kstride = (size_t)m.n_tiles * 64;
     auto request = [&](int i, int kq) {
 #pragma unroll
-        for (int u = 0; u < UT; ++u) wr[i][u] = __builtin_nontemporal_load(wp[u] + (size_t)kq * kstride);
+        for (int u = 0; u < UT; ++u) wr[i][u] = load_weights(m, kq, off[u]);
 #pragma unroll
         for (int u = 0; u < UT; ++u) load_scales<ST, NF>(m, kq, col[u], sr[i][u], zr[i][u]);
     };
-    auto fetch = [&](int kq) {
+    auto fetch = [&](int slot, int kq) {
 #pragma unroll
-        for (int i = 0; i < XL; ++i) xg[i] = *reinterpret_cast<const u32x4 *>(xp[i] + kq * 128);
+        for (int i = 0; i < XL; ++i) xg[slot][i] = *reinterpret_cast<const u32x4 *>(xp[i] + kq * 128);
     };
-    auto put = [&](int buf) {
+    auto put = [&](int slot, int buf) {
 #pragma unroll
-        for (int i = 0; i < XL; ++i) xs[buf][wave + 8 * i][lane] = xg[i];
-    };
-    fetch(k0);
-#pragma unroll
-    for (int i = 0; i < R; ++i) request(i, min(k0 + i, k1 - 1));
-    put(0);
-    fetch(min(k0 + 1, k1 - 1));
-    HX_LDS_BARRIER();
-    for (int k = k0; k < k1; k += R) {
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            if (k + i >= k1) break;                             // uniform over the block
-            contract_block<F16, ST, NB, UT, FL>(wr[i], sr[i], zr[i], m.zeros != nullptr, [&](int s, int b) { return xs[i & 1][s * NB + b][lane]; }, acc);
-            request(i, min(k + i + R, k1 - 1));
-            put((i & 1) ^ 1);                                   // the buffer that every wave left at the last barrier
-            fetch(min(k + i + 2, k1 - 1));
-            HX_LDS_BARRIER();
+        for (int i = 0; i < XL; ++i) {
+            const int f = min(wave + waves * i, 4 * NB - 1), b = f % NB, s = f / NB;
+            xs[buf][f][lane] = xg[slot][i];
+            float v = sum8<F16>(xg[slot][i]);
+            v = sum_rows(v);
+            if (g == 0) reinterpret_cast<float *>(&xsum[buf][b][j])[s] = v;
         }
+    };
+    auto contract = [&](int i) {
+        floatx4 q[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) q[b] = xsum[i & 1][b][j];
+        auto sums = [&](int f, int b) {
+            float v = q[b][f * FL];
+#pragma unroll
+            for (int s = 1; s < FL; ++s) v += q[b][f * FL + s];
+            return floatx4{v, v, v, v};
+        };
+        contract_block<F16, ST, NB, UT, FL>(widen, wr[i], sr[i], zr[i], [&](int s, int b) { return xs[i & 1][s * NB + b][lane]; }, sums, acc);
+    };
+    // Step k + i is contracted from ring slot i and buffer i % 2, while the next step's operand is put into the buffer that every wave left at
+    // the last barrier; the requests go R steps ahead (past the end they repeat the last one's).  Loads return in order: were the operand
+    // fetched fewer steps ahead than the weights, waiting for it would be waiting for them.
+    auto step = [&](int i, int k) {
+        put((i + 1) % R, (i & 1) ^ 1);
+        fetch((i + 1) % R, min(k + 1 + R, k1 - 1));
+        contract(i);
+        request(i, min(k + R, k1 - 1));
+        HX_LDS_BARRIER();
+        __builtin_amdgcn_sched_barrier(0);                      // (side by side two steps do not fit the registers)
+    };
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        fetch(i, min(k0 + i, k1 - 1));
+        request(i, min(k0 + i, k1 - 1));
     }
+    put(0, 0);
+    fetch(0, min(k0 + R, k1 - 1));
+    HX_LDS_BARRIER();
+    int k = k0;
+    for (; k + R <= k1; k += R) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) step(i, k + i);
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+        if (k + i < k1) step(i, k + i);                         // uniform over the block
     const bool own = part == nullptr;
 #pragma unroll
     for (int u = 0; u < UT; ++u) {
@@ -323,6 +434,7 @@ __global__ __launch_bounds__(256) void q4_finish_kernel(Q4View m, const float *_
             v += a;
         }
     }
+    scale_back(out, t, v);
     if (out.best_val == nullptr) {
         if (n0 < np) store_columns(m, out, t, n0, v);
         return;
@@ -348,42 +460,103 @@ __device__ __forceinline__ float load_as(const void *p, size_t at) {
     else return f16_f32(static_cast<const h16_t *>(p)[at]);
 }
 
-// Rows as operand columns: x (+ x2), normalised with the gain g when there is one, as three bf16 parts [3 T][Kp] whose sum is the fp32
-// value; zero beyond K.  A block takes a row.  What is not finite has its value in the first part.
-template <int FROM>
+// Rows as operand columns: x (+ x2), normalised with the gain g when there is one, as two fp16 parts [2 T][Kp] whose sum is the fp32 value times
+// 2^exps[t]; zero beyond K.  A block takes a row, a thread eight neighbouring values at a time, of which the first KEEP stay in registers for the
+// second pass.  V: 16-byte pieces.  A value that is not finite stays so in the first part.
+template <int FROM, bool V>
 __global__ __launch_bounds__(1024) void q4_parts_kernel(const void *__restrict__ x, const void *__restrict__ x2, int64_t ldx, const float *__restrict__ g,
-                                                        float eps, int K, int Kp, int T, h16_t *__restrict__ out) {
-    __shared__ float red[16];
+                                                        float eps, int K, int Kp, int T, h16_t *__restrict__ out, int32_t *__restrict__ exps) {
+    constexpr int KEEP = 4;
+    __shared__ float red[16], red2[16];
     const int t = blockIdx.x;
-    float r = 1.0f;
-    auto value = [&](int k) { return load_as<FROM>(x, (size_t)t * ldx + k) + (x2 != nullptr ? load_as<FROM>(x2, (size_t)t * ldx + k) : 0.f); };
-    if (g != nullptr) {
-        float ss = 0.f;
-        for (int k = threadIdx.x; k < K; k += 1024) {
-            const float v = value(k);
-            ss = fmaf(v, v, ss);
-        }
-        ss = wave_sum(ss);
-        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
-        __syncthreads();
-        ss = 0.f;
-        for (int w = 0; w < 16; ++w) ss += red[w];
-        r = 1.0f / sqrtf(ss / (float)K + eps);
-    }
-    for (int k = threadIdx.x; k < Kp; k += 1024) {
-        float v = 0.f;
-        if (k < K) v = g != nullptr ? value(k) * r * g[k] : value(k);
-        uint32_t p[3] = {__float_as_uint(v) >> 16, 0u, 0u};      // cut off, not rounded: what is left has the same sign and 16 bits
-        if (__builtin_isfinite(v)) {
-            const float rest = v - bf16_f32(p[0]);
-            p[1] = __float_as_uint(rest) >> 16;
-            p[2] = __float_as_uint(rest - bf16_f32(p[1])) >> 16;
-        } else if (v != v) {
-            p[0] = 0x7fc0u;
-        }
+    struct Eight { float v[8]; };
+    auto raw = [&](const void *p, int k) {
+        Eight r;
+        if constexpr (!V) {
 #pragma unroll
-        for (int i = 0; i < 3; ++i) out[((size_t)i * T + t) * Kp + k] = (h16_t)p[i];
+            for (int i = 0; i < 8; ++i) r.v[i] = k + i < K ? load_as<FROM>(p, (size_t)t * ldx + k + i) : 0.f;
+        } else if constexpr (FROM == HX_T_F32) {
+            const float *q = static_cast<const float *>(p) + (size_t)t * ldx + k;
+            const floatx4 a = *reinterpret_cast<const floatx4 *>(q), b = *reinterpret_cast<const floatx4 *>(q + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { r.v[i] = a[i]; r.v[4 + i] = b[i]; }
+        } else {
+            const u32x4 a = *reinterpret_cast<const u32x4 *>(static_cast<const h16_t *>(p) + (size_t)t * ldx + k);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t h = (a[i >> 1] >> (16 * (i & 1))) & 0xffffu;
+                r.v[i] = FROM == HX_T_BF16 ? bf16_f32(h) : f16_f32(h);
+            }
+        }
+        return r;
+    };
+    // eight values from k on, times the gain; their squares without it
+    auto eight = [&](int k, float &ss) {
+        Eight r = raw(x, k);
+        if (x2 != nullptr) {
+            const Eight y = raw(x2, k);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r.v[i] += y.v[i];
+        }
+        if (g != nullptr) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ss = fmaf(r.v[i], r.v[i], ss);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r.v[i] *= k + i < K ? g[k + i] : 0.f;
+        }
+        return r;
+    };
+    Eight kept[KEEP];
+    float ss = 0.f, mx = 0.f;
+#pragma unroll
+    for (int c = 0; c < KEEP; ++c) {
+        const int k = (c * 1024 + threadIdx.x) * 8;
+        if (k < K) {
+            kept[c] = eight(k, ss);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(kept[c].v[i]));
+        }
     }
+    for (int k = (KEEP * 1024 + threadIdx.x) * 8; k < K; k += 8192) {
+        const Eight r = eight(k, ss);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(r.v[i]));
+    }
+    ss = wave_sum(ss);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+    if ((threadIdx.x & 63) == 0) { red[threadIdx.x >> 6] = ss; red2[threadIdx.x >> 6] = mx; }
+    __syncthreads();
+    ss = 0.f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) { ss += red[w]; mx = fmaxf(mx, red2[w]); }
+    const float r = g != nullptr ? 1.0f / sqrtf(ss / (float)K + eps) : 1.0f;
+    int e = 0;
+    if (mx * r > 0.f && mx * r < INFINITY) {
+        (void)frexpf(mx * r, &e);
+        e = 15 - e;                                              // the largest value to [2^14, 2^15)
+    }
+    if (threadIdx.x == 0) exps[t] = e;
+    auto put = [&](int k, const Eight &v) {
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float y = ldexpf(v.v[i] * r, e);
+            const uint32_t h = to_f16(y), l = __builtin_isfinite(y) ? to_f16(y - f16_f32(h)) : 0u;
+            if (i & 1) { hi[i >> 1] |= h << 16; lo[i >> 1] |= l << 16; }
+            else { hi[i >> 1] = h; lo[i >> 1] = l; }
+        }
+        *reinterpret_cast<u32x4 *>(out + (size_t)t * Kp + k) = u32x4{hi[0], hi[1], hi[2], hi[3]};
+        *reinterpret_cast<u32x4 *>(out + (size_t)(T + t) * Kp + k) = u32x4{lo[0], lo[1], lo[2], lo[3]};
+    };
+    const Eight none = {};
+    float unused = 0.f;
+#pragma unroll
+    for (int c = 0; c < KEEP; ++c) {
+        const int k = (c * 1024 + threadIdx.x) * 8;
+        if (k < Kp) put(k, k < K ? kept[c] : none);
+    }
+    for (int k = (KEEP * 1024 + threadIdx.x) * 8; k < Kp; k += 8192) put(k, k < K ? eight(k, unused) : none);
 }
 
 // 16-bit rows that are not 16-byte pieces: a dense copy, zero beyond K
@@ -392,7 +565,7 @@ __global__ __launch_bounds__(256) void q4_copy_kernel(const h16_t *__restrict__ 
 }
 
 // [K][N / 2] bytes, column 2 i in the low nibble of byte i -> the layout above, columns n0 .. n0 + n - 1; a word per thread
-__global__ __launch_bounds__(256) void q4_pack_kernel(const uint8_t *__restrict__ src, int64_t ld, int K, int n0, int n, int n_tiles, int k_blocks, uint32_t *__restrict__ dst) {
+__global__ __launch_bounds__(256) void q4_pack_kernel(const uint8_t *__restrict__ src, int64_t ld, int K, int n0, int n, int n_tiles, int k_blocks, int turn, uint32_t *__restrict__ dst) {
     const size_t idx = (size_t)blockIdx.x * 256 + threadIdx.x;
     if (idx >= (size_t)k_blocks * n_tiles * 256) return;
     const int i = idx & 3, lane = (idx >> 2) & 63, col = (int)((idx >> 8) % n_tiles) * 16 + (lane & 15);
@@ -406,51 +579,86 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const uint8_t *__restrict_
             w |= q << (16 * (e & 1) + 4 * (e >> 1));
         }
     }
-    dst[idx] = w;
+    dst[idx] = w << turn | w >> (32 - turn);
 }
-// scales [groups][N] -> [rows][16 n_tiles], zero beyond; zero points [groups][N / 2] nibbles -> bytes
-__global__ __launch_bounds__(256) void q4_pack_scales_kernel(const void *__restrict__ src, int es, const uint8_t *__restrict__ zsrc, int64_t ld, int groups, int rows, int n0,
-                                                             int n, int np, void *__restrict__ dst, uint8_t *__restrict__ zdst) {
+// scales [groups][N] -> [rows][16 n_tiles], row r from group r / repeat, zero beyond; zero points: nibbles [groups][N / 2] -> bytes 16 + z, zrows rows
+__global__ __launch_bounds__(256) void q4_pack_scales_kernel(const void *__restrict__ src, int es, const uint8_t *__restrict__ zsrc, int64_t ld, int groups, int rows, int zrows,
+                                                             int repeat, int n0, int n, int np, void *__restrict__ dst, uint8_t *__restrict__ zdst) {
     const size_t idx = (size_t)blockIdx.x * 256 + threadIdx.x;
     if (idx >= (size_t)rows * np) return;
-    const int row = (int)(idx / np), col = (int)(idx % np);
-    const bool there = row < groups && col < n;
-    const size_t at = (size_t)row * ld + n0 + col;
+    const int row = (int)(idx / np), col = (int)(idx % np), group = row / repeat;
+    const bool there = group < groups && col < n;
+    const size_t at = (size_t)group * ld + n0 + col;
     if (es == 4) static_cast<float *>(dst)[idx] = there ? static_cast<const float *>(src)[at] : 0.f;
     else static_cast<h16_t *>(dst)[idx] = there ? static_cast<const h16_t *>(src)[at] : (h16_t)0;
-    if (zdst != nullptr) zdst[idx] = there ? (uint8_t)((zsrc[(size_t)row * (ld / 2) + ((n0 + col) >> 1)] >> (4 * ((n0 + col) & 1))) & 15) : (uint8_t)0;
+    if (row < zrows) zdst[idx] = (uint8_t)(16 + (zsrc == nullptr ? 8 : there ? (zsrc[(size_t)group * (ld / 2) + ((n0 + col) >> 1)] >> (4 * ((n0 + col) & 1))) & 15 : 0));
 }
 
-// Tiles of 16 columns per wave of the shared form, and splits of its contraction: one round of blocks for the chip.  Two tiles a wave halve the
-// operand's way through LDS; with 96 operand columns their sums do not fit the registers.
-int shared_tiles(const Q4View &m, int nb) { return m.n_tiles >= 256 * 16 && nb <= 4 ? 2 : 1; }
-int shared_splits(const Q4View &m, int tiles) {
-    const int blocks = (m.n_tiles + 8 * tiles - 1) / (8 * tiles);
-    return std::max(1, std::min({256 / blocks, m.k_blocks / 4, 16}));
+// ---- which form --------------------------------------------------------------------------------------------------
+// Up to 16 operand columns: the few form, with the operand in LDS up to 32 KB of it.  (us, group 128, bf16, operand in LDS / from L2 / shared form:
+// 8192 x 57344, one column 43 / 54 / -; 8192 x 10240, one 12.4 / 15 / -; 4096 x 4096, eight 7.4 / 6.4 / -; 8192 x 57344, twelve - / 56 / 49;
+// 28672 x 8192, four - / 29 / 28)
+constexpr int kLdsOperand = 32 * 1024;
+enum { FEW_LDS_WIDE, FEW_LDS, FEW_LDS_NARROW, FEW_WIDE, FEW, SHARED };
+int form_of(const Q4View &m, int C) {
+    if (C > 16) return SHARED;
+    if (C * m.k_blocks * 256 <= kLdsOperand) return m.n_tiles >= 1024 ? FEW_LDS_WIDE : m.n_tiles >= 256 ? FEW_LDS : FEW_LDS_NARROW;
+    return m.n_tiles >= 1024 ? SHARED : m.n_tiles >= 512 ? FEW_WIDE : FEW;
+}
+int few_tiles(int form) { return form == FEW_LDS_WIDE || form == FEW_WIDE ? 2 : 1; }
+
+// The shared form's blocks: waves per block (one tile of 16 columns each, or two with many operand columns, which halves their way through LDS) and
+// splits of the contraction, by the steps that the fullest CU has to do; a split costs its partial sums and, the first one, a launch (us, 32 columns,
+// 8192 x 10240: 10 waves, four splits 19.2, 8 waves, three 20.1, 16 waves, one 33; 8192 x 57344: 14 waves 57, 16 waves 59, 8 waves 67;
+// 48 columns, 4096 x 50304: one tile 45, two tiles 43; 28672 x 8192, 40 columns: 47 / 43).
+struct SharedShape { int tiles, waves, splits; };
+SharedShape shared_shape(const Q4View &m, int C) {
+    const int tiles = C > 48 || (C > 32 && m.n_tiles >= 512) ? 2 : 1;
+    SharedShape best{tiles, 8, 1};
+    float least = INFINITY;
+    for (int w = 8; w <= (tiles == 2 ? 8 : 16); ++w)
+        for (int sp = 1; sp <= 16 && sp * 4 <= std::max(4, m.k_blocks); ++sp) {
+            const int blocks = (m.n_tiles + w * tiles - 1) / (w * tiles) * sp, steps = (m.k_blocks + sp - 1) / sp;
+            const float cost = (float)((blocks + 255) / 256) * w * (steps + 4) * (1.0f + (sp > 1 ? 0.1f + 0.01f * sp : 0.f));
+            if (cost < least) { least = cost; best = SharedShape{tiles, w, sp}; }
+        }
+    const int per = (m.k_blocks + best.splits - 1) / best.splits;
+    best.splits = (m.k_blocks + per - 1) / per;
+    return best;
 }
 
 template <bool F16, int ST, int FL>
-void launch_few(const Q4View &m, const h16_t *x, int64_t ldx, int C, int T, const Q4Out &out, hipStream_t s) {
-    if (m.n_tiles >= kQ4PairTiles) hipLaunchKernelGGL((q4_few_kernel<F16, ST, 2, FL>), dim3((m.n_tiles + 1) / 2), dim3(512), 0, s, m, x, ldx, C, T, out);
-    else hipLaunchKernelGGL((q4_few_kernel<F16, ST, 1, FL>), dim3(m.n_tiles), dim3(512), 0, s, m, x, ldx, C, T, out);
+void launch_few(const Q4View &m, int form, const h16_t *x, int64_t ldx, int C, int T, const Q4Out &out, hipStream_t s) {
+    const dim3 grid((m.n_tiles + few_tiles(form) - 1) / few_tiles(form));
+    const size_t lds = (size_t)C * m.k_blocks * 256;
+    if (form == FEW_LDS_WIDE) hipLaunchKernelGGL((q4_few_kernel<F16, ST, 2, FL, 4, 2, true>), grid, dim3(256), lds, s, m, x, ldx, C, T, out);
+    else if (form == FEW_LDS) hipLaunchKernelGGL((q4_few_kernel<F16, ST, 1, FL, 4, FL == 1 ? 2 : 4, true>), grid, dim3(256), lds, s, m, x, ldx, C, T, out);
+    else if (form == FEW_LDS_NARROW) hipLaunchKernelGGL((q4_few_kernel<F16, ST, 1, FL, 8, FL == 1 ? 2 : 4, true>), grid, dim3(512), lds, s, m, x, ldx, C, T, out);
+    else if (form == FEW_WIDE) hipLaunchKernelGGL((q4_few_kernel<F16, ST, 2, FL, 8, 2, false>), grid, dim3(512), 0, s, m, x, ldx, C, T, out);
+    else hipLaunchKernelGGL((q4_few_kernel<F16, ST, 1, FL, 4, FL == 1 ? 2 : 4, false>), grid, dim3(256), 0, s, m, x, ldx, C, T, out);
 }
 template <bool F16, int ST, int NB, int FL>
 void launch_shared(const Q4View &m, const h16_t *x, int64_t ldx, int C, int T, const Q4Out &out, float *part, hipStream_t s) {
-    const int ut = shared_tiles(m, NB), splits = shared_splits(m, ut), per = (m.k_blocks + splits - 1) / splits, used = (m.k_blocks + per - 1) / per;
-    const bool own = used == 1 && C == T && out.best_val == nullptr;
-    const dim3 grid((m.n_tiles + 8 * ut - 1) / (8 * ut), used);
-    if constexpr (NB <= 4) {
-        if (ut == 2) hipLaunchKernelGGL((q4_shared_kernel<F16, ST, NB, 2, FL>), grid, dim3(512), 0, s, m, x, ldx, C, T, out, per, own ? nullptr : part);
+    const SharedShape sh = shared_shape(m, C);
+    const int per = (m.k_blocks + sh.splits - 1) / sh.splits;
+    const bool own = sh.splits == 1 && C == T && out.best_val == nullptr;
+    const dim3 grid((m.n_tiles + sh.waves * sh.tiles - 1) / (sh.waves * sh.tiles), sh.splits);
+    if constexpr (NB > 2) {
+        if (sh.tiles == 2) hipLaunchKernelGGL((q4_shared_kernel<F16, ST, NB, 2, FL>), grid, dim3(64 * sh.waves), 0, s, m, x, ldx, C, T, out, per, own ? nullptr : part);
     }
-    if (ut == 1) hipLaunchKernelGGL((q4_shared_kernel<F16, ST, NB, 1, FL>), grid, dim3(512), 0, s, m, x, ldx, C, T, out, per, own ? nullptr : part);
-    if (!own) hipLaunchKernelGGL(q4_finish_kernel, dim3((m.n_tiles * 16 + 1023) / 1024, T), dim3(256), 0, s, m, part, used, C, T, out);
+    if constexpr (NB < 4) {
+        if (sh.tiles == 1) hipLaunchKernelGGL((q4_shared_kernel<F16, ST, NB, 1, FL>), grid, dim3(64 * sh.waves), 0, s, m, x, ldx, C, T, out, per, own ? nullptr : part);
+    }
+    if (!own) hipLaunchKernelGGL(q4_finish_kernel, dim3((m.n_tiles * 16 + 1023) / 1024, T), dim3(256), 0, s, m, part, sh.splits, C, T, out);
 }
 template <bool F16, int ST, int FL>
 void launch_cols(const Q4View &m, const h16_t *x, int64_t ldx, int C, int T, const Q4Out &out, float *part, hipStream_t s) {
-    if (C <= 16) launch_few<F16, ST, FL>(m, x, ldx, C, T, out, s);
+    const int form = form_of(m, C);
+    if (form != SHARED) launch_few<F16, ST, FL>(m, form, x, ldx, C, T, out, s);
+    else if (C <= 16) launch_shared<F16, ST, 1, FL>(m, x, ldx, C, T, out, part, s);
     else if (C <= 32) launch_shared<F16, ST, 2, FL>(m, x, ldx, C, T, out, part, s);
-    else if (C <= 64) launch_shared<F16, ST, 4, FL>(m, x, ldx, C, T, out, part, s);
-    else launch_shared<F16, ST, 6, FL>(m, x, ldx, C, T, out, part, s);
+    else if (C <= 48) launch_shared<F16, ST, 3, FL>(m, x, ldx, C, T, out, part, s);
+    else launch_shared<F16, ST, 4, FL>(m, x, ldx, C, T, out, part, s);
 }
 template <bool F16, int ST>
 void launch_type(const Q4View &m, const h16_t *x, int64_t ldx, int C, int T, const Q4Out &out, float *part, hipStream_t s) {
@@ -461,29 +669,40 @@ void launch_type(const Q4View &m, const h16_t *x, int64_t ldx, int C, int T, con
 
 }  // namespace
 
-size_t q4_part_floats(const Q4View &m) { return (size_t)std::max(shared_splits(m, 1), shared_splits(m, 2)) * 3 * kQ4PartRows * m.n_tiles * 16; }
+size_t q4_part_floats(const Q4View &m) {
+    size_t most = 0;
+    for (int c = 1; c <= kQ4Rows; ++c)
+        if (form_of(m, c) == SHARED) most = std::max(most, (size_t)shared_shape(m, c).splits * c * m.n_tiles * 16);
+    return most;
+}
 int q4_best_units(const Q4View &m, int T) {
-    if (3 * T > 16) return (m.n_tiles * 16 + 1023) / 1024;
-    return m.n_tiles >= kQ4PairTiles ? (m.n_tiles + 1) / 2 : m.n_tiles;
+    const int form = form_of(m, 2 * T);
+    return form == SHARED ? (m.n_tiles * 16 + 1023) / 1024 : (m.n_tiles + few_tiles(form) - 1) / few_tiles(form);
 }
-void launch_q4(const Q4View &m, bool parts, const h16_t *x, int64_t ldx, int T, const Q4Out &out, float *part, hipStream_t s) {
-    const int C = parts ? 3 * T : T;
-    if (m.type == HX_T_F32) launch_type<false, HX_T_F32>(m, x, ldx, C, T, out, part, s);
-    else if (m.type == HX_T_BF16) launch_type<false, HX_T_BF16>(m, x, ldx, C, T, out, part, s);
-    else if (parts) launch_type<false, HX_T_F16>(m, x, ldx, C, T, out, part, s);
-    else launch_type<true, HX_T_F16>(m, x, ldx, C, T, out, part, s);
+void launch_q4(const Q4View &m, const h16_t *x, int64_t ldx, int T, const Q4Out &out, float *part, hipStream_t s) {
+    const int C = out.exps != nullptr ? 2 * T : T;
+    if (m.type == HX_T_F32) launch_type<true, HX_T_F32>(m, x, ldx, C, T, out, part, s);
+    else if (m.type == HX_T_F16) launch_type<true, HX_T_F16>(m, x, ldx, C, T, out, part, s);
+    else if (m.f16) launch_type<true, HX_T_BF16>(m, x, ldx, C, T, out, part, s);
+    else launch_type<false, HX_T_BF16>(m, x, ldx, C, T, out, part, s);
 }
-void launch_q4_parts(int type, const void *x, const void *x2, int64_t ldx, const float *g, float eps, int K, int Kp, int T, h16_t *out, hipStream_t s) {
-    if (type == HX_T_F32) hipLaunchKernelGGL(q4_parts_kernel<HX_T_F32>, dim3(T), dim3(1024), 0, s, x, x2, ldx, g, eps, K, Kp, T, out);
-    else if (type == HX_T_BF16) hipLaunchKernelGGL(q4_parts_kernel<HX_T_BF16>, dim3(T), dim3(1024), 0, s, x, x2, ldx, g, eps, K, Kp, T, out);
-    else hipLaunchKernelGGL(q4_parts_kernel<HX_T_F16>, dim3(T), dim3(1024), 0, s, x, x2, ldx, g, eps, K, Kp, T, out);
+void launch_q4_parts(int type, const void *x, const void *x2, int64_t ldx, const float *g, float eps, int K, int Kp, int T, h16_t *out, int32_t *exps, hipStream_t s) {
+    const size_t es = type == HX_T_F32 ? 4 : 2;
+    const bool pieces = ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(x2)) % 16 == 0) && (ldx * es) % 16 == 0 && K % 8 == 0;
+#define HX_PARTS(TY, VV) hipLaunchKernelGGL((q4_parts_kernel<TY, VV>), dim3(T), dim3(1024), 0, s, x, x2, ldx, g, eps, K, Kp, T, out, exps)
+    if (type == HX_T_F32) { if (pieces) HX_PARTS(HX_T_F32, true); else HX_PARTS(HX_T_F32, false); }
+    else if (type == HX_T_BF16) { if (pieces) HX_PARTS(HX_T_BF16, true); else HX_PARTS(HX_T_BF16, false); }
+    else { if (pieces) HX_PARTS(HX_T_F16, true); else HX_PARTS(HX_T_F16, false); }
+#undef HX_PARTS
 }
 void launch_q4_copy(const h16_t *x, int64_t ldx, int K, int Kp, int T, h16_t *out, hipStream_t s) {
     hipLaunchKernelGGL(q4_copy_kernel, dim3(T), dim3(256), 0, s, x, ldx, K, Kp, out);
 }
-void launch_q4_pack(const Q4View &m, const uint8_t *w4, const void *scales, const uint8_t *zeros, int64_t ld, int K, int n0, hipStream_t s) {
+void launch_q4_pack(const Q4View &m, const uint8_t *w4, const void *scales, const uint8_t *zeros, int64_t ld, int K, int group, int n0, hipStream_t s) {
     const size_t words = (size_t)m.k_blocks * m.n_tiles * 256, cells = (size_t)m.scale_rows * m.n_tiles * 16;
-    hipLaunchKernelGGL(q4_pack_kernel, dim3((unsigned)((words + 255) / 256)), dim3(256), 0, s, w4, ld / 2, K, n0, m.n_valid, m.n_tiles, m.k_blocks, const_cast<uint32_t *>(static_cast<const uint32_t *>(m.w)));
-    hipLaunchKernelGGL(q4_pack_scales_kernel, dim3((unsigned)((cells + 255) / 256)), dim3(256), 0, s, scales, m.type == HX_T_F32 ? 4 : 2, zeros, ld, (K + m.group - 1) / m.group,
-                       m.scale_rows, n0, m.n_valid, m.n_tiles * 16, const_cast<void *>(m.scales), const_cast<uint8_t *>(m.zeros));
+    hipLaunchKernelGGL(q4_pack_kernel, dim3((unsigned)((words + 255) / 256)), dim3(256), 0, s, w4, ld / 2, K, n0, m.n_valid, m.n_tiles, m.k_blocks, m.f16 ? 6 : 3,
+                       const_cast<uint32_t *>(static_cast<const uint32_t *>(m.w)));
+    hipLaunchKernelGGL(q4_pack_scales_kernel, dim3((unsigned)((cells + 255) / 256)), dim3(256), 0, s, scales, m.type == HX_T_F32 ? 4 : 2, zeros, ld, (K + group - 1) / group,
+                       m.scale_rows, m.zeros_row != 0 ? m.scale_rows : 1, std::max(1, group / 128), n0, m.n_valid, m.n_tiles * 16, const_cast<void *>(m.scales),
+                       const_cast<uint8_t *>(m.zeros));
 }

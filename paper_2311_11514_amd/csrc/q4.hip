@@ -10,35 +10,36 @@ static_assert((int)HX_T_F32 == (int)HEXGEN_F32 && (int)HX_T_BF16 == (int)HEXGEN_
 bool q4_group_ok(int group) { return group == 32 || group == 64 || (group > 0 && group % 128 == 0); }
 
 void q4_free(Q4Store *q) {
-    void *ptrs[] = {const_cast<void *>(q->v.w), const_cast<void *>(q->v.scales), const_cast<uint8_t *>(q->v.zeros), q->planes, q->part};
+    void *ptrs[] = {const_cast<void *>(q->v.w), const_cast<void *>(q->v.scales), const_cast<uint8_t *>(q->v.zeros), q->planes, q->exps, q->part};
     for (void *p : ptrs)
         if (p) (void)hipFree(p);
     *q = Q4Store();
 }
 
 namespace {
-hexgen_status_t load_into(Q4Store *q, hexgen_dtype_t dtype, int n_in, int total, int n0, int n, int group, const void *w4, const void *scales,
+hexgen_status_t load_into(Q4Store *q, hexgen_dtype_t dtype, bool parts, int n_in, int total, int n0, int n, int group, const void *w4, const void *scales,
                           const void *zeros, void **tmp) {
     const size_t es = dtype == HEXGEN_F32 ? 4 : 2, groups = ((size_t)n_in + group - 1) / group;
     Q4View &v = q->v;
     q->n_in = n_in;
     v.type = (int)dtype;
-    v.group = group;
+    v.f16 = parts || dtype == HEXGEN_F16;
+    v.group = std::min(group, 128);
     v.n_valid = n;
     v.n_tiles = (n + 15) / 16;
     v.k_blocks = (n_in + 127) / 128;
-    v.scale_rows = ((v.k_blocks * 128 - 1) / group) + 1;
+    v.scale_rows = v.k_blocks * (128 / v.group);
+    v.zeros_row = zeros != nullptr ? v.n_tiles * 16 : 0;
     void *p = nullptr;
     HX_HIP(hipMalloc(&p, (size_t)v.k_blocks * v.n_tiles * 1024));
     v.w = p;
     HX_HIP(hipMalloc(&p, (size_t)v.scale_rows * v.n_tiles * 16 * es));
     v.scales = p;
-    if (zeros != nullptr) {
-        HX_HIP(hipMalloc(&p, (size_t)v.scale_rows * v.n_tiles * 16));
-        v.zeros = static_cast<uint8_t *>(p);
-    }
-    const size_t planes = (size_t)q->padded() * std::max(kQ4Rows, 3 * kQ4PartRows);
-    HX_HIP(hipMalloc(reinterpret_cast<void **>(&q->planes), planes * sizeof(h16_t)));
+    HX_HIP(hipMalloc(&p, (size_t)(zeros != nullptr ? v.scale_rows : 1) * v.n_tiles * 16));
+    v.zeros = static_cast<uint8_t *>(p);
+    static_assert(kQ4Rows == 2 * kQ4PartRows, "one size of planes");
+    HX_HIP(hipMalloc(reinterpret_cast<void **>(&q->planes), (size_t)q->padded() * kQ4Rows * sizeof(h16_t)));
+    HX_HIP(hipMalloc(reinterpret_cast<void **>(&q->exps), kQ4PartRows * sizeof(int32_t)));
     HX_HIP(hipMalloc(reinterpret_cast<void **>(&q->part), q4_part_floats(v) * sizeof(float)));
     const size_t wb = (size_t)n_in * (total / 2), sb = groups * total * es, zb = zeros != nullptr ? groups * (total / 2) : 0;
     const size_t s_at = (wb + 255) / 256 * 256, z_at = s_at + (sb + 255) / 256 * 256;
@@ -47,18 +48,18 @@ hexgen_status_t load_into(Q4Store *q, hexgen_dtype_t dtype, int n_in, int total,
     HX_HIP(hipMemcpy(t, w4, wb, hipMemcpyDefault));
     HX_HIP(hipMemcpy(t + s_at, scales, sb, hipMemcpyDefault));
     if (zeros != nullptr) HX_HIP(hipMemcpy(t + z_at, zeros, zb, hipMemcpyDefault));
-    launch_q4_pack(v, t, t + s_at, zeros != nullptr ? t + z_at : nullptr, total, n_in, n0, nullptr);
+    launch_q4_pack(v, t, t + s_at, zeros != nullptr ? t + z_at : nullptr, total, n_in, group, n0, nullptr);
     HX_HIP(hipGetLastError());
     HX_HIP(hipDeviceSynchronize());
     return HEXGEN_OK;
 }
 }  // namespace
 
-hexgen_status_t q4_load(Q4Store *q, hexgen_dtype_t dtype, int n_in, int total, int n0, int n, int group, const void *w4, const void *scales, const void *zeros) {
+hexgen_status_t q4_load(Q4Store *q, hexgen_dtype_t dtype, bool parts, int n_in, int total, int n0, int n, int group, const void *w4, const void *scales, const void *zeros) {
     HX_HIP(hipDeviceSynchronize());
     q4_free(q);
     void *tmp = nullptr;
-    const hexgen_status_t rc = load_into(q, dtype, n_in, total, n0, n, group, w4, scales, zeros, &tmp);
+    const hexgen_status_t rc = load_into(q, dtype, parts, n_in, total, n0, n, group, w4, scales, zeros, &tmp);
     if (tmp) (void)hipFree(tmp);
     if (rc != HEXGEN_OK) q4_free(q);
     return rc;
@@ -95,7 +96,7 @@ void hexgen_q4_destroy(hexgen_q4_t *q) {
 
 hexgen_status_t hexgen_q4_load(hexgen_q4_t *q, const void *w4, const void *scales, const void *zeros) {
     if (!q || !w4 || !scales) return HEXGEN_ERR_INVALID_ARG;
-    return q4_load(&q->store, q->dtype, q->n_in, q->n_out, 0, q->n_out, q->group, w4, scales, zeros);
+    return q4_load(&q->store, q->dtype, q->dtype == HEXGEN_F32, q->n_in, q->n_out, 0, q->n_out, q->group, w4, scales, zeros);
 }
 
 hexgen_status_t hexgen_q4_project(hexgen_q4_t *q, const void *x, int64_t ldx, int n_rows, void *out, void *stream) {
@@ -112,14 +113,14 @@ hexgen_status_t hexgen_q4_project(hexgen_q4_t *q, const void *x, int64_t ldx, in
     for (int r0 = 0; r0 < n_rows; r0 += chunk) {
         const int n = std::min(chunk, n_rows - r0);
         const unsigned char *xr = static_cast<const unsigned char *>(x) + (size_t)r0 * ldx * es;
-        const Q4Out o{static_cast<unsigned char *>(out) + (size_t)r0 * q->n_out * es, (int)q->dtype, nullptr, nullptr};
+        const Q4Out o{static_cast<unsigned char *>(out) + (size_t)r0 * q->n_out * es, (int)q->dtype, nullptr, nullptr, parts ? st.exps : nullptr};
         if (direct) {
-            launch_q4(st.v, false, reinterpret_cast<const h16_t *>(xr), ldx, n, o, st.part, s);
+            launch_q4(st.v, reinterpret_cast<const h16_t *>(xr), ldx, n, o, st.part, s);
             continue;
         }
-        if (parts) launch_q4_parts((int)q->dtype, xr, nullptr, ldx, nullptr, 0.f, q->n_in, st.padded(), n, st.planes, s);
+        if (parts) launch_q4_parts((int)q->dtype, xr, nullptr, ldx, nullptr, 0.f, q->n_in, st.padded(), n, st.planes, st.exps, s);
         else launch_q4_copy(reinterpret_cast<const h16_t *>(xr), ldx, q->n_in, st.padded(), n, st.planes, s);
-        launch_q4(st.v, parts, st.planes, st.padded(), n, o, st.part, s);
+        launch_q4(st.v, st.planes, st.padded(), n, o, st.part, s);
     }
     HX_HIP(hipGetLastError());
     return HEXGEN_OK;
