@@ -132,40 +132,47 @@ def _i32(seq: Optional[Sequence[int]]):
     return (C.c_int32 * len(seq))(*[int(v) for v in seq])
 
 
+# the current stream's handle of a device without a Stream object around it (which takes longer to make than a launch), where torch has that
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream_handle(stream: Optional[torch.cuda.Stream]) -> Optional[int]:
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device()) or None
     s = stream if stream is not None else torch.cuda.current_stream()
     return s.cuda_stream or None
 
 
-def _empty(shape, dtype, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
-    """A result of a call on `stream`, taken from that stream's memory."""
+def _empty_like_of(t: torch.Tensor, shape, dtype, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """A result of a call on `stream` beside the tensor t, taken from that stream's memory."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device="cuda")
+        return torch.empty(shape, dtype=dtype, device=t.device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device="cuda")
+        return torch.empty(shape, dtype=dtype, device=t.device)
 
 
-def _device_tensor(t: torch.Tensor, name: str, shape, dtype) -> torch.Tensor:
+def _device_tensor(t: torch.Tensor, name: str, shape, dtype) -> None:
     """A tensor that is handed on as a dense device pointer: checked here, where its shape, type and place are known."""
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous {tuple(shape)} tensor of {dtype} is wanted, got {tuple(t.shape)} of {t.dtype}, strides {tuple(t.stride())}")
-    return _on_device(t, name)
+    _on_device(t, name)
 
 
-def _on_device(t: torch.Tensor, name: str) -> torch.Tensor:
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+def _on_device(t: torch.Tensor, name: str) -> None:
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
         raise ValueError(f"{name}: on {t.device}, not on the current GPU")
-    return t
 
 
 def _rows_of_heads(t: torch.Tensor, name: str, rows: int, heads: int, d: int, dtype) -> int:
     """Elements between the rows of a [rows, heads, d] or [rows, heads * d] tensor whose rows are dense."""
-    if tuple(t.shape) not in ((rows, heads, d), (rows, heads * d)) or t.dtype != dtype:
+    flat = t.dim() == 2
+    if t.shape != ((rows, heads * d) if flat else (rows, heads, d)) or t.dtype != dtype:
         raise ValueError(f"{name}: a ({rows}, {heads}, {d}) tensor of {dtype} is wanted, got {tuple(t.shape)} of {t.dtype}")
-    if t.stride(-1) != 1 or (t.dim() == 3 and heads > 1 and t.stride(1) != d):
-        raise ValueError(f"{name}: the elements of a row have to be dense, got strides {tuple(t.stride())}")
+    stride = t.stride()
+    if stride[-1] != 1 or (not flat and heads > 1 and stride[1] != d):
+        raise ValueError(f"{name}: the elements of a row have to be dense, got strides {stride}")
     _on_device(t, name)
-    return t.stride(0) if rows > 1 else heads * d
+    return stride[0] if rows > 1 else heads * d
 
 
 def _torch_dtype(dtype: int):
@@ -333,7 +340,7 @@ class KVCache:
         ldk = _rows_of_heads(k, "k", rows, st.hkv_l, st.head_dim, td)
         ldv = _rows_of_heads(v, "v", rows, st.hkv_l, st.head_dim, td)
         if out is None:
-            out = _empty((rows, st.hq_l, st.head_dim), td, stream)
+            out = _empty_like_of(q, (rows, st.hq_l, st.head_dim), td, stream)
         else:
             _device_tensor(out, "out", (rows, st.hq_l, st.head_dim), td)
         _check(lib.hexgen_kv_tree_attention(self.handle, layer, tree.handle, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
@@ -377,9 +384,9 @@ class Tree:
         """hexgen_tree_accept: draft, chosen int32 [rows] -> (kept [batch], path [rows], tokens [rows]), int32 on the device."""
         for name, t in (("draft", draft), ("chosen", chosen)):
             _device_tensor(t, name, (self.rows,), torch.int32)
-        kept, path, tokens = (_empty((n,), torch.int32, stream) for n in (self.batch, self.rows, self.rows))
-        _check(lib.hexgen_tree_accept(self.handle, _ptr(draft), _ptr(chosen), _ptr(kept), _ptr(path), _ptr(tokens), _stream_handle(stream)),
-               "hexgen_tree_accept")
+        kept, path, tokens = _empty_like_of(draft, (self.batch + 2 * self.rows,), torch.int32, stream).split((self.batch, self.rows, self.rows))
+        _check(lib.hexgen_tree_accept(self.handle, draft.data_ptr(), chosen.data_ptr(), kept.data_ptr(), path.data_ptr(), tokens.data_ptr(),
+                                      _stream_handle(stream)), "hexgen_tree_accept")
         return kept, path, tokens
 
 
@@ -431,7 +438,7 @@ class Q4Matrix:
             raise ValueError(f"x: a (rows, {self.n_in}) tensor of {td} with dense rows is wanted, got {tuple(x.shape)} of {x.dtype}, strides {tuple(x.stride())}")
         _on_device(x, "x")
         if out is None:
-            out = _empty((rows, self.n_out), td, stream)
+            out = _empty_like_of(x, (rows, self.n_out), td, stream)
         else:
             _device_tensor(out, "out", (rows, self.n_out), td)
         _check(lib.hexgen_q4_project(self.handle, x.data_ptr(), x.stride(0) if rows > 1 else self.n_in, rows, out.data_ptr(), _stream_handle(stream)),

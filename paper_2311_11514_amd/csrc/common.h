@@ -164,6 +164,37 @@ __device__ inline void split_pack2(float a, float b, uint32_t &phi, uint32_t &pl
 // a launch has a few hundred blocks).
 __device__ __forceinline__ void dev_store(float *p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ float dev_load(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// two floats at an 8-byte aligned address
+__device__ __forceinline__ void dev_store2(float *p, float a, float b) {
+    const unsigned long long v = (unsigned long long)__float_as_uint(a) | (unsigned long long)__float_as_uint(b) << 32;
+    __hip_atomic_store(reinterpret_cast<unsigned long long *>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 dev_load2(const float *p) {
+    const unsigned long long v = __hip_atomic_load(reinterpret_cast<const unsigned long long *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return float2{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
+}
+// Every thread of a block whose device-scope stores are done: counts the block at `arrived`, which `blocks` blocks share, and says whether it was
+// the last one; that one leaves the counter at zero for the next launch.  `flag`: LDS.
+__device__ __forceinline__ bool tree_arrive(unsigned *arrived, int blocks, int *flag) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // this lane's stores have completed ...
+    __syncthreads();                                      // ... and so have every other lane's of the block ...
+    if (threadIdx.x == 0) {                               // ... before the block counts itself
+        const unsigned before = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *flag = before + 1 == (unsigned)blocks;
+        if (*flag) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    return *flag != 0;
+}
+// largest and sum of a lane's and its partner's value in the other half of the wave: the swap leaves one half's values in each register
+__device__ __forceinline__ float max_halves(float v) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float sum_halves(float v) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
 __device__ inline float wave_sum(float v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);

@@ -186,27 +186,34 @@ struct TreeView {
     const uint32_t *mask;
     int mask_words, rows, batch, max_n;
 };
-// The context of a sequence is cut into runs of chunk tiles of 32 positions, or longer ones where nsplit runs would not reach its end.
-struct TreeSplit {
+// The tree's keys and values where they are not in the cache yet: plain rows, ldk / ldv elements apart; k == NULL: they are
+struct TreeIn {
+    const void *k, *v;
+    int64_t ldk, ldv;
+};
+constexpr int kTreeOrdered = 64;          // sequences whose order of dispatch a plan holds
+// How a launch is laid out.  The context of a sequence is cut into runs of chunk tiles of 32 positions, or longer ones where nsplit runs would
+// not reach its end.
+struct TreePlan {
+    int row_groups;                       // 16 bits: groups of 32 query rows that share a block's tiles, 1, 2 or 4
     int nsplit, chunk;
     float *part_o, *part_ml;              // [nsplit][rows][hq][d] and [nsplit][rows][hq][2] (maximum, sum)
+    unsigned *arrived;                    // per (sequence, kv head, block of rows): runs that have finished; zero between launches
+    uint8_t order[kTreeOrdered];          // the nth sequence to be dispatched
 };
+inline int tree_row_blocks(int max_n, int G, int rows) { return (max_n * G + rows - 1) / rows; }
 // where the 16-bit attention leaves its rows: plain, or as the operand of the decode / prefill projections behind it
 enum { TREE_OUT_ROWS = 0, TREE_OUT_ACT = 1, TREE_OUT_FRAG = 2 };
 struct TreeOut {
     int mode, rows, width;                // width = hq * d
     void *o;
 };
-// groups of 32 query rows that share the tiles of a block: as many as the largest tree fills, 1, 2 or 4
-inline int tree_row_groups(int max_n, int G) { return max_n * G <= 32 ? 1 : max_n * G <= 64 ? 2 : 4; }
 void launch_tree_accept(const TreeView &tv, const int32_t *draft, const int32_t *chosen, int32_t *kept, int32_t *path, int32_t *tokens, hipStream_t s);
 void launch_tree_advance(int32_t *lens, const int32_t *kept, int batch, hipStream_t s);      // lens += kept
-void f32_launch_tree_append(const float *k, int64_t ldk, const float *v, int64_t ldv, float *kc, float *vc, KvGeom kg, const TreeView &tv,
-                            const int32_t *lens, hipStream_t s);
 void f32_launch_tree_rope_append(const float *qkv, int hq_l, KvGeom kg, const TreeView &tv, const int32_t *lens, const float *cos_tab,
                                  const float *sin_tab, float *q, float *kc, float *vc, hipStream_t s);
-void f32_launch_tree_attn(const float *q, int64_t ldq, const float *kc, const float *vc, KvGeom kg, int hq_l, const TreeView &tv,
-                          const int32_t *lens, const TreeSplit &sp, float *o, hipStream_t s);
+void f32_launch_tree_attn(const float *q, int64_t ldq, const TreeIn &in, float *kc, float *vc, KvGeom kg, int hq_l, const TreeView &tv, const int32_t *lens,
+                          const TreePlan &tp, float *o, hipStream_t s);
 void f32_launch_tree_keep(float *kc, float *vc, int64_t layer_stride, int layers, KvGeom kg, int batch, const int32_t *lens, const int32_t *cu,
                           const int32_t *kept, const int32_t *path, hipStream_t s);
 

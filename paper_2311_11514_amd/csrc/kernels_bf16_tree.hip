@@ -4,6 +4,8 @@
 // The G query heads of a kv head and the n nodes of a sequence's tree make R = n G query rows (row r: node r / G, head r % G) that
 // read the same K and V, so every tile of the cache serves all of them: with 8 heads and 16 nodes the attention has 128 flops
 // for every byte of the cache, between the decode kernels (8) and prefill.
+#include <type_traits>
+
 #include "kernels.h"
 #include "kvlayout.h"
 
@@ -12,30 +14,6 @@
 namespace HX_NS {
 
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
-
-// ---- appending ----------------------------------------------------------------------------------------------------
-// rows of a user's projection -> cache slots len + index; a thread takes 8 elements of one head of K and of V
-__global__ __launch_bounds__(256) void tree_append_kernel(const h16_t *__restrict__ k, int64_t ldk, const h16_t *__restrict__ v, int64_t ldv,
-                                                          h16_t *__restrict__ kc, h16_t *__restrict__ vc, KvGeom kg, TreeView tv,
-                                                          const int32_t *__restrict__ lens) {
-    const int per_row = kg.hkv_l * kg.d / 8, idx = blockIdx.x * 256 + threadIdx.x;
-    if (idx >= tv.rows * per_row) return;
-    const int t = idx / per_row, e = (idx - t * per_row) * 8, c = e / kg.d, dd = e - c * kg.d;
-    const TreeRow row = tv.row[t];
-    const int slot = lens[row.seq] + row.index;
-    if (slot >= kg.smax) return;
-    const size_t slab = (size_t)row.seq * kg.seq_stride + (size_t)c * kg.smax * kg.d;
-    *reinterpret_cast<uint4 *>(kc + slab + kv_k_offset(slot, dd, kg.d)) = *reinterpret_cast<const uint4 *>(k + (size_t)t * ldk + e);
-    union { uint4 u; h16_t x[8]; } w;
-    w.u = *reinterpret_cast<const uint4 *>(v + (size_t)t * ldv + e);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) vc[slab + kv_v_offset(slot, dd + i, kg.d)] = w.x[i];
-}
-void launch_tree_append(const h16_t *k, int64_t ldk, const h16_t *v, int64_t ldv, h16_t *kc, h16_t *vc, KvGeom kg, const TreeView &tv,
-                        const int32_t *lens, hipStream_t s) {
-    const int n = tv.rows * (kg.hkv_l * kg.d / 8);
-    hipLaunchKernelGGL(tree_append_kernel, dim3((n + 255) / 256), dim3(256), 0, s, k, ldk, v, ldv, kc, vc, kg, tv, lens);
-}
 
 // The stage's fused projection, raw fp32 [rows][N] -> rotary embedding at len + depth, q as plain rows, k and v into the cache.
 // The projection's columns are in the order of its packed tiles: 16 columns hold elements 8 tl .. 8 tl + 7 of a head and those half a
@@ -119,7 +97,131 @@ __device__ __forceinline__ bool any_odd(h16x8 v) {
     return odd;
 }
 
-// A block of four waves takes 32 RW query rows of one (sequence, kv head) and a run of 32-position tiles; RW groups of 32 rows times
+// Which of the 32 positions of tile t a node attends: bit p for position 32 t + p; the tile reaches the tree's slots (32 t + 31 >= len)
+__device__ __forceinline__ uint32_t tree_sees(const uint32_t *mask, int mask_words, int t, int len) {
+    const int rel = 32 * t - len;                            // index in the tree of the tile's first slot; negative: context before it
+    if (rel < 0) return (mask[0] << -rel) | ((1u << -rel) - 1);
+    const int w = rel >> 5, sh = rel & 31;
+    const uint32_t a = w < mask_words ? mask[w] : 0u, b = w + 1 < mask_words ? mask[w + 1] : 0u;
+    return sh == 0 ? a : (a >> sh) | (b << (32 - sh));
+}
+
+// The running softmax over one tile's scores (sc becomes the weights): m, l and the factor for what was summed up before
+__device__ __forceinline__ float tree_softmax(floatx16 &sc, float &m, float &lsum, float scale_log2e) {
+    float mx = NEG_INF;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) mx = fmaxf(mx, sc[x]);
+    const float m_new = fmaxf(m, max_halves(mx));
+    const float base = m_new == NEG_INF ? 0.f : m_new;       // a row that has seen nothing yet: weights 0, no NaN
+    const float alpha = __builtin_amdgcn_exp2f((m - base) * scale_log2e);
+    m = m_new;
+    float ps = 0.f;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+        // (the difference first: scores near the type's lowest value would not cancel in a multiply-add with -base * scale)
+        sc[x] = __builtin_amdgcn_exp2f((sc[x] - base) * scale_log2e);
+        ps += sc[x];
+    }
+    lsum = lsum * alpha + ps;
+    return alpha;
+}
+// P for k-groups hl (quads 0, 2) and 2 + hl (quads 1, 3) of the second product
+union TreeP { uint32_t u[4]; h16x8 v; };
+__device__ __forceinline__ void tree_pack(const floatx16 &sc, TreeP &p0, TreeP &p1) {
+    p0.u[0] = pack_h16x2(sc[0], sc[1]);   p0.u[1] = pack_h16x2(sc[2], sc[3]);
+    p0.u[2] = pack_h16x2(sc[8], sc[9]);   p0.u[3] = pack_h16x2(sc[10], sc[11]);
+    p1.u[0] = pack_h16x2(sc[4], sc[5]);   p1.u[1] = pack_h16x2(sc[6], sc[7]);
+    p1.u[2] = pack_h16x2(sc[12], sc[13]); p1.u[3] = pack_h16x2(sc[14], sc[15]);
+}
+// O^T += V^T . P^T element by element, over the positions a row attends: for tiles with values that are not finite.  vt: the tile in LDS
+template <int DB>
+__device__ __forceinline__ void tree_slow_tile(const h16_t *vt, const floatx16 &sc, uint32_t sees, int lane, floatx16 (&oacc)[DB]) {
+    const int hl = lane >> 5;
+    for (int pp = 0; pp < 32; ++pp) {
+        float w = 0.f;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) w = x == 4 * (pp >> 3) + (pp & 3) ? sc[x] : w;
+        w = __shfl(w, (lane & 31) + 32 * ((pp >> 2) & 1), 64);
+        if (!((sees >> pp) & 1u)) continue;
+        const int at = (pp & 3) + 4 * (pp >> 4) + 8 * 16 * ((pp & 15) >> 2);    // kvlayout.h: position pp of element 0 of a V tile
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                const int dd = 32 * db + 8 * (x >> 2) + 4 * hl + (x & 3);
+                oacc[db][x] = fmaf(w, h16_to_f32(vt[(dd >> 4) * 512 + (dd & 15) * 8 + at]), oacc[db][x]);
+            }
+    }
+}
+
+// What a block works on.  Block id = 8 slot + xcd: the row blocks of a run of tiles sit next to each other on one XCD and share the run in
+// its L2; sequences in tp.order, the longest first.
+struct TreeWork {
+    int rb, split, c, seq, row0, n, R, len, nt, per, t0, t1;
+    __device__ __forceinline__ bool find(const KvGeom &kg, int G, int nrb, int rows, const TreeView &tv, const int32_t *lens, const TreePlan &tp) {
+        const int slot = blockIdx.x >> 3;
+        rb = slot % nrb;
+        int combo = (slot / nrb) * 8 + (blockIdx.x & 7);
+        if (combo >= tv.batch * kg.hkv_l * tp.nsplit) return false;
+        split = combo % tp.nsplit;
+        combo /= tp.nsplit;
+        c = combo % kg.hkv_l;
+        const int nth = combo / kg.hkv_l;
+        seq = nth < kTreeOrdered ? tp.order[nth] : nth;
+        row0 = tv.cu[seq];
+        n = tv.cu[seq + 1] - row0;
+        R = n * G;
+        if (rb * rows >= R) return false;
+        len = lens[seq];
+        nt = min((len + n + 31) >> 5, kg.smax >> 5);
+        per = max(tp.chunk, (nt + tp.nsplit - 1) / tp.nsplit);
+        t0 = split * per;
+        t1 = min(t0 + per, nt);
+        return t0 < nt;
+    }
+    __device__ __forceinline__ int runs() const { return (nt + per - 1) / per; }
+};
+
+// The rows of a drafted tree that are not in the cache yet (in.k != NULL): positions len .. len + n - 1 of a tile come from the caller's rows.  The
+// 64 RW threads that share the tile put them into LDS over what the cache held there, in the cache's layout (kvlayout.h), and `append`
+// blocks write them to the cache as well; other blocks of the launch may read those slots meanwhile, but put the same rows over what they got.
+template <int D, int RW>
+__device__ __forceinline__ void tree_patch(h16x8 (*st)[64], const TreeIn &in, int t, int len, int n, int row0, int c, int thread, bool append, h16_t *ks, h16_t *vs) {
+    constexpr int KT = D / 32, P8 = D / 8, PIECES = 32 * 2 * P8 / (64 * RW), BATCH = PIECES < 8 ? PIECES : 8;      // 16-byte pieces of K and V per thread
+    for (int b = 0; b < PIECES; b += BATCH) {
+        uint4 r[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int idx = thread + 64 * RW * (b + i), pos = idx / (2 * P8), piece = idx % (2 * P8), e = c * D + 8 * (piece % P8);
+            const int x = min(max(32 * t + pos - len, 0), n - 1);
+            r[i] = piece < P8 ? *reinterpret_cast<const uint4 *>(static_cast<const h16_t *>(in.k) + (size_t)(row0 + x) * in.ldk + e)
+                              : *reinterpret_cast<const uint4 *>(static_cast<const h16_t *>(in.v) + (size_t)(row0 + x) * in.ldv + e);
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int idx = thread + 64 * RW * (b + i), pos = idx / (2 * P8), piece = idx % (2 * P8), dd = 8 * (piece % P8);
+            const int x = 32 * t + pos - len;
+            if (x < 0 || x >= n) continue;
+            // an offset in a tile pair's K (V) fragments is the same in LDS and, from the pair's first tile on, in the cache
+            if (piece < P8) {
+                const size_t at = kv_k_offset(pos, dd, D);
+                *reinterpret_cast<uint4 *>(reinterpret_cast<h16_t *>(st) + at) = r[i];
+                if (append) *reinterpret_cast<uint4 *>(ks + (size_t)t * 32 * D + at) = r[i];
+            } else {
+                union { uint4 u; h16_t e[8]; } w;
+                w.u = r[i];
+#pragma unroll
+                for (int y = 0; y < 8; ++y) {
+                    const size_t at = kv_v_offset(pos, dd + y, D);
+                    reinterpret_cast<h16_t *>(st + 2 * KT)[at] = w.e[y];
+                    if (append) vs[(size_t)t * 32 * D + at] = w.e[y];
+                }
+            }
+        }
+    }
+}
+
+// Many rows: a block of four waves takes 32 RW query rows of one (sequence, kv head) and a run of 32-position tiles; RW groups of 32 rows times
 // CW = 4 / RW neighbouring tiles a step.  The tiles go from HBM to LDS directly, S steps in flight, and S^T = K . Q^T,
 // O^T = V^T . P^T run on the 32 x 32 x 16 MFMA exactly as in the prefill attention: a lane owns one query row, P stays in its
 // registers and is rounded to the element type for the second product (2^-9 per weight for bf16, against 2^-9 of the rounded result;
@@ -127,12 +229,11 @@ __device__ __forceinline__ bool any_odd(h16x8 v) {
 // Tiles that lie in the context need no mask; of a tile that reaches the tree's slots a lane takes 32 bits of its node's ancestors.
 // A weight of zero times an infinity would be a NaN, so a masked tile with a value that is not finite is multiplied out element
 // by element over what each row attends.
-// A long context is cut into runs of sp.chunk tiles (sp.nsplit at most), whose (m, l, o) tree_merge_kernel joins in their order.
+// Contexts are cut into runs of tp.chunk tiles (tp.nsplit at most), whose (m, l, o) tree_merge_kernel joins: a launch of its own, since joining
+// 128 rows of a run moves 64 KB, which one last block would take longer over.
 template <int D, int RW, int S>
-__global__ __launch_bounds__(256, RW == 1 ? 1 : 2) void tree_attn_kernel(const h16_t *__restrict__ q, int64_t ldq, const h16_t *__restrict__ kc,
-                                                                         const h16_t *__restrict__ vc, KvGeom kg, int hq_l, int G, int nrb,
-                                                                         TreeView tv, const int32_t *__restrict__ lens, TreeSplit sp,
-                                                                         TreeOut out, float scale_log2e) {
+__global__ __launch_bounds__(256, RW == 4 ? 3 : 2) void tree_attn_kernel(const h16_t *__restrict__ q, int64_t ldq, TreeIn in, h16_t *kc, h16_t *vc, KvGeom kg, int hq_l, int G, int nrb,
+                                                           TreeView tv, const int32_t *__restrict__ lens, TreePlan tp, TreeOut out, float scale_log2e) {
     constexpr int CW = 4 / RW, ROWS = 32 * RW;
     constexpr int KT = D / 32, DT = D / 16, DB = D / 32, TILES = 2 * KT + DT;
     constexpr int LPT = TILES / RW;                       // 1 KB loads per wave and step: RW waves share a tile position
@@ -141,23 +242,14 @@ __global__ __launch_bounds__(256, RW == 1 ? 1 : 2) void tree_attn_kernel(const h
     __shared__ __align__(16) unsigned char smem[STAGE > MERGE ? STAGE : MERGE];
     __shared__ float s_m[4][32], s_l[4][32];
     h16x8(*stage)[CW][TILES][64] = reinterpret_cast<h16x8(*)[CW][TILES][64]>(smem);
-    // block id = 8 slot + xcd: the row blocks of a run of tiles sit next to each other on one XCD and share the run in its L2
-    const int slot = blockIdx.x >> 3, rb = slot % nrb;
-    int combo = (slot / nrb) * 8 + (blockIdx.x & 7);
-    if (combo >= tv.batch * kg.hkv_l * sp.nsplit) return;
-    const int split = combo % sp.nsplit;
-    combo /= sp.nsplit;
-    const int c = combo % kg.hkv_l, seq = combo / kg.hkv_l;
-    const int row0 = tv.cu[seq], n = tv.cu[seq + 1] - row0, R = n * G;
-    if (rb * ROWS >= R) return;
-    const int len = lens[seq], nt = min((len + n + 31) >> 5, kg.smax >> 5);
-    const int per = max(sp.chunk, (nt + sp.nsplit - 1) / sp.nsplit), t0 = split * per;
-    if (t0 >= nt) return;
-    const int t1 = min(t0 + per, nt), steps = (t1 - t0 + CW - 1) / CW;
+    TreeWork wk;
+    if (!wk.find(kg, G, nrb, ROWS, tv, lens, tp)) return;
+    const int len = wk.len, t0 = wk.t0, t1 = wk.t1, R = wk.R, row0 = wk.row0, steps = (t1 - t0 + CW - 1) / CW;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int rw = wave % RW, cw = wave / RW, hl = lane >> 5;
-    const int r = rb * ROWS + rw * 32 + (lane & 31);
-    const int rr = min(r, R - 1), node = rr / G, head = c * G + (rr - node * G);    // rows past the last repeat it and are not stored
+    const int r = wk.rb * ROWS + rw * 32 + (lane & 31);
+    const bool idle = wk.rb * ROWS + rw * 32 >= R;        // the wave has no row: it feeds the others
+    const int rr = min(r, R - 1), node = rr / G, head = wk.c * G + (rr - node * G);    // rows past the last repeat it and are not stored
     const uint32_t *mask = tv.mask + (size_t)(row0 + node) * tv.mask_words;
 
     h16x8 qf[2 * KT];
@@ -171,8 +263,9 @@ __global__ __launch_bounds__(256, RW == 1 ? 1 : 2) void tree_attn_kernel(const h
         for (int x = 0; x < 16; ++x) oacc[db][x] = 0.f;
     float m = NEG_INF, lsum = 0.f;
 
-    const size_t slab = (size_t)seq * kg.seq_stride + (size_t)c * kg.smax * D;
-    const h16x8 *ks = reinterpret_cast<const h16x8 *>(kc + slab), *vs = reinterpret_cast<const h16x8 *>(vc + slab);
+    const size_t slab = (size_t)wk.seq * kg.seq_stride + (size_t)wk.c * kg.smax * D;
+    h16_t *kslab = kc + slab, *vslab = vc + slab;
+    const h16x8 *ks = reinterpret_cast<const h16x8 *>(kslab), *vs = reinterpret_cast<const h16x8 *>(vslab);
     const unsigned lane_bytes = (unsigned)lane * 16u;
     auto issue = [&](int step) {
         const int t = min(t0 + step * CW + cw, t1 - 1);
@@ -188,93 +281,66 @@ __global__ __launch_bounds__(256, RW == 1 ? 1 : 2) void tree_attn_kernel(const h
 #pragma unroll
     for (int x = 0; x < S - 1; ++x)
         if (x < steps) issue(x);
-    for (int step = 0; step < steps; ++step) {
+    // a step whose tiles all lie in the context (TAIL false), or one that may reach the tree's slots
+    auto walk = [&](int step, auto tail) {
+        constexpr bool TAIL = decltype(tail)::value;
         // steps step + 1 .. step + S - 2 may stay in flight
         if (S > 2 && step + 1 < steps) HX_WAIT_VM(LPT);
         else HX_WAIT_VM(0);
         HX_LDS_BARRIER();
-        if (step + S - 1 < steps) issue(step + S - 1);       // into the buffer that every wave has left
         const int t = t0 + step * CW + cw;
-        if (t >= t1) continue;
+        const bool masked = TAIL && 32 * t + 31 >= len;
+        if constexpr (TAIL) {
+            if (in.k != nullptr) {                            // the same in every wave
+                if (t < t1 && masked) tree_patch<D, RW>(stage[step % S][cw], in, t, len, wk.n, row0, wk.c, rw * 64 + lane, wk.rb == 0, kslab, vslab);
+                __syncthreads();
+            }
+        }
+        if (step + S - 1 < steps) issue(step + S - 1);       // into the buffer that every wave has left
+        if (t >= t1 || idle) return;
         const h16x8(*st)[64] = stage[step % S][cw];
         floatx16 sc;
 #pragma unroll
         for (int x = 0; x < 16; ++x) sc[x] = 0.f;
 #pragma unroll
         for (int kk = 0; kk < 2 * KT; ++kk) sc = hx_mfma32(st[sub * KT + (kk >> 1)][fl + 32 * (kk & 1)], qf[kk], sc);
-        const bool masked = 32 * t + 31 >= len;
         uint32_t sees = 0xffffffffu;
         if (masked) {
-            const int rel = 32 * t - len;                    // index in the tree of the tile's first slot; negative: context before it
-            if (rel < 0) {
-                sees = (mask[0] << -rel) | ((1u << -rel) - 1);
-            } else {
-                const int w = rel >> 5, sh = rel & 31;
-                const uint32_t a = w < tv.mask_words ? mask[w] : 0u, b = w + 1 < tv.mask_words ? mask[w + 1] : 0u;
-                sees = sh == 0 ? a : (a >> sh) | (b << (32 - sh));
-            }
+            sees = tree_sees(mask, tv.mask_words, t, len);
 #pragma unroll
             for (int x = 0; x < 16; ++x) sc[x] = (sees >> (8 * (x >> 2) + 4 * hl + (x & 3))) & 1u ? sc[x] : NEG_INF;
         }
-        float mx = NEG_INF;
-#pragma unroll
-        for (int x = 0; x < 16; ++x) mx = fmaxf(mx, sc[x]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float m_new = fmaxf(m, mx);
-        const float base = m_new == NEG_INF ? 0.f : m_new;   // a row that has seen nothing yet: weights 0, no NaN
-        const float alpha = __builtin_amdgcn_exp2f((m - base) * scale_log2e);
-        m = m_new;
-        float ps = 0.f;
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-            // (the difference first: scores near the type's lowest value would not cancel in a multiply-add with -base * scale)
-            sc[x] = __builtin_amdgcn_exp2f((sc[x] - base) * scale_log2e);
-            ps += sc[x];
-        }
-        lsum = lsum * alpha + ps;
+        const float alpha = tree_softmax(sc, m, lsum, scale_log2e);
         if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
                 for (int x = 0; x < 16; ++x) oacc[db][x] *= alpha;
         }
-        bool odd = false;
-        if (masked) {
+        if constexpr (TAIL) {
+            bool odd = false;
+            if (masked) {
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) odd = odd || any_odd(st[2 * KT + dt][lane]);
-        }
-        if (__builtin_amdgcn_ballot_w64(odd) == 0) {
-            union { uint32_t u[4]; h16x8 v; } p0, p1;        // P for k-groups hl (quads 0, 2) and 2 + hl (quads 1, 3)
-            p0.u[0] = pack_h16x2(sc[0], sc[1]);   p0.u[1] = pack_h16x2(sc[2], sc[3]);
-            p0.u[2] = pack_h16x2(sc[8], sc[9]);   p0.u[3] = pack_h16x2(sc[10], sc[11]);
-            p1.u[0] = pack_h16x2(sc[4], sc[5]);   p1.u[1] = pack_h16x2(sc[6], sc[7]);
-            p1.u[2] = pack_h16x2(sc[12], sc[13]); p1.u[3] = pack_h16x2(sc[14], sc[15]);
-#pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                oacc[db] = hx_mfma32(st[2 * KT + 2 * db + sub][fl], p0.v, oacc[db]);
-                oacc[db] = hx_mfma32(st[2 * KT + 2 * db + sub][fl + 32], p1.v, oacc[db]);
+                for (int dt = 0; dt < DT; ++dt) odd = odd || any_odd(st[2 * KT + dt][lane]);
             }
-        } else {
-            const h16_t *vt = reinterpret_cast<const h16_t *>(st[2 * KT]);
-            for (int pp = 0; pp < 32; ++pp) {
-                float w = 0.f;
-#pragma unroll
-                for (int x = 0; x < 16; ++x) w = x == 4 * (pp >> 3) + (pp & 3) ? sc[x] : w;
-                w = __shfl(w, (lane & 31) + 32 * ((pp >> 2) & 1), 64);
-                if (!((sees >> pp) & 1u)) continue;
-                const int at = (pp & 3) + 4 * (pp >> 4) + 8 * 16 * ((pp & 15) >> 2);    // kvlayout.h: position pp of element 0 of a V tile
-#pragma unroll
-                for (int db = 0; db < DB; ++db)
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        const int dd = 32 * db + 8 * (x >> 2) + 4 * hl + (x & 3);
-                        oacc[db][x] = fmaf(w, h16_to_f32(vt[(dd >> 4) * 512 + (dd & 15) * 8 + at]), oacc[db][x]);
-                    }
+            if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+                tree_slow_tile<DB>(reinterpret_cast<const h16_t *>(st[2 * KT]), sc, sees, lane, oacc);
+                return;
             }
         }
-    }
-    lsum += __shfl_xor(lsum, 32, 64);
-    const int nb = (nt + per - 1) / per;
+        TreeP p0, p1;
+        tree_pack(sc, p0, p1);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+            oacc[db] = hx_mfma32(st[2 * KT + 2 * db + sub][fl], p0.v, oacc[db]);
+            oacc[db] = hx_mfma32(st[2 * KT + 2 * db + sub][fl + 32], p1.v, oacc[db]);
+        }
+    };
+    const int clean = min(max(((len >> 5) - t0) / CW, 0), steps);
+    for (int step = 0; step < clean; ++step) walk(step, std::false_type{});
+    for (int step = clean; step < steps; ++step) walk(step, std::true_type{});
+    lsum = sum_halves(lsum);
+    const int nb = wk.runs();
     const size_t part_row = (size_t)tv.rows * hq_l;
     auto finish = [&](int t, int hd, int dd, const float (&o)[4], float M, float L) {
         if (nb == 1) {
@@ -282,9 +348,9 @@ __global__ __launch_bounds__(256, RW == 1 ? 1 : 2) void tree_attn_kernel(const h
             tree_store4(out, t, hd * D + dd, x);
             return;
         }
-        const size_t e = split * part_row + (size_t)t * hq_l + hd;
-        *reinterpret_cast<floatx4 *>(sp.part_o + e * D + dd) = floatx4{o[0], o[1], o[2], o[3]};
-        if (dd == 0) *reinterpret_cast<float2 *>(sp.part_ml + 2 * e) = float2{M, L};
+        const size_t e = wk.split * part_row + (size_t)t * hq_l + hd;
+        *reinterpret_cast<floatx4 *>(tp.part_o + e * D + dd) = floatx4{o[0], o[1], o[2], o[3]};
+        if (dd == 0) *reinterpret_cast<float2 *>(tp.part_ml + 2 * e) = float2{M, L};
     };
     if constexpr (CW == 1) {
         if (r >= R) return;
@@ -308,7 +374,7 @@ __global__ __launch_bounds__(256, RW == 1 ? 1 : 2) void tree_attn_kernel(const h
                     floatx4{oacc[db][4 * qd], oacc[db][4 * qd + 1], oacc[db][4 * qd + 2], oacc[db][4 * qd + 3]};
         __syncthreads();
         for (int idx = threadIdx.x; idx < ROWS * (D / 4); idx += 256) {
-            const int row = idx / (D / 4), dd = 4 * (idx - row * (D / 4)), grp = row >> 5, i = row & 31, at = rb * ROWS + row;
+            const int row = idx / (D / 4), dd = 4 * (idx - row * (D / 4)), grp = row >> 5, i = row & 31, at = wk.rb * ROWS + row;
             if (at >= R) break;
             float M = NEG_INF, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -323,57 +389,288 @@ __global__ __launch_bounds__(256, RW == 1 ? 1 : 2) void tree_attn_kernel(const h
 #pragma unroll
                 for (int x = 0; x < 4; ++x) o[x] += v[x] * wt;
             }
-            finish(row0 + at / G, c * G + at % G, dd, o, M, L);
+            finish(row0 + at / G, wk.c * G + at % G, dd, o, M, L);
         }
     }
 }
 
-// Joins the runs of every (row, head): D / 4 threads each, runs in the order of the context.
+// Joins the runs of every (row, head): D / 4 threads each, runs in the order of the context, four requested at a time.
 template <int D>
-__global__ __launch_bounds__(256) void tree_merge_kernel(KvGeom kg, int hq_l, TreeView tv, const int32_t *__restrict__ lens, TreeSplit sp,
-                                                         TreeOut out, float scale_log2e) {
+__global__ __launch_bounds__(256) void tree_merge_kernel(KvGeom kg, int hq_l, TreeView tv, const int32_t *__restrict__ lens, TreePlan tp, TreeOut out, float scale_log2e) {
     constexpr int TP = D / 4;
     const int e = blockIdx.x * (256 / TP) + threadIdx.x / TP, dd = 4 * (threadIdx.x % TP);
     if (e >= tv.rows * hq_l) return;
     const int t = e / hq_l, seq = tv.row[t].seq, n = tv.cu[seq + 1] - tv.cu[seq];
-    const int nt = min((lens[seq] + n + 31) >> 5, kg.smax >> 5), per = max(sp.chunk, (nt + sp.nsplit - 1) / sp.nsplit), nb = (nt + per - 1) / per;
+    const int nt = min((lens[seq] + n + 31) >> 5, kg.smax >> 5), per = max(tp.chunk, (nt + tp.nsplit - 1) / tp.nsplit), nb = (nt + per - 1) / per;
     if (nb <= 1) return;
     const size_t part_row = (size_t)tv.rows * hq_l;
-    float M = NEG_INF;
-    for (int u = 0; u < nb; ++u) M = fmaxf(M, sp.part_ml[2 * (u * part_row + e)]);
-    const float b = M == NEG_INF ? 0.f : M;
-    float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int u = 0; u < nb; ++u) {
-        const float2 ml = *reinterpret_cast<const float2 *>(sp.part_ml + 2 * (u * part_row + e));
-        const float wt = __builtin_amdgcn_exp2f((ml.x - b) * scale_log2e);
-        const floatx4 v = *reinterpret_cast<const floatx4 *>(sp.part_o + (u * part_row + e) * D + dd);
-        L += ml.y * wt;
+    float M = NEG_INF, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int u0 = 0; u0 < nb; u0 += 4) {
+        float2 ml[4];
+        floatx4 v[4];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) o[x] += v[x] * wt;
+        for (int u = 0; u < 4; ++u) {
+            const size_t at = min(u0 + u, nb - 1) * part_row + e;
+            ml[u] = *reinterpret_cast<const float2 *>(tp.part_ml + 2 * at);
+            v[u] = *reinterpret_cast<const floatx4 *>(tp.part_o + at * D + dd);
+        }
+        float M4 = M;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) M4 = fmaxf(M4, ml[u].x);
+        const float b = M4 == NEG_INF ? 0.f : M4, alpha = __builtin_amdgcn_exp2f((M - b) * scale_log2e);
+        M = M4;
+        L *= alpha;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) o[x] *= alpha;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (u0 + u >= nb) break;
+            const float wt = __builtin_amdgcn_exp2f((ml[u].x - b) * scale_log2e);
+            L += ml[u].y * wt;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[x] += v[u][x] * wt;
+        }
     }
     const float inv = 1.0f / L, x[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
     tree_store4(out, t, (e - t * hq_l) * D + dd, x);
 }
 
-void launch_tree_attn(const h16_t *q, int64_t ldq, const h16_t *kc, const h16_t *vc, KvGeom kg, int hq_l, const TreeView &tv,
-                      const int32_t *lens, const TreeSplit &sp, const TreeOut &out, hipStream_t s) {
-    const int G = hq_l / kg.hkv_l, groups = tree_row_groups(tv.max_n, G), nrb = (tv.max_n * G + 32 * groups - 1) / (32 * groups);
+// Few rows, or little work in all: a block of eight waves takes 32 query rows and the waves take the run's tiles in turn.  No tile serves two
+// waves, so K and V go straight to registers in the operands' layout (the next tile's K is requested before this tile's softmax), and the
+// waves meet in LDS at the end.  Bound by latency, or by HBM where there are many sequences.  The arithmetic is that of the kernel above.
+// Runs leave (m, l, o) with device-scope stores and count themselves; whoever is last joins them in the order of the context, so that the
+// result does not depend on who that was, and resets the counter.  Nobody waits for anybody.
+template <int D>
+__global__ __launch_bounds__(512, 2) void tree_few_kernel(const h16_t *__restrict__ q, int64_t ldq, TreeIn in, h16_t *kc, h16_t *vc, KvGeom kg, int hq_l, int G, int nrb,
+                                                          TreeView tv, const int32_t *__restrict__ lens, TreePlan tp, TreeOut out, float scale_log2e) {
+    constexpr int W = 8, KT = D / 32, DT = D / 16, DB = D / 32, OS = D + 4;
+    __shared__ __align__(16) float s_o[W][32 * OS];
+    __shared__ float s_m[W][32], s_l[W][32];
+    __shared__ int s_last;
+    TreeWork wk;
+    if (!wk.find(kg, G, nrb, 32, tv, lens, tp)) return;
+    const int len = wk.len, R = wk.R, row0 = wk.row0;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hl = lane >> 5, i32 = lane & 31;
+    const int sub = i32 >> 4, fl = (lane & 15) + 16 * hl;
+    const int rr = min(wk.rb * 32 + i32, R - 1), node = rr / G, head = wk.c * G + (rr - node * G);    // rows past the last repeat it and are not stored
+    const uint32_t *mask = tv.mask + (size_t)(row0 + node) * tv.mask_words;
+    const size_t slab = (size_t)wk.seq * kg.seq_stride + (size_t)wk.c * kg.smax * D;
+    h16_t *kslab = kc + slab, *vslab = vc + slab;
+    const bool fresh = in.k != nullptr;                       // the tree's rows are the caller's, not in the cache yet
+
+    h16x8 kf[2 * KT], vf[2 * DB], qf[2 * KT];
+    // K: lane l takes position l % 32, elements 16 kk + 8 (l / 32) ..; a slot of the tree comes from its row
+    auto load_k = [&](int t) {
+        const h16_t *src = kslab + ((size_t)(2 * t + sub) * KT * 64 + fl) * 8;
+        const int x = 32 * t + i32 - len;
+        if (fresh && 32 * t + 31 >= len && x >= 0 && x < wk.n) {
+            const h16_t *row = static_cast<const h16_t *>(in.k) + (size_t)(row0 + x) * in.ldk + wk.c * D + 8 * hl;
+#pragma unroll
+            for (int kk = 0; kk < 2 * KT; ++kk) kf[kk] = *reinterpret_cast<const h16x8 *>(row + 16 * kk);
+        } else {
+#pragma unroll
+            for (int kk = 0; kk < 2 * KT; ++kk) kf[kk] = *reinterpret_cast<const h16x8 *>(src + ((kk >> 1) * 64 + 32 * (kk & 1)) * 8);
+        }
+    };
+    const int tw = wk.t0 + wave;
+    if (tw < wk.t1) load_k(tw);
+#pragma unroll
+    for (int kk = 0; kk < 2 * KT; ++kk)
+        qf[kk] = *reinterpret_cast<const h16x8 *>(q + (size_t)(row0 + node) * ldq + (size_t)head * D + 16 * kk + 8 * hl);
+    floatx16 oacc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) oacc[db][x] = 0.f;
+    float m = NEG_INF, lsum = 0.f;
+    // a tile in the context (TAIL false), or one that may reach the tree's slots
+    auto walk = [&](int t, auto tail) {
+        constexpr bool TAIL = decltype(tail)::value;
+        const bool masked = TAIL && 32 * t + 31 >= len;
+        // V^T: lane l takes element 32 db + l % 32 and k-group 2 h + l / 32 (kvlayout.h)
+        const h16_t *vsrc = vslab + ((size_t)(t * DT + sub) * 64 + fl) * 8;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) vf[2 * db + h] = *reinterpret_cast<const h16x8 *>(vsrc + (2 * db * 64 + 32 * h) * 8);
+        floatx16 sc;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) sc[x] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < 2 * KT; ++kk) sc = hx_mfma32(kf[kk], qf[kk], sc);
+        uint32_t sees = 0xffffffffu;
+        if (masked) {
+            if (fresh) {
+                // the tree's values over what the cache held there; the first block of rows appends what it has put together
+                const h16_t *rows = static_cast<const h16_t *>(in.v) + (size_t)row0 * in.ldv + wk.c * D + i32;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int g = 2 * h + hl;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int x = 32 * t + (j & 3) + 4 * g + 16 * (j >> 2) - len;
+                        if (x < 0 || x >= wk.n) continue;
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) {
+                            union { h16x8 v; h16_t e[8]; } w;
+                            w.v = vf[2 * db + h];
+                            w.e[j] = rows[(size_t)x * in.ldv + 32 * db];
+                            vf[2 * db + h] = w.v;
+                        }
+                    }
+                }
+                if (wk.rb == 0) {
+                    const int x = 32 * t + i32 - len;
+                    h16_t *dst = kslab + ((size_t)(2 * t + sub) * KT * 64 + fl) * 8;
+                    if (x >= 0 && x < wk.n) {
+#pragma unroll
+                        for (int kk = 0; kk < 2 * KT; ++kk) *reinterpret_cast<h16x8 *>(dst + ((kk >> 1) * 64 + 32 * (kk & 1)) * 8) = kf[kk];
+                    }
+                    h16_t *vdst = vslab + ((size_t)(t * DT + sub) * 64 + fl) * 8;      // whole pieces: slots that are not the tree's keep their values
+#pragma unroll
+                    for (int db = 0; db < DB; ++db)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) *reinterpret_cast<h16x8 *>(vdst + (2 * db * 64 + 32 * h) * 8) = vf[2 * db + h];
+                }
+            }
+            sees = tree_sees(mask, tv.mask_words, t, len);
+#pragma unroll
+            for (int x = 0; x < 16; ++x) sc[x] = (sees >> (8 * (x >> 2) + 4 * hl + (x & 3))) & 1u ? sc[x] : NEG_INF;
+        }
+        if (t + W < wk.t1) load_k(t + W);
+        const float alpha = tree_softmax(sc, m, lsum, scale_log2e);
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) oacc[db][x] *= alpha;
+        if constexpr (TAIL) {
+            bool odd = false;
+            if (masked) {
+#pragma unroll
+                for (int x = 0; x < 2 * DB; ++x) odd = odd || any_odd(vf[x]);
+            }
+            if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+                h16x8 *vt = reinterpret_cast<h16x8 *>(s_o[wave]);      // the wave's own part of the merge buffer, not in use yet
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) vt[(2 * db + sub) * 64 + fl + 32 * h] = vf[2 * db + h];
+                tree_slow_tile<DB>(reinterpret_cast<const h16_t *>(vt), sc, sees, lane, oacc);
+                return;
+            }
+        }
+        TreeP p0, p1;
+        tree_pack(sc, p0, p1);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+            oacc[db] = hx_mfma32(vf[2 * db], p0.v, oacc[db]);
+            oacc[db] = hx_mfma32(vf[2 * db + 1], p1.v, oacc[db]);
+        }
+    };
+    int tile = tw;
+    for (; tile < min(wk.t1, len >> 5); tile += W) walk(tile, std::false_type{});
+    for (; tile < wk.t1; tile += W) walk(tile, std::true_type{});
+    lsum = sum_halves(lsum);
+    if (hl == 0) { s_m[wave][i32] = m; s_l[wave][i32] = lsum; }
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int qd = 0; qd < 4; ++qd)
+            *reinterpret_cast<floatx4 *>(&s_o[wave][i32 * OS + 32 * db + 8 * qd + 4 * hl]) =
+                floatx4{oacc[db][4 * qd], oacc[db][4 * qd + 1], oacc[db][4 * qd + 2], oacc[db][4 * qd + 3]};
+    __syncthreads();
+    const int nb = wk.runs(), rows = min(32, R - wk.rb * 32);
+    const size_t part_row = (size_t)tv.rows * hq_l;
+    constexpr int TP = D / 4, QUADS = 32 * TP / 512;              // threads of a row, and quads of a thread: rows threadIdx.x / TP + i 512 / TP
+    const int dd = 4 * (threadIdx.x % TP);
+#pragma unroll
+    for (int i = 0; i < QUADS; ++i) {
+        const int row = threadIdx.x / TP + i * (512 / TP), at = wk.rb * 32 + row;
+        if (row >= rows) break;
+        float M = NEG_INF, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < W; ++w) M = fmaxf(M, s_m[w][row]);
+        const float b = M == NEG_INF ? 0.f : M;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float wt = __builtin_amdgcn_exp2f((s_m[w][row] - b) * scale_log2e);
+            const floatx4 v = *reinterpret_cast<const floatx4 *>(&s_o[w][row * OS + dd]);
+            L += s_l[w][row] * wt;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[x] += v[x] * wt;
+        }
+        const int t = row0 + at / G, hd = wk.c * G + at % G;
+        if (nb == 1) {
+            const float inv = 1.0f / L, x[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+            tree_store4(out, t, hd * D + dd, x);
+        } else {
+            const size_t e = wk.split * part_row + (size_t)t * hq_l + hd;
+            dev_store2(tp.part_o + e * D + dd, o[0], o[1]);
+            dev_store2(tp.part_o + e * D + dd + 2, o[2], o[3]);
+            if (dd == 0) dev_store2(tp.part_ml + 2 * e, M, L);
+        }
+    }
+    if (nb == 1) return;
+    if (!tree_arrive(tp.arrived + ((size_t)wk.seq * kg.hkv_l + wk.c) * nrb + wk.rb, nb, &s_last)) return;
+    // the last block: a thread requests the (m, l) and sums of its quads of eight runs at once
+#pragma unroll
+    for (int i = 0; i < QUADS; ++i) {
+        const int row = threadIdx.x / TP + i * (512 / TP), at = wk.rb * 32 + row;
+        if (row >= rows) break;
+        const int t = row0 + at / G, hd = wk.c * G + at % G;
+        const size_t e = (size_t)t * hq_l + hd;
+        float M = NEG_INF, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int u0 = 0; u0 < nb; u0 += 8) {
+            float2 ml[8], a[8], b[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const size_t at_u = min(u0 + u, nb - 1) * part_row + e;
+                ml[u] = dev_load2(tp.part_ml + 2 * at_u);
+                a[u] = dev_load2(tp.part_o + at_u * D + dd);
+                b[u] = dev_load2(tp.part_o + at_u * D + dd + 2);
+            }
+            float M8 = M;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) M8 = fmaxf(M8, ml[u].x);
+            const float base = M8 == NEG_INF ? 0.f : M8, alpha = __builtin_amdgcn_exp2f((M - base) * scale_log2e);
+            M = M8;
+            L *= alpha;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[x] *= alpha;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                if (u0 + u >= nb) break;
+                const float wt = __builtin_amdgcn_exp2f((ml[u].x - base) * scale_log2e);
+                L += ml[u].y * wt;
+                o[0] += a[u].x * wt; o[1] += a[u].y * wt; o[2] += b[u].x * wt; o[3] += b[u].y * wt;
+            }
+        }
+        const float inv = 1.0f / L, x[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+        tree_store4(out, t, hd * D + dd, x);
+    }
+}
+
+void launch_tree_attn(const h16_t *q, int64_t ldq, const TreeIn &in, h16_t *kc, h16_t *vc, KvGeom kg, int hq_l, const TreeView &tv, const int32_t *lens,
+                      const TreePlan &tp, const TreeOut &out, hipStream_t s) {
+    const int G = hq_l / kg.hkv_l, nrb = tree_row_blocks(tv.max_n, G, 32 * tp.row_groups);
     const float scale_log2e = 1.4426950408889634f / sqrtf((float)kg.d);
-    const dim3 grid((unsigned)nrb * (unsigned)((tv.batch * kg.hkv_l * sp.nsplit + 7) / 8 * 8));
-#define HX_TREE(DD, RW, S) hipLaunchKernelGGL((tree_attn_kernel<DD, RW, S>), grid, dim3(256), 0, s, q, ldq, kc, vc, kg, hq_l, G, nrb, tv, lens, sp, out, scale_log2e)
+    const dim3 grid((unsigned)nrb * (unsigned)((tv.batch * kg.hkv_l * tp.nsplit + 7) / 8 * 8));
+#define HX_TREE(KERNEL, THREADS) hipLaunchKernelGGL((KERNEL), grid, dim3(THREADS), 0, s, q, ldq, in, kc, vc, kg, hq_l, G, nrb, tv, lens, tp, out, scale_log2e)
+#define HX_MERGE(DD) \
+    hipLaunchKernelGGL(tree_merge_kernel<DD>, dim3((tv.rows * hq_l + 1024 / DD - 1) / (1024 / DD)), dim3(256), 0, s, kg, hq_l, tv, lens, tp, out, scale_log2e)
     if (kg.d == 128) {
-        if (groups == 1) HX_TREE(128, 1, 2);
-        else if (groups == 2) HX_TREE(128, 2, 2);
-        else HX_TREE(128, 4, 3);
+        if (tp.row_groups == 1) HX_TREE(tree_few_kernel<128>, 512);
+        else if (tp.row_groups == 2) HX_TREE((tree_attn_kernel<128, 2, 2>), 256);
+        else HX_TREE((tree_attn_kernel<128, 4, 3>), 256);
+        if (tp.row_groups > 1 && tp.nsplit > 1) HX_MERGE(128);
     } else {
-        if (groups == 1) HX_TREE(64, 1, 2);
-        else if (groups == 2) HX_TREE(64, 2, 2);
-        else HX_TREE(64, 4, 3);
+        if (tp.row_groups == 1) HX_TREE(tree_few_kernel<64>, 512);
+        else if (tp.row_groups == 2) HX_TREE((tree_attn_kernel<64, 2, 2>), 256);
+        else HX_TREE((tree_attn_kernel<64, 4, 3>), 256);
+        if (tp.row_groups > 1 && tp.nsplit > 1) HX_MERGE(64);
     }
 #undef HX_TREE
-    if (sp.nsplit <= 1) return;
-    if (kg.d == 128) hipLaunchKernelGGL(tree_merge_kernel<128>, dim3((tv.rows * hq_l + 7) / 8), dim3(256), 0, s, kg, hq_l, tv, lens, sp, out, scale_log2e);
-    else hipLaunchKernelGGL(tree_merge_kernel<64>, dim3((tv.rows * hq_l + 15) / 16), dim3(256), 0, s, kg, hq_l, tv, lens, sp, out, scale_log2e);
+#undef HX_MERGE
 }
 
 // ---- keeping an accepted path -------------------------------------------------------------------------------------

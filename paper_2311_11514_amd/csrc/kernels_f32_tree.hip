@@ -7,21 +7,6 @@ namespace {
 
 __device__ __forceinline__ floatx4 mfma_f32(float a, float b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
-// rows of a user's projection -> cache slots len + index, four elements of one head of K and of V per thread
-__global__ __launch_bounds__(256) void f32_tree_append_kernel(const float *__restrict__ k, int64_t ldk, const float *__restrict__ v, int64_t ldv,
-                                                              float *__restrict__ kc, float *__restrict__ vc, KvGeom kg, TreeView tv,
-                                                              const int32_t *__restrict__ lens) {
-    const int per_row = kg.hkv_l * kg.d / 4, idx = blockIdx.x * 256 + threadIdx.x;
-    if (idx >= tv.rows * per_row) return;
-    const int t = idx / per_row, e = (idx - t * per_row) * 4, c = e / kg.d, dd = e - c * kg.d;
-    const TreeRow row = tv.row[t];
-    const int slot = lens[row.seq] + row.index;
-    if (slot >= kg.smax) return;
-    const size_t at = (size_t)row.seq * kg.seq_stride + ((size_t)c * kg.smax + slot) * kg.d + dd;
-    *reinterpret_cast<floatx4 *>(kc + at) = *reinterpret_cast<const floatx4 *>(k + (size_t)t * ldk + e);
-    *reinterpret_cast<floatx4 *>(vc + at) = *reinterpret_cast<const floatx4 *>(v + (size_t)t * ldv + e);
-}
-
 // raw projection [rows][(hq + 2 hkv) d] -> rotary embedding at len + depth, q as plain rows, k and v into the cache; a rotary pair per thread
 __global__ __launch_bounds__(256) void f32_tree_rope_append_kernel(const float *__restrict__ qkv, int hq_l, KvGeom kg, TreeView tv,
                                                                    const int32_t *__restrict__ lens, const float *__restrict__ cos_tab,
@@ -51,32 +36,38 @@ __global__ __launch_bounds__(256) void f32_tree_rope_append_kernel(const float *
 
 // A block takes 16 query columns of one (sequence, kv head) -- column j: node j / G, head j % G -- and a run of 16-position tiles, over
 // which its W waves interleave; the products and register layouts are those of the stage's fp32 attention (v_mfma_f32_16x16x4_f32, a
-// lane owns column l % 16 and positions 4 (l / 16) + r, P stays in registers).  Masks, runs and the way of values that are not finite as in
-// the 16-bit kernel.  Bound by the fp32 matrix instructions, 32 cycles for 4 KB of K or V, and by the one round trip per tile and wave.
+// lane owns column l % 16 and positions 4 (l / 16) + r, P stays in registers).  Rows that are not in the cache yet (in.k != NULL) are read from the
+// caller's and appended by the first block of columns.  Masks, runs and the way of values that are not finite as in the 16-bit kernel.
+// Bound by the fp32 matrix instructions, 32 cycles for 4 KB of K or V, and by the one round trip per tile and wave.
 template <int D, int W>
-__global__ __launch_bounds__(64 * W) void f32_tree_attn_kernel(const float *__restrict__ q, int64_t ldq, const float *__restrict__ kc,
-                                                               const float *__restrict__ vc, KvGeom kg, int hq_l, int G, int nrb, TreeView tv,
-                                                               const int32_t *__restrict__ lens, TreeSplit sp, float *__restrict__ o) {
+__global__ __launch_bounds__(64 * W) void f32_tree_attn_kernel(const float *__restrict__ q, int64_t ldq, TreeIn in, float *kc, float *vc, KvGeom kg, int hq_l, int G, int nrb,
+                                                               TreeView tv, const int32_t *__restrict__ lens, TreePlan tp, float *__restrict__ o) {
     constexpr int KT = D / 16, VH = D / 64;
     __shared__ float s_m[W][16], s_l[W][16];
     __shared__ __align__(16) float s_o[W][16][D];
+    __shared__ int s_last;
     const int slot = blockIdx.x >> 3, rb = slot % nrb;
     int combo = (slot / nrb) * 8 + (blockIdx.x & 7);
-    if (combo >= tv.batch * kg.hkv_l * sp.nsplit) return;
-    const int split = combo % sp.nsplit;
-    combo /= sp.nsplit;
-    const int c = combo % kg.hkv_l, seq = combo / kg.hkv_l;
+    if (combo >= tv.batch * kg.hkv_l * tp.nsplit) return;
+    const int split = combo % tp.nsplit;
+    combo /= tp.nsplit;
+    const int c = combo % kg.hkv_l, nth = combo / kg.hkv_l, seq = nth < kTreeOrdered ? tp.order[nth] : nth;
     const int row0 = tv.cu[seq], n = tv.cu[seq + 1] - row0, R = n * G;
     if (rb * 16 >= R) return;
     const int len = lens[seq], last = min(len + n, kg.smax) - 1, nt = (last + 32) >> 5;      // runs count 32 positions, as for 16 bits
-    const int per = max(sp.chunk, (nt + sp.nsplit - 1) / sp.nsplit), t0 = split * per;
+    const int per = max(tp.chunk, (nt + tp.nsplit - 1) / tp.nsplit), t0 = split * per;
     if (t0 >= nt) return;
     const int t1 = min(2 * (t0 + per), (last >> 4) + 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int rr = min(rb * 16 + i, R - 1), node = rr / G, head = c * G + (rr - node * G);
     const uint32_t *mask = tv.mask + (size_t)(row0 + node) * tv.mask_words;
     const size_t slab = (size_t)seq * kg.seq_stride + (size_t)c * kg.smax * D;
-    const float *K = kc + slab, *V = vc + slab;
+    float *K = kc + slab, *V = vc + slab;
+    const float *nk = in.k != nullptr ? static_cast<const float *>(in.k) + (size_t)row0 * in.ldk + c * D : nullptr;
+    const float *nv = in.k != nullptr ? static_cast<const float *>(in.v) + (size_t)row0 * in.ldv + c * D : nullptr;
+    // position p of the keys and values: the cache's, or the tree's row that will be there
+    auto key_at = [&](int p) { return nk != nullptr && p >= len ? nk + (size_t)(p - len) * in.ldk : K + (size_t)p * D; };
+    auto value_at = [&](int p) { return nv != nullptr && p >= len ? nv + (size_t)(p - len) * in.ldv : V + (size_t)p * D; };
     floatx4 qf[KT];
 #pragma unroll
     for (int k = 0; k < KT; ++k) qf[k] = *reinterpret_cast<const floatx4 *>(q + (size_t)(row0 + node) * ldq + (size_t)head * D + 16 * k + 4 * g);
@@ -89,18 +80,35 @@ __global__ __launch_bounds__(64 * W) void f32_tree_attn_kernel(const float *__re
     float m = NEG_INF, lsum = 0.f;
     for (int t = 2 * t0 + wave; t < t1; t += W) {
         floatx4 kf[KT], vf[4][VH];
+        const float *kp = key_at(min(16 * t + i, last)) + 4 * g;
 #pragma unroll
-        for (int k = 0; k < KT; ++k) kf[k] = *reinterpret_cast<const floatx4 *>(K + (size_t)min(16 * t + i, last) * D + 16 * k + 4 * g);
+        for (int k = 0; k < KT; ++k) kf[k] = *reinterpret_cast<const floatx4 *>(kp + 16 * k);
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
+        for (int x = 0; x < 4; ++x) {
+            const float *vp = value_at(min(16 * t + 4 * g + x, last)) + 4 * i;
 #pragma unroll
-            for (int h = 0; h < VH; ++h) vf[x][h] = *reinterpret_cast<const floatx4 *>(V + (size_t)min(16 * t + 4 * g + x, last) * D + 64 * h + 4 * i);
+            for (int h = 0; h < VH; ++h) vf[x][h] = *reinterpret_cast<const floatx4 *>(vp + 64 * h);
+        }
+        const bool masked = 16 * t + 15 >= len;
+        if (masked && nk != nullptr && rb == 0) {              // append; nobody reads these slots in this launch
+            const int p = 16 * t + i;
+            if (p >= len && p <= last) {
+#pragma unroll
+                for (int k = 0; k < KT; ++k) *reinterpret_cast<floatx4 *>(K + (size_t)p * D + 16 * k + 4 * g) = kf[k];
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int pv = 16 * t + 4 * g + x;
+                if (pv < len || pv > last) continue;
+#pragma unroll
+                for (int h = 0; h < VH; ++h) *reinterpret_cast<floatx4 *>(V + (size_t)pv * D + 64 * h + 4 * i) = vf[x][h];
+            }
+        }
         floatx4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < KT; ++k)
 #pragma unroll
             for (int x = 0; x < 4; ++x) s = mfma_f32(kf[k][x], qf[k][x], s);
-        const bool masked = 16 * t + 15 >= len;
         uint32_t sees = 0xffffu;                              // of the tile's 16 positions
         if (masked) {
             const int rel = 16 * t - len;
@@ -155,13 +163,13 @@ __global__ __launch_bounds__(64 * W) void f32_tree_attn_kernel(const float *__re
                 const float w0 = __shfl(pr[0], src, 64), w1 = __shfl(pr[1], src, 64), w2 = __shfl(pr[2], src, 64), w3 = __shfl(pr[3], src, 64);
                 const float w = (pp & 3) == 0 ? w0 : (pp & 3) == 1 ? w1 : (pp & 3) == 2 ? w2 : w3;
                 if (!((sees >> pp) & 1u)) continue;
+                const float *vp = value_at(min(16 * t + pp, last));
 #pragma unroll
                 for (int h = 0; h < VH; ++h)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            oacc[h][e][r] = fmaf(w, V[(size_t)min(16 * t + pp, last) * D + 64 * h + 4 * (4 * g + r) + e], oacc[h][e][r]);
+                        for (int r = 0; r < 4; ++r) oacc[h][e][r] = fmaf(w, vp[64 * h + 4 * (4 * g + r) + e], oacc[h][e][r]);
             }
         }
     }
@@ -195,34 +203,48 @@ __global__ __launch_bounds__(64 * W) void f32_tree_attn_kernel(const float *__re
         if (nb == 1) {
             *reinterpret_cast<floatx4 *>(o + e * D + dd) = acc / L;
         } else {
-            *reinterpret_cast<floatx4 *>(sp.part_o + (split * part_row + e) * D + dd) = acc;
-            if (dd == 0) *reinterpret_cast<float2 *>(sp.part_ml + 2 * (split * part_row + e)) = float2{M, L};
+            float *po = tp.part_o + (split * part_row + e) * D + dd;
+            dev_store2(po, acc[0], acc[1]);
+            dev_store2(po + 2, acc[2], acc[3]);
+            if (dd == 0) dev_store2(tp.part_ml + 2 * (split * part_row + e), M, L);
         }
     }
-}
-
-// joins the runs of every (row, head), D / 4 threads each
-template <int D>
-__global__ __launch_bounds__(256) void f32_tree_merge_kernel(KvGeom kg, int hq_l, TreeView tv, const int32_t *__restrict__ lens, TreeSplit sp,
-                                                             float *__restrict__ o) {
-    constexpr int TP = D / 4;
-    const int e = blockIdx.x * (256 / TP) + threadIdx.x / TP, dd = 4 * (threadIdx.x % TP);
-    if (e >= tv.rows * hq_l) return;
-    const int t = e / hq_l, seq = tv.row[t].seq, n = tv.cu[seq + 1] - tv.cu[seq];
-    const int nt = (min(lens[seq] + n, kg.smax) + 31) >> 5, per = max(sp.chunk, (nt + sp.nsplit - 1) / sp.nsplit), nb = (nt + per - 1) / per;
-    if (nb <= 1) return;
-    const size_t part_row = (size_t)tv.rows * hq_l;
-    float M = NEG_INF, L = 0.f;
-    for (int u = 0; u < nb; ++u) M = fmaxf(M, sp.part_ml[2 * (u * part_row + e)]);
-    const float b = M == NEG_INF ? 0.f : M;
-    floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int u = 0; u < nb; ++u) {
-        const float2 ml = *reinterpret_cast<const float2 *>(sp.part_ml + 2 * (u * part_row + e));
-        const float wt = expf(ml.x - b);
-        L += ml.y * wt;
-        acc += *reinterpret_cast<const floatx4 *>(sp.part_o + (u * part_row + e) * D + dd) * wt;
+    if (nb == 1) return;
+    if (!tree_arrive(tp.arrived + ((size_t)seq * kg.hkv_l + c) * nrb + rb, nb, &s_last)) return;
+    // the last block joins the runs in the order of the context; their maxima are requested all at once
+    float(*s_max)[kTreeMaxSplit] = reinterpret_cast<float(*)[kTreeMaxSplit]>(s_o);
+    for (int idx = threadIdx.x; idx < 16 * nb; idx += 64 * W) {
+        const int j = idx / nb, u = idx - j * nb, at = min(rb * 16 + j, R - 1);
+        s_max[j][u] = dev_load(tp.part_ml + 2 * (u * part_row + (size_t)(row0 + at / G) * hq_l + c * G + at % G));
     }
-    *reinterpret_cast<floatx4 *>(o + (size_t)e * D + dd) = acc / L;
+    __syncthreads();
+    for (int idx = threadIdx.x * 4; idx < 16 * D; idx += 64 * W * 4) {
+        const int j = idx / D, dd = idx % D, at = rb * 16 + j;
+        if (at >= R) break;
+        const size_t e = (size_t)(row0 + at / G) * hq_l + c * G + at % G;
+        float M = NEG_INF, L = 0.f;
+        for (int u = 0; u < nb; ++u) M = fmaxf(M, s_max[j][u]);
+        const float b = M == NEG_INF ? 0.f : M;
+        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int u0 = 0; u0 < nb; u0 += 4) {
+            float2 ml[4], a[4], c2[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const size_t at_u = min(u0 + u, nb - 1) * part_row + e;
+                ml[u] = dev_load2(tp.part_ml + 2 * at_u);
+                a[u] = dev_load2(tp.part_o + at_u * D + dd);
+                c2[u] = dev_load2(tp.part_o + at_u * D + dd + 2);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (u0 + u >= nb) break;
+                const float wt = expf(ml[u].x - b);
+                L += ml[u].y * wt;
+                acc += floatx4{a[u].x, a[u].y, c2[u].x, c2[u].y} * wt;
+            }
+        }
+        *reinterpret_cast<floatx4 *>(o + e * D + dd) = acc / L;
+    }
 }
 
 // slot len + path[j] -> len + j in every layer, one element of K and V per thread (see the 16-bit kernel for the order)
@@ -302,25 +324,17 @@ void launch_tree_accept(const TreeView &tv, const int32_t *draft, const int32_t 
 void launch_tree_advance(int32_t *lens, const int32_t *kept, int batch, hipStream_t s) {
     hipLaunchKernelGGL(tree_advance_kernel, dim3((batch + 63) / 64), dim3(64), 0, s, lens, kept, batch);
 }
-void f32_launch_tree_append(const float *k, int64_t ldk, const float *v, int64_t ldv, float *kc, float *vc, KvGeom kg, const TreeView &tv,
-                            const int32_t *lens, hipStream_t s) {
-    const int n = tv.rows * (kg.hkv_l * kg.d / 4);
-    hipLaunchKernelGGL(f32_tree_append_kernel, dim3((n + 255) / 256), dim3(256), 0, s, k, ldk, v, ldv, kc, vc, kg, tv, lens);
-}
 void f32_launch_tree_rope_append(const float *qkv, int hq_l, KvGeom kg, const TreeView &tv, const int32_t *lens, const float *cos_tab,
                                  const float *sin_tab, float *q, float *kc, float *vc, hipStream_t s) {
     const int n = tv.rows * (hq_l + 2 * kg.hkv_l) * (kg.d / 2);
     hipLaunchKernelGGL(f32_tree_rope_append_kernel, dim3((n + 255) / 256), dim3(256), 0, s, qkv, hq_l, kg, tv, lens, cos_tab, sin_tab, q, kc, vc);
 }
-void f32_launch_tree_attn(const float *q, int64_t ldq, const float *kc, const float *vc, KvGeom kg, int hq_l, const TreeView &tv,
-                          const int32_t *lens, const TreeSplit &sp, float *o, hipStream_t s) {
-    const int G = hq_l / kg.hkv_l, nrb = (tv.max_n * G + 15) / 16;
-    const dim3 grid((unsigned)nrb * (unsigned)((tv.batch * kg.hkv_l * sp.nsplit + 7) / 8 * 8));
-    if (kg.d == 128) hipLaunchKernelGGL((f32_tree_attn_kernel<128, 4>), grid, dim3(256), 0, s, q, ldq, kc, vc, kg, hq_l, G, nrb, tv, lens, sp, o);
-    else hipLaunchKernelGGL((f32_tree_attn_kernel<64, 4>), grid, dim3(256), 0, s, q, ldq, kc, vc, kg, hq_l, G, nrb, tv, lens, sp, o);
-    if (sp.nsplit <= 1) return;
-    if (kg.d == 128) hipLaunchKernelGGL(f32_tree_merge_kernel<128>, dim3((tv.rows * hq_l + 7) / 8), dim3(256), 0, s, kg, hq_l, tv, lens, sp, o);
-    else hipLaunchKernelGGL(f32_tree_merge_kernel<64>, dim3((tv.rows * hq_l + 15) / 16), dim3(256), 0, s, kg, hq_l, tv, lens, sp, o);
+void f32_launch_tree_attn(const float *q, int64_t ldq, const TreeIn &in, float *kc, float *vc, KvGeom kg, int hq_l, const TreeView &tv, const int32_t *lens,
+                          const TreePlan &tp, float *o, hipStream_t s) {
+    const int G = hq_l / kg.hkv_l, nrb = tree_row_blocks(tv.max_n, G, 16);
+    const dim3 grid((unsigned)nrb * (unsigned)((tv.batch * kg.hkv_l * tp.nsplit + 7) / 8 * 8));
+    if (kg.d == 128) hipLaunchKernelGGL((f32_tree_attn_kernel<128, 4>), grid, dim3(256), 0, s, q, ldq, in, kc, vc, kg, hq_l, G, nrb, tv, lens, tp, o);
+    else hipLaunchKernelGGL((f32_tree_attn_kernel<64, 4>), grid, dim3(256), 0, s, q, ldq, in, kc, vc, kg, hq_l, G, nrb, tv, lens, tp, o);
 }
 void f32_launch_tree_keep(float *kc, float *vc, int64_t layer_stride, int layers, KvGeom kg, int batch, const int32_t *lens, const int32_t *cu,
                           const int32_t *kept, const int32_t *path, hipStream_t s) {

@@ -305,10 +305,8 @@ __device__ __forceinline__ float sum8(u32x4 v) {
 
 // the sum over the four rows of 16 lanes, in every lane: each swap leaves the even rows in one register and the odd ones in the other
 __device__ __forceinline__ float sum_rows(float v) {
-    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-    a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return sum_halves(__uint_as_float(a[0]) + __uint_as_float(a[1]));
 }
 
 // More operand columns: the operand outweighs the weights that a tile of 16 columns has, so the waves of a block (eight to sixteen) own UT
@@ -502,7 +500,7 @@ __global__ __launch_bounds__(1024) void q4_parts_kernel(const void *__restrict__
 #pragma unroll
             for (int i = 0; i < 8; ++i) ss = fmaf(r.v[i], r.v[i], ss);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) r.v[i] *= k + i < K ? g[k + i] : 0.f;
+            for (int i = 0; i < 8; ++i) r.v[i] *= V || k + i < K ? g[k + i] : 0.f;
         }
         return r;
     };

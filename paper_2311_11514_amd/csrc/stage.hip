@@ -101,7 +101,7 @@ struct hexgen_stage {
     size_t dec_part_row = 0;         // 16 bits: most floats per row of the split decode projections' partial sums (dec_part_floats)
     int last_decode_rows = 0;        // rows of the last decode call that ran on the weight-streaming kernels
     int ws_batch_cap = 0;
-    float *tree_part = nullptr;      // from the first tree call on: partial results of contexts cut into runs, kTreePartFloats
+    float *tree_part = nullptr;      // from the first tree call on: partial results of contexts cut into runs (kTreePartFloats), kTreeUnits counters
     int64_t weight_bytes = 0;
     Profiler prof;
 };
@@ -142,6 +142,8 @@ struct hexgen_tree {
 namespace {
 
 constexpr size_t kTreePartFloats = (size_t)16 << 20;        // 64 MB
+constexpr long kTreeSharedTiles = 16384;                     // tiles of 32 rows x 32 positions from which blocks share them through LDS
+constexpr long kTreeUnits = 1 << 14;                         // blocks of rows that may share runs: counters behind the partial results
 
 size_t esize(hexgen_dtype_t dt) { return dt == HEXGEN_F32 ? 4 : 2; }
 bool is_h16(hexgen_dtype_t dt) { return dt == HEXGEN_BF16 || dt == HEXGEN_F16; }
@@ -351,26 +353,58 @@ KvGeom geom(const hexgen_stage *st, const hexgen_kv_cache *kv) {
 }
 
 // ---- drafted trees: the attention of every path ----------------------------------------------------------------
-// How many runs the contexts are cut into: enough blocks for the chip, runs of eight tiles at least.
-TreeSplit pick_tree_split(const hexgen_stage *st, const hexgen_kv_cache *kv, const hexgen_tree *tr) {
+// Rows per block, runs and order of a tree attention.  (us; 16 bits, d 128; "few": 32 rows a block and eight waves that each take tiles of their own,
+// 2 and 4: groups of 32 rows that share tiles through LDS; then the runs of a context)
+//   8 heads a kv head, 8 kv heads, 4000 positions: one sequence of 64 nodes: few 33, 2 in four runs 41; eight of 16: few 51, 2 in four 46
+//   32 sequences of 2048: 8 nodes: few 73, 2 64, 2 in two 68, 4 76; 32 nodes: 2 139, 4 114; 16 nodes at 4000: 2 127, 4 140; contexts of
+//   240 .. 4027 and 8 .. 64 nodes: 2 183, 4 202 (three quarters of its rows exist)
+//   one kv head: one sequence of 2048, 26 nodes: few in four runs 17, in eight 16; sixteen of 2048, 32 nodes (128 blocks): few 22, in two runs 27
+TreePlan pick_tree_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, const hexgen_tree *tr) {
     const int G = st->hq_l / st->hkv_l;
-    const int block_rows = is_h16(st->dtype) ? 32 * tree_row_groups(tr->max_n, G) : 16;
-    long work = 0;
+    const bool h16 = is_h16(st->dtype);
     int longest = 1;
-    for (int i = 0; i < tr->batch; ++i) {
-        const int n = tr->cu[i + 1] - tr->cu[i], nt = (kv->lens[i] + n + 31) / 32;
-        if (n == 0) continue;
-        work += (long)((n * G + block_rows - 1) / block_rows) * nt;
-        longest = std::max(longest, nt);
+    struct Work { long blocks = 0, tiles = 0; };             // blocks of that many rows, and the tiles that they walk
+    auto work_of = [&](int rows) {
+        Work w;
+        for (int i = 0; i < tr->batch; ++i) {
+            const int n = tr->cu[i + 1] - tr->cu[i], nt = (kv->lens[i] + n + 31) / 32;
+            if (n == 0) continue;
+            const long rb = (long)((n * G + rows - 1) / rows) * st->hkv_l;
+            w.blocks += rb;
+            w.tiles += rb * nt;
+            longest = std::max(longest, nt);
+        }
+        return w;
+    };
+    TreePlan tp;
+    tp.row_groups = 1;
+    int rows = h16 ? 32 : 16;
+    Work w = work_of(rows);
+    // from there on tiles are shared: in blocks of 64 rows, or of 128 where they give every CU two and hardly more rows that do not exist
+    if (h16 && tr->max_n * G > 32 && w.tiles >= kTreeSharedTiles) {
+        const Work two = work_of(64), four = work_of(128);
+        tp.row_groups = tr->max_n * G > 64 && four.blocks >= 512 && 4 * four.tiles * 100 <= 2 * two.tiles * 108 ? 4 : 2;
+        rows = 32 * tp.row_groups;
+        w = tp.row_groups == 4 ? four : two;
     }
-    work *= st->hkv_l;
-    TreeSplit sp;
-    sp.chunk = (int)std::max(8L, (work + 511) / 512);
-    sp.nsplit = std::min((longest + sp.chunk - 1) / sp.chunk, kTreeMaxSplit);
-    sp.nsplit = (int)std::max((size_t)1, std::min((size_t)sp.nsplit, kTreePartFloats / ((size_t)tr->rows * st->hq_l * (st->d + 2))));
-    sp.part_o = st->tree_part;
-    sp.part_ml = st->tree_part + (size_t)sp.nsplit * tr->rows * st->hq_l * st->d;
-    return sp;
+    tp.chunk = longest;
+    tp.nsplit = 1;
+    if (tp.row_groups > 1) {
+        if (w.blocks < 256) tp.chunk = (int)std::max(8L, (w.tiles + 511) / 512);
+    } else if (w.blocks < 128 && (long)tr->batch * st->hkv_l * tree_row_blocks(tr->max_n, G, rows) <= kTreeUnits) {
+        tp.chunk = (int)std::max(h16 ? 16L : 8L, (w.tiles + 255) / 256);
+    }
+    tp.nsplit = std::min((longest + tp.chunk - 1) / tp.chunk, kTreeMaxSplit);
+    tp.nsplit = (int)std::max((size_t)1, std::min((size_t)tp.nsplit, kTreePartFloats / ((size_t)tr->rows * st->hq_l * (st->d + 2))));
+    tp.part_o = st->tree_part;
+    tp.part_ml = st->tree_part + (size_t)tp.nsplit * tr->rows * st->hq_l * st->d;
+    tp.arrived = reinterpret_cast<unsigned *>(st->tree_part + kTreePartFloats);
+    // longest first; beyond kTreeOrdered sequences as they are (order has to be a permutation of the first ones)
+    const int ordered = std::min(tr->batch, kTreeOrdered);
+    for (int i = 0; i < kTreeOrdered; ++i) tp.order[i] = (uint8_t)i;
+    if (tr->batch <= kTreeOrdered && tp.nsplit == 1)
+        std::stable_sort(tp.order, tp.order + ordered, [&](int a, int b) { return kv->lens[a] > kv->lens[b]; });
+    return tp;
 }
 
 // The raw QKV projection of the trees' rows (16 bits: ws.tree_qkv, packed columns; fp32: ws.qkv32) -> rotated q, cache rows, attention
@@ -378,15 +412,16 @@ void attn_tree(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const Rows &r, 
     Workspace &w = st->ws;
     const KvGeom kg = geom(st, kv);
     const TreeView tv = r.tree->view();
-    const TreeSplit sp = pick_tree_split(st, kv, r.tree);
+    const TreePlan tp = pick_tree_plan(st, kv, r.tree);
+    const TreeIn in{nullptr, nullptr, 0, 0};       // appended by the rotation
     if (is_h16(st->dtype)) {
         h16_t *kc = static_cast<h16_t *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<h16_t *>(kv->v) + (size_t)layer * kv->layer_stride;
         HX_K(st->dtype, launch_tree_rope_append, w.tree_qkv, st->hq_l, kg, tv, kv->d_lens, kv->cos_tab, kv->sin_tab, w.q, kc, vc, s);
-        HX_K(st->dtype, launch_tree_attn, w.q, st->qw, kc, vc, kg, st->hq_l, tv, kv->d_lens, sp, out, s);
+        HX_K(st->dtype, launch_tree_attn, w.q, st->qw, in, kc, vc, kg, st->hq_l, tv, kv->d_lens, tp, out, s);
     } else {
         float *kc = static_cast<float *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<float *>(kv->v) + (size_t)layer * kv->layer_stride;
         f32_launch_tree_rope_append(w.qkv32, st->hq_l, kg, tv, kv->d_lens, kv->cos_tab, kv->sin_tab, w.q32, kc, vc, s);
-        f32_launch_tree_attn(w.q32, st->qw, kc, vc, kg, st->hq_l, tv, kv->d_lens, sp, static_cast<float *>(out.o), s);
+        f32_launch_tree_attn(w.q32, st->qw, in, kc, vc, kg, st->hq_l, tv, kv->d_lens, tp, static_cast<float *>(out.o), s);
     }
 }
 
@@ -784,7 +819,14 @@ hexgen_status_t tree_stage(hexgen_tree *tr, int32_t **words, int *slot) {
 hexgen_status_t ensure_tree_part(hexgen_stage *st, hipStream_t s) {
     if (st->tree_part != nullptr) return HEXGEN_OK;
     HX_TRY(refuse_capture(s));
-    return dmalloc(&st->tree_part, kTreePartFloats);
+    float *p = nullptr;
+    HX_TRY(dmalloc(&p, kTreePartFloats + kTreeUnits));
+    hipError_t e = hipMemset(p + kTreePartFloats, 0, kTreeUnits * sizeof(unsigned));
+    if (e == hipSuccess) e = hipDeviceSynchronize();          // the fill ran on the null stream
+    if (e != hipSuccess) (void)hipFree(p);
+    HX_HIP(e);
+    st->tree_part = p;
+    return HEXGEN_OK;
 }
 hexgen_status_t check_tree(const hexgen_kv_cache *kv, const hexgen_tree *tr) {
     if (!kv->prefilled || tr->batch == 0 || tr->batch != kv->batch) return HEXGEN_ERR_STATE;
@@ -1399,15 +1441,14 @@ hexgen_status_t hexgen_kv_tree_attention(hexgen_kv_cache_t *kv, int layer, const
     HX_TRY(ensure_tree_part(st, s));
     const KvGeom kg = geom(st, kv);
     const TreeView tv = tr->view();
-    const TreeSplit sp = pick_tree_split(st, kv, tr);
+    const TreePlan tp = pick_tree_plan(st, kv, tr);
+    const TreeIn in{k, v, ldk, ldv};
     if (is_h16(st->dtype)) {
         h16_t *kc = static_cast<h16_t *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<h16_t *>(kv->v) + (size_t)layer * kv->layer_stride;
-        HX_K(st->dtype, launch_tree_append, static_cast<const h16_t *>(k), ldk, static_cast<const h16_t *>(v), ldv, kc, vc, kg, tv, kv->d_lens, s);
-        HX_K(st->dtype, launch_tree_attn, static_cast<const h16_t *>(q), ldq, kc, vc, kg, st->hq_l, tv, kv->d_lens, sp, TreeOut{TREE_OUT_ROWS, tr->rows, st->qw, out}, s);
+        HX_K(st->dtype, launch_tree_attn, static_cast<const h16_t *>(q), ldq, in, kc, vc, kg, st->hq_l, tv, kv->d_lens, tp, TreeOut{TREE_OUT_ROWS, tr->rows, st->qw, out}, s);
     } else {
         float *kc = static_cast<float *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<float *>(kv->v) + (size_t)layer * kv->layer_stride;
-        f32_launch_tree_append(static_cast<const float *>(k), ldk, static_cast<const float *>(v), ldv, kc, vc, kg, tv, kv->d_lens, s);
-        f32_launch_tree_attn(static_cast<const float *>(q), ldq, kc, vc, kg, st->hq_l, tv, kv->d_lens, sp, static_cast<float *>(out), s);
+        f32_launch_tree_attn(static_cast<const float *>(q), ldq, in, kc, vc, kg, st->hq_l, tv, kv->d_lens, tp, static_cast<float *>(out), s);
     }
     HX_HIP(hipGetLastError());
     return HEXGEN_OK;
