@@ -143,6 +143,7 @@ namespace {
 
 constexpr size_t kTreePartFloats = (size_t)16 << 20;        // 64 MB
 constexpr long kTreeSharedTiles = 16384;                     // tiles of 32 rows x 32 positions from which blocks share them through LDS
+constexpr long kTreeBlocks = 224;                            // blocks that runs of the contexts may make, of those that have a CU each
 constexpr long kTreeUnits = 1 << 14;                         // blocks of rows that may share runs: counters behind the partial results
 
 size_t esize(hexgen_dtype_t dt) { return dt == HEXGEN_F32 ? 4 : 2; }
@@ -358,7 +359,14 @@ KvGeom geom(const hexgen_stage *st, const hexgen_kv_cache *kv) {
 //   8 heads a kv head, 8 kv heads, 4000 positions: one sequence of 64 nodes: few 33, 2 in four runs 41; eight of 16: few 51, 2 in four 46
 //   32 sequences of 2048: 8 nodes: few 73, 2 64, 2 in two 68, 4 76; 32 nodes: 2 139, 4 114; 16 nodes at 4000: 2 127, 4 140; contexts of
 //   240 .. 4027 and 8 .. 64 nodes: 2 183, 4 202 (three quarters of its rows exist)
-//   one kv head: one sequence of 2048, 26 nodes: few in four runs 17, in eight 16; sixteen of 2048, 32 nodes (128 blocks): few 22, in two runs 27
+// "Few" and fp32 blocks have a CU each: runs must not make more blocks than there are CUs, with some to spare (kTreeBlocks), and a run costs its
+// share of the joining, 0.5 us where a tile of a run costs 0.14, so that the best length goes with the root of the context's.
+//   one kv head, eight heads, runs of 8, 10, 16, 24 tiles and whole: one sequence of 2048, 26 nodes: 18.3, 15.8, 15.4, 17.1, 19.6; sixteen, 8 nodes:
+//   26.5 (288 blocks), 16.6, 16.0, 18.3, 20.3; one of 4000, 16 nodes: 18.2, 18.6, 16.7, 15.3, 28.9; eight of 600: 14.7, 15.5, 14.8, -, 12.3; sixteen of
+//   2048, 32 nodes (128 blocks): in two runs 27, whole 22.  Eight kv heads, one sequence of 1000, 8 nodes: 15.6, 14.7, 16.4, 15.3, 14.7; of 4000, 16
+//   nodes: 43.5, 30.9, 23.0 (256 blocks), 18.1, 30.5
+//   fp32, runs of 4, 8, 10, 16 and whole: four of 2048, 4 kv heads, 8 nodes: 28.9, 29.3 (288 blocks), 22.6, 27.5, 66.5; eight of 600, one kv head:
+//   15.4, 16.9, 18.9, 24.2, 24.3
 TreePlan pick_tree_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, const hexgen_tree *tr) {
     const int G = st->hq_l / st->hkv_l;
     const bool h16 = is_h16(st->dtype);
@@ -392,7 +400,9 @@ TreePlan pick_tree_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, const
     if (tp.row_groups > 1) {
         if (w.blocks < 256) tp.chunk = (int)std::max(8L, (w.tiles + 511) / 512);
     } else if (w.blocks < 128 && (long)tr->batch * st->hkv_l * tree_row_blocks(tr->max_n, G, rows) <= kTreeUnits) {
-        tp.chunk = (int)std::max(h16 ? 16L : 8L, (w.tiles + 255) / 256);
+        const long fit = (w.tiles + kTreeBlocks - 1) / kTreeBlocks;
+        if (!h16) tp.chunk = (int)std::max(4L, fit);
+        else if (longest > 48) tp.chunk = (int)std::max({16L, fit, (long)(2 * std::sqrt((double)longest))});
     }
     tp.nsplit = std::min((longest + tp.chunk - 1) / tp.chunk, kTreeMaxSplit);
     tp.nsplit = (int)std::max((size_t)1, std::min((size_t)tp.nsplit, kTreePartFloats / ((size_t)tr->rows * st->hq_l * (st->d + 2))));
