@@ -136,9 +136,9 @@ def _i32(seq: Optional[Sequence[int]]):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream_handle(stream: Optional[torch.cuda.Stream]) -> Optional[int]:
+def _stream_handle(stream: Optional[torch.cuda.Stream], here: Optional[int] = None) -> Optional[int]:
     if stream is None and _raw_stream is not None:
-        return _raw_stream(torch.cuda.current_device()) or None
+        return _raw_stream(torch.cuda.current_device() if here is None else here) or None
     s = stream if stream is not None else torch.cuda.current_stream()
     return s.cuda_stream or None
 
@@ -151,19 +151,19 @@ def _empty_like_of(t: torch.Tensor, shape, dtype, stream: Optional[torch.cuda.St
         return torch.empty(shape, dtype=dtype, device=t.device)
 
 
-def _device_tensor(t: torch.Tensor, name: str, shape, dtype) -> None:
-    """A tensor that is handed on as a dense device pointer: checked here, where its shape, type and place are known."""
+def _device_tensor(t: torch.Tensor, name: str, shape, dtype, here: int) -> None:
+    """A tensor that is handed on as a dense device pointer: checked here, where its shape, type and place are known (here: the current GPU)."""
     if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous {tuple(shape)} tensor of {dtype} is wanted, got {tuple(t.shape)} of {t.dtype}, strides {tuple(t.stride())}")
-    _on_device(t, name)
+    _on_device(t, name, here)
 
 
-def _on_device(t: torch.Tensor, name: str) -> None:
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+def _on_device(t: torch.Tensor, name: str, here: int) -> None:
+    if not t.is_cuda or t.get_device() != here:
         raise ValueError(f"{name}: on {t.device}, not on the current GPU")
 
 
-def _rows_of_heads(t: torch.Tensor, name: str, rows: int, heads: int, d: int, dtype) -> int:
+def _rows_of_heads(t: torch.Tensor, name: str, rows: int, heads: int, d: int, dtype, here: int) -> int:
     """Elements between the rows of a [rows, heads, d] or [rows, heads * d] tensor whose rows are dense."""
     flat = t.dim() == 2
     if t.shape != ((rows, heads * d) if flat else (rows, heads, d)) or t.dtype != dtype:
@@ -171,12 +171,15 @@ def _rows_of_heads(t: torch.Tensor, name: str, rows: int, heads: int, d: int, dt
     stride = t.stride()
     if stride[-1] != 1 or (not flat and heads > 1 and stride[1] != d):
         raise ValueError(f"{name}: the elements of a row have to be dense, got strides {stride}")
-    _on_device(t, name)
+    _on_device(t, name, here)
     return stride[0] if rows > 1 else heads * d
 
 
+_TORCH_DTYPE = {HEXGEN_F32: torch.float32, HEXGEN_BF16: torch.bfloat16, HEXGEN_F16: torch.float16}
+
+
 def _torch_dtype(dtype: int):
-    return {HEXGEN_F32: torch.float32, HEXGEN_BF16: torch.bfloat16, HEXGEN_F16: torch.float16}[dtype]
+    return _TORCH_DTYPE[dtype]
 
 
 def _dtype_code(dtype) -> int:
@@ -241,12 +244,12 @@ class Stage:
     def decode_tree(self, kv: "KVCache", tree: "Tree", hidden_in: torch.Tensor, out_partial: torch.Tensor,
                     out_resid: Optional[torch.Tensor] = None, stream=None):
         """hexgen_stage_decode_tree: the drafted trees' rows through every layer; the committed lengths stay."""
-        shape, td = (tree.rows, self.hidden), _torch_dtype(self.dtype)
+        shape, td, here = (tree.rows, self.hidden), _torch_dtype(self.dtype), torch.cuda.current_device()
         for name, t in (("hidden_in", hidden_in), ("out_partial", out_partial), ("out_resid", out_resid)):
             if t is not None:
-                _device_tensor(t, name, shape, td)
+                _device_tensor(t, name, shape, td, here)
         _check(lib.hexgen_stage_decode_tree(self.handle, kv.handle, tree.handle, _ptr(hidden_in), _ptr(out_partial),
-                                            _ptr(out_resid), _stream_handle(stream)), "hexgen_stage_decode_tree")
+                                            _ptr(out_resid), _stream_handle(stream, here)), "hexgen_stage_decode_tree")
 
     def decode_static_bytes(self, batch: int) -> int:
         return int(lib.hexgen_stage_decode_static_bytes(self.handle, batch))
@@ -335,16 +338,17 @@ class KVCache:
                        out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """hexgen_kv_tree_attention: q [rows, hq_local, head_dim], k, v [rows, hkv_local, head_dim] of the trees' nodes, rotated; rows may
         be apart (parts of a fused projection).  Returns [rows, hq_local, head_dim]."""
-        st, rows, td = self.stage, tree.rows, _torch_dtype(self.stage.dtype)
-        ldq = _rows_of_heads(q, "q", rows, st.hq_l, st.head_dim, td)
-        ldk = _rows_of_heads(k, "k", rows, st.hkv_l, st.head_dim, td)
-        ldv = _rows_of_heads(v, "v", rows, st.hkv_l, st.head_dim, td)
+        st, rows, here = self.stage, tree.rows, torch.cuda.current_device()
+        td, hq, hkv, d = _TORCH_DTYPE[st.dtype], st.hq_l, st.hkv_l, st.head_dim
+        ldq = _rows_of_heads(q, "q", rows, hq, d, td, here)
+        ldk = _rows_of_heads(k, "k", rows, hkv, d, td, here)
+        ldv = _rows_of_heads(v, "v", rows, hkv, d, td, here)
         if out is None:
-            out = _empty_like_of(q, (rows, st.hq_l, st.head_dim), td, stream)
+            out = _empty_like_of(q, (rows, hq, d), td, stream)
         else:
-            _device_tensor(out, "out", (rows, st.hq_l, st.head_dim), td)
+            _device_tensor(out, "out", (rows, hq, d), td, here)
         _check(lib.hexgen_kv_tree_attention(self.handle, layer, tree.handle, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
-                                            out.data_ptr(), _stream_handle(stream)), "hexgen_kv_tree_attention")
+                                            out.data_ptr(), _stream_handle(stream, here)), "hexgen_kv_tree_attention")
         return out
 
     def keep(self, tree: "Tree", kept: Sequence[int], path: Sequence[int], stream=None):
@@ -382,12 +386,14 @@ class Tree:
 
     def accept(self, draft: torch.Tensor, chosen: torch.Tensor, stream=None):
         """hexgen_tree_accept: draft, chosen int32 [rows] -> (kept [batch], path [rows], tokens [rows]), int32 on the device."""
-        for name, t in (("draft", draft), ("chosen", chosen)):
-            _device_tensor(t, name, (self.rows,), torch.int32)
-        kept, path, tokens = _empty_like_of(draft, (self.batch + 2 * self.rows,), torch.int32, stream).split((self.batch, self.rows, self.rows))
-        _check(lib.hexgen_tree_accept(self.handle, draft.data_ptr(), chosen.data_ptr(), kept.data_ptr(), path.data_ptr(), tokens.data_ptr(),
-                                      _stream_handle(stream)), "hexgen_tree_accept")
-        return kept, path, tokens
+        batch, rows, here = self.batch, self.rows, torch.cuda.current_device()
+        _device_tensor(draft, "draft", (rows,), torch.int32, here)
+        _device_tensor(chosen, "chosen", (rows,), torch.int32, here)
+        out = _empty_like_of(draft, (batch + 2 * rows,), torch.int32, stream)
+        at = out.data_ptr()
+        _check(lib.hexgen_tree_accept(self.handle, draft.data_ptr(), chosen.data_ptr(), at, at + 4 * batch, at + 4 * (batch + rows),
+                                      _stream_handle(stream, here)), "hexgen_tree_accept")
+        return out.split_with_sizes((batch, rows, rows))
 
 
 def stream_copy(dst: torch.Tensor, src: torch.Tensor, blocks: int = 4096, stream=None):
@@ -436,12 +442,13 @@ class Q4Matrix:
         td, rows = _torch_dtype(self.dtype), x.shape[0] if x.dim() == 2 else 0
         if x.dim() != 2 or x.shape[1] != self.n_in or rows < 1 or x.dtype != td or (self.n_in > 1 and x.stride(1) != 1):
             raise ValueError(f"x: a (rows, {self.n_in}) tensor of {td} with dense rows is wanted, got {tuple(x.shape)} of {x.dtype}, strides {tuple(x.stride())}")
-        _on_device(x, "x")
+        here = torch.cuda.current_device()
+        _on_device(x, "x", here)
         if out is None:
             out = _empty_like_of(x, (rows, self.n_out), td, stream)
         else:
-            _device_tensor(out, "out", (rows, self.n_out), td)
-        _check(lib.hexgen_q4_project(self.handle, x.data_ptr(), x.stride(0) if rows > 1 else self.n_in, rows, out.data_ptr(), _stream_handle(stream)),
+            _device_tensor(out, "out", (rows, self.n_out), td, here)
+        _check(lib.hexgen_q4_project(self.handle, x.data_ptr(), x.stride(0) if rows > 1 else self.n_in, rows, out.data_ptr(), _stream_handle(stream, here)),
                "hexgen_q4_project")
         return out
 

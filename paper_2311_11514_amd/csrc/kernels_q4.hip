@@ -15,6 +15,9 @@
 // and the others are a shift or turn of 4, 8 and 12 away.
 // Scales have a row for every group, or for every 128 features where groups are larger; zero points are bytes 16 + z, or one row of 24s.
 #include <algorithm>
+#include <cmath>
+#include <cstddef>
+#include <cstdint>
 #include <type_traits>
 
 #include "kernels.h"
@@ -170,16 +173,18 @@ __device__ __forceinline__ void best_of_lanes(float &bv, int &bi) {
     }
 }
 
-// Up to 16 operand columns (rows times parts; columns beyond C repeat the last one and are not stored).  A block of W waves owns UT
-// tiles of 16 columns over the whole contraction; its waves take the 128-feature blocks in turn and are summed through LDS in wave order, so
-// that no partial result leaves the block.  A wave holds R blocks with their scales in registers, requested that far ahead; every request is
+// Few operand columns (rows times parts), or a small matrix: a block takes up to 16 of them, whole rows (blockIdx.y; columns that are not there repeat
+// the last one and are not stored).  A block of W waves owns UT tiles of 16 columns over the whole contraction; its waves take the 128-feature
+// blocks in turn and are summed through LDS in wave order, so that no partial result leaves the block.  A wave holds R blocks with their scales in registers, requested that far ahead; every request is
 // unconditional (past the end it repeats the last block's), so that the compiler can count what is in flight and waits for the oldest
 // alone.  XLDS: the operand is staged in LDS once, else a wave requests its pieces one block ahead, from L2.
 // Bound by HBM on wide matrices, on small ones by the launch and one round trip.
 // FL: 32-feature steps of a scale's group inside a 128-feature block (4: groups of 128 and more).
 template <bool F16, int ST, int UT, int FL, int W, int R, bool XLDS>
-__global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) void q4_few_kernel(Q4View m, const h16_t *__restrict__ x, int64_t ldx, int C, int T, Q4Out out) {
+__global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) void q4_few_kernel(Q4View m, const h16_t *__restrict__ x, int64_t ldx, int parts, int rows, Q4Out out) {
     constexpr int NF = 4 / FL;
+    const int t0 = blockIdx.y * (16 / parts), T = min(16 / parts, rows - t0), C = parts * T;
+    auto operand = [&](int c) { return x + (size_t)(c / T * rows + t0 + c % T) * ldx; };
     static_assert(R % 2 == 0, "the operand's two slots alternate");
     __shared__ floatx4 red[W][UT][64];
     extern __shared__ __align__(16) u32x4 xs[];                 // XLDS: [k / 8][column]
@@ -192,7 +197,7 @@ __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) v
         off[u] = t * 1024u + lane * 16u;
         col[u] = t * 16u + 4u * g;
     }
-    const h16_t *xp = x + (size_t)min(j, C - 1) * ldx + 8 * g;
+    const h16_t *xp = operand(min(j, C - 1)) + 8 * g;
     const Widen widen = Widen::make<F16>();
     const uint32_t one = F16 ? 0x3c003c00u : 0x3f803f80u;
     const u32x4 ones = {one, one, one, one};
@@ -219,7 +224,7 @@ __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) v
     if constexpr (XLDS) {
         const int pieces = m.k_blocks * 16;
         for (int c = 0; c < C; ++c)
-            for (int p = threadIdx.x; p < pieces; p += 64 * W) xs[p * C + c] = *reinterpret_cast<const u32x4 *>(x + (size_t)c * ldx + 8 * p);
+            for (int p = threadIdx.x; p < pieces; p += 64 * W) xs[p * C + c] = *reinterpret_cast<const u32x4 *>(operand(c) + 8 * p);
         HX_LDS_BARRIER();
     } else {
         fetch(0, min(wave, last));
@@ -260,20 +265,20 @@ __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) v
     for (int u = 0; u < UT; ++u) red[wave][u][lane] = acc[u][0];
     __syncthreads();
     // four columns of one row per thread: waves in order, parts in order
-    const int P = C / T, idx = threadIdx.x;
+    const int idx = threadIdx.x;
     if (idx >= T * UT * 4) return;
     const int t = idx / (UT * 4), u = (idx >> 2) % UT, gg = idx & 3;
     floatx4 v = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < P; ++p) {
+    for (int p = 0; p < parts; ++p) {
         floatx4 a = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < W; ++w) a += red[w][u][p * T + t + 16 * gg];
         v += a;
     }
     const int n0 = (tile0 + u) * 16 + 4 * gg;
-    scale_back(out, t, v);
+    scale_back(out, t0 + t, v);
     if (out.best_val == nullptr) {
-        store_columns(m, out, t, n0, v);
+        store_columns(m, out, t0 + t, n0, v);
         return;
     }
     float bv = -INFINITY;
@@ -281,8 +286,8 @@ __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) v
     take_best(m, n0, v, bv, bi);
     best_of_lanes<UT * 4>(bv, bi);                              // the row's UT * 4 threads are neighbours
     if (idx % (UT * 4) == 0) {
-        out.best_val[(size_t)t * gridDim.x + blockIdx.x] = bv;
-        out.best_id[(size_t)t * gridDim.x + blockIdx.x] = bi;
+        out.best_val[(size_t)(t0 + t) * gridDim.x + blockIdx.x] = bv;
+        out.best_id[(size_t)(t0 + t) * gridDim.x + blockIdx.x] = bi;
     }
 }
 
@@ -309,112 +314,157 @@ __device__ __forceinline__ float sum_rows(float v) {
     return sum_halves(__uint_as_float(a[0]) + __uint_as_float(a[1]));
 }
 
-// More operand columns: the operand outweighs the weights that a tile of 16 columns has, so the waves of a block (eight to sixteen) own UT
-// neighbouring tiles each and walk the same 128-feature blocks, whose operand they share through LDS (two buffers, one barrier a step), the
-// columns' sums with it.  The contraction is split over blockIdx.y where the matrix has too few columns for the chip.  Results that need no more
-// adding up (one split, one part) are stored from here; everything else goes to `part` [split][column of the operand][16 n_tiles] and
-// q4_finish_kernel.
-// Bound by HBM, with many rows by LDS: a wave reads NB KB of operand for every UT KB of weights a quarter as often.
-template <bool F16, int ST, int NB, int UT, int FL>
-__global__ __launch_bounds__(UT == 1 ? 1024 : 512, UT == 1 ? 4 : 2) void q4_shared_kernel(Q4View m, const h16_t *__restrict__ x, int64_t ldx, int C, int T, Q4Out out, int per, float *__restrict__ part) {
-    constexpr int NF = 4 / FL, R = 2, XL = (4 * NB + 7) / 8;    // XL: operand pieces a wave fetches per step, of 4 NB (the last ones more than once)
-    static_assert(R % 2 == 0, "the operand's two buffers alternate");
-    __shared__ u32x4 xs[2][4 * NB][64];
-    __shared__ floatx4 xsum[2][NB][16];                         // [operand tile][column][32-feature step]
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
-    const int waves = blockDim.x >> 6, tile0 = (blockIdx.x * waves + wave) * UT;
+// More operand columns: the operand outweighs the weights that a tile of 16 columns has, so the waves of a block share it through LDS.  Two groups
+// of six to eight waves take the 128-feature blocks in turn; a wave owns two neighbouring tiles, and its group's operand, weights, scales and zero points
+// go to LDS without passing registers, up to S - 1 steps ahead, one barrier a step: sixteen waves with few registers, of which some widen and scale
+// while others are at the matrix unit.  The groups are joined through LDS at the end.  The contraction is split over blockIdx.y where the matrix
+// has too few columns for the chip: splits leave partial sums, `part` [split][column of the operand][16 n_tiles], to q4_finish_kernel.  Without
+// splits the parts are joined, and stored or searched for their largest, here.
+template <int ST, int NB, int FL> struct SharedStage {
+    static constexpr int ES = ST == HX_T_F32 ? 4 : 2, NF = 4 / FL, SP = (NF * 256 * ES + 1023) / 1024;      // SP: requests of 1 KB for the scales of 16 tiles
+    u32x4 x[4 * NB][64], w[16][64];
+    unsigned char s[SP * 1024], z[1024];
+};
+template <bool F16, int ST, int NB, int FL>
+__global__ __launch_bounds__(1024, 4) void q4_shared_kernel(Q4View m, const h16_t *__restrict__ x, uint32_t ldx, int C, int T, Q4Out out, int per, float *__restrict__ part) {
+    typedef SharedStage<ST, NB, FL> Stage;
+    constexpr int NF = Stage::NF, ES = Stage::ES, SP = Stage::SP, UT = 2, XL = (4 * NB + 5) / 6;            // XL: operand pieces a wave fetches (the last ones more than once)
+    constexpr int S = 3 * 2 * sizeof(Stage) <= 159 * 1024 ? 3 : 2, L = UT + XL + 1;     // L: requests of a wave per step
+    constexpr int YS = 260;
+    static_assert((S - 2) * L < 64 && 16 * NB * YS * 4 <= 2 * S * sizeof(Stage), "waits, and the results in the stages' place");
+    __shared__ __align__(16) Stage st[2][S];
+    // the columns' sums: the operand against ones, or with four operand tiles, where the registers do not hold these as well, from whoever fetched the
+    // piece (64 columns, 8192 x 28672: 85 / 68 us; 4096 x 4096 24 / 15.5; 32 columns, 8192 x 57344: 66 / 74; 12: 52 / 56; 48 columns as long)
+    constexpr bool TOLD = NB == 4;
+    __shared__ floatx4 xsum[2][2][TOLD ? NB : 1][16];           // [group][parity of its step][operand tile][column][32-feature step]
+    const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4, waves = blockDim.x >> 7;
+    const int nth = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = nth >= waves ? 1 : 0, wave = nth - grp * waves;
+    const int first = blockIdx.x * waves * UT, np = m.n_tiles * 16;
     const int k0 = blockIdx.y * per, k1 = min(k0 + per, m.k_blocks);
-    uint32_t off[UT], col[UT];
+    // what this wave requests: its tiles (one past the last repeats that and is not stored), its pieces of the operand, a part of the scales or the zeros
+    uint32_t woff[UT], xoff[XL], xat[XL];
 #pragma unroll
-    for (int u = 0; u < UT; ++u) {
-        const uint32_t t = min(tile0 + u, m.n_tiles - 1);
-        off[u] = t * 1024u + lane * 16u;
-        col[u] = t * 16u + 4u * g;
-    }
-    const h16_t *xp[XL];
+    for (int u = 0; u < UT; ++u) woff[u] = min(first + wave * UT + u, m.n_tiles - 1) * 1024u + lane * 16u;
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
-        const int f = min(wave + waves * i, 4 * NB - 1), b = f % NB, s = f / NB;
-        xp[i] = x + (size_t)min(16 * b + j, C - 1) * ldx + s * 32 + 8 * g;
+        xat[i] = min(wave + waves * i, 4 * NB - 1);
+        xoff[i] = (min(16 * (int)(xat[i] % NB) + j, C - 1) * ldx + (xat[i] / NB) * 32 + 8 * g) * 2;
     }
+    const int sp = min(wave, SP);
+    const unsigned char *sbase = sp < SP ? static_cast<const unsigned char *>(m.scales) : m.zeros;
+    const uint32_t srow = sp < SP ? np * ES : m.zeros_row;
+    const int sf = sp < SP ? (sp * 1024 + lane * 16) / (256 * ES) : lane >> 4, scol = sp < SP ? (sp * 1024 + lane * 16) % (256 * ES) / ES : 16 * (lane & 15);
+    const uint32_t soff = min(sf, NF - 1) * srow + (sp < SP ? min(first * 16 + scol, np - 16 / ES) * ES : min(first * 16 + scol, np - 16));
+    const unsigned lds = hx_lds_addr(&st[grp][0]);
+    auto issue = [&](int k, int b) {
+        const int kq = min(k, k1 - 1);
+        const unsigned at = lds + b * sizeof(Stage);
+        const unsigned char *wk = static_cast<const unsigned char *>(m.w) + (size_t)kq * m.n_tiles * 1024;
+#pragma unroll
+        for (int u = 0; u < UT; ++u) hx_load_lds16(at + offsetof(Stage, w) + (wave * UT + u) * 1024, woff[u], wk);
+#pragma unroll
+        for (int i = 0; i < XL; ++i) hx_load_lds16(at + xat[i] * 1024, xoff[i], x + kq * 128);
+        hx_load_lds16(at + offsetof(Stage, s) + sp * 1024, soff, sbase + (size_t)kq * NF * srow);
+    };
     const Widen widen = Widen::make<F16>();
+    const uint32_t one = F16 ? 0x3c003c00u : 0x3f803f80u;
+    const u32x4 ones = {one, one, one, one};
     floatx4 acc[UT][NB];
 #pragma unroll
     for (int u = 0; u < UT; ++u)
 #pragma unroll
         for (int b = 0; b < NB; ++b) acc[u][b] = floatx4{0.f, 0.f, 0.f, 0.f};
-    u32x4 wr[R][UT], xg[R][XL];
-    scale_raw<ST> sr[R][UT][NF];
-    uint32_t zr[R][UT][NF];
-    auto request = [&](int i, int kq) {
 #pragma unroll
-        for (int u = 0; u < UT; ++u) wr[i][u] = load_weights(m, kq, off[u]);
+    for (int i = 0; i < S - 1; ++i) issue(k0 + grp + 2 * i, i);
+    int b0 = 0, bl = S - 1, parity = 0;                         // buffers of this step and of the one that is S - 1 steps ahead
+    for (int k = k0 + grp; k - grp < k1; k += 2, parity ^= 1) {
+        HX_WAIT_VM((S - 2) * L);                                // this step's share of this wave; behind the barrier everybody's
+        if constexpr (TOLD) {
 #pragma unroll
-        for (int u = 0; u < UT; ++u) load_scales<ST, NF>(m, kq, col[u], sr[i][u], zr[i][u]);
-    };
-    auto fetch = [&](int slot, int kq) {
-#pragma unroll
-        for (int i = 0; i < XL; ++i) xg[slot][i] = *reinterpret_cast<const u32x4 *>(xp[i] + kq * 128);
-    };
-    auto put = [&](int slot, int buf) {
-#pragma unroll
-        for (int i = 0; i < XL; ++i) {
-            const int f = min(wave + waves * i, 4 * NB - 1), b = f % NB, s = f / NB;
-            xs[buf][f][lane] = xg[slot][i];
-            float v = sum8<F16>(xg[slot][i]);
-            v = sum_rows(v);
-            if (g == 0) reinterpret_cast<float *>(&xsum[buf][b][j])[s] = v;
+            for (int i = 0; i < XL; ++i) {
+                const float v = sum_rows(sum8<F16>(st[grp][b0].x[xat[i]][lane]));
+                if (g == 0) reinterpret_cast<float *>(&xsum[grp][parity][xat[i] % NB][j])[xat[i] / NB] = v;
+            }
         }
-    };
-    auto contract = [&](int i) {
-        floatx4 q[NB];
-#pragma unroll
-        for (int b = 0; b < NB; ++b) q[b] = xsum[i & 1][b][j];
-        auto sums = [&](int f, int b) {
-            float v = q[b][f * FL];
-#pragma unroll
-            for (int s = 1; s < FL; ++s) v += q[b][f * FL + s];
-            return floatx4{v, v, v, v};
-        };
-        contract_block<F16, ST, NB, UT, FL>(widen, wr[i], sr[i], zr[i], [&](int s, int b) { return xs[i & 1][s * NB + b][lane]; }, sums, acc);
-    };
-    // Step k + i is contracted from ring slot i and buffer i % 2, while the next step's operand is put into the buffer that every wave left at
-    // the last barrier; the requests go R steps ahead (past the end they repeat the last one's).  Loads return in order: were the operand
-    // fetched fewer steps ahead than the weights, waiting for it would be waiting for them.
-    auto step = [&](int i, int k) {
-        put((i + 1) % R, (i & 1) ^ 1);
-        fetch((i + 1) % R, min(k + 1 + R, k1 - 1));
-        contract(i);
-        request(i, min(k + R, k1 - 1));
         HX_LDS_BARRIER();
-        __builtin_amdgcn_sched_barrier(0);                      // (side by side two steps do not fit the registers)
-    };
+        issue(k + 2 * (S - 1), bl);                             // (everybody has left that buffer)
+        bl = b0;
+        const Stage &cur = st[grp][b0];
+        b0 = b0 + 1 == S ? 0 : b0 + 1;
+        if (k >= k1) break;                                     // the second group, after an odd number of steps
+        u32x4 w[UT];
+        scale_raw<ST> sc[UT][NF];
+        uint32_t zc[UT][NF];
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-        fetch(i, min(k0 + i, k1 - 1));
-        request(i, min(k0 + i, k1 - 1));
+        for (int u = 0; u < UT; ++u) {
+            const int tile = wave * UT + u;
+            w[u] = cur.w[tile][lane];
+#pragma unroll
+            for (int f = 0; f < NF; ++f) {
+                sc[u][f] = *reinterpret_cast<const scale_raw<ST> *>(cur.s + (f * 256 + tile * 16 + 4 * g) * ES);
+                zc[u][f] = *reinterpret_cast<const uint32_t *>(cur.z + f * 256 + tile * 16 + 4 * g);
+            }
+        }
+        auto sums = [&](int f, int b) {
+            if constexpr (TOLD) {
+                const float *q = reinterpret_cast<const float *>(&xsum[grp][parity][b][j]) + f * FL;
+                float v = q[0];
+#pragma unroll
+                for (int i = 1; i < FL; ++i) v += q[i];
+                return floatx4{v, v, v, v};
+            } else {
+                floatx4 X = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = f * FL; i < f * FL + FL; ++i) X = mfma<F16>(ones, cur.x[i * NB + b][lane], X);
+                return X;
+            }
+        };
+        contract_block<F16, ST, NB, UT, FL>(widen, w, sc, zc, [&](int i, int b) { return cur.x[i * NB + b][lane]; }, sums, acc);
     }
-    put(0, 0);
-    fetch(0, min(k0 + R, k1 - 1));
+    HX_WAIT_VM(0);                                              // nothing is on its way into the stages any more
     HX_LDS_BARRIER();
-    int k = k0;
-    for (; k + R <= k1; k += R) {
+    float *ys = reinterpret_cast<float *>(&st[0][0]);
+    if (grp == 1) {
 #pragma unroll
-        for (int i = 0; i < R; ++i) step(i, k + i);
+        for (int u = 0; u < UT; ++u)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) *reinterpret_cast<floatx4 *>(ys + (16 * b + j) * YS + (wave * UT + u) * 16 + 4 * g) = acc[u][b];
     }
+    HX_LDS_BARRIER();
+    if (grp == 0) {
 #pragma unroll
-    for (int i = 0; i < R; ++i)
-        if (k + i < k1) step(i, k + i);                         // uniform over the block
-    const bool own = part == nullptr;
+        for (int u = 0; u < UT; ++u) {
+            const int tile = first + wave * UT + u;
 #pragma unroll
-    for (int u = 0; u < UT; ++u) {
-        if (tile0 + u >= m.n_tiles) continue;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int c = 16 * b + j, n0 = (tile0 + u) * 16 + 4 * g;
-            if (c >= C) continue;
-            if (own) store_columns(m, out, c, n0, acc[u][b]);
-            else *reinterpret_cast<floatx4 *>(part + ((size_t)blockIdx.y * C + c) * (m.n_tiles * 16) + n0) = acc[u][b];
+            for (int b = 0; b < NB; ++b) {
+                const int c = 16 * b + j;
+                floatx4 *at = reinterpret_cast<floatx4 *>(ys + c * YS + (wave * UT + u) * 16 + 4 * g);
+                const floatx4 v = acc[u][b] + *at;
+                if (part == nullptr) *at = v;
+                else if (c < C && tile < m.n_tiles) *reinterpret_cast<floatx4 *>(part + ((size_t)blockIdx.y * C + c) * np + tile * 16 + 4 * g) = v;
+            }
+        }
+    }
+    if (part != nullptr) return;
+    HX_LDS_BARRIER();
+    // parts in order, a wave per row, four columns per lane
+    const int n0 = first * 16 + 4 * lane;
+    const bool there = lane < waves * UT * 4 && n0 < np;
+    for (int t = nth; t < T; t += 2 * waves) {
+        floatx4 v = *reinterpret_cast<const floatx4 *>(ys + t * YS + 4 * lane);
+        for (int c = t + T; c < C; c += T) v += *reinterpret_cast<const floatx4 *>(ys + c * YS + 4 * lane);
+        scale_back(out, t, v);
+        if (out.best_val == nullptr) {
+            if (there) store_columns(m, out, t, n0, v);
+            continue;
+        }
+        float bv = -INFINITY;
+        int bi = 0x7fffffff;
+        if (there) take_best(m, n0, v, bv, bi);
+        best_of_lanes<64>(bv, bi);
+        if (lane == 0) {
+            out.best_val[(size_t)t * gridDim.x + blockIdx.x] = bv;
+            out.best_id[(size_t)t * gridDim.x + blockIdx.x] = bi;
         }
     }
 }
@@ -593,61 +643,75 @@ __global__ __launch_bounds__(256) void q4_pack_scales_kernel(const void *__restr
 }
 
 // ---- which form --------------------------------------------------------------------------------------------------
-// Up to 16 operand columns: the few form, with the operand in LDS up to 32 KB of it.  (us, group 128, bf16, operand in LDS / from L2 / shared form:
-// 8192 x 57344, one column 43 / 54 / -; 8192 x 10240, one 12.4 / 15 / -; 4096 x 4096, eight 7.4 / 6.4 / -; 8192 x 57344, twelve - / 56 / 49;
-// 28672 x 8192, four - / 29 / 28)
-constexpr int kLdsOperand = 32 * 1024;
+// By tiles of 16 columns (n), 128-feature blocks (k) and operand columns (C).  us for group 128, bf16:
+//   n >= 512: the few form with the operand in LDS up to 4 columns, or 8 of a matrix below n = 1024, and 32 KB, else the shared form (k = 64, n = 1792:
+//   one column 27.8 / 33.6, four 34.5 / 30.1, eight - / 31.1; k = 16, n = 1792: four 11.2 / 12.8, eight 13.6 / 12.9; n = 640: eight 8.2 / 9.7).  One
+//   tile a block below n = 1024 with one or two columns (k = 64, n = 640: one tile 14.0, two 15.6)
+//   n < 512, k > 64: eight waves and the operand in LDS up to 64 KB of it, else the shared form (k = 64, n = 160, one column: 7.1, four waves from L2
+//   8.3, shared 12.2; k = 224, one column 14.8 / 20.6 / 17.3, four - / 21.8 / 17.4)
+//   else the few form with the operand from L2, in groups of 16 columns: four waves while it makes 256 blocks, eight waves and two tiles while it makes
+//   512, or 1024 where contractions are short, else the shared form (k = 32, n = 160: 8 columns 6.5 / 7.5 / 10.2, 24: 11.6 / 9.5 / 11.9, 64: 18.6 /
+//   16.4 / 14.8; k = 16, n = 256, 64 columns: 15.6 / 11.4 / 13.3)
+// Groups of 32 have four times the scales, for which two tiles leave no registers: one tile a block while that makes 256 blocks, or little work, and with
+// n >= 512 up to 8 columns of a matrix below n = 1024 (k = 64, n = 1792, one column: one tile 44.9, two 49.6, shared 42.0; k = 16, n = 640, four: 9.6 /
+// 11.0 / 10.8; k = 64, n = 256, 24 columns: 23.0 / 19.8 / 15.8; k = 4, n = 256, 48: 6.6 / 8.9 / 10.0)
 enum { FEW_LDS_WIDE, FEW_LDS, FEW_LDS_NARROW, FEW_WIDE, FEW, SHARED };
 int form_of(const Q4View &m, int C) {
-    if (C > 16) return SHARED;
-    if (C * m.k_blocks * 256 <= kLdsOperand) return m.n_tiles >= 1024 ? FEW_LDS_WIDE : m.n_tiles >= 256 ? FEW_LDS : FEW_LDS_NARROW;
-    return m.n_tiles >= 1024 ? SHARED : m.n_tiles >= 512 ? FEW_WIDE : FEW;
+    const int n = m.n_tiles, k = m.k_blocks, blocks = n * ((C + 15) / 16), operand = C > 16 ? INT32_MAX : C * k * 256;
+    const bool one = m.group == 32;
+    if (n >= 512) {
+        if (operand > 32 * 1024 || C > (n < 1024 ? 8 : one ? 0 : 4)) return SHARED;
+        return n < 1024 && (one || C <= 2) ? FEW_LDS : FEW_LDS_WIDE;
+    }
+    if (k >= 64 && operand <= 64 * 1024) return FEW_LDS_NARROW;
+    if (k > 64) return SHARED;
+    if (one) return blocks <= 256 || (long)blocks * k <= 8192 ? FEW : SHARED;
+    return blocks <= 256 ? FEW : blocks <= (k <= 16 ? 1024 : 512) ? FEW_WIDE : SHARED;
 }
 int few_tiles(int form) { return form == FEW_LDS_WIDE || form == FEW_WIDE ? 2 : 1; }
 
-// The shared form's blocks: waves per block (one tile of 16 columns each, or two with many operand columns, which halves their way through LDS) and
-// splits of the contraction, by the steps that the fullest CU has to do; a split costs its partial sums and, the first one, a launch (us, 32 columns,
-// 8192 x 10240: 10 waves, four splits 19.2, 8 waves, three 20.1, 16 waves, one 33; 8192 x 57344: 14 waves 57, 16 waves 59, 8 waves 67;
-// 48 columns, 4096 x 50304: one tile 45, two tiles 43; 28672 x 8192, 40 columns: 47 / 43).
-struct SharedShape { int tiles, waves, splits; };
+// The shared form's blocks: waves per group (two tiles of 16 columns each) and splits of the contraction, by the steps that the fullest CU has to
+// do; a split costs its partial sums and, the first one, a launch (us, bf16: 8192 x 57344, 32 columns: 8 waves 66, 7 73, 8 and two splits 77; 8192 x
+// 10240: 6 waves and four splits 21, 8 and four 23, 7 and two 35; 28672 x 8192, 40 columns: 8 waves and eight splits 48, 7 and four 64).
+struct SharedShape { int waves, splits; };
 SharedShape shared_shape(const Q4View &m, int C) {
-    const int tiles = C > 48 || (C > 32 && m.n_tiles >= 512) ? 2 : 1;
-    SharedShape best{tiles, 8, 1};
+    SharedShape best{8, 1};
     float least = INFINITY;
-    for (int w = 8; w <= (tiles == 2 ? 8 : 16); ++w)
+    for (int w = 8; w >= 6; --w)
         for (int sp = 1; sp <= 16 && sp * 4 <= std::max(4, m.k_blocks); ++sp) {
-            const int blocks = (m.n_tiles + w * tiles - 1) / (w * tiles) * sp, steps = (m.k_blocks + sp - 1) / sp;
+            const int blocks = (m.n_tiles + 2 * w - 1) / (2 * w) * sp, steps = (m.k_blocks + sp - 1) / sp;
             const float cost = (float)((blocks + 255) / 256) * w * (steps + 4) * (1.0f + (sp > 1 ? 0.1f + 0.01f * sp : 0.f));
-            if (cost < least) { least = cost; best = SharedShape{tiles, w, sp}; }
+            if (cost < least) { least = cost; best = SharedShape{w, sp}; }
         }
     const int per = (m.k_blocks + best.splits - 1) / best.splits;
     best.splits = (m.k_blocks + per - 1) / per;
     return best;
 }
 
+int shared_blocks(const Q4View &m, const SharedShape &sh) { return (m.n_tiles + 2 * sh.waves - 1) / (2 * sh.waves); }
+
 template <bool F16, int ST, int FL>
 void launch_few(const Q4View &m, int form, const h16_t *x, int64_t ldx, int C, int T, const Q4Out &out, hipStream_t s) {
-    const dim3 grid((m.n_tiles + few_tiles(form) - 1) / few_tiles(form));
-    const size_t lds = (size_t)C * m.k_blocks * 256;
-    if (form == FEW_LDS_WIDE) hipLaunchKernelGGL((q4_few_kernel<F16, ST, 2, FL, 4, 2, true>), grid, dim3(256), lds, s, m, x, ldx, C, T, out);
-    else if (form == FEW_LDS) hipLaunchKernelGGL((q4_few_kernel<F16, ST, 1, FL, 4, FL == 1 ? 2 : 4, true>), grid, dim3(256), lds, s, m, x, ldx, C, T, out);
-    else if (form == FEW_LDS_NARROW) hipLaunchKernelGGL((q4_few_kernel<F16, ST, 1, FL, 8, FL == 1 ? 2 : 4, true>), grid, dim3(512), lds, s, m, x, ldx, C, T, out);
-    else if (form == FEW_WIDE) hipLaunchKernelGGL((q4_few_kernel<F16, ST, 2, FL, 8, 2, false>), grid, dim3(512), 0, s, m, x, ldx, C, T, out);
-    else hipLaunchKernelGGL((q4_few_kernel<F16, ST, 1, FL, 4, FL == 1 ? 2 : 4, false>), grid, dim3(256), 0, s, m, x, ldx, C, T, out);
+    const int parts = C / T, rows = 16 / parts;
+    const dim3 grid((m.n_tiles + few_tiles(form) - 1) / few_tiles(form), (T + rows - 1) / rows);
+    const size_t lds = (size_t)std::min(C, 16) * m.k_blocks * 256;
+#define HX_FEW(UT, W, R, XLDS) hipLaunchKernelGGL((q4_few_kernel<F16, ST, UT, FL, W, R, XLDS>), grid, dim3(64 * W), XLDS ? lds : 0, s, m, x, ldx, parts, T, out)
+    if constexpr (FL > 1) {
+        if (form == FEW_LDS_WIDE) HX_FEW(2, 4, 2, true);
+        else if (form == FEW_WIDE) HX_FEW(2, 8, 2, false);
+    }
+    if (form == FEW_LDS) HX_FEW(1, 4, (FL == 1 ? 2 : 4), true);
+    else if (form == FEW_LDS_NARROW) HX_FEW(1, 8, (FL == 1 ? 2 : 4), true);
+    else if (form == FEW) HX_FEW(1, 4, (FL == 1 ? 2 : 4), false);
+#undef HX_FEW
 }
 template <bool F16, int ST, int NB, int FL>
 void launch_shared(const Q4View &m, const h16_t *x, int64_t ldx, int C, int T, const Q4Out &out, float *part, hipStream_t s) {
     const SharedShape sh = shared_shape(m, C);
     const int per = (m.k_blocks + sh.splits - 1) / sh.splits;
-    const bool own = sh.splits == 1 && C == T && out.best_val == nullptr;
-    const dim3 grid((m.n_tiles + sh.waves * sh.tiles - 1) / (sh.waves * sh.tiles), sh.splits);
-    if constexpr (NB > 2) {
-        if (sh.tiles == 2) hipLaunchKernelGGL((q4_shared_kernel<F16, ST, NB, 2, FL>), grid, dim3(64 * sh.waves), 0, s, m, x, ldx, C, T, out, per, own ? nullptr : part);
-    }
-    if constexpr (NB < 4) {
-        if (sh.tiles == 1) hipLaunchKernelGGL((q4_shared_kernel<F16, ST, NB, 1, FL>), grid, dim3(64 * sh.waves), 0, s, m, x, ldx, C, T, out, per, own ? nullptr : part);
-    }
-    if (!own) hipLaunchKernelGGL(q4_finish_kernel, dim3((m.n_tiles * 16 + 1023) / 1024, T), dim3(256), 0, s, m, part, sh.splits, C, T, out);
+    const dim3 grid(shared_blocks(m, sh), sh.splits);
+    hipLaunchKernelGGL((q4_shared_kernel<F16, ST, NB, FL>), grid, dim3(128 * sh.waves), 0, s, m, x, (uint32_t)ldx, C, T, out, per, sh.splits == 1 ? nullptr : part);
+    if (sh.splits > 1) hipLaunchKernelGGL(q4_finish_kernel, dim3((m.n_tiles * 16 + 1023) / 1024, T), dim3(256), 0, s, m, part, sh.splits, C, T, out);
 }
 template <bool F16, int ST, int FL>
 void launch_cols(const Q4View &m, const h16_t *x, int64_t ldx, int C, int T, const Q4Out &out, float *part, hipStream_t s) {
@@ -670,12 +734,14 @@ void launch_type(const Q4View &m, const h16_t *x, int64_t ldx, int C, int T, con
 size_t q4_part_floats(const Q4View &m) {
     size_t most = 0;
     for (int c = 1; c <= kQ4Rows; ++c)
-        if (form_of(m, c) == SHARED) most = std::max(most, (size_t)shared_shape(m, c).splits * c * m.n_tiles * 16);
+        if (form_of(m, c) == SHARED && shared_shape(m, c).splits > 1) most = std::max(most, (size_t)shared_shape(m, c).splits * c * m.n_tiles * 16);
     return most;
 }
 int q4_best_units(const Q4View &m, int T) {
     const int form = form_of(m, 2 * T);
-    return form == SHARED ? (m.n_tiles * 16 + 1023) / 1024 : (m.n_tiles + few_tiles(form) - 1) / few_tiles(form);
+    if (form != SHARED) return (m.n_tiles + few_tiles(form) - 1) / few_tiles(form);
+    const SharedShape sh = shared_shape(m, 2 * T);
+    return sh.splits > 1 ? (m.n_tiles * 16 + 1023) / 1024 : shared_blocks(m, sh);
 }
 void launch_q4(const Q4View &m, const h16_t *x, int64_t ldx, int T, const Q4Out &out, float *part, hipStream_t s) {
     const int C = out.exps != nullptr ? 2 * T : T;

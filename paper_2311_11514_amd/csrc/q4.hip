@@ -108,7 +108,7 @@ hexgen_status_t hexgen_q4_project(hexgen_q4_t *q, const void *x, int64_t ldx, in
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool parts = q->dtype == HEXGEN_F32;
     // 16-bit rows of whole 128-feature blocks in 16-byte pieces are the operand as they are
-    const bool direct = !parts && reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx % 8 == 0 && q->n_in % 128 == 0;
+    const bool direct = !parts && reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx % 8 == 0 && ldx <= (1 << 24) && q->n_in % 128 == 0;
     const int chunk = parts ? kQ4PartRows : kQ4Rows;
     for (int r0 = 0; r0 < n_rows; r0 += chunk) {
         const int n = std::min(chunk, n_rows - r0);
