@@ -143,12 +143,12 @@ def _stream_handle(stream: Optional[torch.cuda.Stream], here: Optional[int] = No
     return s.cuda_stream or None
 
 
-def _empty_like_of(t: torch.Tensor, shape, dtype, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
-    """A result of a call on `stream` beside the tensor t, taken from that stream's memory."""
+def _empty_beside(t: torch.Tensor, shape, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """A result of a call on `stream`, of the type and on the device of t, taken from that stream's memory."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=t.device)
+        return t.new_empty(shape)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=t.device)
+        return t.new_empty(shape)
 
 
 def _device_tensor(t: torch.Tensor, name: str, shape, dtype, here: int) -> None:
@@ -344,7 +344,7 @@ class KVCache:
         ldk = _rows_of_heads(k, "k", rows, hkv, d, td, here)
         ldv = _rows_of_heads(v, "v", rows, hkv, d, td, here)
         if out is None:
-            out = _empty_like_of(q, (rows, hq, d), td, stream)
+            out = _empty_beside(q, (rows, hq, d), stream)
         else:
             _device_tensor(out, "out", (rows, hq, d), td, here)
         _check(lib.hexgen_kv_tree_attention(self.handle, layer, tree.handle, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv,
@@ -389,7 +389,7 @@ class Tree:
         batch, rows, here = self.batch, self.rows, torch.cuda.current_device()
         _device_tensor(draft, "draft", (rows,), torch.int32, here)
         _device_tensor(chosen, "chosen", (rows,), torch.int32, here)
-        out = _empty_like_of(draft, (batch + 2 * rows,), torch.int32, stream)
+        out = _empty_beside(draft, (batch + 2 * rows,), stream)
         at = out.data_ptr()
         _check(lib.hexgen_tree_accept(self.handle, draft.data_ptr(), chosen.data_ptr(), at, at + 4 * batch, at + 4 * (batch + rows),
                                       _stream_handle(stream, here)), "hexgen_tree_accept")
@@ -445,7 +445,7 @@ class Q4Matrix:
         here = torch.cuda.current_device()
         _on_device(x, "x", here)
         if out is None:
-            out = _empty_like_of(x, (rows, self.n_out), td, stream)
+            out = _empty_beside(x, (rows, self.n_out), stream)
         else:
             _device_tensor(out, "out", (rows, self.n_out), td, here)
         _check(lib.hexgen_q4_project(self.handle, x.data_ptr(), x.stride(0) if rows > 1 else self.n_in, rows, out.data_ptr(), _stream_handle(stream, here)),
