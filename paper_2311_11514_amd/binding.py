@@ -151,19 +151,24 @@ def _empty_beside(t: torch.Tensor, shape, stream: Optional[torch.cuda.Stream]) -
         return t.new_empty(shape)
 
 
-def _device_tensor(t: torch.Tensor, name: str, shape, dtype, here: int) -> None:
+def _device_tensor(t: torch.Tensor, name: str, shape, dtype, here: Optional[int] = None) -> None:
     """A tensor that is handed on as a dense device pointer: checked here, where its shape, type and place are known (here: the current GPU)."""
     if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous {tuple(shape)} tensor of {dtype} is wanted, got {tuple(t.shape)} of {t.dtype}, strides {tuple(t.stride())}")
     _on_device(t, name, here)
 
 
-def _on_device(t: torch.Tensor, name: str, here: int) -> None:
-    if not t.is_cuda or t.get_device() != here:
+def _here(t: torch.Tensor) -> int:
+    """The current GPU, asked once per call; -1, which no tensor is on, where the call's first tensor is not on a GPU at all."""
+    return torch.cuda.current_device() if t.is_cuda else -1
+
+
+def _on_device(t: torch.Tensor, name: str, here: Optional[int] = None) -> None:
+    if not t.is_cuda or t.get_device() != (_here(t) if here is None else here):
         raise ValueError(f"{name}: on {t.device}, not on the current GPU")
 
 
-def _rows_of_heads(t: torch.Tensor, name: str, rows: int, heads: int, d: int, dtype, here: int) -> int:
+def _rows_of_heads(t: torch.Tensor, name: str, rows: int, heads: int, d: int, dtype, here: Optional[int] = None) -> int:
     """Elements between the rows of a [rows, heads, d] or [rows, heads * d] tensor whose rows are dense."""
     flat = t.dim() == 2
     if t.shape != ((rows, heads * d) if flat else (rows, heads, d)) or t.dtype != dtype:
@@ -244,7 +249,7 @@ class Stage:
     def decode_tree(self, kv: "KVCache", tree: "Tree", hidden_in: torch.Tensor, out_partial: torch.Tensor,
                     out_resid: Optional[torch.Tensor] = None, stream=None):
         """hexgen_stage_decode_tree: the drafted trees' rows through every layer; the committed lengths stay."""
-        shape, td, here = (tree.rows, self.hidden), _torch_dtype(self.dtype), torch.cuda.current_device()
+        shape, td, here = (tree.rows, self.hidden), _torch_dtype(self.dtype), _here(hidden_in)
         for name, t in (("hidden_in", hidden_in), ("out_partial", out_partial), ("out_resid", out_resid)):
             if t is not None:
                 _device_tensor(t, name, shape, td, here)
@@ -338,7 +343,7 @@ class KVCache:
                        out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """hexgen_kv_tree_attention: q [rows, hq_local, head_dim], k, v [rows, hkv_local, head_dim] of the trees' nodes, rotated; rows may
         be apart (parts of a fused projection).  Returns [rows, hq_local, head_dim]."""
-        st, rows, here = self.stage, tree.rows, torch.cuda.current_device()
+        st, rows, here = self.stage, tree.rows, _here(q)
         td, hq, hkv, d = _TORCH_DTYPE[st.dtype], st.hq_l, st.hkv_l, st.head_dim
         ldq = _rows_of_heads(q, "q", rows, hq, d, td, here)
         ldk = _rows_of_heads(k, "k", rows, hkv, d, td, here)
@@ -386,7 +391,7 @@ class Tree:
 
     def accept(self, draft: torch.Tensor, chosen: torch.Tensor, stream=None):
         """hexgen_tree_accept: draft, chosen int32 [rows] -> (kept [batch], path [rows], tokens [rows]), int32 on the device."""
-        batch, rows, here = self.batch, self.rows, torch.cuda.current_device()
+        batch, rows, here = self.batch, self.rows, _here(draft)
         _device_tensor(draft, "draft", (rows,), torch.int32, here)
         _device_tensor(chosen, "chosen", (rows,), torch.int32, here)
         out = _empty_beside(draft, (batch + 2 * rows,), stream)
@@ -442,7 +447,7 @@ class Q4Matrix:
         td, rows = _torch_dtype(self.dtype), x.shape[0] if x.dim() == 2 else 0
         if x.dim() != 2 or x.shape[1] != self.n_in or rows < 1 or x.dtype != td or (self.n_in > 1 and x.stride(1) != 1):
             raise ValueError(f"x: a (rows, {self.n_in}) tensor of {td} with dense rows is wanted, got {tuple(x.shape)} of {x.dtype}, strides {tuple(x.stride())}")
-        here = torch.cuda.current_device()
+        here = _here(x)
         _on_device(x, "x", here)
         if out is None:
             out = _empty_beside(x, (rows, self.n_out), stream)
