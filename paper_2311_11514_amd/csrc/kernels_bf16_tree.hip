@@ -436,8 +436,8 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(KvGeom kg, int hq_l, Tr
 }
 
 // Few rows, or little work in all: a block of eight waves takes 32 query rows and the waves take the run's tiles in turn.  No tile serves two
-// waves, so K and V go straight to registers in the operands' layout (the next tile's K is requested before this tile's softmax), and the
-// waves meet in LDS at the end.  Bound by latency, or by HBM where there are many sequences.  The arithmetic is that of the kernel above.
+// waves, so K and V go straight to registers in the operands' layout (the next tile's K is requested before this tile's softmax); the query rows, the
+// same for all waves, wait in LDS (in registers they would make this kernel spill), and there the waves meet at the end.  Bound by latency, or by HBM where there are many sequences.  The arithmetic is that of the kernel above.
 // Runs leave (m, l, o) with device-scope stores and count themselves; whoever is last joins them in the order of the context, so that the
 // result does not depend on who that was, and resets the counter.  Nobody waits for anybody.
 template <int D>
@@ -445,6 +445,7 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(const h16_t *__restric
                                                           TreeView tv, const int32_t *__restrict__ lens, TreePlan tp, TreeOut out, float scale_log2e) {
     constexpr int W = 8, KT = D / 32, DT = D / 16, DB = D / 32, OS = D + 4;
     __shared__ __align__(16) float s_o[W][32 * OS];
+    __shared__ h16x8 s_q[2 * KT][64];
     __shared__ float s_m[W][32], s_l[W][32];
     __shared__ int s_last;
     TreeWork wk;
@@ -458,12 +459,13 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(const h16_t *__restric
     h16_t *kslab = kc + slab, *vslab = vc + slab;
     const bool fresh = in.k != nullptr;                       // the tree's rows are the caller's, not in the cache yet
 
-    h16x8 kf[2 * KT], vf[2 * DB], qf[2 * KT];
+    h16x8 kf[2 * KT], vf[2 * DB];
+    const int clean = min(wk.t1, len >> 5);                   // tiles before it lie in the context
     // K: lane l takes position l % 32, elements 16 kk + 8 (l / 32) ..; a slot of the tree comes from its row
-    auto load_k = [&](int t) {
+    auto load_k = [&](int t, auto tail) {
         const h16_t *src = kslab + ((size_t)(2 * t + sub) * KT * 64 + fl) * 8;
         const int x = 32 * t + i32 - len;
-        if (fresh && 32 * t + 31 >= len && x >= 0 && x < wk.n) {
+        if (decltype(tail)::value && fresh && x >= 0 && x < wk.n) {
             const h16_t *row = static_cast<const h16_t *>(in.k) + (size_t)(row0 + x) * in.ldk + wk.c * D + 8 * hl;
 #pragma unroll
             for (int kk = 0; kk < 2 * KT; ++kk) kf[kk] = *reinterpret_cast<const h16x8 *>(row + 16 * kk);
@@ -472,53 +474,70 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(const h16_t *__restric
             for (int kk = 0; kk < 2 * KT; ++kk) kf[kk] = *reinterpret_cast<const h16x8 *>(src + ((kk >> 1) * 64 + 32 * (kk & 1)) * 8);
         }
     };
+    static_assert(2 * KT <= W, "a piece of the query rows per wave");
+    h16x8 qf;
+    if (wave < 2 * KT) qf = *reinterpret_cast<const h16x8 *>(q + (size_t)(row0 + node) * ldq + (size_t)head * D + 16 * wave + 8 * hl);
     const int tw = wk.t0 + wave;
-    if (tw < wk.t1) load_k(tw);
-#pragma unroll
-    for (int kk = 0; kk < 2 * KT; ++kk)
-        qf[kk] = *reinterpret_cast<const h16x8 *>(q + (size_t)(row0 + node) * ldq + (size_t)head * D + 16 * kk + 8 * hl);
+    if (tw < clean) load_k(tw, std::false_type{});
+    if (wave < 2 * KT) s_q[wave][lane] = qf;
+    HX_LDS_BARRIER();
     floatx16 oacc[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int x = 0; x < 16; ++x) oacc[db][x] = 0.f;
     float m = NEG_INF, lsum = 0.f;
-    // a tile in the context (TAIL false), or one that may reach the tree's slots
+    // a tile in the context (TAIL false), or one that reaches the tree's slots
     auto walk = [&](int t, auto tail) {
         constexpr bool TAIL = decltype(tail)::value;
-        const bool masked = TAIL && 32 * t + 31 >= len;
+        if constexpr (TAIL) load_k(t, tail);
         // V^T: lane l takes element 32 db + l % 32 and k-group 2 h + l / 32 (kvlayout.h)
         const h16_t *vsrc = vslab + ((size_t)(t * DT + sub) * 64 + fl) * 8;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int h = 0; h < 2; ++h) vf[2 * db + h] = *reinterpret_cast<const h16x8 *>(vsrc + (2 * db * 64 + 32 * h) * 8);
+        // the tree's values among them, element by element from the rows (slots of others take some row of the tree, not used), all requested at once:
+        // one after the other they were most of a short call
+        union Piece { h16x8 v; h16_t e[8]; uint32_t u[4]; } own[TAIL ? 2 * DB : 1];
+        uint32_t sees = 0xffffffffu;
+        if constexpr (TAIL) {
+            if (fresh) {
+                const h16_t *rows = static_cast<const h16_t *>(in.v) + (size_t)row0 * in.ldv + wk.c * D + i32;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int x = 32 * t + (j & 3) + 4 * (2 * h + hl) + 16 * (j >> 2) - len;
+                        const h16_t *row = rows + min(max(x, 0), wk.n - 1) * in.ldv;
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) own[2 * db + h].e[j] = row[32 * db];
+                    }
+            }
+            sees = tree_sees(mask, tv.mask_words, t, len);
+        }
         floatx16 sc;
 #pragma unroll
         for (int x = 0; x < 16; ++x) sc[x] = 0.f;
 #pragma unroll
-        for (int kk = 0; kk < 2 * KT; ++kk) sc = hx_mfma32(kf[kk], qf[kk], sc);
-        uint32_t sees = 0xffffffffu;
-        if (masked) {
+        for (int kk = 0; kk < 2 * KT; ++kk) sc = hx_mfma32(kf[kk], s_q[kk][lane], sc);
+        if constexpr (TAIL) {
             if (fresh) {
-                // the tree's values over what the cache held there; the first block of rows appends what it has put together
-                const h16_t *rows = static_cast<const h16_t *>(in.v) + (size_t)row0 * in.ldv + wk.c * D + i32;
+                // over what the cache held there; the first block of rows appends what it has put together
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int g = 2 * h + hl;
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int x = 32 * t + (j & 3) + 4 * g + 16 * (j >> 2) - len;
-                        if (x < 0 || x >= wk.n) continue;
+                    for (int i = 0; i < 4; ++i) {
+                        const int x = 32 * t + 2 * (i & 1) + 4 * (2 * h + hl) + 16 * (i >> 1) - len;     // of elements 2 i and 2 i + 1
+                        const uint32_t take = (x >= 0 && x < wk.n ? 0xffffu : 0u) | (x >= -1 && x < wk.n - 1 ? 0xffff0000u : 0u);
 #pragma unroll
                         for (int db = 0; db < DB; ++db) {
-                            union { h16x8 v; h16_t e[8]; } w;
+                            Piece w;
                             w.v = vf[2 * db + h];
-                            w.e[j] = rows[(size_t)x * in.ldv + 32 * db];
+                            w.u[i] = (own[2 * db + h].u[i] & take) | (w.u[i] & ~take);
                             vf[2 * db + h] = w.v;
                         }
                     }
-                }
                 if (wk.rb == 0) {
                     const int x = 32 * t + i32 - len;
                     h16_t *dst = kslab + ((size_t)(2 * t + sub) * KT * 64 + fl) * 8;
@@ -533,11 +552,10 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(const h16_t *__restric
                         for (int h = 0; h < 2; ++h) *reinterpret_cast<h16x8 *>(vdst + (2 * db * 64 + 32 * h) * 8) = vf[2 * db + h];
                 }
             }
-            sees = tree_sees(mask, tv.mask_words, t, len);
 #pragma unroll
             for (int x = 0; x < 16; ++x) sc[x] = (sees >> (8 * (x >> 2) + 4 * hl + (x & 3))) & 1u ? sc[x] : NEG_INF;
         }
-        if (t + W < wk.t1) load_k(t + W);
+        if (!TAIL && t + W < clean) load_k(t + W, std::false_type{});
         const float alpha = tree_softmax(sc, m, lsum, scale_log2e);
 #pragma unroll
         for (int db = 0; db < DB; ++db)
@@ -545,10 +563,8 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(const h16_t *__restric
             for (int x = 0; x < 16; ++x) oacc[db][x] *= alpha;
         if constexpr (TAIL) {
             bool odd = false;
-            if (masked) {
 #pragma unroll
-                for (int x = 0; x < 2 * DB; ++x) odd = odd || any_odd(vf[x]);
-            }
+            for (int x = 0; x < 2 * DB; ++x) odd = odd || any_odd(vf[x]);
             if (__builtin_amdgcn_ballot_w64(odd) != 0) {
                 h16x8 *vt = reinterpret_cast<h16x8 *>(s_o[wave]);      // the wave's own part of the merge buffer, not in use yet
 #pragma unroll
@@ -568,7 +584,7 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(const h16_t *__restric
         }
     };
     int tile = tw;
-    for (; tile < min(wk.t1, len >> 5); tile += W) walk(tile, std::false_type{});
+    for (; tile < clean; tile += W) walk(tile, std::false_type{});
     for (; tile < wk.t1; tile += W) walk(tile, std::true_type{});
     lsum = sum_halves(lsum);
     if (hl == 0) { s_m[wave][i32] = m; s_l[wave][i32] = lsum; }
