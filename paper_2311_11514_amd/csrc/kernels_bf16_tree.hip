@@ -586,14 +586,17 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(const h16_t *__restric
     int tile = tw;
     for (; tile < clean; tile += W) walk(tile, std::false_type{});
     for (; tile < wk.t1; tile += W) walk(tile, std::true_type{});
-    lsum = sum_halves(lsum);
-    if (hl == 0) { s_m[wave][i32] = m; s_l[wave][i32] = lsum; }
+    const int live = min(W, wk.t1 - wk.t0);                   // waves that had a tile
+    if (wave < live) {
+        lsum = sum_halves(lsum);
+        if (hl == 0) { s_m[wave][i32] = m; s_l[wave][i32] = lsum; }
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+        for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int qd = 0; qd < 4; ++qd)
-            *reinterpret_cast<floatx4 *>(&s_o[wave][i32 * OS + 32 * db + 8 * qd + 4 * hl]) =
-                floatx4{oacc[db][4 * qd], oacc[db][4 * qd + 1], oacc[db][4 * qd + 2], oacc[db][4 * qd + 3]};
+            for (int qd = 0; qd < 4; ++qd)
+                *reinterpret_cast<floatx4 *>(&s_o[wave][i32 * OS + 32 * db + 8 * qd + 4 * hl]) =
+                    floatx4{oacc[db][4 * qd], oacc[db][4 * qd + 1], oacc[db][4 * qd + 2], oacc[db][4 * qd + 3]};
+    }
     __syncthreads();
     const int nb = wk.runs(), rows = min(32, R - wk.rb * 32);
     const size_t part_row = (size_t)tv.rows * hq_l;
@@ -605,10 +608,11 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(const h16_t *__restric
         if (row >= rows) break;
         float M = NEG_INF, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < W; ++w) M = fmaxf(M, s_m[w][row]);
+        for (int w = 0; w < W; ++w) M = fmaxf(M, s_m[min(w, live - 1)][row]);
         const float b = M == NEG_INF ? 0.f : M;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
+            if (w >= live) break;
             const float wt = __builtin_amdgcn_exp2f((s_m[w][row] - b) * scale_log2e);
             const floatx4 v = *reinterpret_cast<const floatx4 *>(&s_o[w][row * OS + dd]);
             L += s_l[w][row] * wt;
