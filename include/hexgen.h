@@ -217,8 +217,9 @@ hexgen_status_t hexgen_tree_accept(const hexgen_tree_t *tr, const int32_t *draft
  * arrays may be changed when it returns; it enqueues on `stream` and cannot be recorded into a graph (HEXGEN_ERR_DEVICE).
  * All three: HEXGEN_ERR_STATE unless the cache holds a batch (prefill, set_lengths, commit) and the trees are set for just as many
  * sequences; HEXGEN_ERR_CAPACITY when a context and its tree exceed max_seq.  hexgen_stage_decode_tree and
- * hexgen_kv_tree_attention can be recorded once a call of that size has run outside a graph; they read lengths and
- * trees from the device when replayed.
+ * hexgen_kv_tree_attention can be recorded once a call of that size has run outside a graph.  A recording is for trees of
+ * the recorded counts; a replay reads the lengths and the parents that hold then from the device, and leaves out what would
+ * pass max_seq.  Calls on one stage, replays among them, may not overlap in time (they share its workspace).
  */
 hexgen_status_t hexgen_stage_decode_tree(hexgen_stage_t *st, hexgen_kv_cache_t *kv, const hexgen_tree_t *tr, const void *hidden_in,
                                          void *out_partial, void *out_resid, void *stream);
@@ -277,8 +278,8 @@ hexgen_status_t hexgen_head_load_q4(hexgen_head_t *hd, const void *g_final, cons
  *   hexgen_q4_load: w4, bytes [n_in][n_out / 2], column 2 i in the low and 2 i + 1 in the high nibble of byte i; scales
  *     [ceil(n_in / group)][n_out]; zeros, bytes [ceil(n_in / group)][n_out / 2] as w4, or NULL for 8 everywhere.  Host or device memory; the
  *     library keeps a repacked copy; synchronises.
- *   hexgen_q4_project: x device [n_rows, n_in], rows ldx >= n_in elements apart; y device [n_rows, n_out], dense, aligned to two elements.
- *     Enqueues on `stream`.  Up to 64 rows (fp32: 32) read the matrix once.  Products and sums are fp32, with one rounding to dtype;
+ *   hexgen_q4_project: x device [n_rows, n_in], rows ldx >= n_in elements apart; y device [n_rows, n_out], dense, aligned to two elements, apart
+ *     from x.  Enqueues on `stream`.  Up to 64 rows (fp32: 32) read the matrix once.  Products and sums are fp32, with one rounding to dtype;
  *     a row that holds an infinity or a NaN gives NaN.  HEXGEN_ERR_STATE before hexgen_q4_load.  Calls on one handle may not overlap in
  *     time (they share its workspace).  Can be recorded into a graph.
  */

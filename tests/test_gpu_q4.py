@@ -80,6 +80,19 @@ def test_project_wide_matrix(dtype, n_rows):
     check(m.project(x.cuda()), x64, w, big, dtype, 128, f"{dtype} {n_rows} x 384 x 66000")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("n_in,n_out", [(8400, 206), (300, 4104), (130, 8256), (2000, 8200)])
+def test_project_long_and_wide_matrices(dtype, group, n_in, n_out):
+    """Long contractions, in one block and split; matrices of a few hundred tiles in groups of operand columns; operands that LDS holds and not."""
+    arrays, w, big = matrix(dtype, n_in, n_out, group, True, seed=5)
+    m = hx.Q4Matrix(n_in, n_out, group, dtype)
+    m.load(*arrays)
+    for n in (1, 4, 8, 9, 17, 33, 40, 64):
+        x, x64 = rows(dtype, n, n_in, seed=n)
+        check(m.project(x.cuda()), x64, w, big, dtype, group, f"{dtype} {n} x {n_in} x {n_out}, groups of {group}")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_strides_alignment_and_the_callers_output(dtype):
     arrays, w, big = matrix(dtype, 512, 100, 128, True)
@@ -194,6 +207,25 @@ def test_head_greedy(dtype, hidden, vocab, tp, group, zeros, n_rows):
             assert (np.abs(val - best[:, 1]) <= slack).all()
             assert (tok[clear] == part.argmax(1)[clear] + r * vocab // tp).all()
         assert decisive >= 0.8 * tp * n_rows, "too many near-ties"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hidden,vocab,n_rows", [(8448, 1000, 7), (256, 4200, 21), (8448, 1000, 1)])
+def test_head_greedy_split_and_grouped(dtype, hidden, vocab, n_rows):
+    """The arg-max behind a split contraction, and over groups of operand columns."""
+    arrays, w, big = matrix(dtype, hidden, vocab, 64, True, seed=11)
+    a, _ = rows(dtype, n_rows, hidden, seed=2)
+    gain = torch.ones(hidden, dtype=TORCH[dtype])
+    y, off = _head_reference(a, None, gain, w, big, 1e-5, 64)
+    hd = hx.Head(hidden, vocab, 1, 0, dtype)
+    hd.load_q4(gain, *arrays, group=64)
+    for _ in range(2):
+        tok, val = hd.greedy(a.cuda())
+        torch.cuda.synchronize()
+        tok, val, slack = tok.cpu().numpy(), val.cpu().double().numpy(), off.max(1)
+        assert (np.abs(val - y.max(1)) <= slack).all()
+        # the chosen column is one that the bound does not rule out
+        assert (y[np.arange(n_rows), tok] >= y.max(1) - 2 * slack).all()
 
 
 def test_head_ties_go_to_the_lowest_column_and_loads_replace_each_other():

@@ -157,6 +157,18 @@ def test_rows_join_the_cache_and_nothing_else_changes(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_contexts_from_device_memory_are_those_from_the_host(dtype):
+    st = hx.Stage(512, 4, 2, 256, 1, 1, 0, dtype)
+    kv = st.kv_cache_create(2, 64)
+    k, v = (torch.randn(45, 2, 128, generator=torch.Generator().manual_seed(i)).to(tr.TORCH[dtype]) for i in range(2))
+    kv.fill(0, 0, k, v)
+    kv.fill(0, 1, k.cuda(), v.cuda())
+    kv.set_lengths([45, 45])
+    for a, b, want in zip(kv.read(0, 0, 0, 45), kv.read(0, 1, 0, 45), (k, v)):
+        assert torch.equal(a, want.float()) and torch.equal(b, a)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_parts_of_a_fused_projection_and_an_output_of_the_callers(dtype):
     c = Case(dtype, 8, 2, 64, [100, 3], _trees([9, 4]))
     want = c.attend()
