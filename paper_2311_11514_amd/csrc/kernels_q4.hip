@@ -178,7 +178,8 @@ __device__ __forceinline__ void best_of_lanes(float &bv, int &bi) {
 // blocks in turn and are summed through LDS in wave order, so that no partial result leaves the block.  A wave holds R blocks with their scales in registers, requested that far ahead; every request is
 // unconditional (past the end it repeats the last block's), so that the compiler can count what is in flight and waits for the oldest
 // alone.  XLDS: the operand is staged in LDS once, else a wave requests its pieces one block ahead, from L2.
-// Bound by HBM on wide matrices, on small ones by the launch and one round trip.
+// Bound by HBM on wide matrices, on small ones by the launch and one round trip (bf16, one row: 8192 x 10240 13.4 us, 3.2 TB/s; the arg-max form, 8192 x
+// 32000, two columns 28.4, 4.7 TB/s; 4096 x 4096 5.9).
 // FL: 32-feature steps of a scale's group inside a 128-feature block (4: groups of 128 and more).
 template <bool F16, int ST, int UT, int FL, int W, int R, bool XLDS>
 __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) void q4_few_kernel(Q4View m, const h16_t *__restrict__ x, int64_t ldx, int parts, int rows, Q4Out out) {
@@ -320,6 +321,9 @@ __device__ __forceinline__ float sum_rows(float v) {
 // while others are at the matrix unit.  The groups are joined through LDS at the end.  The contraction is split over blockIdx.y where the matrix
 // has too few columns for the chip: splits leave partial sums, `part` [split][column of the operand][16 n_tiles], to q4_finish_kernel.  Without
 // splits the parts are joined, and stored or searched for their largest, here.
+// Bound by HBM up to 16 columns (8192 x 57344, twelve rows 48 us, 5 TB/s), beyond by the vector unit (28 operations a lane to widen a tile's block, some
+// 10 for its scales and zero points, 8 per operand tile to apply them) and the matrix unit, which overlap little: 32 columns 66 .. 74 us, 4096 x 50304
+// with 48 columns 46.  Weights in registers with one step ahead took 64, 77 and 53; one group of eight waves five steps ahead 60, 80 and 46.
 template <int ST, int NB, int FL> struct SharedStage {
     static constexpr int ES = ST == HX_T_F32 ? 4 : 2, NF = 4 / FL, SP = (NF * 256 * ES + 1023) / 1024;      // SP: requests of 1 KB for the scales of 16 tiles
     u32x4 x[4 * NB][64], w[16][64];
