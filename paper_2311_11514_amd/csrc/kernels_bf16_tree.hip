@@ -442,7 +442,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(KvGeom kg, int hq_l, Tr
 // waves, so K and V go straight to registers in the operands' layout (the next tile's K is requested before this tile's softmax); the query rows, the
 // same for all waves, wait in LDS (in registers they would make this kernel spill), and there the waves meet at the end.  Bound by latency, or by HBM where there are
 // many sequences: d 128, one kv head of eight, one sequence of 2048 with 26 nodes 13.4 us, sixteen with 8 nodes 15.9 (1.1 TB/s), a context of a
-// tile or two 8.4; eight kv heads, one sequence of 4000 with 16 nodes 18.5.  The arithmetic is that of the kernel above.
+// tile or two 8.4; eight kv heads, one sequence of 4000 with 16 nodes 17.0.  The arithmetic is that of the kernel above.
 // Runs leave (m, l, o) with device-scope stores and count themselves; whoever is last joins them in the order of the context, so that the
 // result does not depend on who that was, and resets the counter.  Nobody waits for anybody.
 template <int D>

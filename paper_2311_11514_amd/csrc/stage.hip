@@ -356,17 +356,18 @@ KvGeom geom(const hexgen_stage *st, const hexgen_kv_cache *kv) {
 // ---- drafted trees: the attention of every path ----------------------------------------------------------------
 // Rows per block, runs and order of a tree attention.  (us; 16 bits, d 128; "few": 32 rows a block and eight waves that each take tiles of their own,
 // 2 and 4: groups of 32 rows that share tiles through LDS; then the runs of a context)
-//   8 heads a kv head, 8 kv heads, 4000 positions: one sequence of 64 nodes: few 33, 2 in four runs 41; eight of 16: few 51, 2 in four 46
-//   32 sequences of 2048: 8 nodes: few 73, 2 64, 2 in two 68, 4 76; 32 nodes: 2 139, 4 114; 16 nodes at 4000: 2 127, 4 140; contexts of
-//   240 .. 4027 and 8 .. 64 nodes: 2 183, 4 202 (three quarters of its rows exist)
+//   8 heads a kv head, 8 kv heads, 4000 positions: one sequence of 64 nodes: few 30, 2 in four runs 41; eight of 16: few 47, 2 in four 46
+//   32 sequences of 2048: 8 nodes: few 68, 2 64, 2 in two 67, 4 77; 32 nodes: 2 126, 4 116; 16 nodes at 4000: 2 127, 4 144; contexts of
+//   240 .. 4027 and 8 .. 64 nodes: 2 181, 4 198 (three quarters of its rows exist)
 // "Few" and fp32 blocks have a CU each: runs must not make more blocks than there are CUs, with some to spare (kTreeBlocks), and a run costs its
-// share of the joining, 0.5 us where a tile of a run costs 0.14, so that the best length goes with the root of the context's.
-//   one kv head, eight heads, runs of 8, 10, 16, 24 tiles and whole: one sequence of 2048, 26 nodes: 18.3, 15.8, 15.4, 17.1, 19.6; sixteen, 8 nodes:
-//   26.5 (288 blocks), 16.6, 16.0, 18.3, 20.3; one of 4000, 16 nodes: 18.2, 18.6, 16.7, 15.3, 28.9; eight of 600: 14.7, 15.5, 14.8, -, 12.3; sixteen of
-//   2048, 32 nodes (128 blocks): in two runs 27, whole 22.  Eight kv heads, one sequence of 1000, 8 nodes: 15.6, 14.7, 16.4, 15.3, 14.7; of 4000, 16
-//   nodes: 43.5, 30.9, 23.0 (256 blocks), 18.1, 30.5
-//   fp32, runs of 4, 8, 10, 16 and whole: four of 2048, 4 kv heads, 8 nodes: 28.9, 29.3 (288 blocks), 22.6, 27.5, 66.5; eight of 600, one kv head:
-//   15.4, 16.9, 18.9, 24.2, 24.3
+// share of the joining, 0.5 us where a tile of a run costs 0.14, so that the best length goes with the root of the context's; whole rounds of the
+// eight waves, which also leave little to the last run, the one with the tree.
+//   one kv head, eight heads, runs of 8, 10, 16, 24 tiles and whole: one sequence of 2048, 26 nodes: 16.9, 14.1, 13.5, 16.4, 18.8; sixteen, 8 nodes:
+//   24.3 (288 blocks), 16.3, 15.1, 18.1, 20.0; one of 4000, 16 nodes: 17.3, 17.7, 16.2, 14.0, 27.6 (runs of 22 tiles 16.2); eight of 600: 13.7, 15.5,
+//   13.7, 11.9, 11.9; sixteen of 2048, 32 nodes (128 blocks): in two runs 24, whole 21.  Eight kv heads, one sequence of 1000, 8 nodes: 14.9, 13.7,
+//   16.7, 14.8, 13.9; of 4000, 16 nodes: 38.7, 27.0, 20.6 (256 blocks), 16.9, 29.1
+//   fp32, runs of 4, 8, 10, 16 and whole: four of 2048, 4 kv heads, 8 nodes: 29.1, 29.0 (288 blocks), 22.8, 27.5, 66.8; eight of 600, one kv head:
+//   15.6, 17.0, 19.0, 24.1, 24.4
 TreePlan pick_tree_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, const hexgen_tree *tr) {
     const int G = st->hq_l / st->hkv_l;
     const bool h16 = is_h16(st->dtype);
@@ -402,7 +403,7 @@ TreePlan pick_tree_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, const
     } else if (w.blocks < 128 && (long)tr->batch * st->hkv_l * tree_row_blocks(tr->max_n, G, rows) <= kTreeUnits) {
         const long fit = (w.tiles + kTreeBlocks - 1) / kTreeBlocks;
         if (!h16) tp.chunk = (int)std::max(4L, fit);
-        else if (longest > 48) tp.chunk = (int)std::max({16L, fit, (long)(2 * std::sqrt((double)longest))});
+        else if (longest > 48) tp.chunk = (int)((std::max({16L, fit, (long)(2 * std::sqrt((double)longest))}) + 7) / 8 * 8);
     }
     tp.nsplit = std::min((longest + tp.chunk - 1) / tp.chunk, kTreeMaxSplit);
     tp.nsplit = (int)std::max((size_t)1, std::min((size_t)tp.nsplit, kTreePartFloats / ((size_t)tr->rows * st->hq_l * (st->d + 2))));
