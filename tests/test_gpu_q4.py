@@ -82,7 +82,7 @@ def test_project_wide_matrix(dtype, n_rows):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("group", [32, 64, 128])
-@pytest.mark.parametrize("n_in,n_out", [(8400, 206), (300, 4104), (130, 8256), (2000, 8200)])
+@pytest.mark.parametrize("n_in,n_out", [(8192, 96), (8400, 206), (300, 4104), (130, 8256), (2000, 8200)])
 def test_project_long_and_wide_matrices(dtype, group, n_in, n_out):
     """Long contractions, in one block and split; matrices of a few hundred tiles in groups of operand columns; operands that LDS holds and not."""
     arrays, w, big = matrix(dtype, n_in, n_out, group, True, seed=5)
