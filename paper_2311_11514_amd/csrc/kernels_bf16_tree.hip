@@ -231,7 +231,7 @@ __device__ __forceinline__ void tree_patch(h16x8 (*st)[64], const TreeIn &in, in
 // by element over what each row attends.
 // Contexts are cut into runs of tp.chunk tiles (tp.nsplit at most), whose (m, l, o) tree_merge_kernel joins: a launch of its own, since joining
 // 128 rows of a run moves 64 KB, which one last block would take longer over.
-// Bound by HBM with few nodes, by the softmax's vector work and the matrix unit one behind the other with many: d 128, 64 query and 8 kv heads, 32
+// Bound by HBM with few nodes, by each wave's chain of LDS reads, products and softmax with many (matrix cores 34 % busy, vector units 45 %): d 128, 64 query and 8 kv heads, 32
 // sequences of 4000: 16 nodes 127 us (4.1 TB/s), 64 nodes 354 (757 TFLOP/s); contexts of 240 .. 4027 and 8 .. 64 nodes 184 (435 TFLOP/s: a quarter of
 // the blocks' rows do not exist, and the long contexts end late).
 template <int D, int RW, int S>
