@@ -94,6 +94,49 @@ def test_long_contexts_in_runs_match_64_bits(dtype, hq, hkv, d, lens, counts):
     c.check(c.attend())
 
 
+WIDE = [                                             # enough tiles that blocks share them
+    (64, 8, 128, [2148, 2099, 2181, 2148, 2200, 2147, 2149, 2144], [16] * 7 + [9]),                        # 64 rows a block, in runs
+    (64, 8, 64, [2148, 2099, 2181, 2148, 2200, 2147, 2149, 2144], [16] * 7 + [9]),
+    (64, 8, 128, [860 + 9 * i for i in range(15)] + [3], [20] * 12 + [0, 1, 33, 18]),                       # 64 rows, whole contexts
+    (64, 8, 128, [230 + 9 * i for i in range(16)], [64 - (i % 4) for i in range(16)]),                      # 128 rows
+    (64, 8, 64, [230 + 9 * i for i in range(16)], [64 - (i % 4) for i in range(16)]),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("hq,hkv,d,lens,counts", WIDE)
+def test_blocks_that_share_tiles_match_64_bits(dtype, hq, hkv, d, lens, counts):
+    c = Case(dtype, hq, hkv, d, lens, _trees(counts, seed=5), seed=8)
+    out = c.attend()
+    c.check(out)
+    assert torch.equal(c.attend(), out)                # the same bits, from rows that are in the cache by now as well
+
+
+@pytest.mark.parametrize("hq,hkv,d,lens,counts", WIDE)
+def test_blocks_that_share_tiles_and_slots_that_are_nobodys(hq, hkv, d, lens, counts):
+    """NaN behind every tree, and an infinity in the rows of the last node of each, which no other node attends."""
+    c = Case("bf16", hq, hkv, d, lens, _trees(counts, seed=6), max_seq=max(lens) + 128, seed=9, fill=False)
+    for b, n in enumerate(lens):
+        pad = torch.full((128, hkv, d), float("nan"))
+        c.kv.fill(0, b, *[torch.cat([x.float(), pad]) for x in c.ctx[0][b]])
+    c.kv.set_lengths(lens)
+    c.check(c.attend())
+    last = np.cumsum([len(t) for t in c.trees])[[len(t) > 0 for t in c.trees]] - 1
+    c.v[last] = float("inf")
+    out = c.attend().double().cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        o, bound = c.reference()
+    good = np.setdiff1d(np.arange(c.rows), last)
+    assert (np.abs(out[good] - o[good]) <= bound[good]).all() and not np.isfinite(out[last]).any()
+
+
+def test_more_sequences_than_the_plan_orders():
+    """Sequences beyond the 64 that are dispatched by length."""
+    for dtype in ("bf16", "f32"):
+        c = Case(dtype, 4, 2, 64, [(37 * i) % 150 for i in range(75)], _trees([(i % 5) + (i % 7 == 0) for i in range(75)], seed=2), seed=4)
+        c.check(c.attend())
+
+
 @pytest.mark.parametrize("width", [1, 2, 255])
 def test_tree_shapes(width):
     """A chain (plain causal attention), a binary tree, a star."""
