@@ -125,13 +125,33 @@ __device__ __forceinline__ float tree_softmax(floatx16 &sc, float &m, float &lsu
     lsum = lsum * alpha + ps;
     return alpha;
 }
-// P for k-groups hl (quads 0, 2) and 2 + hl (quads 1, 3) of the second product
+// P for k-groups hl (quads 0, 2) and 2 + hl (quads 1, 3) of the second product, in two parts like every fp32 activation of the decode kernels: one
+// part alone would put a rounding of every weight on top of the result's own (a third more error), and the matrix cores have room for both.
+// hi is cut off, not rounded, and lo is at least the type's smallest number (bf16: normal number) where hi is not zero: both parts of a weight are
+// positive, or zero with it, so that an infinite value of the context comes out as infinite and one of a position that is not attended not at all.
 union TreeP { uint32_t u[4]; h16x8 v; };
-__device__ __forceinline__ void tree_pack(const floatx16 &sc, TreeP &p0, TreeP &p1) {
-    p0.u[0] = pack_h16x2(sc[0], sc[1]);   p0.u[1] = pack_h16x2(sc[2], sc[3]);
-    p0.u[2] = pack_h16x2(sc[8], sc[9]);   p0.u[3] = pack_h16x2(sc[10], sc[11]);
-    p1.u[0] = pack_h16x2(sc[4], sc[5]);   p1.u[1] = pack_h16x2(sc[6], sc[7]);
-    p1.u[2] = pack_h16x2(sc[12], sc[13]); p1.u[3] = pack_h16x2(sc[14], sc[15]);
+__device__ __forceinline__ void tree_pack2(float a, float b, uint32_t &hi, uint32_t &lo) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    float ah, bh;
+#ifdef HX_ELEM_F16
+    constexpr unsigned short LEAST = 1;
+    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
+#else
+    constexpr unsigned short LEAST = 0x80;
+    hi = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+#endif
+    h16x2_to_f32(hi, ah, bh);
+    const u16x2 least = __builtin_elementwise_min(__builtin_bit_cast(u16x2, hi), u16x2{LEAST, LEAST});
+    lo = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, pack_h16x2(a - ah, b - bh)), least));
+}
+__device__ __forceinline__ void tree_pack(const floatx16 &sc, TreeP (&p)[2], TreeP (&lo)[2]) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int x = 4 * g + 2 * (i & 1) + 8 * (i >> 1);
+            tree_pack2(sc[x], sc[x + 1], p[g].u[i], lo[g].u[i]);
+        }
 }
 // O^T += V^T . P^T element by element, over the positions a row attends: for tiles with values that are not finite.  vt: the tile in LDS
 template <int DB>
@@ -331,13 +351,16 @@ __global__ __launch_bounds__(256, RW == 4 ? 3 : 2) void tree_attn_kernel(const h
                 return;
             }
         }
-        TreeP p0, p1;
-        tree_pack(sc, p0, p1);
+        TreeP p[2], lo[2];
+        tree_pack(sc, p, lo);
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-            oacc[db] = hx_mfma32(st[2 * KT + 2 * db + sub][fl], p0.v, oacc[db]);
-            oacc[db] = hx_mfma32(st[2 * KT + 2 * db + sub][fl + 32], p1.v, oacc[db]);
-        }
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const h16x8 v = st[2 * KT + 2 * db + sub][fl + 32 * g];
+                oacc[db] = hx_mfma32(v, lo[g].v, oacc[db]);
+                oacc[db] = hx_mfma32(v, p[g].v, oacc[db]);
+            }
     };
     const int clean = min(max(((len >> 5) - t0) / CW, 0), steps);
     for (int step = 0; step < clean; ++step) walk(step, std::false_type{});
@@ -580,13 +603,15 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(const h16_t *__restric
                 return;
             }
         }
-        TreeP p0, p1;
-        tree_pack(sc, p0, p1);
+        TreeP p[2], lo[2];
+        tree_pack(sc, p, lo);
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-            oacc[db] = hx_mfma32(vf[2 * db], p0.v, oacc[db]);
-            oacc[db] = hx_mfma32(vf[2 * db + 1], p1.v, oacc[db]);
-        }
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                oacc[db] = hx_mfma32(vf[2 * db + g], lo[g].v, oacc[db]);
+                oacc[db] = hx_mfma32(vf[2 * db + g], p[g].v, oacc[db]);
+            }
     };
     int tile = tw;
     for (; tile < clean; tile += W) walk(tile, std::false_type{});
