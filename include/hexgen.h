@@ -205,7 +205,8 @@ hexgen_status_t hexgen_tree_accept(const hexgen_tree_t *tr, const int32_t *draft
                                    int32_t *path, int32_t *tokens, void *stream);
 
 /* hexgen_stage_decode_tree: the trees' rows through every layer of the stage.  hidden_in, out_partial, out_resid as for prefill, one
- * row per node.  The committed lengths and the decode steps' count do not change, so the call may be repeated.
+ * row per node.  The committed lengths and the decode steps' count do not change, so the call may be repeated.  Up to 32 rows are
+ * computed as decode steps are, with every activation in two parts (16-bit types); more rows as a prefill is, with activations rounded once.
  * hexgen_kv_tree_attention: one layer's attention alone, for callers with projections of their own.  Device pointers, dtype, one row per
  * node: q [rows, hq_local, d] and k [rows, hkv_local, d] rotated at the nodes' positions, v [rows, hkv_local, d]; rows are ldq, ldk and ldv
  * elements apart (multiples of 8 for 16-bit types, of 4 for fp32, and 16-byte aligned pointers: HEXGEN_ERR_INVALID_ARG otherwise), so

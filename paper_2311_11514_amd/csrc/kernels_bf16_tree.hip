@@ -20,7 +20,7 @@ typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
 // head further.  A thread takes four rotary pairs.  q is rounded to the element type here, once, as in the prefill path.
 __global__ __launch_bounds__(256) void tree_rope_append_kernel(const float *__restrict__ qkv, int hq_l, KvGeom kg, TreeView tv,
                                                                const int32_t *__restrict__ lens, const float *__restrict__ cos_tab,
-                                                               const float *__restrict__ sin_tab, h16_t *__restrict__ q,
+                                                               const float *__restrict__ sin_tab, h16_t *__restrict__ q, h16_t *__restrict__ q_lo,
                                                                h16_t *__restrict__ kc, h16_t *__restrict__ vc) {
     const int d = kg.d, half = d >> 1, tph = d >> 4, heads = hq_l + 2 * kg.hkv_l, per_row = heads * tph * 2;
     const int idx = blockIdx.x * 256 + threadIdx.x;
@@ -38,13 +38,19 @@ __global__ __launch_bounds__(256) void tree_rope_append_kernel(const float *__re
         hi = hi * c4 + lo * s4;
         lo = l;
     }
-    union { uint2 u; h16_t x[4]; } a, b;
-    a.u = uint2{pack_h16x2(lo[0], lo[1]), pack_h16x2(lo[2], lo[3])};
-    b.u = uint2{pack_h16x2(hi[0], hi[1]), pack_h16x2(hi[2], hi[3])};
+    union { uint2 u; h16_t x[4]; } a, b, al, bl;       // the element type's parts of both halves' four elements, and what they leave
+    split_pack2(lo[0], lo[1], a.u.x, al.u.x);
+    split_pack2(lo[2], lo[3], a.u.y, al.u.y);
+    split_pack2(hi[0], hi[1], b.u.x, bl.u.x);
+    split_pack2(hi[2], hi[3], b.u.y, bl.u.y);
     if (head < hq_l) {
-        h16_t *dst = q + ((size_t)t * hq_l + head) * d;
-        *reinterpret_cast<uint2 *>(dst + i0) = a.u;
-        *reinterpret_cast<uint2 *>(dst + half + i0) = b.u;
+        const size_t at = ((size_t)t * hq_l + head) * d + i0;
+        *reinterpret_cast<uint2 *>(q + at) = a.u;
+        *reinterpret_cast<uint2 *>(q + at + half) = b.u;
+        if (q_lo != nullptr) {
+            *reinterpret_cast<uint2 *>(q_lo + at) = al.u;
+            *reinterpret_cast<uint2 *>(q_lo + at + half) = bl.u;
+        }
         return;
     }
     const bool key = head < hq_l + kg.hkv_l;
@@ -61,9 +67,9 @@ __global__ __launch_bounds__(256) void tree_rope_append_kernel(const float *__re
     }
 }
 void launch_tree_rope_append(const float *qkv, int hq_l, KvGeom kg, const TreeView &tv, const int32_t *lens, const float *cos_tab,
-                             const float *sin_tab, h16_t *q, h16_t *kc, h16_t *vc, hipStream_t s) {
+                             const float *sin_tab, h16_t *q, h16_t *q_lo, h16_t *kc, h16_t *vc, hipStream_t s) {
     const int n = tv.rows * (hq_l + 2 * kg.hkv_l) * (kg.d >> 4) * 2;
-    hipLaunchKernelGGL(tree_rope_append_kernel, dim3((n + 255) / 256), dim3(256), 0, s, qkv, hq_l, kg, tv, lens, cos_tab, sin_tab, q, kc, vc);
+    hipLaunchKernelGGL(tree_rope_append_kernel, dim3((n + 255) / 256), dim3(256), 0, s, qkv, hq_l, kg, tv, lens, cos_tab, sin_tab, q, q_lo, kc, vc);
 }
 
 // ---- attention ----------------------------------------------------------------------------------------------------
@@ -254,8 +260,9 @@ __device__ __forceinline__ void tree_patch(h16x8 (*st)[64], const TreeIn &in, in
 // Bound by HBM with few nodes, by each wave's chain of LDS reads, products and softmax with many (matrix cores 34 % busy, vector units 45 %): d 128, 64 query and 8 kv heads, 32
 // sequences of 4000: 16 nodes 127 us (4.1 TB/s), 64 nodes 354 (757 TFLOP/s); contexts of 240 .. 4027 and 8 .. 64 nodes 184 (435 TFLOP/s: a quarter of
 // the blocks' rows do not exist, and the long contexts end late).
-template <int D, int RW, int S>
-__global__ __launch_bounds__(256, RW == 4 ? 3 : 2) void tree_attn_kernel(const h16_t *__restrict__ q, int64_t ldq, TreeIn in, h16_t *kc, h16_t *vc, KvGeom kg, int hq_l, int G, int nrb,
+// QLO: the query rows come in two parts.
+template <int D, int RW, int S, bool QLO>
+__global__ __launch_bounds__(256, RW == 4 ? 3 : 2) void tree_attn_kernel(const h16_t *__restrict__ q, const h16_t *__restrict__ q_lo, int64_t ldq, TreeIn in, h16_t *kc, h16_t *vc, KvGeom kg, int hq_l, int G, int nrb,
                                                            TreeView tv, const int32_t *__restrict__ lens, TreePlan tp, TreeOut out, float scale_log2e) {
     constexpr int CW = 4 / RW, ROWS = 32 * RW;
     constexpr int KT = D / 32, DT = D / 16, DB = D / 32, TILES = 2 * KT + DT;
@@ -275,10 +282,13 @@ __global__ __launch_bounds__(256, RW == 4 ? 3 : 2) void tree_attn_kernel(const h
     const int rr = min(r, R - 1), node = rr / G, head = wk.c * G + (rr - node * G);    // rows past the last repeat it and are not stored
     const uint32_t *mask = tv.mask + (size_t)(row0 + node) * tv.mask_words;
 
-    h16x8 qf[2 * KT];
+    h16x8 qf[2 * KT], ql[QLO ? 2 * KT : 1];
 #pragma unroll
-    for (int kk = 0; kk < 2 * KT; ++kk)
-        qf[kk] = *reinterpret_cast<const h16x8 *>(q + (size_t)(row0 + node) * ldq + (size_t)head * D + 16 * kk + 8 * hl);
+    for (int kk = 0; kk < 2 * KT; ++kk) {
+        const size_t at = (size_t)(row0 + node) * ldq + (size_t)head * D + 16 * kk + 8 * hl;
+        qf[kk] = *reinterpret_cast<const h16x8 *>(q + at);
+        if constexpr (QLO) ql[kk] = *reinterpret_cast<const h16x8 *>(q_lo + at);
+    }
     floatx16 oacc[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -326,7 +336,11 @@ __global__ __launch_bounds__(256, RW == 4 ? 3 : 2) void tree_attn_kernel(const h
 #pragma unroll
         for (int x = 0; x < 16; ++x) sc[x] = 0.f;
 #pragma unroll
-        for (int kk = 0; kk < 2 * KT; ++kk) sc = hx_mfma32(st[sub * KT + (kk >> 1)][fl + 32 * (kk & 1)], qf[kk], sc);
+        for (int kk = 0; kk < 2 * KT; ++kk) {
+            const h16x8 k = st[sub * KT + (kk >> 1)][fl + 32 * (kk & 1)];
+            if constexpr (QLO) sc = hx_mfma32(k, ql[kk], sc);
+            sc = hx_mfma32(k, qf[kk], sc);
+        }
         uint32_t sees = 0xffffffffu;
         if (masked) {
             sees = tree_sees(mask, tv.mask_words, t, len);
@@ -468,12 +482,12 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(KvGeom kg, int hq_l, Tr
 // tile or two 8.4; eight kv heads, one sequence of 4000 with 16 nodes 17.0.  The arithmetic is that of the kernel above.
 // Runs leave (m, l, o) with device-scope stores and count themselves; whoever is last joins them in the order of the context, so that the
 // result does not depend on who that was, and resets the counter.  Nobody waits for anybody.
-template <int D>
-__global__ __launch_bounds__(512, 2) void tree_few_kernel(const h16_t *__restrict__ q, int64_t ldq, TreeIn in, h16_t *kc, h16_t *vc, KvGeom kg, int hq_l, int G, int nrb,
+template <int D, bool QLO>
+__global__ __launch_bounds__(512, 2) void tree_few_kernel(const h16_t *__restrict__ q, const h16_t *__restrict__ q_lo, int64_t ldq, TreeIn in, h16_t *kc, h16_t *vc, KvGeom kg, int hq_l, int G, int nrb,
                                                           TreeView tv, const int32_t *__restrict__ lens, TreePlan tp, TreeOut out, float scale_log2e) {
     constexpr int W = 8, KT = D / 32, DT = D / 16, DB = D / 32, OS = D + 4;
     __shared__ __align__(16) float s_o[W][32 * OS];
-    __shared__ h16x8 s_q[2 * KT][64];
+    __shared__ h16x8 s_q[QLO ? 2 : 1][2 * KT][64];
     __shared__ float s_m[W][32], s_l[W][32];
     __shared__ int s_last;
     TreeWork wk;
@@ -503,11 +517,18 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(const h16_t *__restric
         }
     };
     static_assert(2 * KT <= W, "a piece of the query rows per wave");
-    h16x8 qf;
-    if (wave < 2 * KT) qf = *reinterpret_cast<const h16x8 *>(q + (size_t)(row0 + node) * ldq + (size_t)head * D + 16 * wave + 8 * hl);
+    h16x8 qf, ql;
+    const size_t q_at = (size_t)(row0 + node) * ldq + (size_t)head * D + 16 * wave + 8 * hl;
+    if (wave < 2 * KT) {
+        qf = *reinterpret_cast<const h16x8 *>(q + q_at);
+        if constexpr (QLO) ql = *reinterpret_cast<const h16x8 *>(q_lo + q_at);
+    }
     const int tw = wk.t0 + wave;
     if (tw < clean) load_k(tw, std::false_type{});
-    if (wave < 2 * KT) s_q[wave][lane] = qf;
+    if (wave < 2 * KT) {
+        s_q[0][wave][lane] = qf;
+        if constexpr (QLO) s_q[1][wave][lane] = ql;
+    }
     HX_LDS_BARRIER();
     floatx16 oacc[DB];
 #pragma unroll
@@ -548,7 +569,11 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(const h16_t *__restric
 #pragma unroll
         for (int x = 0; x < 16; ++x) sc[x] = 0.f;
 #pragma unroll
-        for (int kk = 0; kk < 2 * KT; ++kk) sc = hx_mfma32(kf[kk], s_q[kk][lane], sc);
+        for (int part = QLO ? 1 : 0; part >= 0; --part) {
+#pragma unroll
+            for (int kk = 0; kk < 2 * KT; ++kk) sc = hx_mfma32(kf[kk], s_q[part][kk][lane], sc);
+            if (part > 0) __builtin_amdgcn_sched_barrier(0);      // one part's pieces at a time in registers
+        }
         if constexpr (TAIL) {
             if (fresh) {
                 // over what the cache held there; the first block of rows appends what it has put together
@@ -700,27 +725,24 @@ __global__ __launch_bounds__(512, 2) void tree_few_kernel(const h16_t *__restric
     }
 }
 
-void launch_tree_attn(const h16_t *q, int64_t ldq, const TreeIn &in, h16_t *kc, h16_t *vc, KvGeom kg, int hq_l, const TreeView &tv, const int32_t *lens,
-                      const TreePlan &tp, const TreeOut &out, hipStream_t s) {
+void launch_tree_attn(const h16_t *q, const h16_t *q_lo, int64_t ldq, const TreeIn &in, h16_t *kc, h16_t *vc, KvGeom kg, int hq_l, const TreeView &tv,
+                      const int32_t *lens, const TreePlan &tp, const TreeOut &out, hipStream_t s) {
     const int G = hq_l / kg.hkv_l, nrb = tree_row_blocks(tv.max_n, G, 32 * tp.row_groups);
     const float scale_log2e = 1.4426950408889634f / sqrtf((float)kg.d);
     const dim3 grid((unsigned)nrb * (unsigned)((tv.batch * kg.hkv_l * tp.nsplit + 7) / 8 * 8));
-#define HX_TREE(KERNEL, THREADS) hipLaunchKernelGGL((KERNEL), grid, dim3(THREADS), 0, s, q, ldq, in, kc, vc, kg, hq_l, G, nrb, tv, lens, tp, out, scale_log2e)
-#define HX_MERGE(DD) \
-    hipLaunchKernelGGL(tree_merge_kernel<DD>, dim3((tv.rows * hq_l + 1024 / DD - 1) / (1024 / DD)), dim3(256), 0, s, kg, hq_l, tv, lens, tp, out, scale_log2e)
-    if (kg.d == 128) {
-        if (tp.row_groups == 1) HX_TREE(tree_few_kernel<128>, 512);
-        else if (tp.row_groups == 2) HX_TREE((tree_attn_kernel<128, 2, 2>), 256);
-        else HX_TREE((tree_attn_kernel<128, 4, 3>), 256);
-        if (tp.row_groups > 1 && tp.nsplit > 1) HX_MERGE(128);
-    } else {
-        if (tp.row_groups == 1) HX_TREE(tree_few_kernel<64>, 512);
-        else if (tp.row_groups == 2) HX_TREE((tree_attn_kernel<64, 2, 2>), 256);
-        else HX_TREE((tree_attn_kernel<64, 4, 3>), 256);
-        if (tp.row_groups > 1 && tp.nsplit > 1) HX_MERGE(64);
-    }
+#define HX_TREE(KERNEL, THREADS) hipLaunchKernelGGL((KERNEL), grid, dim3(THREADS), 0, s, q, q_lo, ldq, in, kc, vc, kg, hq_l, G, nrb, tv, lens, tp, out, scale_log2e)
+#define HX_TREE_D(DD)                                                                                                                              \
+    do {                                                                                                                                           \
+        if (tp.row_groups == 1) { if (q_lo != nullptr) HX_TREE((tree_few_kernel<DD, true>), 512); else HX_TREE((tree_few_kernel<DD, false>), 512); } \
+        else if (tp.row_groups == 2) { if (q_lo != nullptr) HX_TREE((tree_attn_kernel<DD, 2, 2, true>), 256); else HX_TREE((tree_attn_kernel<DD, 2, 2, false>), 256); } \
+        else HX_TREE((tree_attn_kernel<DD, 4, 3, false>), 256);                                                                                    \
+        if (tp.row_groups > 1 && tp.nsplit > 1)                                                                                                    \
+            hipLaunchKernelGGL(tree_merge_kernel<DD>, dim3((tv.rows * hq_l + 1024 / DD - 1) / (1024 / DD)), dim3(256), 0, s, kg, hq_l, tv, lens, tp, out, scale_log2e); \
+    } while (0)
+    if (kg.d == 128) HX_TREE_D(128);
+    else HX_TREE_D(64);
 #undef HX_TREE
-#undef HX_MERGE
+#undef HX_TREE_D
 }
 
 // ---- keeping an accepted path -------------------------------------------------------------------------------------

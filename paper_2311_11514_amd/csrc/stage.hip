@@ -368,7 +368,8 @@ KvGeom geom(const hexgen_stage *st, const hexgen_kv_cache *kv) {
 //   16.7, 14.8, 13.9; of 4000, 16 nodes: 38.7, 27.0, 20.6 (256 blocks), 16.9, 29.1
 //   fp32, runs of 4, 8, 10, 16 and whole: four of 2048, 4 kv heads, 8 nodes: 29.1, 29.0 (288 blocks), 22.8, 27.5, 66.8; eight of 600, one kv head:
 //   15.6, 17.0, 19.0, 24.1, 24.4
-TreePlan pick_tree_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, const hexgen_tree *tr) {
+// two_parts: the query rows come in two parts, which blocks of 128 rows have no registers for (and up to kDecodeMaxRows rows do not fill them)
+TreePlan pick_tree_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, const hexgen_tree *tr, bool two_parts) {
     const int G = st->hq_l / st->hkv_l;
     const bool h16 = is_h16(st->dtype);
     int longest = 1;
@@ -392,7 +393,7 @@ TreePlan pick_tree_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, const
     // from there on tiles are shared: in blocks of 64 rows, or of 128 where they give every CU two and hardly more rows that do not exist
     if (h16 && tr->max_n * G > 32 && w.tiles >= kTreeSharedTiles) {
         const Work two = work_of(64), four = work_of(128);
-        tp.row_groups = tr->max_n * G > 64 && four.blocks >= 512 && 4 * four.tiles * 100 <= 2 * two.tiles * 108 ? 4 : 2;
+        tp.row_groups = !two_parts && tr->max_n * G > 64 && four.blocks >= 512 && 4 * four.tiles * 100 <= 2 * two.tiles * 108 ? 4 : 2;
         rows = 32 * tp.row_groups;
         w = tp.row_groups == 4 ? four : two;
     }
@@ -423,12 +424,13 @@ void attn_tree(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const Rows &r, 
     Workspace &w = st->ws;
     const KvGeom kg = geom(st, kv);
     const TreeView tv = r.tree->view();
-    const TreePlan tp = pick_tree_plan(st, kv, r.tree);
+    h16_t *q_lo = r.decode ? w.q_lo : nullptr;     // 16 bits: on the decode kernels as exact as a decode step, beyond as a prefill
+    const TreePlan tp = pick_tree_plan(st, kv, r.tree, q_lo != nullptr);
     const TreeIn in{nullptr, nullptr, 0, 0};       // appended by the rotation
     if (is_h16(st->dtype)) {
         h16_t *kc = static_cast<h16_t *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<h16_t *>(kv->v) + (size_t)layer * kv->layer_stride;
-        HX_K(st->dtype, launch_tree_rope_append, w.tree_qkv, st->hq_l, kg, tv, kv->d_lens, kv->cos_tab, kv->sin_tab, w.q, kc, vc, s);
-        HX_K(st->dtype, launch_tree_attn, w.q, st->qw, in, kc, vc, kg, st->hq_l, tv, kv->d_lens, tp, out, s);
+        HX_K(st->dtype, launch_tree_rope_append, w.tree_qkv, st->hq_l, kg, tv, kv->d_lens, kv->cos_tab, kv->sin_tab, w.q, q_lo, kc, vc, s);
+        HX_K(st->dtype, launch_tree_attn, w.q, q_lo, st->qw, in, kc, vc, kg, st->hq_l, tv, kv->d_lens, tp, out, s);
     } else {
         float *kc = static_cast<float *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<float *>(kv->v) + (size_t)layer * kv->layer_stride;
         f32_launch_tree_rope_append(w.qkv32, st->hq_l, kg, tv, kv->d_lens, kv->cos_tab, kv->sin_tab, w.q32, kc, vc, s);
@@ -1452,11 +1454,11 @@ hexgen_status_t hexgen_kv_tree_attention(hexgen_kv_cache_t *kv, int layer, const
     HX_TRY(ensure_tree_part(st, s));
     const KvGeom kg = geom(st, kv);
     const TreeView tv = tr->view();
-    const TreePlan tp = pick_tree_plan(st, kv, tr);
+    const TreePlan tp = pick_tree_plan(st, kv, tr, false);
     const TreeIn in{k, v, ldk, ldv};
     if (is_h16(st->dtype)) {
         h16_t *kc = static_cast<h16_t *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<h16_t *>(kv->v) + (size_t)layer * kv->layer_stride;
-        HX_K(st->dtype, launch_tree_attn, static_cast<const h16_t *>(q), ldq, in, kc, vc, kg, st->hq_l, tv, kv->d_lens, tp, TreeOut{TREE_OUT_ROWS, tr->rows, st->qw, out}, s);
+        HX_K(st->dtype, launch_tree_attn, static_cast<const h16_t *>(q), nullptr, ldq, in, kc, vc, kg, st->hq_l, tv, kv->d_lens, tp, TreeOut{TREE_OUT_ROWS, tr->rows, st->qw, out}, s);
     } else {
         float *kc = static_cast<float *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<float *>(kv->v) + (size_t)layer * kv->layer_stride;
         f32_launch_tree_attn(static_cast<const float *>(q), ldq, in, kc, vc, kg, st->hq_l, tv, kv->d_lens, tp, static_cast<float *>(out), s);
