@@ -280,8 +280,8 @@ hexgen_status_t hexgen_head_load_q4(hexgen_head_t *hd, const void *g_final, cons
  *     [ceil(n_in / group)][n_out]; zeros, bytes [ceil(n_in / group)][n_out / 2] as w4, or NULL for 8 everywhere.  Host or device memory; the
  *     library keeps a repacked copy; synchronises.
  *   hexgen_q4_project: x device [n_rows, n_in], rows ldx >= n_in elements apart; y device [n_rows, n_out], dense, aligned to two elements, apart
- *     from x.  Enqueues on `stream`.  Up to 64 rows (fp32: 32) read the matrix once.  Products and sums are fp32, with one rounding to dtype;
- *     a row that holds an infinity or a NaN gives NaN.  HEXGEN_ERR_STATE before hexgen_q4_load.  Calls on one handle may not overlap in
+ *     from x.  Enqueues on `stream`.  Up to 64 rows (fp32: 32) read the matrix once.  Products and sums are fp32, with one rounding to dtype,
+ *     over the whole range of the rows (scales up to 1e25 in magnitude); a row that holds an infinity or a NaN gives NaN.  HEXGEN_ERR_STATE before hexgen_q4_load.  Calls on one handle may not overlap in
  *     time (they share its workspace).  Can be recorded into a graph.
  */
 typedef struct hexgen_q4 hexgen_q4_t;              /* opaque, library-owned */

@@ -223,23 +223,25 @@ struct Q4View {
     const void *w;              // [k_blocks][n_tiles][64 lanes][16 bytes]
     const void *scales;         // [scale_rows][16 n_tiles], of the matrix's type
     const uint8_t *zeros;       // rows of 16 n_tiles bytes 16 + z, zeros_row apart (0: one row for all)
-    int type, f16, group, n_tiles, n_valid, k_blocks, scale_rows, zeros_row;    // f16: the operand's type; group: 32, 64 or 128, as the scales are laid out
+    int type, group, n_tiles, n_valid, k_blocks, scale_rows, zeros_row;    // group: 32, 64 or 128, as the scales are laid out
 };
 // y [T][n_valid] of `type`, aligned to two elements; or, with best_val, per row and block of columns the largest value and its column (lowest
-// wins ties).  exps: the operand is two parts per row (launch_q4_parts)
+// wins ties).  The operand: `parts` columns per row, and where exps is given scaled by 2^exps[row] (launch_q4_parts)
 struct Q4Out {
     void *y;
     int type;
     float *best_val;
     int32_t *best_id;
     const int32_t *exps;
+    int parts;
 };
-constexpr int kQ4Rows = 64, kQ4PartRows = 32;     // rows of one launch, of 16-bit operands and of two-part ones
+constexpr int kQ4Rows = 64, kQ4PartRows = 32;     // rows of one launch, of one-part operands and of two-part ones
 size_t q4_part_floats(const Q4View &m);           // scratch of a launch, `part`
 int q4_best_units(const Q4View &m, int T);        // candidates per row of T two-part rows
-// x: T columns of the operand (parts: 2 T), ldx elements apart, 16-byte aligned, 128 k_blocks elements that are zero beyond the matrix's input features
+// x: parts * T columns of the operand, fp16, ldx elements apart, 16-byte aligned, 128 k_blocks elements that are zero beyond the matrix's input features
 void launch_q4(const Q4View &m, const h16_t *x, int64_t ldx, int T, const Q4Out &out, float *part, hipStream_t s);
-void launch_q4_parts(int type, const void *x, const void *x2, int64_t ldx, const float *g, float eps, int K, int Kp, int T, h16_t *out, int32_t *exps, hipStream_t s);
+void launch_q4_parts(int type, const void *x, const void *x2, int64_t ldx, const float *g, float eps, int K, int Kp, int T, int parts, h16_t *out, int32_t *exps,
+                     hipStream_t s);
 void launch_q4_copy(const h16_t *x, int64_t ldx, int K, int Kp, int T, h16_t *out, hipStream_t s);
 // w4 [K][ld / 2], scales [groups][ld], zeros [groups][ld / 2] or NULL (device): columns n0 .. n0 + n_valid - 1 into m's arrays
 void launch_q4_pack(const Q4View &m, const uint8_t *w4, const void *scales, const uint8_t *zeros, int64_t ld, int K, int group, int n0, hipStream_t s);

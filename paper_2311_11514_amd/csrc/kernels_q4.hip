@@ -1,17 +1,19 @@
 // Products of a few rows with a matrix of 4-bit weights that carry a scale, and possibly a zero point, per group of input features:
 //   y[t][n] = sum over groups g of s[g][n] * sum over k in g of (q[k][n] - z[g][n]) * x[t][k],   q, z = 0 .. 15.
 //
-// The matrix instructions take the weights as 16 + q: a nibble in the top mantissa bits of 1.0 * 2^4 (bf16: bits 3 .. 6 under
-// 0x4180, fp16: bits 6 .. 9 under 0x4c00) is that number exactly, one shift and one and-or per pair.  A group's sum S over (16 + q) x and
+// The matrix instructions take the weights as 16 + q: a nibble in the top mantissa bits of 1.0 * 2^4 (fp16: bits 6 .. 9 under 0x4c00) is that
+// number exactly, one shift and one and-or per pair.  A group's sum S over (16 + q) x and
 // the sum X over x alone (the same operand against ones: it arrives in the lanes that need it) give s * (S - (16 + z) X); products of
-// 5-bit and 8- or 11-bit numbers are exact in fp32, and 16 is the smallest offset that needs no arithmetic on the weights, so that S
+// 5-bit and 11-bit numbers are exact in fp32, and 16 is the smallest offset that needs no arithmetic on the weights, so that S
 // and its sum with X lose little of what the group's sum has.
-// fp32 rows are cut into two fp16 parts, x 2^e = hi + lo with e such that the row's largest value fits the type (22 bits of a value, 2^-39 of the
-// row's largest), that take two columns of the operand; their products are added up per part and joined, and scaled back, at the end.
+// The operand is fp16.  bf16 and fp32 rows are scaled to it, x 2^e with e such that the row's largest value fits the type, and the results scaled
+// back: no sum over a group passes fp32's range on the way.  A bf16 row takes one column of the operand (exact down to 2^-29 of the row's
+// largest value, and to 2^-40 of that below); an fp32 row two, x 2^e = hi + lo (22 bits of a value, 2^-39 of the row's largest), whose products are
+// added up per part and joined at the end.
 //
 // Layout: blocks of 16 columns x 128 input features, 1 KB, [k / 128][n / 16][lane][4 words]: word i of lane l holds features
 // 128 kq + 32 i + 8 (l / 16) + 0 .. 7 of column 16 tile + l % 16, what one lane of v_mfma_f32_16x16x32 contributes to four steps, in one
-// 16-byte request.  Feature 2 p + h sits in bits 16 h + 4 p of the word turned left by 3 (bf16) or 6 (fp16), so that pair 0 is in place
+// 16-byte request.  Feature 2 p + h sits in bits 16 h + 4 p of the word turned left by 6, so that pair 0 is in place
 // and the others are a shift or turn of 4, 8 and 12 away.
 // Scales have a row for every group, or for every 128 features where groups are larger; zero points are bytes 16 + z, or one row of 24s.
 #include <algorithm>
@@ -25,7 +27,6 @@
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((__vector_size__(16))) __bf16 b16x8;
 typedef __attribute__((__vector_size__(16))) _Float16 f16x8;
 
 __device__ __forceinline__ float bf16_f32(uint32_t v) { return __uint_as_float(v << 16); }
@@ -48,20 +49,17 @@ __device__ __forceinline__ uint16_t to_f16(float x) {
     return u;
 }
 
-template <bool F16>
 __device__ __forceinline__ floatx4 mfma(u32x4 a, u32x4 b, floatx4 c) {
-    if constexpr (F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, a), __builtin_bit_cast(b16x8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 // Eight nibbles -> eight times 16 + q.  The constants are kept in registers out of the compiler's sight: an and-or takes no literals on this
 // processor, and with constants that it knows the compiler makes two operations of it.
 struct Widen {
     uint32_t mask, sixteen;
-    template <bool F16>
     __device__ __forceinline__ static Widen make() {
         Widen w;
-        asm("s_mov_b32 %0, %1" : "=s"(w.mask) : "i"(F16 ? 0x03c003c0 : 0x00780078));
-        asm("v_mov_b32 %0, %1" : "=v"(w.sixteen) : "i"(F16 ? 0x4c004c00 : 0x41804180));
+        asm("s_mov_b32 %0, %1" : "=s"(w.mask) : "i"(0x03c003c0));
+        asm("v_mov_b32 %0, %1" : "=v"(w.sixteen) : "i"(0x4c004c00));
         return w;
     }
     __device__ __forceinline__ u32x4 operator()(uint32_t w) const {
@@ -81,7 +79,7 @@ __device__ __forceinline__ floatx4 scale4(const scale_raw<ST> &v) {
 
 // acc += a 128-feature block's share: UT weight tiles against NB operand tiles, x(step, tile) the operand of 32 features, sums(f, tile)
 // the sum of its columns over the features of group f
-template <bool F16, int ST, int NB, int UT, int FL, typename XF, typename SF>
+template <int ST, int NB, int UT, int FL, typename XF, typename SF>
 __device__ __forceinline__ void contract_block(const Widen &widen, const u32x4 (&w)[UT], const scale_raw<ST> (&s)[UT][4 / FL], const uint32_t (&z)[UT][4 / FL], XF x, SF sums,
                                                floatx4 (&acc)[UT][NB]) {
 #pragma unroll
@@ -100,7 +98,7 @@ __device__ __forceinline__ void contract_block(const Widen &widen, const u32x4 (
             for (int b = 0; b < NB; ++b) {
                 const u32x4 xb = x(st, b);
 #pragma unroll
-                for (int u = 0; u < UT; ++u) S[u][b] = mfma<F16>(a[u], xb, S[u][b]);
+                for (int u = 0; u < UT; ++u) S[u][b] = mfma(a[u], xb, S[u][b]);
             }
         }
         floatx4 s4[UT], z4[UT];
@@ -145,7 +143,7 @@ __device__ __forceinline__ void store_pair(const Q4Out &out, size_t at, float a,
     else if (out.type == HX_T_BF16) *reinterpret_cast<uint32_t *>(static_cast<h16_t *>(out.y) + at) = to_bf16(a) | (uint32_t)to_bf16(b) << 16;
     else *reinterpret_cast<uint32_t *>(static_cast<h16_t *>(out.y) + at) = to_f16(a) | (uint32_t)to_f16(b) << 16;
 }
-// the power of two that a row's parts were made with
+// the power of two that a row was scaled with
 __device__ __forceinline__ void scale_back(const Q4Out &out, int t, floatx4 &v) {
     if (out.exps == nullptr) return;
     const int e = out.exps[t];
@@ -181,7 +179,7 @@ __device__ __forceinline__ void best_of_lanes(float &bv, int &bi) {
 // Bound by HBM on wide matrices, on small ones by the launch and one round trip (bf16, one row: 8192 x 10240 13.4 us, 3.2 TB/s; the arg-max form, 8192 x
 // 32000, two columns 28.4, 4.7 TB/s; 4096 x 4096 5.9).
 // FL: 32-feature steps of a scale's group inside a 128-feature block (4: groups of 128 and more).
-template <bool F16, int ST, int UT, int FL, int W, int R, bool XLDS>
+template <int ST, int UT, int FL, int W, int R, bool XLDS>
 __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) void q4_few_kernel(Q4View m, const h16_t *__restrict__ x, int64_t ldx, int parts, int rows, Q4Out out) {
     constexpr int NF = 4 / FL;
     const int t0 = blockIdx.y * (16 / parts), T = min(16 / parts, rows - t0), C = parts * T;
@@ -199,8 +197,8 @@ __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) v
         col[u] = t * 16u + 4u * g;
     }
     const h16_t *xp = operand(min(j, C - 1)) + 8 * g;
-    const Widen widen = Widen::make<F16>();
-    const uint32_t one = F16 ? 0x3c003c00u : 0x3f803f80u;
+    const Widen widen = Widen::make();
+    const uint32_t one = 0x3c003c00u;
     const u32x4 ones = {one, one, one, one};
     floatx4 acc[UT][1];
 #pragma unroll
@@ -240,10 +238,10 @@ __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) v
         auto sums = [&](int f, int) {
             floatx4 X = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int s = f * FL; s < f * FL + FL; ++s) X = mfma<F16>(ones, xb[s], X);
+            for (int s = f * FL; s < f * FL + FL; ++s) X = mfma(ones, xb[s], X);
             return X;
         };
-        contract_block<F16, ST, 1, UT, FL>(widen, wr[i], sr[i], zr[i], [&](int s, int) { return xb[s]; }, sums, acc);
+        contract_block<ST, 1, UT, FL>(widen, wr[i], sr[i], zr[i], [&](int s, int) { return xb[s]; }, sums, acc);
     };
     int kq = wave;
     for (int rd = 0; rd < full; ++rd) {
@@ -293,19 +291,11 @@ __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) v
 }
 
 // the sum of eight elements
-template <bool F16>
 __device__ __forceinline__ float sum8(u32x4 v) {
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (F16) {
-            typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-            s = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, (uint32_t)v[i]), f16x2{(_Float16)1.f, (_Float16)1.f}, s, false);
-        } else {
-            typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
-            s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b16x2, (uint32_t)v[i]), b16x2{(__bf16)1.f, (__bf16)1.f}, s, false);
-        }
-    }
+    for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, (uint32_t)v[i]), f16x2{(_Float16)1.f, (_Float16)1.f}, s, false);
     return s;
 }
 
@@ -329,7 +319,7 @@ template <int ST, int NB, int FL> struct SharedStage {
     u32x4 x[4 * NB][64], w[16][64];
     unsigned char s[SP * 1024], z[1024];
 };
-template <bool F16, int ST, int NB, int FL>
+template <int ST, int NB, int FL>
 __global__ __launch_bounds__(1024, 4) void q4_shared_kernel(Q4View m, const h16_t *__restrict__ x, uint32_t ldx, int C, int T, Q4Out out, int per, float *__restrict__ part) {
     typedef SharedStage<ST, NB, FL> Stage;
     constexpr int NF = Stage::NF, ES = Stage::ES, SP = Stage::SP, UT = 2, XL = (4 * NB + 5) / 6;            // XL: operand pieces a wave fetches (the last ones more than once)
@@ -370,8 +360,8 @@ __global__ __launch_bounds__(1024, 4) void q4_shared_kernel(Q4View m, const h16_
         for (int i = 0; i < XL; ++i) hx_load_lds16(at + xat[i] * 1024, xoff[i], x + kq * 128);
         hx_load_lds16(at + offsetof(Stage, s) + sp * 1024, soff, sbase + (size_t)kq * NF * srow);
     };
-    const Widen widen = Widen::make<F16>();
-    const uint32_t one = F16 ? 0x3c003c00u : 0x3f803f80u;
+    const Widen widen = Widen::make();
+    const uint32_t one = 0x3c003c00u;
     const u32x4 ones = {one, one, one, one};
     floatx4 acc[UT][NB];
 #pragma unroll
@@ -386,7 +376,7 @@ __global__ __launch_bounds__(1024, 4) void q4_shared_kernel(Q4View m, const h16_
         if constexpr (TOLD) {
 #pragma unroll
             for (int i = 0; i < XL; ++i) {
-                const float v = sum_rows(sum8<F16>(st[grp][b0].x[xat[i]][lane]));
+                const float v = sum_rows(sum8(st[grp][b0].x[xat[i]][lane]));
                 if (g == 0) reinterpret_cast<float *>(&xsum[grp][parity][xat[i] % NB][j])[xat[i] / NB] = v;
             }
         }
@@ -419,11 +409,11 @@ __global__ __launch_bounds__(1024, 4) void q4_shared_kernel(Q4View m, const h16_
             } else {
                 floatx4 X = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = f * FL; i < f * FL + FL; ++i) X = mfma<F16>(ones, cur.x[i * NB + b][lane], X);
+                for (int i = f * FL; i < f * FL + FL; ++i) X = mfma(ones, cur.x[i * NB + b][lane], X);
                 return X;
             }
         };
-        contract_block<F16, ST, NB, UT, FL>(widen, w, sc, zc, [&](int i, int b) { return cur.x[i * NB + b][lane]; }, sums, acc);
+        contract_block<ST, NB, UT, FL>(widen, w, sc, zc, [&](int i, int b) { return cur.x[i * NB + b][lane]; }, sums, acc);
     }
     HX_WAIT_VM(0);                                              // nothing is on its way into the stages any more
     HX_LDS_BARRIER();
@@ -512,10 +502,10 @@ __device__ __forceinline__ float load_as(const void *p, size_t at) {
     else return f16_f32(static_cast<const h16_t *>(p)[at]);
 }
 
-// Rows as operand columns: x (+ x2), normalised with the gain g when there is one, as two fp16 parts [2 T][Kp] whose sum is the fp32 value times
-// 2^exps[t]; zero beyond K.  A block takes a row, a thread eight neighbouring values at a time, of which the first KEEP stay in registers for the
+// Rows as operand columns: x (+ x2), normalised with the gain g when there is one, times 2^exps[t] as one fp16 number [T][Kp], or as two [2 T][Kp] whose
+// sum is that value; zero beyond K.  A block takes a row, a thread eight neighbouring values at a time, of which the first KEEP stay in registers for the
 // second pass.  V: 16-byte pieces.  A value that is not finite stays so in the first part.
-template <int FROM, bool V>
+template <int FROM, bool V, int PARTS>
 __global__ __launch_bounds__(1024) void q4_parts_kernel(const void *__restrict__ x, const void *__restrict__ x2, int64_t ldx, const float *__restrict__ g,
                                                         float eps, int K, int Kp, int T, h16_t *__restrict__ out, int32_t *__restrict__ exps) {
     constexpr int KEEP = 4;
@@ -599,7 +589,7 @@ __global__ __launch_bounds__(1024) void q4_parts_kernel(const void *__restrict__
             else { hi[i >> 1] = h; lo[i >> 1] = l; }
         }
         *reinterpret_cast<u32x4 *>(out + (size_t)t * Kp + k) = u32x4{hi[0], hi[1], hi[2], hi[3]};
-        *reinterpret_cast<u32x4 *>(out + (size_t)(T + t) * Kp + k) = u32x4{lo[0], lo[1], lo[2], lo[3]};
+        if constexpr (PARTS == 2) *reinterpret_cast<u32x4 *>(out + (size_t)(T + t) * Kp + k) = u32x4{lo[0], lo[1], lo[2], lo[3]};
     };
     const Eight none = {};
     float unused = 0.f;
@@ -617,7 +607,7 @@ __global__ __launch_bounds__(256) void q4_copy_kernel(const h16_t *__restrict__ 
 }
 
 // [K][N / 2] bytes, column 2 i in the low nibble of byte i -> the layout above, columns n0 .. n0 + n - 1; a word per thread
-__global__ __launch_bounds__(256) void q4_pack_kernel(const uint8_t *__restrict__ src, int64_t ld, int K, int n0, int n, int n_tiles, int k_blocks, int turn, uint32_t *__restrict__ dst) {
+__global__ __launch_bounds__(256) void q4_pack_kernel(const uint8_t *__restrict__ src, int64_t ld, int K, int n0, int n, int n_tiles, int k_blocks, uint32_t *__restrict__ dst) {
     const size_t idx = (size_t)blockIdx.x * 256 + threadIdx.x;
     if (idx >= (size_t)k_blocks * n_tiles * 256) return;
     const int i = idx & 3, lane = (idx >> 2) & 63, col = (int)((idx >> 8) % n_tiles) * 16 + (lane & 15);
@@ -631,7 +621,7 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const uint8_t *__restrict_
             w |= q << (16 * (e & 1) + 4 * (e >> 1));
         }
     }
-    dst[idx] = w << turn | w >> (32 - turn);
+    dst[idx] = w << 6 | w >> 26;
 }
 // scales [groups][N] -> [rows][16 n_tiles], row r from group r / repeat, zero beyond; zero points: nibbles [groups][N / 2] -> bytes 16 + z, zrows rows
 __global__ __launch_bounds__(256) void q4_pack_scales_kernel(const void *__restrict__ src, int es, const uint8_t *__restrict__ zsrc, int64_t ld, int groups, int rows, int zrows,
@@ -694,12 +684,12 @@ SharedShape shared_shape(const Q4View &m, int C) {
 
 int shared_blocks(const Q4View &m, const SharedShape &sh) { return (m.n_tiles + 2 * sh.waves - 1) / (2 * sh.waves); }
 
-template <bool F16, int ST, int FL>
+template <int ST, int FL>
 void launch_few(const Q4View &m, int form, const h16_t *x, int64_t ldx, int C, int T, const Q4Out &out, hipStream_t s) {
     const int parts = C / T, rows = 16 / parts;
     const dim3 grid((m.n_tiles + few_tiles(form) - 1) / few_tiles(form), (T + rows - 1) / rows);
     const size_t lds = (size_t)std::min(C, 16) * m.k_blocks * 256;
-#define HX_FEW(UT, W, R, XLDS) hipLaunchKernelGGL((q4_few_kernel<F16, ST, UT, FL, W, R, XLDS>), grid, dim3(64 * W), XLDS ? lds : 0, s, m, x, ldx, parts, T, out)
+#define HX_FEW(UT, W, R, XLDS) hipLaunchKernelGGL((q4_few_kernel<ST, UT, FL, W, R, XLDS>), grid, dim3(64 * W), XLDS ? lds : 0, s, m, x, ldx, parts, T, out)
     if constexpr (FL > 1) {
         if (form == FEW_LDS_WIDE) HX_FEW(2, 4, 2, true);
         else if (form == FEW_WIDE) HX_FEW(2, 8, 2, false);
@@ -709,28 +699,28 @@ void launch_few(const Q4View &m, int form, const h16_t *x, int64_t ldx, int C, i
     else if (form == FEW) HX_FEW(1, 4, (FL == 1 ? 2 : 4), false);
 #undef HX_FEW
 }
-template <bool F16, int ST, int NB, int FL>
+template <int ST, int NB, int FL>
 void launch_shared(const Q4View &m, const h16_t *x, int64_t ldx, int C, int T, const Q4Out &out, float *part, hipStream_t s) {
     const SharedShape sh = shared_shape(m, C);
     const int per = (m.k_blocks + sh.splits - 1) / sh.splits;
     const dim3 grid(shared_blocks(m, sh), sh.splits);
-    hipLaunchKernelGGL((q4_shared_kernel<F16, ST, NB, FL>), grid, dim3(128 * sh.waves), 0, s, m, x, (uint32_t)ldx, C, T, out, per, sh.splits == 1 ? nullptr : part);
+    hipLaunchKernelGGL((q4_shared_kernel<ST, NB, FL>), grid, dim3(128 * sh.waves), 0, s, m, x, (uint32_t)ldx, C, T, out, per, sh.splits == 1 ? nullptr : part);
     if (sh.splits > 1) hipLaunchKernelGGL(q4_finish_kernel, dim3((m.n_tiles * 16 + 1023) / 1024, T), dim3(256), 0, s, m, part, sh.splits, C, T, out);
 }
-template <bool F16, int ST, int FL>
+template <int ST, int FL>
 void launch_cols(const Q4View &m, const h16_t *x, int64_t ldx, int C, int T, const Q4Out &out, float *part, hipStream_t s) {
     const int form = form_of(m, C);
-    if (form != SHARED) launch_few<F16, ST, FL>(m, form, x, ldx, C, T, out, s);
-    else if (C <= 16) launch_shared<F16, ST, 1, FL>(m, x, ldx, C, T, out, part, s);
-    else if (C <= 32) launch_shared<F16, ST, 2, FL>(m, x, ldx, C, T, out, part, s);
-    else if (C <= 48) launch_shared<F16, ST, 3, FL>(m, x, ldx, C, T, out, part, s);
-    else launch_shared<F16, ST, 4, FL>(m, x, ldx, C, T, out, part, s);
+    if (form != SHARED) launch_few<ST, FL>(m, form, x, ldx, C, T, out, s);
+    else if (C <= 16) launch_shared<ST, 1, FL>(m, x, ldx, C, T, out, part, s);
+    else if (C <= 32) launch_shared<ST, 2, FL>(m, x, ldx, C, T, out, part, s);
+    else if (C <= 48) launch_shared<ST, 3, FL>(m, x, ldx, C, T, out, part, s);
+    else launch_shared<ST, 4, FL>(m, x, ldx, C, T, out, part, s);
 }
-template <bool F16, int ST>
+template <int ST>
 void launch_type(const Q4View &m, const h16_t *x, int64_t ldx, int C, int T, const Q4Out &out, float *part, hipStream_t s) {
-    if (m.group >= 128) launch_cols<F16, ST, 4>(m, x, ldx, C, T, out, part, s);
-    else if (m.group == 64) launch_cols<F16, ST, 2>(m, x, ldx, C, T, out, part, s);
-    else launch_cols<F16, ST, 1>(m, x, ldx, C, T, out, part, s);
+    if (m.group >= 128) launch_cols<ST, 4>(m, x, ldx, C, T, out, part, s);
+    else if (m.group == 64) launch_cols<ST, 2>(m, x, ldx, C, T, out, part, s);
+    else launch_cols<ST, 1>(m, x, ldx, C, T, out, part, s);
 }
 
 }  // namespace
@@ -748,19 +738,24 @@ int q4_best_units(const Q4View &m, int T) {
     return sh.splits > 1 ? (m.n_tiles * 16 + 1023) / 1024 : shared_blocks(m, sh);
 }
 void launch_q4(const Q4View &m, const h16_t *x, int64_t ldx, int T, const Q4Out &out, float *part, hipStream_t s) {
-    const int C = out.exps != nullptr ? 2 * T : T;
-    if (m.type == HX_T_F32) launch_type<true, HX_T_F32>(m, x, ldx, C, T, out, part, s);
-    else if (m.type == HX_T_F16) launch_type<true, HX_T_F16>(m, x, ldx, C, T, out, part, s);
-    else if (m.f16) launch_type<true, HX_T_BF16>(m, x, ldx, C, T, out, part, s);
-    else launch_type<false, HX_T_BF16>(m, x, ldx, C, T, out, part, s);
+    const int C = out.parts * T;
+    if (m.type == HX_T_F32) launch_type<HX_T_F32>(m, x, ldx, C, T, out, part, s);
+    else if (m.type == HX_T_F16) launch_type<HX_T_F16>(m, x, ldx, C, T, out, part, s);
+    else launch_type<HX_T_BF16>(m, x, ldx, C, T, out, part, s);
 }
-void launch_q4_parts(int type, const void *x, const void *x2, int64_t ldx, const float *g, float eps, int K, int Kp, int T, h16_t *out, int32_t *exps, hipStream_t s) {
+void launch_q4_parts(int type, const void *x, const void *x2, int64_t ldx, const float *g, float eps, int K, int Kp, int T, int parts, h16_t *out, int32_t *exps,
+                     hipStream_t s) {
     const size_t es = type == HX_T_F32 ? 4 : 2;
     const bool pieces = ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(x2)) % 16 == 0) && (ldx * es) % 16 == 0 && K % 8 == 0;
-#define HX_PARTS(TY, VV) hipLaunchKernelGGL((q4_parts_kernel<TY, VV>), dim3(T), dim3(1024), 0, s, x, x2, ldx, g, eps, K, Kp, T, out, exps)
-    if (type == HX_T_F32) { if (pieces) HX_PARTS(HX_T_F32, true); else HX_PARTS(HX_T_F32, false); }
-    else if (type == HX_T_BF16) { if (pieces) HX_PARTS(HX_T_BF16, true); else HX_PARTS(HX_T_BF16, false); }
-    else { if (pieces) HX_PARTS(HX_T_F16, true); else HX_PARTS(HX_T_F16, false); }
+#define HX_PARTS(TY, N)                                                                                                                                \
+    do {                                                                                                                                               \
+        if (pieces) hipLaunchKernelGGL((q4_parts_kernel<TY, true, N>), dim3(T), dim3(1024), 0, s, x, x2, ldx, g, eps, K, Kp, T, out, exps);            \
+        else hipLaunchKernelGGL((q4_parts_kernel<TY, false, N>), dim3(T), dim3(1024), 0, s, x, x2, ldx, g, eps, K, Kp, T, out, exps);                  \
+    } while (0)
+    if (type == HX_T_F32) HX_PARTS(HX_T_F32, 2);
+    else if (type == HX_T_F16) HX_PARTS(HX_T_F16, 2);
+    else if (parts == 2) HX_PARTS(HX_T_BF16, 2);
+    else HX_PARTS(HX_T_BF16, 1);
 #undef HX_PARTS
 }
 void launch_q4_copy(const h16_t *x, int64_t ldx, int K, int Kp, int T, h16_t *out, hipStream_t s) {
@@ -768,7 +763,7 @@ void launch_q4_copy(const h16_t *x, int64_t ldx, int K, int Kp, int T, h16_t *ou
 }
 void launch_q4_pack(const Q4View &m, const uint8_t *w4, const void *scales, const uint8_t *zeros, int64_t ld, int K, int group, int n0, hipStream_t s) {
     const size_t words = (size_t)m.k_blocks * m.n_tiles * 256, cells = (size_t)m.scale_rows * m.n_tiles * 16;
-    hipLaunchKernelGGL(q4_pack_kernel, dim3((unsigned)((words + 255) / 256)), dim3(256), 0, s, w4, ld / 2, K, n0, m.n_valid, m.n_tiles, m.k_blocks, m.f16 ? 6 : 3,
+    hipLaunchKernelGGL(q4_pack_kernel, dim3((unsigned)((words + 255) / 256)), dim3(256), 0, s, w4, ld / 2, K, n0, m.n_valid, m.n_tiles, m.k_blocks,
                        const_cast<uint32_t *>(static_cast<const uint32_t *>(m.w)));
     hipLaunchKernelGGL(q4_pack_scales_kernel, dim3((unsigned)((cells + 255) / 256)), dim3(256), 0, s, scales, m.type == HX_T_F32 ? 4 : 2, zeros, ld, (K + group - 1) / group,
                        m.scale_rows, m.zeros_row != 0 ? m.scale_rows : 1, std::max(1, group / 128), n0, m.n_valid, m.n_tiles * 16, const_cast<void *>(m.scales),

@@ -17,13 +17,12 @@ void q4_free(Q4Store *q) {
 }
 
 namespace {
-hexgen_status_t load_into(Q4Store *q, hexgen_dtype_t dtype, bool parts, int n_in, int total, int n0, int n, int group, const void *w4, const void *scales,
+hexgen_status_t load_into(Q4Store *q, hexgen_dtype_t dtype, int n_in, int total, int n0, int n, int group, const void *w4, const void *scales,
                           const void *zeros, void **tmp) {
     const size_t es = dtype == HEXGEN_F32 ? 4 : 2, groups = ((size_t)n_in + group - 1) / group;
     Q4View &v = q->v;
     q->n_in = n_in;
     v.type = (int)dtype;
-    v.f16 = parts || dtype == HEXGEN_F16;
     v.group = std::min(group, 128);
     v.n_valid = n;
     v.n_tiles = (n + 15) / 16;
@@ -39,7 +38,7 @@ hexgen_status_t load_into(Q4Store *q, hexgen_dtype_t dtype, bool parts, int n_in
     v.zeros = static_cast<uint8_t *>(p);
     static_assert(kQ4Rows == 2 * kQ4PartRows, "one size of planes");
     HX_HIP(hipMalloc(reinterpret_cast<void **>(&q->planes), (size_t)q->padded() * kQ4Rows * sizeof(h16_t)));
-    HX_HIP(hipMalloc(reinterpret_cast<void **>(&q->exps), kQ4PartRows * sizeof(int32_t)));
+    HX_HIP(hipMalloc(reinterpret_cast<void **>(&q->exps), kQ4Rows * sizeof(int32_t)));
     HX_HIP(hipMalloc(reinterpret_cast<void **>(&q->part), q4_part_floats(v) * sizeof(float)));
     const size_t wb = (size_t)n_in * (total / 2), sb = groups * total * es, zb = zeros != nullptr ? groups * (total / 2) : 0;
     const size_t s_at = (wb + 255) / 256 * 256, z_at = s_at + (sb + 255) / 256 * 256;
@@ -55,11 +54,11 @@ hexgen_status_t load_into(Q4Store *q, hexgen_dtype_t dtype, bool parts, int n_in
 }
 }  // namespace
 
-hexgen_status_t q4_load(Q4Store *q, hexgen_dtype_t dtype, bool parts, int n_in, int total, int n0, int n, int group, const void *w4, const void *scales, const void *zeros) {
+hexgen_status_t q4_load(Q4Store *q, hexgen_dtype_t dtype, int n_in, int total, int n0, int n, int group, const void *w4, const void *scales, const void *zeros) {
     HX_HIP(hipDeviceSynchronize());
     q4_free(q);
     void *tmp = nullptr;
-    const hexgen_status_t rc = load_into(q, dtype, parts, n_in, total, n0, n, group, w4, scales, zeros, &tmp);
+    const hexgen_status_t rc = load_into(q, dtype, n_in, total, n0, n, group, w4, scales, zeros, &tmp);
     if (tmp) (void)hipFree(tmp);
     if (rc != HEXGEN_OK) q4_free(q);
     return rc;
@@ -96,7 +95,7 @@ void hexgen_q4_destroy(hexgen_q4_t *q) {
 
 hexgen_status_t hexgen_q4_load(hexgen_q4_t *q, const void *w4, const void *scales, const void *zeros) {
     if (!q || !w4 || !scales) return HEXGEN_ERR_INVALID_ARG;
-    return q4_load(&q->store, q->dtype, q->dtype == HEXGEN_F32, q->n_in, q->n_out, 0, q->n_out, q->group, w4, scales, zeros);
+    return q4_load(&q->store, q->dtype, q->n_in, q->n_out, 0, q->n_out, q->group, w4, scales, zeros);
 }
 
 hexgen_status_t hexgen_q4_project(hexgen_q4_t *q, const void *x, int64_t ldx, int n_rows, void *out, void *stream) {
@@ -106,19 +105,20 @@ hexgen_status_t hexgen_q4_project(hexgen_q4_t *q, const void *x, int64_t ldx, in
     const Q4Store &st = q->store;
     if (st.v.w == nullptr) return HEXGEN_ERR_STATE;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const bool parts = q->dtype == HEXGEN_F32;
-    // 16-bit rows of whole 128-feature blocks in 16-byte pieces are the operand as they are
-    const bool direct = !parts && reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx % 8 == 0 && ldx <= (1 << 24) && q->n_in % 128 == 0;
-    const int chunk = parts ? kQ4PartRows : kQ4Rows;
+    const int parts = q->dtype == HEXGEN_F32 ? 2 : 1;
+    const bool scaled = q->dtype != HEXGEN_F16;
+    // fp16 rows of whole 128-feature blocks in 16-byte pieces are the operand as they are
+    const bool direct = !scaled && reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx % 8 == 0 && ldx <= (1 << 24) && q->n_in % 128 == 0;
+    const int chunk = parts == 2 ? kQ4PartRows : kQ4Rows;
     for (int r0 = 0; r0 < n_rows; r0 += chunk) {
         const int n = std::min(chunk, n_rows - r0);
         const unsigned char *xr = static_cast<const unsigned char *>(x) + (size_t)r0 * ldx * es;
-        const Q4Out o{static_cast<unsigned char *>(out) + (size_t)r0 * q->n_out * es, (int)q->dtype, nullptr, nullptr, parts ? st.exps : nullptr};
+        const Q4Out o{static_cast<unsigned char *>(out) + (size_t)r0 * q->n_out * es, (int)q->dtype, nullptr, nullptr, scaled ? st.exps : nullptr, parts};
         if (direct) {
             launch_q4(st.v, reinterpret_cast<const h16_t *>(xr), ldx, n, o, st.part, s);
             continue;
         }
-        if (parts) launch_q4_parts((int)q->dtype, xr, nullptr, ldx, nullptr, 0.f, q->n_in, st.padded(), n, st.planes, st.exps, s);
+        if (scaled) launch_q4_parts((int)q->dtype, xr, nullptr, ldx, nullptr, 0.f, q->n_in, st.padded(), n, parts, st.planes, st.exps, s);
         else launch_q4_copy(reinterpret_cast<const h16_t *>(xr), ldx, q->n_in, st.padded(), n, st.planes, s);
         launch_q4(st.v, st.planes, st.padded(), n, o, st.part, s);
     }

@@ -1790,7 +1790,7 @@ hexgen_status_t hexgen_head_load_q4(hexgen_head_t *hd, const void *g_final, cons
     HX_HIP(hipDeviceSynchronize());
     drop_head_matrix(hd);
     HX_TRY(load_gain(hd, g_final));
-    hexgen_status_t rc = q4_load(&hd->q4, hd->dtype, true, hd->H, hd->V, hd->r * hd->Vl, hd->Vl, group, w4, scales, zeros);
+    hexgen_status_t rc = q4_load(&hd->q4, hd->dtype, hd->H, hd->V, hd->r * hd->Vl, hd->Vl, group, w4, scales, zeros);
     size_t cands = 0;
     if (rc == HEXGEN_OK)
         for (int t = 1; t <= kQ4PartRows; ++t) cands = std::max(cands, (size_t)t * q4_best_units(hd->q4.v, t));
@@ -1819,8 +1819,8 @@ hexgen_status_t hexgen_head_greedy(hexgen_head_t *hd, const void *hidden_a, cons
         const char *b = hidden_b ? static_cast<const char *>(hidden_b) + (size_t)r0 * H * es : nullptr;
         if (q4) {
             // normalised rows in full precision, as two-part operand; the arg-max over the blocks' best columns
-            launch_q4_parts((int)hd->dtype, a, b, H, hd->g, hd->eps, H, hd->q4.padded(), n, hd->q4.planes, hd->q4.exps, s);
-            launch_q4(hd->q4.v, hd->q4.planes, hd->q4.padded(), n, Q4Out{nullptr, 0, hd->q4_val, hd->q4_id, hd->q4.exps}, hd->q4.part, s);
+            launch_q4_parts((int)hd->dtype, a, b, H, hd->g, hd->eps, H, hd->q4.padded(), n, 2, hd->q4.planes, hd->q4.exps, s);
+            launch_q4(hd->q4.v, hd->q4.planes, hd->q4.padded(), n, Q4Out{nullptr, 0, hd->q4_val, hd->q4_id, hd->q4.exps, 2}, hd->q4.part, s);
             launch_row_best(hd->q4_val, hd->q4_id, q4_best_units(hd->q4.v, n), n, hd->r * hd->Vl, token_out + r0, logit_out ? logit_out + r0 : nullptr, s);
         } else if (is_h16(hd->dtype)) {
             // same kernels as a decode projection: prologue (x = a + b, x * g as hi/lo operand, sums of squares),
