@@ -222,7 +222,7 @@ enum { HX_T_F32 = 0, HX_T_BF16 = 1, HX_T_F16 = 2 };     // = hexgen_dtype_t
 struct Q4View {
     const void *w;              // [k_blocks][n_tiles][64 lanes][16 bytes]
     const void *scales;         // [scale_rows][16 n_tiles], of the matrix's type
-    const uint8_t *zeros;       // rows of 16 n_tiles bytes 16 + z, zeros_row apart (0: one row for all)
+    const uint8_t *zeros;       // rows of 16 n_tiles bytes, zeros_row apart (0: one row for all)
     int type, group, n_tiles, n_valid, k_blocks, scale_rows, zeros_row;    // group: 32, 64 or 128, as the scales are laid out
 };
 // y [T][n_valid] of `type`, aligned to two elements; or, with best_val, per row and block of columns the largest value and its column (lowest

@@ -1,11 +1,10 @@
 // Products of a few rows with a matrix of 4-bit weights that carry a scale, and possibly a zero point, per group of input features:
 //   y[t][n] = sum over groups g of s[g][n] * sum over k in g of (q[k][n] - z[g][n]) * x[t][k],   q, z = 0 .. 15.
 //
-// The matrix instructions take the weights as 16 + q: a nibble in the top mantissa bits of 1.0 * 2^4 (fp16: bits 6 .. 9 under 0x4c00) is that
-// number exactly, one shift and one and-or per pair.  A group's sum S over (16 + q) x and
-// the sum X over x alone (the same operand against ones: it arrives in the lanes that need it) give s * (S - (16 + z) X); products of
-// 5-bit and 11-bit numbers are exact in fp32, and 16 is the smallest offset that needs no arithmetic on the weights, so that S
-// and its sum with X lose little of what the group's sum has.
+// The matrix instructions take the weights as q - z, exactly: a nibble in the mantissa bits of 16 (256) is 16 + q (256 + q), from which one packed
+// subtraction takes 16 + z (256 + z).  Products with 11-bit numbers are exact in fp32, so that a group's sum is off by its own roundings alone, in
+// relation to |q - z| |x|.  (Sums over 16 + q with the offset taken off behind them need no subtraction, but then a large x whose weight is its zero
+// point drowns the rest of its group.)
 // The operand is fp16.  bf16 and fp32 rows are scaled to it, x 2^e with e such that the row's largest value fits the type, and the results scaled
 // back: no sum over a group passes fp32's range on the way.  A bf16 row takes one column of the operand (exact down to 2^-29 of the row's
 // largest value, and to 2^-40 of that below); an fp32 row two, x 2^e = hi + lo (22 bits of a value, 2^-39 of the row's largest), whose products are
@@ -13,9 +12,9 @@
 //
 // Layout: blocks of 16 columns x 128 input features, 1 KB, [k / 128][n / 16][lane][4 words]: word i of lane l holds features
 // 128 kq + 32 i + 8 (l / 16) + 0 .. 7 of column 16 tile + l % 16, what one lane of v_mfma_f32_16x16x32 contributes to four steps, in one
-// 16-byte request.  Feature 2 p + h sits in bits 16 h + 4 p of the word turned left by 6, so that pair 0 is in place
-// and the others are a shift or turn of 4, 8 and 12 away.
-// Scales have a row for every group, or for every 128 features where groups are larger; zero points are bytes 16 + z, or one row of 24s.
+// 16-byte request.  Feature 2 p + h sits in bits 16 h + 4 p (p = 3: 16 (1 - h) + 12) of the word turned left by 6: pairs 0 and 3 are where fp16 has
+// them under the exponents of 16 and 256, pairs 2 and 1 after one turn by 8.
+// Scales have a row for every group, or for every 128 features where groups are larger; zero points are bytes, or one row of 8s.
 #include <algorithm>
 #include <cmath>
 #include <cstddef>
@@ -52,19 +51,27 @@ __device__ __forceinline__ uint16_t to_f16(float x) {
 __device__ __forceinline__ floatx4 mfma(u32x4 a, u32x4 b, floatx4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
-// Eight nibbles -> eight times 16 + q.  The constants are kept in registers out of the compiler's sight: an and-or takes no literals on this
+// Eight nibbles -> eight times q - z.  The constants are kept in registers out of the compiler's sight: an and-or takes no literals on this
 // processor, and with constants that it knows the compiler makes two operations of it.
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+struct Zero { uint32_t of16, of256; };                          // -(16 + z) and -(256 + z), twice each
 struct Widen {
-    uint32_t mask, sixteen;
+    uint32_t mask16, mask256, is16, is256;
     __device__ __forceinline__ static Widen make() {
         Widen w;
-        asm("s_mov_b32 %0, %1" : "=s"(w.mask) : "i"(0x03c003c0));
-        asm("v_mov_b32 %0, %1" : "=v"(w.sixteen) : "i"(0x4c004c00));
+        asm("s_mov_b32 %0, %1" : "=s"(w.mask16) : "i"(0x03c003c0));
+        asm("s_mov_b32 %0, %1" : "=s"(w.mask256) : "i"(0x003c003c));
+        asm("v_mov_b32 %0, %1" : "=v"(w.is16) : "i"(0x4c004c00));
+        asm("v_mov_b32 %0, %1" : "=v"(w.is256) : "i"(0x5c005c00));
         return w;
     }
-    __device__ __forceinline__ u32x4 operator()(uint32_t w) const {
-        return u32x4{(w & mask) | sixteen, (__builtin_amdgcn_alignbit(w, w, 4) & mask) | sixteen, (__builtin_amdgcn_alignbit(w, w, 8) & mask) | sixteen,
-                     (__builtin_amdgcn_alignbit(w, w, 12) & mask) | sixteen};
+    __device__ __forceinline__ static Zero zero(uint32_t z) { return Zero{0xcc00cc00u + __umul24(z, 0x400040u), 0xdc00dc00u + __umul24(z, 0x40004u)}; }
+    __device__ __forceinline__ static uint32_t add(uint32_t a, uint32_t b) {
+        return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, a) + __builtin_bit_cast(f16x2, b));
+    }
+    __device__ __forceinline__ u32x4 operator()(uint32_t w, const Zero &z) const {
+        const uint32_t r = __builtin_amdgcn_alignbit(w, w, 8);
+        return u32x4{add((w & mask16) | is16, z.of16), add((r & mask256) | is256, z.of256), add((r & mask16) | is16, z.of16), add((w & mask256) | is256, z.of256)};
     }
 };
 
@@ -77,10 +84,9 @@ __device__ __forceinline__ floatx4 scale4(const scale_raw<ST> &v) {
     else return floatx4{f16_f32(v.x & 0xffffu), f16_f32(v.x >> 16), f16_f32(v.y & 0xffffu), f16_f32(v.y >> 16)};
 }
 
-// acc += a 128-feature block's share: UT weight tiles against NB operand tiles, x(step, tile) the operand of 32 features, sums(f, tile)
-// the sum of its columns over the features of group f
-template <int ST, int NB, int UT, int FL, typename XF, typename SF>
-__device__ __forceinline__ void contract_block(const Widen &widen, const u32x4 (&w)[UT], const scale_raw<ST> (&s)[UT][4 / FL], const uint32_t (&z)[UT][4 / FL], XF x, SF sums,
+// acc += a 128-feature block's share: UT weight tiles against NB operand tiles, x(step, tile) the operand of 32 features
+template <int ST, int NB, int UT, int FL, typename XF>
+__device__ __forceinline__ void contract_block(const Widen &widen, const u32x4 (&w)[UT], const scale_raw<ST> (&s)[UT][4 / FL], const uint32_t (&z)[UT][4 / FL], XF x,
                                                floatx4 (&acc)[UT][NB]) {
 #pragma unroll
     for (int f = 0; f < 4 / FL; ++f) {
@@ -89,33 +95,31 @@ __device__ __forceinline__ void contract_block(const Widen &widen, const u32x4 (
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int u = 0; u < UT; ++u) S[u][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+        Zero zero[UT];
+#pragma unroll
+        for (int u = 0; u < UT; ++u) zero[u] = Widen::zero(z[u][f]);
 #pragma unroll
         for (int st = f * FL; st < f * FL + FL; ++st) {
             u32x4 a[UT];
 #pragma unroll
-            for (int u = 0; u < UT; ++u) a[u] = widen(w[u][st]);
+            for (int u = 0; u < UT; ++u) a[u] = widen(w[u][st], zero[u]);
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 const u32x4 xb = x(st, b);
 #pragma unroll
                 for (int u = 0; u < UT; ++u) S[u][b] = mfma(a[u], xb, S[u][b]);
             }
+            if (UT > 1 && NB == 1) __builtin_amdgcn_sched_barrier(0);      // one step's weights at a time: more of them do not fit the registers
         }
-        floatx4 s4[UT], z4[UT];
+        floatx4 s4[UT];
 #pragma unroll
-        for (int u = 0; u < UT; ++u) {
-            s4[u] = scale4<ST>(s[u][f]);
+        for (int u = 0; u < UT; ++u) s4[u] = scale4<ST>(s[u][f]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) z4[u][r] = (float)((z[u][f] >> (8 * r)) & 255u);
-        }
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const floatx4 X = sums(f, b);
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int u = 0; u < UT; ++u)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[u][b][r] = fmaf(s4[u][r], fmaf(-z4[u][r], X[r], S[u][b][r]), acc[u][b][r]);
-        }
+                for (int r = 0; r < 4; ++r) acc[u][b][r] = fmaf(s4[u][r], S[u][b][r], acc[u][b][r]);
         if (FL < 4) {                                           // one group's sums at a time: side by side they do not fit the registers
 #pragma unroll
             for (int u = 0; u < UT; ++u)
@@ -125,14 +129,15 @@ __device__ __forceinline__ void contract_block(const Widen &widen, const u32x4 (
         }
     }
 }
-// the scales and zero points of a 128-feature block for four columns from `col` on
+// the scales of a 128-feature block for four columns from `col` on, what the lane has of the result, and the zero points of column `zcol`, of whose
+// weights it holds a part
 template <int ST, int NF>
-__device__ __forceinline__ void load_scales(const Q4View &m, int kq, uint32_t col, scale_raw<ST> (&s)[NF], uint32_t (&z)[NF]) {
+__device__ __forceinline__ void load_scales(const Q4View &m, int kq, uint32_t col, uint32_t zcol, scale_raw<ST> (&s)[NF], uint32_t (&z)[NF]) {
 #pragma unroll
     for (int f = 0; f < NF; ++f) {
         const size_t row = kq * NF + f;                         // the same in every lane
         s[f] = *reinterpret_cast<const scale_raw<ST> *>(static_cast<const unsigned char *>(m.scales) + row * (m.n_tiles * 16) * (ST == HX_T_F32 ? 4 : 2) + col * (ST == HX_T_F32 ? 4u : 2u));
-        z[f] = *reinterpret_cast<const uint32_t *>(m.zeros + row * m.zeros_row + col);
+        z[f] = m.zeros[row * m.zeros_row + zcol];
     }
 }
 __device__ __forceinline__ u32x4 load_weights(const Q4View &m, int kq, uint32_t off) {
@@ -143,12 +148,12 @@ __device__ __forceinline__ void store_pair(const Q4Out &out, size_t at, float a,
     else if (out.type == HX_T_BF16) *reinterpret_cast<uint32_t *>(static_cast<h16_t *>(out.y) + at) = to_bf16(a) | (uint32_t)to_bf16(b) << 16;
     else *reinterpret_cast<uint32_t *>(static_cast<h16_t *>(out.y) + at) = to_f16(a) | (uint32_t)to_f16(b) << 16;
 }
-// the power of two that a row was scaled with
-__device__ __forceinline__ void scale_back(const Q4Out &out, int t, floatx4 &v) {
-    if (out.exps == nullptr) return;
-    const int e = out.exps[t];
+// The result of a row: sums that are not finite (the row holds an infinity or a NaN) become NaN, and the power of two that the row was scaled with
+// is taken off.
+__device__ __forceinline__ void settle(const Q4Out &out, int t, floatx4 &v) {
+    const int e = out.exps == nullptr ? 0 : out.exps[t];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = ldexpf(v[r], -e);
+    for (int r = 0; r < 4; ++r) v[r] = __builtin_isfinite(v[r]) ? ldexpf(v[r], -e) : NAN;
 }
 // four columns from n0 on of row t (n_valid is even, so that columns come in pairs)
 __device__ __forceinline__ void store_columns(const Q4View &m, const Q4Out &out, int t, int n0, floatx4 v) {
@@ -189,17 +194,16 @@ __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) v
     extern __shared__ __align__(16) u32x4 xs[];                 // XLDS: [k / 8][column]
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     const int tile0 = blockIdx.x * UT;
-    uint32_t off[UT], col[UT];
+    uint32_t off[UT], col[UT], zcol[UT];
 #pragma unroll
     for (int u = 0; u < UT; ++u) {
         const uint32_t t = min(tile0 + u, m.n_tiles - 1);      // a last tile of its own: the block's second repeats it, not stored
         off[u] = t * 1024u + lane * 16u;
         col[u] = t * 16u + 4u * g;
+        zcol[u] = t * 16u + j;
     }
     const h16_t *xp = operand(min(j, C - 1)) + 8 * g;
     const Widen widen = Widen::make();
-    const uint32_t one = 0x3c003c00u;
-    const u32x4 ones = {one, one, one, one};
     floatx4 acc[UT][1];
 #pragma unroll
     for (int u = 0; u < UT; ++u) acc[u][0] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -210,7 +214,7 @@ __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) v
 #pragma unroll
         for (int u = 0; u < UT; ++u) wr[i][u] = load_weights(m, kq, off[u]);
 #pragma unroll
-        for (int u = 0; u < UT; ++u) load_scales<ST, NF>(m, kq, col[u], sr[i][u], zr[i][u]);
+        for (int u = 0; u < UT; ++u) load_scales<ST, NF>(m, kq, col[u], zcol[u], sr[i][u], zr[i][u]);
     };
     auto fetch = [&](int i, int kq) {
 #pragma unroll
@@ -231,17 +235,7 @@ __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) v
     }
     const u32x4 *xl = xs + g * C + min(j, C - 1);
     auto contract = [&](int i, int kq) {
-        u32x4 xb[4];
-#pragma unroll
-        for (int s = 0; s < 4; ++s) xb[s] = XLDS ? xl[(kq * 4 + s) * 4 * C] : xr[XLDS ? 0 : i & 1][s];
-        // the columns' sums: the same operand against ones, which leaves them in the lanes that need them
-        auto sums = [&](int f, int) {
-            floatx4 X = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = f * FL; s < f * FL + FL; ++s) X = mfma(ones, xb[s], X);
-            return X;
-        };
-        contract_block<ST, 1, UT, FL>(widen, wr[i], sr[i], zr[i], [&](int s, int) { return xb[s]; }, sums, acc);
+        contract_block<ST, 1, UT, FL>(widen, wr[i], sr[i], zr[i], [&](int s, int) { return XLDS ? xl[(kq * 4 + s) * 4 * C] : xr[XLDS ? 0 : i & 1][s]; }, acc);
     };
     int kq = wave;
     for (int rd = 0; rd < full; ++rd) {
@@ -275,7 +269,7 @@ __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) v
         v += a;
     }
     const int n0 = (tile0 + u) * 16 + 4 * gg;
-    scale_back(out, t0 + t, v);
+    settle(out, t0 + t, v);
     if (out.best_val == nullptr) {
         store_columns(m, out, t0 + t, n0, v);
         return;
@@ -288,21 +282,6 @@ __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) v
         out.best_val[(size_t)(t0 + t) * gridDim.x + blockIdx.x] = bv;
         out.best_id[(size_t)(t0 + t) * gridDim.x + blockIdx.x] = bi;
     }
-}
-
-// the sum of eight elements
-__device__ __forceinline__ float sum8(u32x4 v) {
-    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, (uint32_t)v[i]), f16x2{(_Float16)1.f, (_Float16)1.f}, s, false);
-    return s;
-}
-
-// the sum over the four rows of 16 lanes, in every lane: each swap leaves the even rows in one register and the odd ones in the other
-__device__ __forceinline__ float sum_rows(float v) {
-    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return sum_halves(__uint_as_float(a[0]) + __uint_as_float(a[1]));
 }
 
 // More operand columns: the operand outweighs the weights that a tile of 16 columns has, so the waves of a block share it through LDS.  Two groups
@@ -327,10 +306,6 @@ __global__ __launch_bounds__(1024, 4) void q4_shared_kernel(Q4View m, const h16_
     constexpr int YS = 260;
     static_assert((S - 2) * L < 64 && 16 * NB * YS * 4 <= 2 * S * sizeof(Stage), "waits, and the results in the stages' place");
     __shared__ __align__(16) Stage st[2][S];
-    // the columns' sums: the operand against ones, or with four operand tiles, where the registers do not hold these as well, from whoever fetched the
-    // piece (64 columns, 8192 x 28672: 85 / 68 us; 4096 x 4096 24 / 15.5; 32 columns, 8192 x 57344: 66 / 74; 12: 52 / 56; 48 columns as long)
-    constexpr bool TOLD = NB == 4;
-    __shared__ floatx4 xsum[2][2][TOLD ? NB : 1][16];           // [group][parity of its step][operand tile][column][32-feature step]
     const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4, waves = blockDim.x >> 7;
     const int nth = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = nth >= waves ? 1 : 0, wave = nth - grp * waves;
     const int first = blockIdx.x * waves * UT, np = m.n_tiles * 16;
@@ -361,8 +336,6 @@ __global__ __launch_bounds__(1024, 4) void q4_shared_kernel(Q4View m, const h16_
         hx_load_lds16(at + offsetof(Stage, s) + sp * 1024, soff, sbase + (size_t)kq * NF * srow);
     };
     const Widen widen = Widen::make();
-    const uint32_t one = 0x3c003c00u;
-    const u32x4 ones = {one, one, one, one};
     floatx4 acc[UT][NB];
 #pragma unroll
     for (int u = 0; u < UT; ++u)
@@ -370,16 +343,9 @@ __global__ __launch_bounds__(1024, 4) void q4_shared_kernel(Q4View m, const h16_
         for (int b = 0; b < NB; ++b) acc[u][b] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < S - 1; ++i) issue(k0 + grp + 2 * i, i);
-    int b0 = 0, bl = S - 1, parity = 0;                         // buffers of this step and of the one that is S - 1 steps ahead
-    for (int k = k0 + grp; k - grp < k1; k += 2, parity ^= 1) {
+    int b0 = 0, bl = S - 1;                                     // buffers of this step and of the one that is S - 1 steps ahead
+    for (int k = k0 + grp; k - grp < k1; k += 2) {
         HX_WAIT_VM((S - 2) * L);                                // this step's share of this wave; behind the barrier everybody's
-        if constexpr (TOLD) {
-#pragma unroll
-            for (int i = 0; i < XL; ++i) {
-                const float v = sum_rows(sum8(st[grp][b0].x[xat[i]][lane]));
-                if (g == 0) reinterpret_cast<float *>(&xsum[grp][parity][xat[i] % NB][j])[xat[i] / NB] = v;
-            }
-        }
         HX_LDS_BARRIER();
         issue(k + 2 * (S - 1), bl);                             // (everybody has left that buffer)
         bl = b0;
@@ -396,24 +362,10 @@ __global__ __launch_bounds__(1024, 4) void q4_shared_kernel(Q4View m, const h16_
 #pragma unroll
             for (int f = 0; f < NF; ++f) {
                 sc[u][f] = *reinterpret_cast<const scale_raw<ST> *>(cur.s + (f * 256 + tile * 16 + 4 * g) * ES);
-                zc[u][f] = *reinterpret_cast<const uint32_t *>(cur.z + f * 256 + tile * 16 + 4 * g);
+                zc[u][f] = cur.z[f * 256 + tile * 16 + j];
             }
         }
-        auto sums = [&](int f, int b) {
-            if constexpr (TOLD) {
-                const float *q = reinterpret_cast<const float *>(&xsum[grp][parity][b][j]) + f * FL;
-                float v = q[0];
-#pragma unroll
-                for (int i = 1; i < FL; ++i) v += q[i];
-                return floatx4{v, v, v, v};
-            } else {
-                floatx4 X = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int i = f * FL; i < f * FL + FL; ++i) X = mfma(ones, cur.x[i * NB + b][lane], X);
-                return X;
-            }
-        };
-        contract_block<ST, NB, UT, FL>(widen, w, sc, zc, [&](int i, int b) { return cur.x[i * NB + b][lane]; }, sums, acc);
+        contract_block<ST, NB, UT, FL>(widen, w, sc, zc, [&](int i, int b) { return cur.x[i * NB + b][lane]; }, acc);
     }
     HX_WAIT_VM(0);                                              // nothing is on its way into the stages any more
     HX_LDS_BARRIER();
@@ -447,7 +399,7 @@ __global__ __launch_bounds__(1024, 4) void q4_shared_kernel(Q4View m, const h16_
     for (int t = nth; t < T; t += 2 * waves) {
         floatx4 v = *reinterpret_cast<const floatx4 *>(ys + t * YS + 4 * lane);
         for (int c = t + T; c < C; c += T) v += *reinterpret_cast<const floatx4 *>(ys + c * YS + 4 * lane);
-        scale_back(out, t, v);
+        settle(out, t, v);
         if (out.best_val == nullptr) {
             if (there) store_columns(m, out, t, n0, v);
             continue;
@@ -476,7 +428,7 @@ __global__ __launch_bounds__(256) void q4_finish_kernel(Q4View m, const float *_
             v += a;
         }
     }
-    scale_back(out, t, v);
+    settle(out, t, v);
     if (out.best_val == nullptr) {
         if (n0 < np) store_columns(m, out, t, n0, v);
         return;
@@ -618,12 +570,12 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const uint8_t *__restrict_
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const uint32_t q = k0 + e < K ? (src[(size_t)(k0 + e) * ld + (at >> 1)] >> (4 * (at & 1))) & 15u : 0u;
-            w |= q << (16 * (e & 1) + 4 * (e >> 1));
+            w |= q << (16 * ((e & 1) ^ (e >> 1 == 3)) + 4 * (e >> 1));
         }
     }
     dst[idx] = w << 6 | w >> 26;
 }
-// scales [groups][N] -> [rows][16 n_tiles], row r from group r / repeat, zero beyond; zero points: nibbles [groups][N / 2] -> bytes 16 + z, zrows rows
+// scales [groups][N] -> [rows][16 n_tiles], row r from group r / repeat, zero beyond; zero points: nibbles [groups][N / 2] -> bytes, zrows rows
 __global__ __launch_bounds__(256) void q4_pack_scales_kernel(const void *__restrict__ src, int es, const uint8_t *__restrict__ zsrc, int64_t ld, int groups, int rows, int zrows,
                                                              int repeat, int n0, int n, int np, void *__restrict__ dst, uint8_t *__restrict__ zdst) {
     const size_t idx = (size_t)blockIdx.x * 256 + threadIdx.x;
@@ -633,7 +585,7 @@ __global__ __launch_bounds__(256) void q4_pack_scales_kernel(const void *__restr
     const size_t at = (size_t)group * ld + n0 + col;
     if (es == 4) static_cast<float *>(dst)[idx] = there ? static_cast<const float *>(src)[at] : 0.f;
     else static_cast<h16_t *>(dst)[idx] = there ? static_cast<const h16_t *>(src)[at] : (h16_t)0;
-    if (row < zrows) zdst[idx] = (uint8_t)(16 + (zsrc == nullptr ? 8 : there ? (zsrc[(size_t)group * (ld / 2) + ((n0 + col) >> 1)] >> (4 * ((n0 + col) & 1))) & 15 : 0));
+    if (row < zrows) zdst[idx] = (uint8_t)(zsrc == nullptr ? 8 : there ? (zsrc[(size_t)group * (ld / 2) + ((n0 + col) >> 1)] >> (4 * ((n0 + col) & 1))) & 15 : 0);
 }
 
 // ---- which form --------------------------------------------------------------------------------------------------
