@@ -238,8 +238,15 @@ struct Q4Out {
 constexpr int kQ4Rows = 64, kQ4PartRows = 32;     // rows of one launch, of one-part operands and of two-part ones
 size_t q4_part_floats(const Q4View &m);           // scratch of a launch, `part`
 int q4_best_units(const Q4View &m, int T);        // candidates per row of T two-part rows
-// x: parts * T columns of the operand, fp16, ldx elements apart, 16-byte aligned, 128 k_blocks elements that are zero beyond the matrix's input features
-void launch_q4(const Q4View &m, const h16_t *x, int64_t ldx, int T, const Q4Out &out, float *part, hipStream_t s);
+// The operand: parts * T columns, fp16 (bf16: where q4_takes_bf16 says so), ldx elements apart, 16-byte aligned, 128 k_blocks elements that are zero
+// beyond the matrix's input features
+struct Q4In {
+    const h16_t *x;
+    int64_t ldx;
+    bool bf16;
+};
+bool q4_takes_bf16(const Q4View &m, int T);
+void launch_q4(const Q4View &m, const Q4In &in, int T, const Q4Out &out, float *part, hipStream_t s);
 void launch_q4_parts(int type, const void *x, const void *x2, int64_t ldx, const float *g, float eps, int K, int Kp, int T, int parts, h16_t *out, int32_t *exps,
                      hipStream_t s);
 void launch_q4_copy(const h16_t *x, int64_t ldx, int K, int Kp, int T, h16_t *out, hipStream_t s);

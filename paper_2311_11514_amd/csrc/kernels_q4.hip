@@ -5,7 +5,8 @@
 // subtraction takes 16 + z (256 + z).  Products with 11-bit numbers are exact in fp32, so that a group's sum is off by its own roundings alone, in
 // relation to |q - z| |x|.  (Sums over 16 + q with the offset taken off behind them need no subtraction, but then a large x whose weight is its zero
 // point drowns the rest of its group.)
-// The operand is fp16.  bf16 and fp32 rows are scaled to it, x 2^e with e such that the row's largest value fits the type, and the results scaled
+// The operand is fp16, or bf16 where a small matrix meets few of them and the weights can be converted once more.  Other bf16 rows and fp32 rows are
+// scaled to fp16, x 2^e with e such that the row's largest value fits the type, and the results scaled
 // back: no sum over a group passes fp32's range on the way.  A bf16 row takes one column of the operand (exact down to 2^-29 of the row's
 // largest value, and to 2^-40 of that below); an fp32 row two, x 2^e = hi + lo (22 bits of a value, 2^-39 of the row's largest), whose products are
 // added up per part and joined at the end.
@@ -26,6 +27,7 @@
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((__vector_size__(16))) __bf16 b16x8;
 typedef __attribute__((__vector_size__(16))) _Float16 f16x8;
 
 __device__ __forceinline__ float bf16_f32(uint32_t v) { return __uint_as_float(v << 16); }
@@ -48,10 +50,12 @@ __device__ __forceinline__ uint16_t to_f16(float x) {
     return u;
 }
 
+template <bool BF>
 __device__ __forceinline__ floatx4 mfma(u32x4 a, u32x4 b, floatx4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    if constexpr (BF) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b16x8, a), __builtin_bit_cast(b16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
-// Eight nibbles -> eight times q - z.  The constants are kept in registers out of the compiler's sight: an and-or takes no literals on this
+// Eight nibbles -> eight times q - z, as fp16, or, through fp32, as bf16 (BF; 21 operations instead of 9).  The constants are kept in registers out of the compiler's sight: an and-or takes no literals on this
 // processor, and with constants that it knows the compiler makes two operations of it.
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 struct Zero { uint32_t of16, of256; };                          // -(16 + z) and -(256 + z), twice each
@@ -69,9 +73,18 @@ struct Widen {
     __device__ __forceinline__ static uint32_t add(uint32_t a, uint32_t b) {
         return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, a) + __builtin_bit_cast(f16x2, b));
     }
+    template <bool BF>
     __device__ __forceinline__ u32x4 operator()(uint32_t w, const Zero &z) const {
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
         const uint32_t r = __builtin_amdgcn_alignbit(w, w, 8);
-        return u32x4{add((w & mask16) | is16, z.of16), add((r & mask256) | is256, z.of256), add((r & mask16) | is16, z.of16), add((w & mask256) | is256, z.of256)};
+        u32x4 v = {add((w & mask16) | is16, z.of16), add((r & mask256) | is256, z.of256), add((r & mask16) | is16, z.of16), add((w & mask256) | is256, z.of256)};
+        if constexpr (BF) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                v[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(__builtin_convertvector(__builtin_bit_cast(f16x2, (uint32_t)v[i]), f32x2), b16x2));
+        }
+        return v;
     }
 };
 
@@ -85,7 +98,7 @@ __device__ __forceinline__ floatx4 scale4(const scale_raw<ST> &v) {
 }
 
 // acc += a 128-feature block's share: UT weight tiles against NB operand tiles, x(step, tile) the operand of 32 features
-template <int ST, int NB, int UT, int FL, typename XF>
+template <int ST, int NB, int UT, int FL, bool BF, typename XF>
 __device__ __forceinline__ void contract_block(const Widen &widen, const u32x4 (&w)[UT], const scale_raw<ST> (&s)[UT][4 / FL], const uint32_t (&z)[UT][4 / FL], XF x,
                                                floatx4 (&acc)[UT][NB]) {
 #pragma unroll
@@ -102,12 +115,12 @@ __device__ __forceinline__ void contract_block(const Widen &widen, const u32x4 (
         for (int st = f * FL; st < f * FL + FL; ++st) {
             u32x4 a[UT];
 #pragma unroll
-            for (int u = 0; u < UT; ++u) a[u] = widen(w[u][st], zero[u]);
+            for (int u = 0; u < UT; ++u) a[u] = widen.template operator()<BF>(w[u][st], zero[u]);
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 const u32x4 xb = x(st, b);
 #pragma unroll
-                for (int u = 0; u < UT; ++u) S[u][b] = mfma(a[u], xb, S[u][b]);
+                for (int u = 0; u < UT; ++u) S[u][b] = mfma<BF>(a[u], xb, S[u][b]);
             }
             if (UT > 1 && NB == 1) __builtin_amdgcn_sched_barrier(0);      // one step's weights at a time: more of them do not fit the registers
         }
@@ -148,10 +161,15 @@ __device__ __forceinline__ void store_pair(const Q4Out &out, size_t at, float a,
     else if (out.type == HX_T_BF16) *reinterpret_cast<uint32_t *>(static_cast<h16_t *>(out.y) + at) = to_bf16(a) | (uint32_t)to_bf16(b) << 16;
     else *reinterpret_cast<uint32_t *>(static_cast<h16_t *>(out.y) + at) = to_f16(a) | (uint32_t)to_f16(b) << 16;
 }
+// the power of two that a row whose largest magnitude is mx is scaled with: to [2^14, 2^15); a row of zeros or with an infinity as it is
+__device__ __forceinline__ int row_power(float mx) {
+    int e = 15;
+    if (mx > 0.f && mx < INFINITY) (void)frexpf(mx, &e);
+    return 15 - e;
+}
 // The result of a row: sums that are not finite (the row holds an infinity or a NaN) become NaN, and the power of two that the row was scaled with
 // is taken off.
-__device__ __forceinline__ void settle(const Q4Out &out, int t, floatx4 &v) {
-    const int e = out.exps == nullptr ? 0 : out.exps[t];
+__device__ __forceinline__ void settle(int e, floatx4 &v) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) v[r] = __builtin_isfinite(v[r]) ? ldexpf(v[r], -e) : NAN;
 }
@@ -184,13 +202,29 @@ __device__ __forceinline__ void best_of_lanes(float &bv, int &bi) {
 // Bound by HBM on wide matrices, on small ones by the launch and one round trip (bf16, one row: 8192 x 10240 13.4 us, 3.2 TB/s; the arg-max form, 8192 x
 // 32000, two columns 28.4, 4.7 TB/s; 4096 x 4096 5.9).
 // FL: 32-feature steps of a scale's group inside a 128-feature block (4: groups of 128 and more).
-template <int ST, int UT, int FL, int W, int R, bool XLDS>
+// OP_BF16: the operand is bf16 as it is.  Its sums, which have not seen their scale yet, may leave fp32's range (from values of 1.8e35 on): columns whose
+// result is not finite are done once more, with the operand 2^-64 of itself.  OP_SCALED (with XLDS): the operand is bf16 and becomes fp16 on its way to LDS.
+// The first costs 48 operations for every weight tile's block, the second a round trip and two barriers a launch, a launch in front of this one 2.7 us
+// (us, one row: 2048 x 1024 4.3 / 4.6 / 7.0, 4096 x 4096 6.8 / 6.2 / 8.2, 8192 x 10240 17.2 / 13.9 / 16.4; four rows of 4096 x 4096 6.9 / 8.5 / 9.0).
+enum { OP_F16, OP_BF16, OP_SCALED };
+constexpr int kScaled = 32 * 1024;                              // bytes of an operand that is scaled so: 8 pieces for each of 256 threads
+__device__ __forceinline__ uint32_t max_of_16_lanes(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xf, 0xf, false));       // the lanes turned by 1, 2, 4 and 8
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xf, 0xf, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xf, 0xf, false));
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, false));
+}
+template <int ST, int UT, int FL, int W, int R, bool XLDS, int OP>
 __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) void q4_few_kernel(Q4View m, const h16_t *__restrict__ x, int64_t ldx, int parts, int rows, Q4Out out) {
     constexpr int NF = 4 / FL;
     const int t0 = blockIdx.y * (16 / parts), T = min(16 / parts, rows - t0), C = parts * T;
     auto operand = [&](int c) { return x + (size_t)(c / T * rows + t0 + c % T) * ldx; };
     static_assert(R % 2 == 0, "the operand's two slots alternate");
+    constexpr bool BF = OP == OP_BF16;
+    static_assert(OP != OP_SCALED || (XLDS && 8 * 64 * W * 16 >= kScaled), "rows are scaled on their way to LDS, all at once");
     __shared__ floatx4 red[W][UT][64];
+    __shared__ uint32_t s_most[16];                             // OP_SCALED: bits of a column's largest magnitude, and its power of two
+    __shared__ int s_power[16];
     extern __shared__ __align__(16) u32x4 xs[];                 // XLDS: [k / 8][column]
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     const int tile0 = blockIdx.x * UT;
@@ -220,14 +254,57 @@ __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) v
 #pragma unroll
         for (int s = 0; s < 4; ++s) xr[i][s] = *reinterpret_cast<const u32x4 *>(xp + kq * 128 + s * 32);
     };
+    // OP_SCALED: a thread's pieces of the operand, every 64 W-th, so that 16 lanes have neighbours of one column; requested in front of the weights
+    u32x4 raw[OP == OP_SCALED ? 8 : 1];
+    int raw_col[OP == OP_SCALED ? 8 : 1], raw_piece[OP == OP_SCALED ? 8 : 1], mine_of_operand = 0;
+    if constexpr (OP == OP_SCALED) {
+        const int pieces = m.k_blocks * 16, step_c = 64 * W / pieces, step_p = 64 * W % pieces;
+        mine_of_operand = (C * pieces + 64 * W - 1) / (64 * W);
+        int c = threadIdx.x / pieces, p = threadIdx.x - c * pieces;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (i >= mine_of_operand) break;
+            raw_col[i] = c;                                     // C and more: past the end
+            raw_piece[i] = p;
+            raw[i] = *reinterpret_cast<const u32x4 *>(operand(min(c, C - 1)) + 8 * p);
+            c += step_c;
+            p += step_p;
+            if (p >= pieces) { p -= pieces; ++c; }
+        }
+    }
     // ring slot i holds block wave + i W of the round
     const int last = m.k_blocks - 1, mine = (last - wave + W) / W, full = mine / R;
 #pragma unroll
     for (int i = 0; i < R; ++i) request(i, min(wave + i * W, last));
     if constexpr (XLDS) {
         const int pieces = m.k_blocks * 16;
-        for (int c = 0; c < C; ++c)
-            for (int p = threadIdx.x; p < pieces; p += 64 * W) xs[p * C + c] = *reinterpret_cast<const u32x4 *>(operand(c) + 8 * p);
+        if constexpr (OP == OP_SCALED) {
+            if (threadIdx.x < 16) s_most[threadIdx.x] = 0;
+            HX_LDS_BARRIER();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (i >= mine_of_operand) break;
+                uint32_t most = 0;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) most = max(most, max(raw[i][x] & 0x7fffu, (raw[i][x] >> 16) & 0x7fffu));
+                most = max_of_16_lanes(most);
+                if ((lane & 15) == 0 && raw_col[i] < C) atomicMax(&s_most[raw_col[i]], most);
+            }
+            HX_LDS_BARRIER();
+            if ((int)threadIdx.x < C) s_power[threadIdx.x] = row_power(bf16_f32(s_most[threadIdx.x]));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (i >= mine_of_operand || raw_col[i] >= C) break;
+                const int e = row_power(bf16_f32(s_most[raw_col[i]]));
+                u32x4 h;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) h[x] = to_f16(ldexpf(bf16_f32(raw[i][x] & 0xffffu), e)) | (uint32_t)to_f16(ldexpf(bf16_f32(raw[i][x] >> 16), e)) << 16;
+                xs[raw_piece[i] * C + raw_col[i]] = h;
+            }
+        } else {
+            for (int c = 0; c < C; ++c)
+                for (int p = threadIdx.x; p < pieces; p += 64 * W) xs[p * C + c] = *reinterpret_cast<const u32x4 *>(operand(c) + 8 * p);
+        }
         HX_LDS_BARRIER();
     } else {
         fetch(0, min(wave, last));
@@ -235,7 +312,7 @@ __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) v
     }
     const u32x4 *xl = xs + g * C + min(j, C - 1);
     auto contract = [&](int i, int kq) {
-        contract_block<ST, 1, UT, FL>(widen, wr[i], sr[i], zr[i], [&](int s, int) { return XLDS ? xl[(kq * 4 + s) * 4 * C] : xr[XLDS ? 0 : i & 1][s]; }, acc);
+        contract_block<ST, 1, UT, FL, BF>(widen, wr[i], sr[i], zr[i], [&](int s, int) { return XLDS ? xl[(kq * 4 + s) * 4 * C] : xr[XLDS ? 0 : i & 1][s]; }, acc);
     };
     int kq = wave;
     for (int rd = 0; rd < full; ++rd) {
@@ -254,6 +331,36 @@ __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) v
             if constexpr (!XLDS) fetch(i & 1, min(kq + (i + 2) * W, last));
         }
     }
+    if constexpr (BF) {
+        bool odd = false;
+#pragma unroll
+        for (int u = 0; u < UT; ++u)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) odd = odd || !__builtin_isfinite(acc[u][0][r]);
+        unsigned long long any = __builtin_amdgcn_ballot_w64(odd);
+        if (any != 0) {
+            any |= any >> 32;
+            const bool mine_odd = ((any | any >> 16) >> j) & 1;        // this lane's column
+            floatx4 again[UT][1];
+#pragma unroll
+            for (int u = 0; u < UT; ++u) again[u][0] = floatx4{0.f, 0.f, 0.f, 0.f};
+            for (int k = wave; k <= last; k += W) {
+                request(0, k);
+                u32x4 xs64[4];
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const u32x4 v = XLDS ? xl[(k * 4 + s) * 4 * C] : *reinterpret_cast<const u32x4 *>(xp + k * 128 + s * 32);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        xs64[s][i] = to_bf16(bf16_f32(v[i] & 0xffffu) * 0x1p-64f) | (uint32_t)to_bf16(bf16_f32(v[i] >> 16) * 0x1p-64f) << 16;
+                }
+                contract_block<ST, 1, UT, FL, BF>(widen, wr[0], sr[0], zr[0], [&](int s, int) { return xs64[s]; }, again);
+            }
+#pragma unroll
+            for (int u = 0; u < UT; ++u)
+                if (mine_odd) acc[u][0] = again[u][0] * 0x1p64f;
+        }
+    }
 #pragma unroll
     for (int u = 0; u < UT; ++u) red[wave][u][lane] = acc[u][0];
     __syncthreads();
@@ -269,7 +376,7 @@ __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) v
         v += a;
     }
     const int n0 = (tile0 + u) * 16 + 4 * gg;
-    settle(out, t0 + t, v);
+    settle(OP == OP_SCALED ? s_power[t] : out.exps == nullptr ? 0 : out.exps[t0 + t], v);
     if (out.best_val == nullptr) {
         store_columns(m, out, t0 + t, n0, v);
         return;
@@ -365,7 +472,7 @@ __global__ __launch_bounds__(1024, 4) void q4_shared_kernel(Q4View m, const h16_
                 zc[u][f] = cur.z[f * 256 + tile * 16 + j];
             }
         }
-        contract_block<ST, NB, UT, FL>(widen, w, sc, zc, [&](int i, int b) { return cur.x[i * NB + b][lane]; }, acc);
+        contract_block<ST, NB, UT, FL, false>(widen, w, sc, zc, [&](int i, int b) { return cur.x[i * NB + b][lane]; }, acc);
     }
     HX_WAIT_VM(0);                                              // nothing is on its way into the stages any more
     HX_LDS_BARRIER();
@@ -399,7 +506,7 @@ __global__ __launch_bounds__(1024, 4) void q4_shared_kernel(Q4View m, const h16_
     for (int t = nth; t < T; t += 2 * waves) {
         floatx4 v = *reinterpret_cast<const floatx4 *>(ys + t * YS + 4 * lane);
         for (int c = t + T; c < C; c += T) v += *reinterpret_cast<const floatx4 *>(ys + c * YS + 4 * lane);
-        settle(out, t, v);
+        settle(out.exps == nullptr ? 0 : out.exps[t], v);
         if (out.best_val == nullptr) {
             if (there) store_columns(m, out, t, n0, v);
             continue;
@@ -428,7 +535,7 @@ __global__ __launch_bounds__(256) void q4_finish_kernel(Q4View m, const float *_
             v += a;
         }
     }
-    settle(out, t, v);
+    settle(out.exps == nullptr ? 0 : out.exps[t], v);
     if (out.best_val == nullptr) {
         if (n0 < np) store_columns(m, out, t, n0, v);
         return;
@@ -525,11 +632,7 @@ __global__ __launch_bounds__(1024) void q4_parts_kernel(const void *__restrict__
 #pragma unroll
     for (int w = 0; w < 16; ++w) { ss += red[w]; mx = fmaxf(mx, red2[w]); }
     const float r = g != nullptr ? 1.0f / sqrtf(ss / (float)K + eps) : 1.0f;
-    int e = 0;
-    if (mx * r > 0.f && mx * r < INFINITY) {
-        (void)frexpf(mx * r, &e);
-        e = 15 - e;                                              // the largest value to [2^14, 2^15)
-    }
+    const int e = row_power(mx * r);
     if (threadIdx.x == 0) exps[t] = e;
     auto put = [&](int k, const Eight &v) {
         uint32_t hi[4], lo[4];
@@ -601,14 +704,17 @@ __global__ __launch_bounds__(256) void q4_pack_scales_kernel(const void *__restr
 // Groups of 32 have four times the scales, for which two tiles leave no registers: one tile a block while that makes 256 blocks, or little work, and with
 // n >= 512 up to 8 columns of a matrix below n = 1024 (k = 64, n = 1792, one column: one tile 44.9, two 49.6, shared 42.0; k = 16, n = 640, four: 9.6 /
 // 11.0 / 10.8; k = 64, n = 256, 24 columns: 23.0 / 19.8 / 15.8; k = 4, n = 256, 48: 6.6 / 8.9 / 10.0)
+// bf16 operands, below n = 512: with one or two columns through LDS, where they are scaled, from n = 256 on, else as they are (k = 32, n = 480: one column
+// 7.6 / 8.7, two 8.4 / 8.9, four 10.3 / 9.0; n = 256: one 6.2 / 6.8, two 6.9 / 6.8; k = 64, n = 80: one 8.3 / 8.2, two 9.6 / 8.5).
 enum { FEW_LDS_WIDE, FEW_LDS, FEW_LDS_NARROW, FEW_WIDE, FEW, SHARED };
-int form_of(const Q4View &m, int C) {
+int form_of(const Q4View &m, int C, bool bf16) {
     const int n = m.n_tiles, k = m.k_blocks, blocks = n * ((C + 15) / 16), operand = C > 16 ? INT32_MAX : C * k * 256;
     const bool one = m.group == 32;
     if (n >= 512) {
-        if (operand > 32 * 1024 || C > (n < 1024 ? 8 : one ? 0 : 4)) return SHARED;
+        if (operand > kScaled || C > (n < 1024 ? 8 : one ? 0 : 4)) return SHARED;
         return n < 1024 && (one || C <= 2) ? FEW_LDS : FEW_LDS_WIDE;
     }
+    if (bf16 && n >= 256 && C <= 2 && operand <= kScaled) return FEW_LDS;
     if (k >= 64 && operand <= 64 * 1024) return FEW_LDS_NARROW;
     if (k > 64) return SHARED;
     if (one) return blocks <= 256 || (long)blocks * k <= 8192 ? FEW : SHARED;
@@ -637,42 +743,51 @@ SharedShape shared_shape(const Q4View &m, int C) {
 int shared_blocks(const Q4View &m, const SharedShape &sh) { return (m.n_tiles + 2 * sh.waves - 1) / (2 * sh.waves); }
 
 template <int ST, int FL>
-void launch_few(const Q4View &m, int form, const h16_t *x, int64_t ldx, int C, int T, const Q4Out &out, hipStream_t s) {
+void launch_few(const Q4View &m, int form, const Q4In &in, int C, int T, const Q4Out &out, hipStream_t s) {
     const int parts = C / T, rows = 16 / parts;
     const dim3 grid((m.n_tiles + few_tiles(form) - 1) / few_tiles(form), (T + rows - 1) / rows);
     const size_t lds = (size_t)std::min(C, 16) * m.k_blocks * 256;
-#define HX_FEW(UT, W, R, XLDS) hipLaunchKernelGGL((q4_few_kernel<ST, UT, FL, W, R, XLDS>), grid, dim3(64 * W), XLDS ? lds : 0, s, m, x, ldx, parts, T, out)
+#define HX_FEW(UT, W, R, XLDS, BF16_AS)                                                                                                                       \
+    do {                                                                                                                                                      \
+        if constexpr (ST == HX_T_BF16) {                                                                                                                      \
+            if (in.bf16) {                                                                                                                                    \
+                hipLaunchKernelGGL((q4_few_kernel<ST, UT, FL, W, R, XLDS, BF16_AS>), grid, dim3(64 * W), XLDS ? lds : 0, s, m, in.x, in.ldx, parts, T, out);  \
+                break;                                                                                                                                        \
+            }                                                                                                                                                 \
+        }                                                                                                                                                     \
+        hipLaunchKernelGGL((q4_few_kernel<ST, UT, FL, W, R, XLDS, OP_F16>), grid, dim3(64 * W), XLDS ? lds : 0, s, m, in.x, in.ldx, parts, T, out);           \
+    } while (0)
     if constexpr (FL > 1) {
-        if (form == FEW_LDS_WIDE) HX_FEW(2, 4, 2, true);
-        else if (form == FEW_WIDE) HX_FEW(2, 8, 2, false);
+        if (form == FEW_LDS_WIDE) HX_FEW(2, 4, 2, true, OP_SCALED);
+        else if (form == FEW_WIDE) HX_FEW(2, 8, 2, false, OP_BF16);
     }
-    if (form == FEW_LDS) HX_FEW(1, 4, (FL == 1 ? 2 : 4), true);
-    else if (form == FEW_LDS_NARROW) HX_FEW(1, 8, (FL == 1 ? 2 : 4), true);
-    else if (form == FEW) HX_FEW(1, 4, (FL == 1 ? 2 : 4), false);
+    if (form == FEW_LDS) HX_FEW(1, 4, (FL == 1 ? 2 : 4), true, OP_SCALED);
+    else if (form == FEW_LDS_NARROW) HX_FEW(1, 8, (FL == 1 ? 2 : 4), true, OP_BF16);
+    else if (form == FEW) HX_FEW(1, 4, (FL == 1 ? 2 : 4), false, OP_BF16);
 #undef HX_FEW
 }
 template <int ST, int NB, int FL>
-void launch_shared(const Q4View &m, const h16_t *x, int64_t ldx, int C, int T, const Q4Out &out, float *part, hipStream_t s) {
+void launch_shared(const Q4View &m, const Q4In &in, int C, int T, const Q4Out &out, float *part, hipStream_t s) {
     const SharedShape sh = shared_shape(m, C);
     const int per = (m.k_blocks + sh.splits - 1) / sh.splits;
     const dim3 grid(shared_blocks(m, sh), sh.splits);
-    hipLaunchKernelGGL((q4_shared_kernel<ST, NB, FL>), grid, dim3(128 * sh.waves), 0, s, m, x, (uint32_t)ldx, C, T, out, per, sh.splits == 1 ? nullptr : part);
+    hipLaunchKernelGGL((q4_shared_kernel<ST, NB, FL>), grid, dim3(128 * sh.waves), 0, s, m, in.x, (uint32_t)in.ldx, C, T, out, per, sh.splits == 1 ? nullptr : part);
     if (sh.splits > 1) hipLaunchKernelGGL(q4_finish_kernel, dim3((m.n_tiles * 16 + 1023) / 1024, T), dim3(256), 0, s, m, part, sh.splits, C, T, out);
 }
 template <int ST, int FL>
-void launch_cols(const Q4View &m, const h16_t *x, int64_t ldx, int C, int T, const Q4Out &out, float *part, hipStream_t s) {
-    const int form = form_of(m, C);
-    if (form != SHARED) launch_few<ST, FL>(m, form, x, ldx, C, T, out, s);
-    else if (C <= 16) launch_shared<ST, 1, FL>(m, x, ldx, C, T, out, part, s);
-    else if (C <= 32) launch_shared<ST, 2, FL>(m, x, ldx, C, T, out, part, s);
-    else if (C <= 48) launch_shared<ST, 3, FL>(m, x, ldx, C, T, out, part, s);
-    else launch_shared<ST, 4, FL>(m, x, ldx, C, T, out, part, s);
+void launch_cols(const Q4View &m, const Q4In &in, int C, int T, const Q4Out &out, float *part, hipStream_t s) {
+    const int form = form_of(m, C, in.bf16);
+    if (form != SHARED) launch_few<ST, FL>(m, form, in, C, T, out, s);
+    else if (C <= 16) launch_shared<ST, 1, FL>(m, in, C, T, out, part, s);
+    else if (C <= 32) launch_shared<ST, 2, FL>(m, in, C, T, out, part, s);
+    else if (C <= 48) launch_shared<ST, 3, FL>(m, in, C, T, out, part, s);
+    else launch_shared<ST, 4, FL>(m, in, C, T, out, part, s);
 }
 template <int ST>
-void launch_type(const Q4View &m, const h16_t *x, int64_t ldx, int C, int T, const Q4Out &out, float *part, hipStream_t s) {
-    if (m.group >= 128) launch_cols<ST, 4>(m, x, ldx, C, T, out, part, s);
-    else if (m.group == 64) launch_cols<ST, 2>(m, x, ldx, C, T, out, part, s);
-    else launch_cols<ST, 1>(m, x, ldx, C, T, out, part, s);
+void launch_type(const Q4View &m, const Q4In &in, int C, int T, const Q4Out &out, float *part, hipStream_t s) {
+    if (m.group >= 128) launch_cols<ST, 4>(m, in, C, T, out, part, s);
+    else if (m.group == 64) launch_cols<ST, 2>(m, in, C, T, out, part, s);
+    else launch_cols<ST, 1>(m, in, C, T, out, part, s);
 }
 
 }  // namespace
@@ -680,20 +795,21 @@ void launch_type(const Q4View &m, const h16_t *x, int64_t ldx, int C, int T, con
 size_t q4_part_floats(const Q4View &m) {
     size_t most = 0;
     for (int c = 1; c <= kQ4Rows; ++c)
-        if (form_of(m, c) == SHARED && shared_shape(m, c).splits > 1) most = std::max(most, (size_t)shared_shape(m, c).splits * c * m.n_tiles * 16);
+        if (form_of(m, c, false) == SHARED && shared_shape(m, c).splits > 1) most = std::max(most, (size_t)shared_shape(m, c).splits * c * m.n_tiles * 16);
     return most;
 }
 int q4_best_units(const Q4View &m, int T) {
-    const int form = form_of(m, 2 * T);
+    const int form = form_of(m, 2 * T, false);
     if (form != SHARED) return (m.n_tiles + few_tiles(form) - 1) / few_tiles(form);
     const SharedShape sh = shared_shape(m, 2 * T);
     return sh.splits > 1 ? (m.n_tiles * 16 + 1023) / 1024 : shared_blocks(m, sh);
 }
-void launch_q4(const Q4View &m, const h16_t *x, int64_t ldx, int T, const Q4Out &out, float *part, hipStream_t s) {
+bool q4_takes_bf16(const Q4View &m, int T) { return form_of(m, T, true) != SHARED; }
+void launch_q4(const Q4View &m, const Q4In &in, int T, const Q4Out &out, float *part, hipStream_t s) {
     const int C = out.parts * T;
-    if (m.type == HX_T_F32) launch_type<HX_T_F32>(m, x, ldx, C, T, out, part, s);
-    else if (m.type == HX_T_F16) launch_type<HX_T_F16>(m, x, ldx, C, T, out, part, s);
-    else launch_type<HX_T_BF16>(m, x, ldx, C, T, out, part, s);
+    if (m.type == HX_T_F32) launch_type<HX_T_F32>(m, in, C, T, out, part, s);
+    else if (m.type == HX_T_F16) launch_type<HX_T_F16>(m, in, C, T, out, part, s);
+    else launch_type<HX_T_BF16>(m, in, C, T, out, part, s);
 }
 void launch_q4_parts(int type, const void *x, const void *x2, int64_t ldx, const float *g, float eps, int K, int Kp, int T, int parts, h16_t *out, int32_t *exps,
                      hipStream_t s) {

@@ -105,22 +105,19 @@ hexgen_status_t hexgen_q4_project(hexgen_q4_t *q, const void *x, int64_t ldx, in
     const Q4Store &st = q->store;
     if (st.v.w == nullptr) return HEXGEN_ERR_STATE;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const int parts = q->dtype == HEXGEN_F32 ? 2 : 1;
-    const bool scaled = q->dtype != HEXGEN_F16;
-    // fp16 rows of whole 128-feature blocks in 16-byte pieces are the operand as they are
-    const bool direct = !scaled && reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx % 8 == 0 && ldx <= (1 << 24) && q->n_in % 128 == 0;
-    const int chunk = parts == 2 ? kQ4PartRows : kQ4Rows;
+    const int parts = q->dtype == HEXGEN_F32 ? 2 : 1, chunk = parts == 2 ? kQ4PartRows : kQ4Rows;
+    // 16-bit rows of whole 128-feature blocks in 16-byte pieces are an operand as they are
+    const bool pieces = parts == 1 && reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx % 8 == 0 && ldx <= (1 << 24) && q->n_in % 128 == 0;
     for (int r0 = 0; r0 < n_rows; r0 += chunk) {
         const int n = std::min(chunk, n_rows - r0);
         const unsigned char *xr = static_cast<const unsigned char *>(x) + (size_t)r0 * ldx * es;
+        const bool bf16 = q->dtype == HEXGEN_BF16 && q4_takes_bf16(st.v, n), scaled = q->dtype != HEXGEN_F16 && !bf16;
         const Q4Out o{static_cast<unsigned char *>(out) + (size_t)r0 * q->n_out * es, (int)q->dtype, nullptr, nullptr, scaled ? st.exps : nullptr, parts};
-        if (direct) {
-            launch_q4(st.v, reinterpret_cast<const h16_t *>(xr), ldx, n, o, st.part, s);
-            continue;
-        }
+        Q4In in{st.planes, st.padded(), bf16};
         if (scaled) launch_q4_parts((int)q->dtype, xr, nullptr, ldx, nullptr, 0.f, q->n_in, st.padded(), n, parts, st.planes, st.exps, s);
+        else if (pieces) in = Q4In{reinterpret_cast<const h16_t *>(xr), ldx, bf16};
         else launch_q4_copy(reinterpret_cast<const h16_t *>(xr), ldx, q->n_in, st.padded(), n, st.planes, s);
-        launch_q4(st.v, st.planes, st.padded(), n, o, st.part, s);
+        launch_q4(st.v, in, n, o, st.part, s);
     }
     HX_HIP(hipGetLastError());
     return HEXGEN_OK;

@@ -1820,7 +1820,7 @@ hexgen_status_t hexgen_head_greedy(hexgen_head_t *hd, const void *hidden_a, cons
         if (q4) {
             // normalised rows in full precision, as two-part operand; the arg-max over the blocks' best columns
             launch_q4_parts((int)hd->dtype, a, b, H, hd->g, hd->eps, H, hd->q4.padded(), n, 2, hd->q4.planes, hd->q4.exps, s);
-            launch_q4(hd->q4.v, hd->q4.planes, hd->q4.padded(), n, Q4Out{nullptr, 0, hd->q4_val, hd->q4_id, hd->q4.exps, 2}, hd->q4.part, s);
+            launch_q4(hd->q4.v, Q4In{hd->q4.planes, hd->q4.padded(), false}, n, Q4Out{nullptr, 0, hd->q4_val, hd->q4_id, hd->q4.exps, 2}, hd->q4.part, s);
             launch_row_best(hd->q4_val, hd->q4_id, q4_best_units(hd->q4.v, n), n, hd->r * hd->Vl, token_out + r0, logit_out ? logit_out + r0 : nullptr, s);
         } else if (is_h16(hd->dtype)) {
             // same kernels as a decode projection: prologue (x = a + b, x * g as hi/lo operand, sums of squares),
