@@ -221,6 +221,7 @@ hexgen_status_t hexgen_tree_accept(const hexgen_tree_t *tr, const int32_t *draft
  * hexgen_kv_tree_attention can be recorded once a call of that size has run outside a graph.  A recording is for trees of
  * the recorded counts; a replay reads the lengths and the parents that hold then from the device, and leaves out what would
  * pass max_seq.  Calls on one stage, replays among them, may not overlap in time (they share its workspace).
+ * A call with more rows or sequences than any before it replaces that workspace: what was recorded earlier has to be recorded again.
  */
 hexgen_status_t hexgen_stage_decode_tree(hexgen_stage_t *st, hexgen_kv_cache_t *kv, const hexgen_tree_t *tr, const void *hidden_in,
                                          void *out_partial, void *out_resid, void *stream);

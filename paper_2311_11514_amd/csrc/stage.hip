@@ -189,6 +189,7 @@ hexgen_status_t ensure_workspace(hexgen_stage *st, int rows, int batch) {
     HX_HIP(hipDeviceSynchronize());
     rows = std::max(rows, w.cap_rows);
     batch = std::max(batch, st->ws_batch_cap);
+    const bool trees = w.tree_qkv != nullptr;        // a stage that has taken trees can be recorded doing so, whatever ran in between
     free_ws(w);
     st->ws_batch_cap = 0;
     const size_t T = (size_t)rows, T16 = (size_t)round_up(rows, 16);
@@ -221,6 +222,7 @@ hexgen_status_t ensure_workspace(hexgen_stage *st, int rows, int batch) {
         HX_HIP(hipMemset(w.n, 0, T16 * st->H * sizeof(h16_t)));
         HX_HIP(hipMemset(w.o, 0, T16 * st->qw * sizeof(h16_t)));
         HX_HIP(hipMemset(w.u, 0, T16 * st->F_l * sizeof(h16_t)));
+        if (trees) HX_TRY(dmalloc(&w.tree_qkv, T * st->nqkv));
     } else {
         HX_TRY(dmalloc(&w.qkv32, T * st->nqkv));
         HX_TRY(dmalloc(&w.q32, T * st->qw));
