@@ -217,10 +217,12 @@ hexgen_status_t hexgen_tree_accept(const hexgen_tree_t *tr, const int32_t *draft
  * drops the whole tree) move to the slots behind the context, in every layer, and the committed lengths grow by kept[i].  The
  * arrays may be changed when it returns; it enqueues on `stream` and cannot be recorded into a graph (HEXGEN_ERR_DEVICE).
  * All three: HEXGEN_ERR_STATE unless the cache holds a batch (prefill, set_lengths, commit) and the trees are set for just as many
- * sequences; HEXGEN_ERR_CAPACITY when a context and its tree exceed max_seq.  hexgen_stage_decode_tree and
- * hexgen_kv_tree_attention can be recorded once a call of that size has run outside a graph.  A recording is for trees of
- * the recorded counts; a replay reads the lengths and the parents that hold then from the device, and leaves out what would
- * pass max_seq.  Calls on one stage, replays among them, may not overlap in time (they share its workspace).
+ * sequences; HEXGEN_ERR_CAPACITY when a context and its tree exceed max_seq.
+ * hexgen_stage_decode_tree and hexgen_kv_tree_attention: HEXGEN_ERR_CAPACITY also for more than a launch takes (sequences x kv heads x
+ * ceil(nodes of the largest tree x heads per kv head / 32) from 2^23 on; fp32: / 16, from 2^24 on).  They can be recorded once a call of that
+ * size has run outside a graph.  A recording is for trees of the recorded counts; a replay reads the lengths and the parents that hold
+ * then from the device, and leaves out what would pass max_seq.  Calls on one stage, replays among them, may not overlap in time (they share
+ * its workspace).
  * A call with more rows or sequences than any before it replaces that workspace: what was recorded earlier has to be recorded again.
  */
 hexgen_status_t hexgen_stage_decode_tree(hexgen_stage_t *st, hexgen_kv_cache_t *kv, const hexgen_tree_t *tr, const void *hidden_in,

@@ -22,8 +22,8 @@ __global__ __launch_bounds__(256) void tree_rope_append_kernel(const float *__re
                                                                const int32_t *__restrict__ lens, const float *__restrict__ cos_tab,
                                                                const float *__restrict__ sin_tab, h16_t *__restrict__ q, h16_t *__restrict__ q_lo,
                                                                h16_t *__restrict__ kc, h16_t *__restrict__ vc) {
-    const int d = kg.d, half = d >> 1, tph = d >> 4, heads = hq_l + 2 * kg.hkv_l, per_row = heads * tph * 2;
-    const int idx = blockIdx.x * 256 + threadIdx.x;
+    const int d = kg.d, half = d >> 1, tph = d >> 4, heads = hq_l + 2 * kg.hkv_l;
+    const unsigned idx = blockIdx.x * 256u + threadIdx.x, per_row = heads * tph * 2;
     if (idx >= tv.rows * per_row) return;
     const int t = idx / per_row, rem = idx - t * per_row, head = rem / (2 * tph), tl = (rem >> 1) % tph, i0 = 8 * tl + 4 * (rem & 1);
     const TreeRow row = tv.row[t];
@@ -68,7 +68,7 @@ __global__ __launch_bounds__(256) void tree_rope_append_kernel(const float *__re
 }
 void launch_tree_rope_append(const float *qkv, int hq_l, KvGeom kg, const TreeView &tv, const int32_t *lens, const float *cos_tab,
                              const float *sin_tab, h16_t *q, h16_t *q_lo, h16_t *kc, h16_t *vc, hipStream_t s) {
-    const int n = tv.rows * (hq_l + 2 * kg.hkv_l) * (kg.d >> 4) * 2;
+    const unsigned n = (unsigned)tv.rows * (hq_l + 2 * kg.hkv_l) * (kg.d >> 4) * 2;
     hipLaunchKernelGGL(tree_rope_append_kernel, dim3((n + 255) / 256), dim3(256), 0, s, qkv, hq_l, kg, tv, lens, cos_tab, sin_tab, q, q_lo, kc, vc);
 }
 

@@ -12,9 +12,10 @@ __global__ __launch_bounds__(256) void f32_tree_rope_append_kernel(const float *
                                                                    const int32_t *__restrict__ lens, const float *__restrict__ cos_tab,
                                                                    const float *__restrict__ sin_tab, float *__restrict__ q,
                                                                    float *__restrict__ kc, float *__restrict__ vc) {
-    const int d = kg.d, half = d >> 1, heads = hq_l + 2 * kg.hkv_l, idx = blockIdx.x * 256 + threadIdx.x;
-    if (idx >= tv.rows * heads * half) return;
-    const int t = idx / (heads * half), rem = idx - t * heads * half, head = rem / half, i = rem - head * half;
+    const int d = kg.d, half = d >> 1, heads = hq_l + 2 * kg.hkv_l;
+    const unsigned idx = blockIdx.x * 256u + threadIdx.x, per_row = heads * half;
+    if (idx >= tv.rows * per_row) return;
+    const int t = idx / per_row, rem = idx - t * per_row, head = rem / half, i = rem - head * half;
     const TreeRow row = tv.row[t];
     const int len = lens[row.seq], slot = len + row.index;
     if (slot >= kg.smax) return;
@@ -327,7 +328,7 @@ void launch_tree_advance(int32_t *lens, const int32_t *kept, int batch, hipStrea
 }
 void f32_launch_tree_rope_append(const float *qkv, int hq_l, KvGeom kg, const TreeView &tv, const int32_t *lens, const float *cos_tab,
                                  const float *sin_tab, float *q, float *kc, float *vc, hipStream_t s) {
-    const int n = tv.rows * (hq_l + 2 * kg.hkv_l) * (kg.d / 2);
+    const unsigned n = (unsigned)tv.rows * (hq_l + 2 * kg.hkv_l) * (kg.d / 2);
     hipLaunchKernelGGL(f32_tree_rope_append_kernel, dim3((n + 255) / 256), dim3(256), 0, s, qkv, hq_l, kg, tv, lens, cos_tab, sin_tab, q, kc, vc);
 }
 void f32_launch_tree_attn(const float *q, int64_t ldq, const TreeIn &in, float *kc, float *vc, KvGeom kg, int hq_l, const TreeView &tv, const int32_t *lens,

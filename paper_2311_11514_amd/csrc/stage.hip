@@ -401,9 +401,11 @@ TreePlan pick_tree_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, const
     }
     tp.chunk = longest;
     tp.nsplit = 1;
+    // (runs only where blocks that have no rows, which sequences with smaller trees than the largest have, do not multiply with them without end)
+    const bool few_units = (long)tr->batch * st->hkv_l * tree_row_blocks(tr->max_n, G, rows) <= kTreeUnits;
     if (tp.row_groups > 1) {
-        if (w.blocks < 256) tp.chunk = (int)std::max(8L, (w.tiles + 511) / 512);
-    } else if (w.blocks < 128 && (long)tr->batch * st->hkv_l * tree_row_blocks(tr->max_n, G, rows) <= kTreeUnits) {
+        if (w.blocks < 256 && few_units) tp.chunk = (int)std::max(8L, (w.tiles + 511) / 512);
+    } else if (w.blocks < 128 && few_units) {
         const long fit = (w.tiles + kTreeBlocks - 1) / kTreeBlocks;
         if (!h16) tp.chunk = (int)std::max(4L, fit);
         else if (longest > 48) tp.chunk = (int)((std::max({16L, fit, (long)(2 * std::sqrt((double)longest))}) + 7) / 8 * 8);
@@ -810,7 +812,7 @@ void free_layer(Layer &l) {
 
 
 // ---- drafted trees: storage and checks ----------------------------------------------------------------------------
-constexpr int kTreeMaxBatch = 1 << 15, kTreeMaxRows = 1 << 16;      // what the grids and 32-bit indexes of the tree kernels take
+constexpr int kTreeMaxBatch = 1 << 15, kTreeMaxRows = 1 << 16;      // what a grid's second dimension and 32-bit indexes of rows take
 static_assert(kTreeMaxNodes == HEXGEN_TREE_MAX_NODES, "one limit");
 
 hexgen_status_t tree_storage(hexgen_tree *tr) {
@@ -842,6 +844,15 @@ hexgen_status_t ensure_tree_part(hexgen_stage *st, hipStream_t s) {
     HX_HIP(e);
     st->tree_part = p;
     return HEXGEN_OK;
+}
+// Launches have less than 2^32 threads.  The attention's grid has blocks for every sequence as for the largest tree, 32 rows and 512 threads each (fp32: 16
+// and 256; other forms have less), the rotation a thread for four rotary pairs of a row (fp32: one), the joining of runs d / 4 for a head of one.
+hexgen_status_t check_tree_launches(const hexgen_stage *st, const hexgen_tree *tr) {
+    const bool h16 = is_h16(st->dtype);
+    const uint64_t rows = tr->rows, most = UINT32_MAX - 4096;
+    const uint64_t blocks = (uint64_t)tree_row_blocks(tr->max_n, st->hq_l / st->hkv_l, h16 ? 32 : 16) * ((uint64_t)tr->batch * st->hkv_l + 7);
+    const uint64_t rotary = rows * (st->hq_l + 2 * st->hkv_l) * (st->d / (h16 ? 8 : 2)), joining = rows * st->hq_l * (st->d / 4);
+    return blocks * (h16 ? 512 : 256) > most || rotary > most || joining > most ? HEXGEN_ERR_CAPACITY : HEXGEN_OK;
 }
 hexgen_status_t check_tree(const hexgen_kv_cache *kv, const hexgen_tree *tr) {
     if (!kv->prefilled || tr->batch == 0 || tr->batch != kv->batch) return HEXGEN_ERR_STATE;
@@ -1452,6 +1463,7 @@ hexgen_status_t hexgen_kv_tree_attention(hexgen_kv_cache_t *kv, int layer, const
     const uintptr_t bits = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(out);
     if (bits % 16 || (ldq | ldk | ldv) % (16 / (int)esize(st->dtype)) || ldq < st->qw || ldk < kw || ldv < kw) return HEXGEN_ERR_INVALID_ARG;
     HX_TRY(check_tree(kv, tr));
+    HX_TRY(check_tree_launches(st, tr));
     hipStream_t s = static_cast<hipStream_t>(stream);
     HX_TRY(ensure_tree_part(st, s));
     const KvGeom kg = geom(st, kv);
@@ -1474,6 +1486,7 @@ hexgen_status_t hexgen_stage_decode_tree(hexgen_stage_t *st, hexgen_kv_cache_t *
     if (!st || !kv || !tr || !hidden_in || !out_partial || kv->st != st) return HEXGEN_ERR_INVALID_ARG;
     HX_TRY(check_loaded(st));
     HX_TRY(check_tree(kv, tr));
+    HX_TRY(check_tree_launches(st, tr));
     HX_TRY(check_rope(st, kv));
     hipStream_t s = static_cast<hipStream_t>(stream);
     Rows r;
