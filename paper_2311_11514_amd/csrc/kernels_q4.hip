@@ -833,7 +833,7 @@ void launch_q4_pack(const Q4View &m, const uint8_t *w4, const void *scales, cons
     const size_t words = (size_t)m.k_blocks * m.n_tiles * 256, cells = (size_t)m.scale_rows * m.n_tiles * 16;
     hipLaunchKernelGGL(q4_pack_kernel, dim3((unsigned)((words + 255) / 256)), dim3(256), 0, s, w4, ld / 2, K, n0, m.n_valid, m.n_tiles, m.k_blocks,
                        const_cast<uint32_t *>(static_cast<const uint32_t *>(m.w)));
-    hipLaunchKernelGGL(q4_pack_scales_kernel, dim3((unsigned)((cells + 255) / 256)), dim3(256), 0, s, scales, m.type == HX_T_F32 ? 4 : 2, zeros, ld, (K + group - 1) / group,
+    hipLaunchKernelGGL(q4_pack_scales_kernel, dim3((unsigned)((cells + 255) / 256)), dim3(256), 0, s, scales, m.type == HX_T_F32 ? 4 : 2, zeros, ld, (int)(((int64_t)K + group - 1) / group),
                        m.scale_rows, m.zeros_row != 0 ? m.scale_rows : 1, std::max(1, group / 128), n0, m.n_valid, m.n_tiles * 16, const_cast<void *>(m.scales),
                        const_cast<uint8_t *>(m.zeros));
 }

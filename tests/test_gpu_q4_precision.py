@@ -82,3 +82,19 @@ def test_the_largest_value_beside_the_smallest(dtype):
         x64 = x.double().numpy()
         y = x64 @ w
         assert (np.abs(m.project(x.cuda()).double().cpu().numpy() - y) <= exact_bound(y, x64, w, dtype, group)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("group", [512, 1 << 20, 2 ** 31 - 128])
+def test_groups_longer_than_the_matrix(dtype, group):
+    """One group for all features, up to the largest group there is."""
+    arrays, w, big = matrix(dtype, 384, 64, group, True, seed=24)
+    m = hx.Q4Matrix(384, 64, group, dtype)
+    m.load(*arrays)
+    head = hx.Head(384, 64, 1, 0, dtype)
+    head.load_q4(torch.ones(384), *arrays, group=group)
+    x, x64 = rows(dtype, 3, 384)
+    y = x64 @ w
+    assert (np.abs(m.project(x.cuda()).double().cpu().numpy() - y) <= exact_bound(y, x64, w, dtype, group)).all()
+    token, logit = head.greedy(x.cuda())
+    assert (logit > 0).all() and (y[np.arange(3), token.cpu().numpy()] >= 0.99 * y.max(1)).all()
