@@ -129,7 +129,10 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 def _i32(seq: Optional[Sequence[int]]):
     if seq is None:
         return None
-    return (C.c_int32 * len(seq))(*[int(v) for v in seq])
+    values = [int(v) for v in seq]
+    if values and not -1 << 31 <= min(values) <= max(values) < 1 << 31:      # ctypes would cut them off
+        raise ValueError(f"32-bit integers are wanted, got {min(values)} .. {max(values)}")
+    return (C.c_int32 * len(values))(*values)
 
 
 # the current stream's handle of a device without a Stream object around it (which takes longer to make than a launch), where torch has that
