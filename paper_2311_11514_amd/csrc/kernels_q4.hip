@@ -692,18 +692,20 @@ __global__ __launch_bounds__(256) void q4_pack_scales_kernel(const void *__restr
 }
 
 // ---- which form --------------------------------------------------------------------------------------------------
-// By tiles of 16 columns (n), 128-feature blocks (k) and operand columns (C).  us for group 128, bf16:
+// By tiles of 16 columns (n), 128-feature blocks (k) and operand columns (C).  us for group 128, fp16 where nothing else is said:
 //   n >= 512: the few form with the operand in LDS up to 4 columns, or 8 of a matrix below n = 1024, and 32 KB, else the shared form (k = 64, n = 1792:
-//   one column 27.8 / 33.6, four 34.5 / 30.1, eight - / 31.1; k = 16, n = 1792: four 11.2 / 12.8, eight 13.6 / 12.9; n = 640: eight 8.2 / 9.7).  One
-//   tile a block below n = 1024 with one or two columns (k = 64, n = 640: one tile 14.0, two 15.6)
-//   n < 512, k > 64: eight waves and the operand in LDS up to 64 KB of it, else the shared form (k = 64, n = 160, one column: 7.1, four waves from L2
-//   8.3, shared 12.2; k = 224, one column 14.8 / 20.6 / 17.3, four - / 21.8 / 17.4)
+//   one column 26.2 / 27.9, four 31.2 / 27.7; k = 16, n = 1792: four 10.6 / 12.2, eight 13.3 / 12.5; eight, n = 1020: 9.2 / 10.8, 1280: 11.5 / 11.1; k = 32:
+//   n = 640: 12.6 / 11.4, 1032: 19.3 / 14.4).  One tile a block with one or two columns while that makes no more than three blocks a CU, else two (one column,
+//   k = 32: n = 640: one tile 8.8, two 9.6, n = 800: 10.2, 9.5, n = 1536: 15.7, 13.3; k = 64: n = 520: 12.5, 13.9, n = 640: 13.2, 14.9, n = 800: 16.0, 15.4).
+//   bf16 rows of the few form save the launch that scales them: up to 16 columns and 16 KB (k = 4, n = 640, sixteen 6.2 / 9.4; n = 1792, eight 6.5 / 9.4)
+//   n < 512, k > 64: eight waves and the operand in LDS up to 64 KB of it, else the shared form (k = 64, n = 160, one column 6.9, four waves from L2 8.4,
+//   shared 12.1; k = 224 14.2 / 20.9 / 17.0)
 //   else the few form with the operand from L2, in groups of 16 columns: four waves while it makes 256 blocks, eight waves and two tiles while it makes
-//   512, or 1024 where contractions are short, else the shared form (k = 32, n = 160: 8 columns 6.5 / 7.5 / 10.2, 24: 11.6 / 9.5 / 11.9, 64: 18.6 /
-//   16.4 / 14.8; k = 16, n = 256, 64 columns: 15.6 / 11.4 / 13.3)
+//   512, or 1024 where contractions are short, else the shared form (k = 32, n = 160: 8 columns 6.6 / 7.6 / 10.2, 24: 11.7 / 9.5 / 11.6, 64: 18.5 / 16.2 / 13.9; k = 16, n = 256, 64 columns:
+//   15.8 / 11.5 / 12.4)
 // Groups of 32 have four times the scales, for which two tiles leave no registers: one tile a block while that makes 256 blocks, or little work, and with
-// n >= 512 up to 8 columns of a matrix below n = 1024 (k = 64, n = 1792, one column: one tile 44.9, two 49.6, shared 42.0; k = 16, n = 640, four: 9.6 /
-// 11.0 / 10.8; k = 64, n = 256, 24 columns: 23.0 / 19.8 / 15.8; k = 4, n = 256, 48: 6.6 / 8.9 / 10.0)
+// n >= 512 up to 8 columns of a matrix below n = 1024 (k = 64, n = 1792, one column: one tile 41.6, shared 33.2; n = 640: 20.1, 18.0; k = 4, n = 640, four: 5.2,
+// 6.2; k = 64, n = 256, 24 columns 23.1 / 14.4; k = 4, n = 256, 48 6.6 / 9.2)
 // bf16 operands, below n = 512: with one or two columns through LDS, where they are scaled, from n = 256 on, else as they are (k = 32, n = 480: one column
 // 7.6 / 8.7, two 8.4 / 8.9, four 10.3 / 9.0; n = 256: one 6.2 / 6.8, two 6.9 / 6.8; k = 64, n = 80: one 8.3 / 8.2, two 9.6 / 8.5).
 enum { FEW_LDS_WIDE, FEW_LDS, FEW_LDS_NARROW, FEW_WIDE, FEW, SHARED };
@@ -711,8 +713,9 @@ int form_of(const Q4View &m, int C, bool bf16) {
     const int n = m.n_tiles, k = m.k_blocks, blocks = n * ((C + 15) / 16), operand = C > 16 ? INT32_MAX : C * k * 256;
     const bool one = m.group == 32;
     if (n >= 512) {
-        if (operand > kScaled || C > (n < 1024 ? 8 : one ? 0 : 4)) return SHARED;
-        return n < 1024 && (one || C <= 2) ? FEW_LDS : FEW_LDS_WIDE;
+        const int most = bf16 && !one && operand <= kScaled / 2 ? 16 : n < 1024 ? 8 : one ? 0 : 4;
+        if (operand > kScaled || C > most) return SHARED;
+        return one || (n <= 768 && C <= 2) ? FEW_LDS : FEW_LDS_WIDE;
     }
     if (bf16 && n >= 256 && C <= 2 && operand <= kScaled) return FEW_LDS;
     if (k >= 64 && operand <= 64 * 1024) return FEW_LDS_NARROW;
