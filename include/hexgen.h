@@ -268,7 +268,7 @@ hexgen_status_t hexgen_head_greedy(hexgen_head_t *hd, const void *hidden_a, cons
 void            hexgen_head_destroy(hexgen_head_t *hd);
 
 /* hexgen_head_load_q4: the same head with its matrix in 4 bits (the layout of hexgen_q4_load with n_in = hidden, n_out = vocab, which has
- * to be even): hexgen_head_greedy then reads a quarter of the bytes.  Rows are normalised and multiplied in full precision.  Either load
+ * to be even): hexgen_head_greedy then reads a quarter of the bytes.  Rows are normalised and multiplied in fp32 (22 bits of a value).  Either load
  * replaces what the other one left.
  */
 hexgen_status_t hexgen_head_load_q4(hexgen_head_t *hd, const void *g_final, const void *w4, const void *scales, const void *zeros,
@@ -276,15 +276,16 @@ hexgen_status_t hexgen_head_load_q4(hexgen_head_t *hd, const void *g_final, cons
 
 /* ---- products with 4-bit weights ---------------------------------------------------------------------------------
  * y = x . w for the few rows of a decode step, w[k][n] = (q[k][n] - z[k / group][n]) * s[k / group][n] with q and z in 0 .. 15: the
- * weights of a projection, a draft model's or a quantised stage's, at half a byte each.
+ * weights of a projection in a caller's own layers, at half a byte each.
  *   hexgen_q4_create: n_in input features, n_out columns (even), group of 32, 64 or a multiple of 128 input features (the last one of a column may
  *     be shorter); dtype is the type of x, y and the scales (HEXGEN_ERR_SHAPE for other sizes).  Allocates no device memory.
  *   hexgen_q4_load: w4, bytes [n_in][n_out / 2], column 2 i in the low and 2 i + 1 in the high nibble of byte i; scales
  *     [ceil(n_in / group)][n_out]; zeros, bytes [ceil(n_in / group)][n_out / 2] as w4, or NULL for 8 everywhere.  Host or device memory; the
  *     library keeps a repacked copy; synchronises.
  *   hexgen_q4_project: x device [n_rows, n_in], rows ldx >= n_in elements apart; y device [n_rows, n_out], dense, aligned to two elements, apart
- *     from x.  Enqueues on `stream`.  Up to 64 rows (fp32: 32) read the matrix once.  Products and sums are fp32, with one rounding to dtype,
- *     over the whole range of the rows (scales up to 1e25 in magnitude); a row that holds an infinity or a NaN gives NaN.  HEXGEN_ERR_STATE before hexgen_q4_load.  Calls on one handle may not overlap in
+ *     from x.  Enqueues on `stream`.  Up to 64 rows (fp32: 32) read the matrix once.  Weights are exact, products and sums fp32, with one
+ *     rounding to dtype.  No sum of finite values overflows before its group's scale is applied (scales up to 1e25 in magnitude).  Values of a bf16
+ *     or fp32 row that are 2^-29 (2^-15) of its largest or less may be off by 2^-40 (2^-39) of that.  A row that holds an infinity or a NaN gives NaN.  HEXGEN_ERR_STATE before hexgen_q4_load.  Calls on one handle may not overlap in
  *     time (they share its workspace).  Can be recorded into a graph.
  */
 typedef struct hexgen_q4 hexgen_q4_t;              /* opaque, library-owned */

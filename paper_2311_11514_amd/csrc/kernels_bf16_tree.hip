@@ -249,16 +249,16 @@ __device__ __forceinline__ void tree_patch(h16x8 (*st)[64], const TreeIn &in, in
 
 // Many rows: a block of four waves takes 32 RW query rows of one (sequence, kv head) and a run of 32-position tiles; RW groups of 32 rows times
 // CW = 4 / RW neighbouring tiles a step.  The tiles go from HBM to LDS directly, S steps in flight, and S^T = K . Q^T,
-// O^T = V^T . P^T run on the 32 x 32 x 16 MFMA exactly as in the prefill attention: a lane owns one query row, P stays in its
-// registers and is rounded to the element type for the second product (bf16: 2^-8 of a weight, as much as the result's own rounding; the
-// weights' sum takes them unrounded).
+// O^T = V^T . P^T run on the 32 x 32 x 16 MFMA as in the prefill attention: a lane owns one query row, P stays in its
+// registers and goes into the second product in two parts (tree_pack2; with one part, which leaves results a fifth to a third less exact, the times
+// below were 127, 354 and 182).
 // Tiles that lie in the context need no mask; of a tile that reaches the tree's slots a lane takes 32 bits of its node's ancestors.
 // A weight of zero times an infinity would be a NaN, so a masked tile with a value that is not finite is multiplied out element
 // by element over what each row attends.
 // Contexts are cut into runs of tp.chunk tiles (tp.nsplit at most), whose (m, l, o) tree_merge_kernel joins: a launch of its own, since joining
 // 128 rows of a run moves 64 KB, which one last block would take longer over.
-// Bound by HBM with few nodes, by each wave's chain of LDS reads, products and softmax with many (matrix cores 34 % busy, vector units 45 %): d 128, 64 query and 8 kv heads, 32
-// sequences of 4000: 16 nodes 127 us (4.1 TB/s), 64 nodes 354 (757 TFLOP/s); contexts of 240 .. 4027 and 8 .. 64 nodes 184 (435 TFLOP/s: a quarter of
+// Bound by HBM with few nodes, by each wave's chain of LDS reads, products and softmax with many (matrix cores 44 % busy, vector units 53 %): d 128, 64 query and 8 kv heads, 32
+// sequences of 4000: 16 nodes 139 us (3.8 TB/s), 64 nodes 447 (600 TFLOP/s); contexts of 240 .. 4027 and 8 .. 64 nodes 209 (383 TFLOP/s: a quarter of
 // the blocks' rows do not exist, and the long contexts end late).
 // QLO: the query rows come in two parts.
 template <int D, int RW, int S, bool QLO>
@@ -478,8 +478,8 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(KvGeom kg, int hq_l, Tr
 // Few rows, or little work in all: a block of eight waves takes 32 query rows and the waves take the run's tiles in turn.  No tile serves two
 // waves, so K and V go straight to registers in the operands' layout (the next tile's K is requested before this tile's softmax); the query rows, the
 // same for all waves, wait in LDS (in registers they would make this kernel spill), and there the waves meet at the end.  Bound by latency, or by HBM where there are
-// many sequences: d 128, one kv head of eight, one sequence of 2048 with 26 nodes 13.4 us, sixteen with 8 nodes 15.9 (1.1 TB/s), a context of a
-// tile or two 8.4; eight kv heads, one sequence of 4000 with 16 nodes 17.0.  The arithmetic is that of the kernel above.
+// many sequences: d 128, one kv head of eight, one sequence of 2048 with 26 nodes 13.6 us, sixteen with 8 nodes 15.7 (1.1 TB/s), a context of a
+// tile or two 8.5; eight kv heads, one sequence of 4000 with 16 nodes 17.3.  The arithmetic is that of the kernel above.
 // Runs leave (m, l, o) with device-scope stores and count themselves; whoever is last joins them in the order of the context, so that the
 // result does not depend on who that was, and resets the counter.  Nobody waits for anybody.
 template <int D, bool QLO>

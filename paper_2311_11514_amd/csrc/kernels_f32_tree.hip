@@ -40,7 +40,7 @@ __global__ __launch_bounds__(256) void f32_tree_rope_append_kernel(const float *
 // lane owns column l % 16 and positions 4 (l / 16) + r, P stays in registers).  Rows that are not in the cache yet (in.k != NULL) are read from the
 // caller's and appended by the first block of columns.  Masks, runs and the way of values that are not finite as in the 16-bit kernel.
 // Bound by the fp32 matrix instructions, 32 cycles for 4 KB of K or V, and by the one round trip per tile and wave: d 128, 16 query and 4 kv heads, four
-// sequences of 2048 with 8 nodes 22.5 us, eight of 600, one kv head 15.5; d 64, a context of 40 with five nodes 5.7, half of that the launch.
+// sequences of 2048 with 8 nodes 22.5 us, eight of 600, one kv head 15.3; d 64, a context of 40 with five nodes 5.7, half of that the launch.
 template <int D, int W>
 __global__ __launch_bounds__(64 * W) void f32_tree_attn_kernel(const float *__restrict__ q, int64_t ldq, TreeIn in, float *kc, float *vc, KvGeom kg, int hq_l, int G, int nrb,
                                                                TreeView tv, const int32_t *__restrict__ lens, TreePlan tp, float *__restrict__ o) {

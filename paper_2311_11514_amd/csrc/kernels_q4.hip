@@ -199,8 +199,8 @@ __device__ __forceinline__ void best_of_lanes(float &bv, int &bi) {
 // blocks in turn and are summed through LDS in wave order, so that no partial result leaves the block.  A wave holds R blocks with their scales in registers, requested that far ahead; every request is
 // unconditional (past the end it repeats the last block's), so that the compiler can count what is in flight and waits for the oldest
 // alone.  XLDS: the operand is staged in LDS once, else a wave requests its pieces one block ahead, from L2.
-// Bound by HBM on wide matrices, on small ones by the launch and one round trip (bf16, one row: 8192 x 10240 13.4 us, 3.2 TB/s; the arg-max form, 8192 x
-// 32000, two columns 28.4, 4.7 TB/s; 4096 x 4096 5.9).
+// Bound by HBM on wide matrices, on small ones by the launch and one round trip (bf16, one row: 8192 x 10240 13.9 us, 3.1 TB/s; the arg-max form, 8192 x
+// 32000, two columns 28.4, 4.7 TB/s; 4096 x 4096 6.1).
 // FL: 32-feature steps of a scale's group inside a 128-feature block (4: groups of 128 and more).
 // OP_BF16: the operand is bf16 as it is.  Its sums, which have not seen their scale yet, may leave fp32's range (from values of 1.8e35 on): columns whose
 // result is not finite are done once more, with the operand 2^-64 of itself.  OP_SCALED (with XLDS): the operand is bf16 and becomes fp16 on its way to LDS.
@@ -397,9 +397,9 @@ __global__ __launch_bounds__(64 * W, UT == 1 || FL == 4 ? 4 : FL == 2 ? 3 : 2) v
 // while others are at the matrix unit.  The groups are joined through LDS at the end.  The contraction is split over blockIdx.y where the matrix
 // has too few columns for the chip: splits leave partial sums, `part` [split][column of the operand][16 n_tiles], to q4_finish_kernel.  Without
 // splits the parts are joined, and stored or searched for their largest, here.
-// Bound by HBM up to 16 columns (8192 x 57344, twelve rows 48 us, 5 TB/s), beyond by the vector unit (28 operations a lane to widen a tile's block, some
-// 10 for its scales and zero points, 8 per operand tile to apply them) and the matrix unit, which overlap little: 32 columns 66 .. 74 us, 4096 x 50304
-// with 48 columns 46.  Weights in registers with one step ahead took 64, 77 and 53; one group of eight waves five steps ahead 60, 80 and 46.
+// Bound by HBM up to 16 columns (8192 x 57344, twelve rows 46 us, 5.2 TB/s), beyond by the vector unit (36 operations a lane to widen a tile's block, some
+// 8 for its scales and zero points, 4 per operand tile to apply them) and the matrix unit, which overlap little: 32 columns 57 us, 4096 x 50304
+// with 48 columns 42.
 template <int ST, int NB, int FL> struct SharedStage {
     static constexpr int ES = ST == HX_T_F32 ? 4 : 2, NF = 4 / FL, SP = (NF * 256 * ES + 1023) / 1024;      // SP: requests of 1 KB for the scales of 16 tiles
     u32x4 x[4 * NB][64], w[16][64];
@@ -726,8 +726,8 @@ int form_of(const Q4View &m, int C, bool bf16) {
 int few_tiles(int form) { return form == FEW_LDS_WIDE || form == FEW_WIDE ? 2 : 1; }
 
 // The shared form's blocks: waves per group (two tiles of 16 columns each) and splits of the contraction, by the steps that the fullest CU has to
-// do; a split costs its partial sums and, the first one, a launch (us, bf16: 8192 x 57344, 32 columns: 8 waves 66, 7 73, 8 and two splits 77; 8192 x
-// 10240: 6 waves and four splits 21, 8 and four 23, 7 and two 35; 28672 x 8192, 40 columns: 8 waves and eight splits 48, 7 and four 64).
+// do; a split costs its partial sums and, the first one, a launch (us, fp16: 8192 x 57344, 32 columns: 8 waves 57, 8 and two splits 68; 8192 x
+// 10240, 32 columns: 6 waves and four splits 19, 8 and four 21, 7 and two 30; 28672 x 8192, 40 columns: 8 waves and eight splits 42, 7 and four 55).
 struct SharedShape { int waves, splits; };
 SharedShape shared_shape(const Q4View &m, int C) {
     SharedShape best{8, 1};

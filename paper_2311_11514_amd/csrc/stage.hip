@@ -358,18 +358,19 @@ KvGeom geom(const hexgen_stage *st, const hexgen_kv_cache *kv) {
 // ---- drafted trees: the attention of every path ----------------------------------------------------------------
 // Rows per block, runs and order of a tree attention.  (us; 16 bits, d 128; "few": 32 rows a block and eight waves that each take tiles of their own,
 // 2 and 4: groups of 32 rows that share tiles through LDS; then the runs of a context)
-//   8 heads a kv head, 8 kv heads, 4000 positions: one sequence of 64 nodes: few 30, 2 in four runs 41; eight of 16: few 47, 2 in four 46
-//   32 sequences of 2048: 8 nodes: few 68, 2 64, 2 in two 67, 4 77; 32 nodes: 2 126, 4 116; 16 nodes at 4000: 2 127, 4 144; contexts of
-//   240 .. 4027 and 8 .. 64 nodes: 2 181, 4 198 (three quarters of its rows exist)
+//   8 heads a kv head, 8 kv heads, 4000 positions: one sequence of 64 nodes: few 35, 2 in runs of 24 tiles 38; eight of 16: few 48, 2 in four runs 51
+//   32 sequences of 2048: 4 nodes: few 56, 2 60, 4 80; 8 nodes: few 69, 2 64, 2 in two 71, 4 88; 32 nodes: few 222, 2 156, 4 140; 16 nodes at 4000: few
+//   189, 2 141, 4 171; 64 nodes at 4000: 2 503, 4 448; contexts of 240 .. 4027 and 8 .. 64 nodes: few 268, 2 211, 4 234 (three quarters of its rows exist)
 // "Few" and fp32 blocks have a CU each: runs must not make more blocks than there are CUs, with some to spare (kTreeBlocks), and a run costs its
 // share of the joining, 0.5 us where a tile of a run costs 0.14, so that the best length goes with the root of the context's; whole rounds of the
 // eight waves, which also leave little to the last run, the one with the tree.
-//   one kv head, eight heads, runs of 8, 10, 16, 24 tiles and whole: one sequence of 2048, 26 nodes: 16.9, 14.1, 13.5, 16.4, 18.8; sixteen, 8 nodes:
-//   24.3 (288 blocks), 16.3, 15.1, 18.1, 20.0; one of 4000, 16 nodes: 17.3, 17.7, 16.2, 14.0, 27.6 (runs of 22 tiles 16.2); eight of 600: 13.7, 15.5,
-//   13.7, 11.9, 11.9; sixteen of 2048, 32 nodes (128 blocks): in two runs 24, whole 21.  Eight kv heads, one sequence of 1000, 8 nodes: 14.9, 13.7,
-//   16.7, 14.8, 13.9; of 4000, 16 nodes: 38.7, 27.0, 20.6 (256 blocks), 16.9, 29.1
-//   fp32, runs of 4, 8, 10, 16 and whole: four of 2048, 4 kv heads, 8 nodes: 29.1, 29.0 (288 blocks), 22.8, 27.5, 66.8; eight of 600, one kv head:
-//   15.6, 17.0, 19.0, 24.1, 24.4
+//   one kv head, eight heads, runs of 8, 16, 24, 32 tiles and whole: one sequence of 2048, 26 nodes: 16.9, 13.7, 17.0, 15.3, 20.0; sixteen, 8 nodes:
+//   24.5 (288 blocks), 15.5, 18.5, 17.2, 21.0; one of 4000, 16 nodes: 17.6, 16.9, 14.3, 19.1, 31.1; eight of 600: 13.8, 14.0, 12.7, 12.6, 12.7
+//   From 128 blocks on whole contexts: 2048, 32 nodes, sixteen sequences: in runs of 48 tiles 21.8, whole 22.6; of 4000: in two runs 32.6, whole 37.0;
+//   eight kv heads, sixteen of 4000 with 4 nodes: in two 58.8, whole 59.1.  Eight kv heads, one sequence of 1000, 8 nodes, runs of 8, 16, 24 and whole: 15.2,
+//   17.3, 15.2, 15.1; of 4000, 16 nodes: 39.1, 21.8 (256 blocks), 17.2, 32.2
+//   fp32: four of 2048, 4 kv heads, 8 nodes: runs of 8 tiles 29.0 (288 blocks), 10 22.5, 16 27.4, 24 32.7, whole 66.7; eight of 600, one kv head: 4 15.5,
+//   8 17.0, 16 24.1, whole 24.4
 // two_parts: the query rows come in two parts, which blocks of 128 rows have no registers for (and up to kDecodeMaxRows rows do not fill them)
 TreePlan pick_tree_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, const hexgen_tree *tr, bool two_parts) {
     const int G = st->hq_l / st->hkv_l;
