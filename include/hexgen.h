@@ -214,12 +214,12 @@ hexgen_status_t hexgen_tree_accept(const hexgen_tree_t *tr, const int32_t *draft
  * cache as above.  What a node does not attend has no influence on its row, infinities and NaN included.
  * hexgen_kv_cache_keep: HOST kept[batch] and HOST path[rows] as hexgen_tree_accept lays them out, from that call or from another rule of
  * acceptance: the rows of every path (root first, each node a child of the one before it: HEXGEN_ERR_SHAPE otherwise; kept[i] = 0
- * drops the whole tree) move to the slots behind the context, in every layer, and the committed lengths grow by kept[i].  The
- * arrays may be changed when it returns; it enqueues on `stream` and cannot be recorded into a graph (HEXGEN_ERR_DEVICE).
+ * drops the whole tree) move to the slots behind the context, in every layer, and the committed lengths grow by kept[i] (not where
+ * replayed steps have taken a length so far that max_seq would be passed).  The arrays may be changed when it returns; it enqueues on `stream` and cannot be recorded into a graph (HEXGEN_ERR_DEVICE).
  * All three: HEXGEN_ERR_STATE unless the cache holds a batch (prefill, set_lengths, commit) and the trees are set for just as many
  * sequences; HEXGEN_ERR_CAPACITY when a context and its tree exceed max_seq.
  * hexgen_stage_decode_tree and hexgen_kv_tree_attention: HEXGEN_ERR_CAPACITY also for more than a launch takes (sequences x kv heads x
- * ceil(nodes of the largest tree x heads per kv head / 32) from 2^23 on; fp32: / 16, from 2^24 on).  They can be recorded once a call of that
+ * ceil(nodes of the largest tree x heads per kv head / 32) from about 2^23 on; fp32: / 16, 2^24).  They can be recorded once a call of that
  * size has run outside a graph.  A recording is for trees of the recorded counts; a replay reads the lengths and the parents that hold
  * then from the device, and leaves out what would pass max_seq.  Calls on one stage, replays among them, may not overlap in time (they share
  * its workspace).
@@ -285,8 +285,9 @@ hexgen_status_t hexgen_head_load_q4(hexgen_head_t *hd, const void *g_final, cons
  *   hexgen_q4_project: x device [n_rows, n_in], rows ldx >= n_in elements apart; y device [n_rows, n_out], dense, aligned to two elements, apart
  *     from x.  Enqueues on `stream`.  Up to 64 rows (fp32: 32) read the matrix once.  Weights are exact, products and sums fp32, with one
  *     rounding to dtype.  No sum of finite values overflows before its group's scale is applied (scales up to 1e25 in magnitude).  Values of a bf16
- *     or fp32 row that are 2^-29 (2^-15) of its largest or less may be off by 2^-40 (2^-39) of that.  A row that holds an infinity or a NaN gives NaN.  HEXGEN_ERR_STATE before hexgen_q4_load.  Calls on one handle may not overlap in
- *     time (they share its workspace).  Can be recorded into a graph.
+ *     or fp32 row that are 2^-29 (2^-15) of its largest or less may be off by 2^-40 (2^-39) of that.  A row that holds an infinity or a NaN gives NaN.
+ *     HEXGEN_ERR_STATE before hexgen_q4_load.  Calls on one handle may not overlap in time (they share its workspace).  Can be recorded into a
+ *     graph, which another load makes invalid.
  */
 typedef struct hexgen_q4 hexgen_q4_t;              /* opaque, library-owned */
 hexgen_status_t hexgen_q4_create(int n_in, int n_out, int group, hexgen_dtype_t dtype, hexgen_q4_t **out);

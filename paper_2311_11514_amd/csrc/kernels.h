@@ -209,7 +209,7 @@ struct TreeOut {
     void *o;
 };
 void launch_tree_accept(const TreeView &tv, const int32_t *draft, const int32_t *chosen, int32_t *kept, int32_t *path, int32_t *tokens, hipStream_t s);
-void launch_tree_advance(int32_t *lens, const int32_t *kept, int batch, hipStream_t s);      // lens += kept
+void launch_tree_advance(int32_t *lens, const int32_t *kept, int batch, int smax, hipStream_t s);      // lens += kept, up to smax
 void f32_launch_tree_rope_append(const float *qkv, int hq_l, KvGeom kg, const TreeView &tv, const int32_t *lens, const float *cos_tab,
                                  const float *sin_tab, float *q, float *kc, float *vc, hipStream_t s);
 void f32_launch_tree_attn(const float *q, int64_t ldq, const TreeIn &in, float *kc, float *vc, KvGeom kg, int hq_l, const TreeView &tv, const int32_t *lens,

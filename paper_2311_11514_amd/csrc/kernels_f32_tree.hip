@@ -275,9 +275,10 @@ __global__ __launch_bounds__(256) void f32_tree_keep_kernel(float *__restrict__ 
     }
 }
 
-__global__ void tree_advance_kernel(int32_t *__restrict__ lens, const int32_t *__restrict__ kept, int batch) {
+// a path that would pass the cache (replayed steps have taken its length beyond what the host knows) has not been moved and is not counted either
+__global__ void tree_advance_kernel(int32_t *__restrict__ lens, const int32_t *__restrict__ kept, int batch, int smax) {
     const int i = blockIdx.x * 64 + threadIdx.x;
-    if (i < batch) lens[i] += kept[i];
+    if (i < batch && lens[i] + kept[i] <= smax) lens[i] += kept[i];
 }
 
 // One wave per sequence walks its tree: the 64 lanes look at four nodes each for the first child of the current node whose drafted
@@ -323,8 +324,8 @@ __global__ __launch_bounds__(64) void tree_accept_kernel(TreeView tv, const int3
 void launch_tree_accept(const TreeView &tv, const int32_t *draft, const int32_t *chosen, int32_t *kept, int32_t *path, int32_t *tokens, hipStream_t s) {
     hipLaunchKernelGGL(tree_accept_kernel, dim3(tv.batch), dim3(64), 0, s, tv, draft, chosen, kept, path, tokens);
 }
-void launch_tree_advance(int32_t *lens, const int32_t *kept, int batch, hipStream_t s) {
-    hipLaunchKernelGGL(tree_advance_kernel, dim3((batch + 63) / 64), dim3(64), 0, s, lens, kept, batch);
+void launch_tree_advance(int32_t *lens, const int32_t *kept, int batch, int smax, hipStream_t s) {
+    hipLaunchKernelGGL(tree_advance_kernel, dim3((batch + 63) / 64), dim3(64), 0, s, lens, kept, batch, smax);
 }
 void f32_launch_tree_rope_append(const float *qkv, int hq_l, KvGeom kg, const TreeView &tv, const int32_t *lens, const float *cos_tab,
                                  const float *sin_tab, float *q, float *kc, float *vc, hipStream_t s) {

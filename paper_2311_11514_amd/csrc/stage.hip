@@ -1540,7 +1540,7 @@ hexgen_status_t hexgen_kv_cache_keep(hexgen_kv_cache_t *kv, hexgen_tree_t *tr, c
              d_path, s);
     else
         f32_launch_tree_keep(static_cast<float *>(kv->k), static_cast<float *>(kv->v), kv->layer_stride, st->L, kg, tr->batch, kv->d_lens, tr->dev, d_kept, d_path, s);
-    launch_tree_advance(kv->d_lens, d_kept, tr->batch, s);
+    launch_tree_advance(kv->d_lens, d_kept, tr->batch, kv->smax, s);
     HX_HIP(hipGetLastError());
     for (int i = 0; i < tr->batch; ++i) kv->lens[i] += kept[i];
     return HEXGEN_OK;

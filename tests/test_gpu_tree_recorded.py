@@ -41,3 +41,32 @@ def test_recorded_behind_a_larger_prefill(dtype):
         st.decode_tree(kv, tree, x, *want)
         torch.cuda.synchronize()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_path_that_passes_the_cache_is_not_counted(dtype):
+    """Replays of a recorded decode step take the device's length from 11 to 29 of 32, of which the host knows 12: keeping five rows does nothing, and
+    the next tree's rows follow the 29th position."""
+    cfg = StageConfig("rec", dtype, 512, 8, 2, 512, 1, 1, (0,), batch=1, seed=6)
+    st = make_gpu_stage(cfg, 0, [generate.layer_weights(cfg, 0)])
+    kv, tree = st.kv_cache_create(1, 32), hx.Tree(1, 8)
+    kv.set_lengths([10])
+    x = to_dev(generate.hidden_rows(cfg, 1), cfg)
+    p, r = torch.empty_like(x), torch.empty_like(x)
+    st.decode(kv, 0, x, p, r)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        st.decode(kv, 1, x, p, r)
+    for _ in range(18):
+        graph.replay()
+    tree.set([5], [-1, 0, 1, 2, 3])
+    rows = to_dev(generate.hidden_rows(cfg, 5, stream_id=1), cfg)
+    st.decode_tree(kv, tree, rows, torch.empty_like(rows))
+    kv.keep(tree, [5], [0, 1, 2, 3, 4])
+    tree.set([1], [-1])
+    q, k, v = (torch.full((1, heads, 64), 0.5 + heads, dtype=x.dtype, device="cuda") for heads in (8, 2, 2))
+    kv.tree_attention(0, tree, q, k, v)
+    torch.cuda.synchronize()
+    for got, want in zip(kv.read(0, 0, 29, 1), (k, v)):
+        assert torch.equal(got, want.float().cpu())
