@@ -175,6 +175,8 @@ hexgen_status_t hexgen_kv_cache_fill(hexgen_kv_cache_t *kv, int layer, int seq, 
                                      const float *k, const float *v);
 hexgen_status_t hexgen_kv_cache_set_lengths(hexgen_kv_cache_t *kv, const int32_t *lens, int batch);
 hexgen_status_t hexgen_kv_cache_get_lengths(hexgen_kv_cache_t *kv, int32_t *lens_out, int batch);
+/* Sequences that the cache holds (of its last prefill, set_lengths, commit or eviction into it); 0 when there are none, -1 for NULL. */
+int             hexgen_kv_cache_batch(const hexgen_kv_cache_t *kv);
 
 /* ---- drafted trees (speculative decoding) --------------------------------------------------------------------
  * A step of speculative decoding takes, per sequence, a tree of drafted tokens through the model at once and keeps the path that the
@@ -231,6 +233,46 @@ hexgen_status_t hexgen_kv_tree_attention(hexgen_kv_cache_t *kv, int layer, const
                                          const void *k, int64_t ldk, const void *v, int64_t ldv, void *out, void *stream);
 hexgen_status_t hexgen_kv_cache_keep(hexgen_kv_cache_t *kv, hexgen_tree_t *tr, const int32_t *kept, const int32_t *path,
                                      void *stream);
+
+/* ---- long requests in a cache of bounded size ----------------------------------------------------------------------
+ * New rows of any number per sequence -- one token, a chunk of a prompt, a whole one -- that attend a sliding window and the first positions
+ * of their context, the sums of the attention weights that they leave behind, and the eviction of what they did not need.
+ * counts: HOST int32 [batch], new rows of every sequence, 0 or more, packed sequence by sequence; NULL = one each.  Row x of sequence i stands at slot
+ * p = len_i + x and attends the slots j <= p with p - j < window or j < sinks (window >= 1, so every row attends itself; any window beyond
+ * max_seq: all of its context; sinks 0: the window alone).
+ * weights: device fp32 accumulators, dense [batch][hkv_local][max_seq] (hexgen_stage_extend: [n_layers][batch][hkv_local][max_seq]), to
+ * each of which the call adds the softmax weights that its slot got, over the call's rows and the query heads of the kv head; slots that no row
+ * attends, and those behind the rows, stay as they are.  May be NULL.  The sums have one order: the same call gives the same bits.
+ *
+ *   hexgen_kv_window_attention: one layer's attention alone, for callers with projections of their own.  q, k, v, out and their row strides as for
+ *     hexgen_kv_tree_attention, q and k rotated at the rows' positions (slots; or, behind evictions, whatever positions the caller's keys carry).  k and v join
+ *     `layer`'s cache at the rows' slots, uncommitted: hexgen_kv_cache_commit once all layers have processed the rows.  What a row
+ *     does not attend has no influence on it, infinities and NaN included.
+ *   hexgen_stage_extend: the rows through every layer of the stage, rotated at their slots; buffers as for hexgen_stage_prefill.  The committed
+ *     lengths grow by counts; the decode steps' count does not change.  Up to 32 rows are computed as decode steps are, more as a prefill is.
+ *   hexgen_kv_cache_evict: of every sequence's len_i slots min(len_i, keep) stay, in their order: the first `sinks`, the last `recent`, and of the others those
+ *     with the largest weights (of equal ones the lowest slots; NaN below everything), chosen for every layer and kv head by weights [n_layers][batch][hkv_local]
+ *     [max_seq] (not changed); weights NULL: the newest.  They become slots 0 .. of dst, a cache of the same stage, or kv itself; what dst holds
+ *     behind them stays as it is.  rotate != 0: keys are rotated back by as many positions as they move, with one more rounding to the cache's type, so that the kept
+ *     slots read as a context of their own (for stages, which rotate at slots); 0: keys keep the positions they were rotated at.
+ *     Device outputs, rows of dst's max_seq: slots int32 [n_layers][batch][hkv_local][dst max_seq], the slots that stayed, filled up with -1; weights_out fp32 of the same
+ *     shape (NULL when weights is), their weights, filled up with 0 (in place: may be weights itself).  dst's committed lengths become min(len_i, keep); a dst that is not kv starts
+ *     its decode steps at 0.  HEXGEN_ERR_INVALID_ARG when sinks + recent > keep; HEXGEN_ERR_CAPACITY unless dst takes the batch and min(keep, max_seq) slots;
+ *     HEXGEN_ERR_DEVICE when it would be recorded.  Drafted rows that are not committed are dropped.
+ * All three enqueue on `stream`; HEXGEN_ERR_STATE unless the cache holds a batch (prefill, set_lengths, commit), of just `batch` sequences; HEXGEN_ERR_SHAPE when
+ * there is no row at all; HEXGEN_ERR_CAPACITY when a context and its rows exceed max_seq, or for more than a launch takes.  The attention and
+ * hexgen_stage_extend can be recorded once a call of that size has run outside a graph (with weights, if it is to gather them); a recording is for its counts, window and sinks,
+ * a replay reads the lengths that hold then, leaves out what would pass max_seq, and advances (extend) the lengths on the device.  Calls on one stage, replays among them, may not
+ * overlap in time (they share its workspace).  A call with more rows or sequences than any before it replaces that workspace: what was recorded
+ * earlier has to be recorded again.
+ */
+hexgen_status_t hexgen_kv_window_attention(hexgen_kv_cache_t *kv, int layer, const int32_t *counts, int batch, const void *q, int64_t ldq,
+                                           const void *k, int64_t ldk, const void *v, int64_t ldv, int window, int sinks, float *weights,
+                                           void *out, void *stream);
+hexgen_status_t hexgen_stage_extend(hexgen_stage_t *st, hexgen_kv_cache_t *kv, const void *hidden_in, const int32_t *counts, int batch,
+                                    int window, int sinks, float *weights, void *out_partial, void *out_resid, void *stream);
+hexgen_status_t hexgen_kv_cache_evict(hexgen_kv_cache_t *kv, hexgen_kv_cache_t *dst, int keep, int sinks, int recent, const float *weights,
+                                      float *weights_out, int rotate, int32_t *slots, void *stream);
 
 /* Debug tap: at the entry of `layer` during prefill / decode, the fp32 residual stream
  * [rows, hidden] is copied to `h_dump` (device).  NULL removes the tap.

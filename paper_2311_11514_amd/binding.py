@@ -52,6 +52,10 @@ SIGNATURES = {
     "hexgen_stage_decode_tree": (_i, [_vp] * 7),
     "hexgen_kv_tree_attention": (_i, [_vp, _i, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]),
     "hexgen_kv_cache_keep": (_i, [_vp, _vp, _ip, _ip, _vp]),
+    "hexgen_kv_cache_batch": (_i, [_vp]),
+    "hexgen_kv_window_attention": (_i, [_vp, _i, _ip, _i, _vp, _i64, _vp, _i64, _vp, _i64, _i, _i, _vp, _vp, _vp]),
+    "hexgen_stage_extend": (_i, [_vp, _vp, _vp, _ip, _i, _i, _i, _vp, _vp, _vp, _vp]),
+    "hexgen_kv_cache_evict": (_i, [_vp, _vp, _i, _i, _i, _vp, _vp, _i, _vp, _vp]),
     "hexgen_stage_weight_bytes": (_i64, [_vp]),
     "hexgen_stream_copy": (_i, [_vp, _vp, _i64, _i, _vp]),
     "hexgen_stream_read": (_i, [_vp, _vp, _i64, _i, _vp]),
@@ -183,6 +187,23 @@ def _rows_of_heads(t: torch.Tensor, name: str, rows: int, heads: int, d: int, dt
     return stride[0] if rows > 1 else heads * d
 
 
+def _int32(value, name: str) -> int:
+    """A scalar that the C interface takes in 32 bits, which ctypes would cut off."""
+    value = int(value)
+    if not -1 << 31 <= value < 1 << 31:
+        raise ValueError(f"{name}: a 32-bit integer is wanted, got {value}")
+    return value
+
+
+def _span(counts: Optional[Sequence[int]], given: int, window: Optional[int]):
+    """(counts, sequences, rows, window) of a call whose first tensor has `given` rows; counts None: one row each; window None: one that nothing reaches."""
+    window = (1 << 31) - 1 if window is None else _int32(window, "window")
+    if counts is None:
+        return None, given, given, window
+    counts = [int(x) for x in counts]
+    return _i32(counts + [0]), len(counts), sum(x for x in counts if x > 0), window      # (one entry too many: an empty list has no address of its own)
+
+
 _TORCH_DTYPE = {HEXGEN_F32: torch.float32, HEXGEN_BF16: torch.bfloat16, HEXGEN_F16: torch.float16}
 
 
@@ -259,6 +280,20 @@ class Stage:
         _check(lib.hexgen_stage_decode_tree(self.handle, kv.handle, tree.handle, _ptr(hidden_in), _ptr(out_partial),
                                             _ptr(out_resid), _stream_handle(stream, here)), "hexgen_stage_decode_tree")
 
+    def extend(self, kv: "KVCache", hidden_in: torch.Tensor, out_partial: torch.Tensor, out_resid: Optional[torch.Tensor] = None,
+               counts: Optional[Sequence[int]] = None, window: Optional[int] = None, sinks: int = 0, weights: Optional[torch.Tensor] = None, stream=None):
+        """hexgen_stage_extend: counts[i] new rows of every sequence (None: one each) through every layer, behind the committed contexts, attending a
+        window (None: everything) and the first `sinks` positions; weights float32 [n_layers, batch, hkv_local, max_seq], added to."""
+        c, batch, rows, window = _span(counts, hidden_in.shape[0], window)
+        shape, td, here = (rows, self.hidden), _torch_dtype(self.dtype), _here(hidden_in)
+        for name, t in (("hidden_in", hidden_in), ("out_partial", out_partial), ("out_resid", out_resid)):
+            if t is not None:
+                _device_tensor(t, name, shape, td, here)
+        if weights is not None:
+            _device_tensor(weights, "weights", (self.n_layers, batch, self.hkv_l, kv.max_seq), torch.float32, here)
+        _check(lib.hexgen_stage_extend(self.handle, kv.handle, _ptr(hidden_in), c, batch, window, _int32(sinks, "sinks"), _ptr(weights), _ptr(out_partial),
+                                       _ptr(out_resid), _stream_handle(stream, here)), "hexgen_stage_extend")
+
     def decode_static_bytes(self, batch: int) -> int:
         return int(lib.hexgen_stage_decode_static_bytes(self.handle, batch))
 
@@ -303,7 +338,7 @@ class KVCache:
     def __init__(self, stage: Stage, max_batch: int, max_seq: int):
         h = C.c_void_p()
         _check(lib.hexgen_kv_cache_create(stage.handle, max_batch, max_seq, C.byref(h)), "hexgen_kv_cache_create")
-        self.handle, self.stage = h, stage
+        self.handle, self.stage, self.max_batch, self.max_seq = h, stage, max_batch, max_seq
 
     def close(self, _lib=lib):
         if getattr(self, "handle", None):
@@ -365,6 +400,48 @@ class KVCache:
         if len(kept) != tree.batch or len(path) != tree.rows:
             raise ValueError(f"keep: {tree.batch} counts and {tree.rows} path entries are wanted, got {len(kept)} and {len(path)}")
         _check(lib.hexgen_kv_cache_keep(self.handle, tree.handle, _i32(kept), _i32(path), _stream_handle(stream)), "hexgen_kv_cache_keep")
+
+    def window_attention(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, counts: Optional[Sequence[int]] = None,
+                         window: Optional[int] = None, sinks: int = 0, weights: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                         stream=None) -> torch.Tensor:
+        """hexgen_kv_window_attention: counts[i] new rows of every sequence (None: one each), q [rows, hq_local, head_dim], k, v [rows, hkv_local,
+        head_dim], rotated; rows may be apart (parts of a fused projection).  A row attends the last `window` slots (None: all), its own among them, and the first
+        `sinks`.  weights float32 [batch, hkv_local, max_seq]: the attention weights' sums are added to it.  Returns [rows, hq_local, head_dim]."""
+        st, here = self.stage, _here(q)
+        c, batch, rows, window = _span(counts, q.shape[0], window)
+        td, hq, hkv, d = _TORCH_DTYPE[st.dtype], st.hq_l, st.hkv_l, st.head_dim
+        ldq = _rows_of_heads(q, "q", rows, hq, d, td, here)
+        ldk = _rows_of_heads(k, "k", rows, hkv, d, td, here)
+        ldv = _rows_of_heads(v, "v", rows, hkv, d, td, here)
+        if weights is not None:
+            _device_tensor(weights, "weights", (batch, hkv, self.max_seq), torch.float32, here)
+        if out is None:
+            out = _empty_beside(q, (rows, hq, d), stream)
+        else:
+            _device_tensor(out, "out", (rows, hq, d), td, here)
+        _check(lib.hexgen_kv_window_attention(self.handle, layer, c, batch, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, window, _int32(sinks, "sinks"),
+                                              None if weights is None else weights.data_ptr(), out.data_ptr(), _stream_handle(stream, here)),
+               "hexgen_kv_window_attention")
+        return out
+
+    def evict(self, keep: int, sinks: int = 0, recent: int = 0, weights: Optional[torch.Tensor] = None, rotate: bool = False, into: Optional["KVCache"] = None,
+              stream=None):
+        """hexgen_kv_cache_evict: of every sequence `keep` slots stay per layer and kv head, the first `sinks`, the last `recent` and of the others the heaviest by weights
+        float32 [n_layers, batch, hkv_local, max_seq] (None: the newest), and move to the front of `into` (None: of this cache); rotate: their keys turn back by
+        the distance.  Returns (slots int32 [n_layers, batch, hkv_local, into.max_seq] filled up with -1, their weights filled up with 0 or None); without
+        `into` the given weights are updated and returned."""
+        st, dst = self.stage, self if into is None else into
+        batch = int(lib.hexgen_kv_cache_batch(self.handle))
+        keep, sinks, recent = _int32(keep, "keep"), _int32(sinks, "sinks"), _int32(recent, "recent")
+        shape = (st.n_layers, max(batch, 1), st.hkv_l, dst.max_seq)
+        if weights is not None:
+            _device_tensor(weights, "weights", (st.n_layers, batch, st.hkv_l, self.max_seq), torch.float32)
+        with torch.cuda.stream(stream):                        # results from the memory of the stream that the call is on
+            slots = torch.empty(shape, dtype=torch.int32, device="cuda")
+            left = weights if weights is None or dst is self else torch.empty(shape, dtype=torch.float32, device="cuda")
+        _check(lib.hexgen_kv_cache_evict(self.handle, dst.handle, keep, sinks, recent, None if weights is None else weights.data_ptr(),
+                                         None if left is None else left.data_ptr(), int(rotate), slots.data_ptr(), _stream_handle(stream)), "hexgen_kv_cache_evict")
+        return slots, left
 
 
 class Tree:

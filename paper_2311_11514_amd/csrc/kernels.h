@@ -217,6 +217,67 @@ void f32_launch_tree_attn(const float *q, int64_t ldq, const TreeIn &in, float *
 void f32_launch_tree_keep(float *kc, float *vc, int64_t layer_stride, int layers, KvGeom kg, int batch, const int32_t *lens, const int32_t *cu,
                           const int32_t *kept, const int32_t *path, hipStream_t s);
 
+// ---- windowed rows (kernels_bf16_window.hip, kernels_f32_window.hip) ---------------------------------------------
+constexpr int kWinSeqs = 256;             // sequences of one launch
+constexpr int kWinMaxSplit = 32;          // runs that a row's tiles are cut into
+// New rows of sequences seq0 .. seq0 + batch - 1, which stand behind the committed contexts: rows cu[i] .. cu[i + 1] - 1 of the call's are the ith one's.
+// The row at slot p attends slots j <= p with p - j < window or j < sinks.  Passed by value: a launch needs no copy to the device, and can be recorded.
+struct WinCall {
+    int seq0, batch, max_n, rows;         // rows: of the whole call
+    int window, sinks, max_seq;           // window, sinks: at most kWinFar
+    int32_t cu[kWinSeqs + 1];
+    uint8_t order[kWinSeqs];              // the nth sequence to be dispatched
+};
+constexpr int kWinFar = 1 << 30;
+// How a launch is laid out: a row's tiles are cut into runs of `chunk`, or longer ones where nsplit runs would not reach the end
+struct WinPlan {
+    bool shared;                          // 16 bits: blocks of 128 rows that share tiles through LDS, not cut; otherwise blocks of 32 (fp32: 16)
+    int nsplit, chunk;
+    float *part_o, *part_ml;              // as in TreePlan
+    unsigned *arrived;
+    float *stat;                          // [rows][hq][2], or NULL: a row's largest score and the reciprocal of its sum, for the weights
+};
+inline int win_row_blocks(int max_n, int G, int rows) { return (int)(((int64_t)max_n * G + rows - 1) / rows); }
+// Caller-owned accumulators of attention weights, [sequence of the cache's batch][kv head][max_seq]
+void f32_launch_win_rope_append(const float *qkv, int hq_l, KvGeom kg, const WinCall &wc, const int32_t *lens, const float *cos_tab, const float *sin_tab,
+                                float *q, float *kc, float *vc, hipStream_t s);
+void f32_launch_win_append(const TreeIn &in, float *kc, float *vc, KvGeom kg, const WinCall &wc, const int32_t *lens, hipStream_t s);
+void f32_launch_win_attn(const float *q, int64_t ldq, const TreeIn &in, float *kc, float *vc, KvGeom kg, int hq_l, const WinCall &wc, const int32_t *lens,
+                         const WinPlan &wp, float *o, hipStream_t s);
+void f32_launch_win_weights(const float *q, int64_t ldq, const float *kc, KvGeom kg, int hq_l, const WinCall &wc, const int32_t *lens, const float *stat,
+                            float *weights, int max_tiles, hipStream_t s);
+void launch_win_advance(int32_t *lens, const WinCall &wc, hipStream_t s);          // lens += the call's rows, up to max_seq
+
+// ---- eviction ----------------------------------------------------------------------------------------------------------
+// Per (layer, sequence, kv head) of [layers][batch][hkv]: which of n = min(lens, max_seq) slots stay, in order, -1 behind them (slots: rows of dst_seq), and their
+// weights to the front (rows of max_seq -> rows of dst_seq; out == w and dst_seq == max_seq: in place)
+struct EvictCall {
+    int layers, batch, hkv, max_seq, dst_seq, keep, sinks, recent;
+    const float *w;
+    float *w_out;
+    int32_t *slots;
+};
+void launch_evict_select(const EvictCall &ec, const int32_t *lens, hipStream_t s);
+// the kept rows of a cache, src -> dst (the same memory: in place), keys rotated back by how far they move where cos_tab is given; then
+// dst_lens = what is left, zero behind the batch
+struct EvictMove {
+    const void *ks, *vs;
+    void *kd, *vd;
+    int64_t src_layer, dst_layer;         // elements between layers
+    KvGeom src, dst;
+    const float *cos_tab, *sin_tab;
+    const int32_t *lens;
+    int32_t *dst_lens;
+    int dst_batch;                        // entries of dst_lens
+};
+// blocks that share a unit's chunks of 32 rows; in place one takes them all, in order
+inline int evict_blocks(const EvictCall &ec, const EvictMove &m) {
+    if (m.ks == m.kd) return 1;
+    const int rows = ec.keep < ec.dst_seq ? ec.keep : ec.dst_seq;
+    return (rows + 31) / 32;
+}
+void f32_launch_evict_move(const EvictCall &ec, const EvictMove &m, hipStream_t s);
+
 // ---- 4-bit weights (kernels_q4.hip) ---------------------------------------------------------------------------------
 enum { HX_T_F32 = 0, HX_T_BF16 = 1, HX_T_F16 = 2 };     // = hexgen_dtype_t
 struct Q4View {

@@ -1,0 +1,670 @@
+// Attention of new rows over the cache with a sliding window and first positions that stay visible, 16-bit types: appending the rows, the attention, the
+// sums of its weights, and the move of what an eviction keeps.  Compiled once per 16-bit element type (see common.h) into namespace HX_NS.
+//
+// The G query heads of a kv head and the n new rows of a sequence make R = n G query rows (row r: new row r / G, head r % G) that share the tiles of the
+// cache, as the nodes of a drafted tree do; here a row attends slots j <= p with p - j < window or j < sinks, so that blocks of rows have tile lists
+// of their own (WinTiles), most of them without a mask.
+#include <algorithm>
+#include <type_traits>
+
+#include "attn_rows.h"
+#include "window.h"
+
+namespace HX_NS {
+
+// ---- appending ------------------------------------------------------------------------------------------------------
+// The stage's fused projection, raw fp32 [rows][N], columns in the order of its packed tiles -> rotary embedding at len + row, q as plain rows (in two parts
+// where q_lo is given), k and v into the cache.  A thread takes four rotary pairs.
+__global__ __launch_bounds__(256) void win_rope_append_kernel(const float *__restrict__ qkv, int hq_l, KvGeom kg, WinCall wc, const int32_t *__restrict__ lens,
+                                                              const float *__restrict__ cos_tab, const float *__restrict__ sin_tab, h16_t *__restrict__ q,
+                                                              h16_t *__restrict__ q_lo, h16_t *__restrict__ kc, h16_t *__restrict__ vc) {
+    const int d = kg.d, half = d >> 1, tph = d >> 4, heads = hq_l + 2 * kg.hkv_l;
+    const unsigned idx = blockIdx.x * 256u + threadIdx.x, per_row = heads * tph * 2;
+    const int first = wc.cu[0], t = first + (int)(idx / per_row), rem = idx % per_row, head = rem / (2 * tph), tl = (rem >> 1) % tph, i0 = 8 * tl + 4 * (rem & 1);
+    if (t >= wc.cu[wc.batch]) return;
+    int lo_seq = 0, hi_seq = wc.batch;                        // the last sequence whose first row is not behind t
+    while (hi_seq - lo_seq > 1) {
+        const int mid = (lo_seq + hi_seq) >> 1;
+        if (wc.cu[mid] <= t) lo_seq = mid;
+        else hi_seq = mid;
+    }
+    const int seq = wc.seq0 + lo_seq, slot = lens[seq] + t - wc.cu[lo_seq];
+    if (slot >= wc.max_seq) return;
+    const float *src = qkv + (size_t)t * heads * d + (size_t)(head * tph + tl) * 16 + 4 * (rem & 1);
+    floatx4 lo = *reinterpret_cast<const floatx4 *>(src), hi = *reinterpret_cast<const floatx4 *>(src + 8);
+    if (head < hq_l + kg.hkv_l) {
+        const size_t at = (size_t)slot * half + i0;
+        const floatx4 c4 = *reinterpret_cast<const floatx4 *>(cos_tab + at), s4 = *reinterpret_cast<const floatx4 *>(sin_tab + at);
+        const floatx4 l = lo * c4 - hi * s4;
+        hi = hi * c4 + lo * s4;
+        lo = l;
+    }
+    union { uint2 u; h16_t x[4]; } a, b, al, bl;             // the element type's parts of both halves' four elements, and what they leave
+    split_pack2(lo[0], lo[1], a.u.x, al.u.x);
+    split_pack2(lo[2], lo[3], a.u.y, al.u.y);
+    split_pack2(hi[0], hi[1], b.u.x, bl.u.x);
+    split_pack2(hi[2], hi[3], b.u.y, bl.u.y);
+    if (head < hq_l) {
+        const size_t at = ((size_t)t * hq_l + head) * d + i0;
+        *reinterpret_cast<uint2 *>(q + at) = a.u;
+        *reinterpret_cast<uint2 *>(q + at + half) = b.u;
+        if (q_lo != nullptr) {
+            *reinterpret_cast<uint2 *>(q_lo + at) = al.u;
+            *reinterpret_cast<uint2 *>(q_lo + at + half) = bl.u;
+        }
+        return;
+    }
+    const bool key = head < hq_l + kg.hkv_l;
+    const size_t slab = (size_t)seq * kg.seq_stride + (size_t)(head - hq_l - (key ? 0 : kg.hkv_l)) * kg.smax * d;
+    if (key) {
+        *reinterpret_cast<uint2 *>(kc + slab + kv_k_offset(slot, i0, d)) = a.u;
+        *reinterpret_cast<uint2 *>(kc + slab + kv_k_offset(slot, half + i0, d)) = b.u;
+    } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            vc[slab + kv_v_offset(slot, i0 + x, d)] = a.x[x];
+            vc[slab + kv_v_offset(slot, half + i0 + x, d)] = b.x[x];
+        }
+    }
+}
+void launch_win_rope_append(const float *qkv, int hq_l, KvGeom kg, const WinCall &wc, const int32_t *lens, const float *cos_tab, const float *sin_tab,
+                            h16_t *q, h16_t *q_lo, h16_t *kc, h16_t *vc, hipStream_t s) {
+    const unsigned n = (unsigned)(wc.cu[wc.batch] - wc.cu[0]) * (hq_l + 2 * kg.hkv_l) * (kg.d >> 4) * 2;
+    hipLaunchKernelGGL(win_rope_append_kernel, dim3((n + 255) / 256), dim3(256), 0, s, qkv, hq_l, kg, wc, lens, cos_tab, sin_tab, q, q_lo, kc, vc);
+}
+
+// Plain rows into the cache, a block per tile of 32 slots: K in pieces of 16 bytes, V through LDS, so that the tile's transposed pieces are written whole
+template <int D>
+__global__ __launch_bounds__(256) void win_append_kernel(TreeIn in, h16_t *__restrict__ kc, h16_t *__restrict__ vc, KvGeom kg, WinCall wc, const int32_t *__restrict__ lens) {
+    constexpr int P8 = D / 8, PIECES = 32 * P8 / 256;
+    __shared__ __align__(16) h16_t s_v[32][D + 8];
+    const int nth = blockIdx.z, seq = wc.seq0 + nth, c = blockIdx.y, row0 = wc.cu[nth], len = lens[seq];
+    const int n = min(wc.cu[nth + 1] - row0, wc.max_seq - len), t = (len >> 5) + blockIdx.x;
+    if (32 * t >= len + n || n <= 0) return;
+    const size_t slab = (size_t)seq * kg.seq_stride + (size_t)c * kg.smax * D;
+    uint4 k[PIECES], v[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int idx = threadIdx.x + 256 * i, e = c * D + 8 * (idx % P8), x = min(max(32 * t + idx / P8 - len, 0), n - 1);
+        k[i] = *reinterpret_cast<const uint4 *>(static_cast<const h16_t *>(in.k) + (size_t)(row0 + x) * in.ldk + e);
+        v[i] = *reinterpret_cast<const uint4 *>(static_cast<const h16_t *>(in.v) + (size_t)(row0 + x) * in.ldv + e);
+    }
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int idx = threadIdx.x + 256 * i, pos = idx / P8, dd = 8 * (idx % P8), x = 32 * t + pos - len;
+        *reinterpret_cast<uint4 *>(&s_v[pos][dd]) = v[i];
+        if (x >= 0 && x < n) *reinterpret_cast<uint4 *>(kc + slab + kv_k_offset(32 * t + pos, dd, D)) = k[i];
+    }
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < 4 * D; idx += 256) {
+        const int dd = idx % D, g = idx / D;                  // kvlayout.h: positions 4 g .. 4 g + 3 and 16 + 4 g .. + 3 of element dd are 16 bytes
+        union { uint4 u; h16_t e[8]; } w;
+        bool whole = true;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int pos = 4 * g + (j & 3) + 16 * (j >> 2), x = 32 * t + pos - len;
+            w.e[j] = s_v[pos][dd];
+            whole = whole && x >= 0 && x < n;
+        }
+        h16_t *dst = vc + slab + kv_v_offset(32 * t + 4 * g, dd, D);
+        if (whole) {
+            *reinterpret_cast<uint4 *>(dst) = w.u;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int x = 32 * t + 4 * g + (j & 3) + 16 * (j >> 2) - len;
+                if (x >= 0 && x < n) dst[j] = w.e[j];
+            }
+        }
+    }
+}
+void launch_win_append(const TreeIn &in, h16_t *kc, h16_t *vc, KvGeom kg, const WinCall &wc, const int32_t *lens, hipStream_t s) {
+    const dim3 grid(wc.max_n / 32 + 2, kg.hkv_l, wc.batch);  // a sequence's rows may begin and end inside a tile
+    if (kg.d == 128) hipLaunchKernelGGL(win_append_kernel<128>, grid, dim3(256), 0, s, in, kc, vc, kg, wc, lens);
+    else hipLaunchKernelGGL(win_append_kernel<64>, grid, dim3(256), 0, s, in, kc, vc, kg, wc, lens);
+}
+
+// ---- attention, few rows ----------------------------------------------------------------------------------------------
+// A block of eight waves takes 32 query rows and a run of their tiles, which the waves take in turn, K and V straight to registers in the operands'
+// layout (the next unmasked tile's K is requested before this tile's softmax); the waves meet in LDS.  S^T = K . Q^T and O^T = V^T . P^T with P in
+// two parts (tree_pack2).  Rows that are not in the cache yet (in.k != NULL: a sequence's rows are one block's then) are put over the tile and appended by
+// the run that holds their tile.  Runs leave (m, l, o) with device-scope stores; the last to arrive joins them in the order of the context.
+// A weight of zero times an infinity would be a NaN: a masked tile with a value that is not finite is multiplied out over what each row attends.
+template <int D, bool QLO>
+__global__ __launch_bounds__(512, 2) void win_few_kernel(const h16_t *__restrict__ q, const h16_t *__restrict__ q_lo, int64_t ldq, TreeIn in, h16_t *kc, h16_t *vc,
+                                                         KvGeom kg, int hq_l, int G, int nrb, WinCall wc, const int32_t *__restrict__ lens, WinPlan wp, TreeOut out,
+                                                         float scale_log2e) {
+    constexpr int W = 8, KT = D / 32, DT = D / 16, DB = D / 32, OS = D + 4;
+    __shared__ __align__(16) float s_o[W][32 * OS];
+    __shared__ h16x8 s_q[QLO ? 2 : 1][2 * KT][64];
+    __shared__ float s_m[W][32], s_l[W][32];
+    __shared__ int s_last;
+    WinWork wk;
+    const bool fresh = in.k != nullptr;
+    if (!wk.find(kg.hkv_l, G, nrb, 32, wc, lens, wp, fresh)) return;
+    const int len = wk.len, R = wk.R, row0 = wk.row0;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hl = lane >> 5, i32 = lane & 31;
+    const int sub = i32 >> 4, fl = (lane & 15) + 16 * hl;
+    const int rr = min(wk.rb * 32 + i32, R - 1), node = rr / G, head = wk.c * G + (rr - node * G);    // rows past the last repeat it and are not stored
+    const int qpos = len + node;
+    const size_t slab = (size_t)wk.seq * kg.seq_stride + (size_t)wk.c * kg.smax * D;
+    h16_t *kslab = kc + slab, *vslab = vc + slab;
+    h16x8 kf[2 * KT], vf[2 * DB];
+    const int clean = min(wk.v1, wk.tiles.clean);
+    // K: lane l takes position l % 32, elements 16 kk + 8 (l / 32) ..; a new row's slot comes from the row
+    auto load_k = [&](int t, auto tail) {
+        const h16_t *src = kslab + ((size_t)(2 * t + sub) * KT * 64 + fl) * 8;
+        const int x = 32 * t + i32 - len;
+        if (decltype(tail)::value && fresh && x >= 0 && x < wk.n) {
+            const h16_t *row = static_cast<const h16_t *>(in.k) + (size_t)(row0 + x) * in.ldk + wk.c * D + 8 * hl;
+#pragma unroll
+            for (int kk = 0; kk < 2 * KT; ++kk) kf[kk] = *reinterpret_cast<const h16x8 *>(row + 16 * kk);
+        } else {
+#pragma unroll
+            for (int kk = 0; kk < 2 * KT; ++kk) kf[kk] = *reinterpret_cast<const h16x8 *>(src + ((kk >> 1) * 64 + 32 * (kk & 1)) * 8);
+        }
+    };
+    static_assert(2 * KT <= W, "a piece of the query rows per wave");
+    h16x8 qf, ql;
+    const size_t q_at = (size_t)(row0 + node) * ldq + (size_t)head * D + 16 * wave + 8 * hl;
+    if (wave < 2 * KT) {
+        qf = *reinterpret_cast<const h16x8 *>(q + q_at);
+        if constexpr (QLO) ql = *reinterpret_cast<const h16x8 *>(q_lo + q_at);
+    }
+    int v = wk.v0 + wave;
+    if (v < clean) load_k(wk.tiles.at(v), std::false_type{});
+    if (wave < 2 * KT) {
+        s_q[0][wave][lane] = qf;
+        if constexpr (QLO) s_q[1][wave][lane] = ql;
+    }
+    HX_LDS_BARRIER();
+    floatx16 oacc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) oacc[db][x] = 0.f;
+    float m = NEG_INF, lsum = 0.f;
+    // a tile that every row attends and the cache holds (TAIL false), or one that needs a mask or new rows
+    auto walk = [&](int t, auto tail) {
+        constexpr bool TAIL = decltype(tail)::value;
+        if constexpr (TAIL) load_k(t, tail);
+        const bool patch = TAIL && fresh && 32 * t + 31 >= len;     // the same in every lane
+        // V^T: lane l takes element 32 db + l % 32 and k-group 2 h + l / 32 (kvlayout.h)
+        const h16_t *vsrc = vslab + ((size_t)(t * DT + sub) * 64 + fl) * 8;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) vf[2 * db + h] = *reinterpret_cast<const h16x8 *>(vsrc + (2 * db * 64 + 32 * h) * 8);
+        // the new rows' values among them, all requested at once (slots of others take some row, not used)
+        union Piece { h16x8 v; h16_t e[8]; uint32_t u[4]; } own[TAIL ? 2 * DB : 1];
+        uint32_t sees = 0xffffffffu;
+        if constexpr (TAIL) {
+            if (patch) {
+                const h16_t *rows = static_cast<const h16_t *>(in.v) + (size_t)row0 * in.ldv + wk.c * D + i32;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int x = 32 * t + (j & 3) + 4 * (2 * h + hl) + 16 * (j >> 2) - len;
+                        const h16_t *row = rows + min(max(x, 0), wk.n - 1) * in.ldv;
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) own[2 * db + h].e[j] = row[32 * db];
+                    }
+            }
+            sees = win_sees(32 * t, qpos, wc.window, wc.sinks);
+        }
+        floatx16 sc;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) sc[x] = 0.f;
+#pragma unroll
+        for (int part = QLO ? 1 : 0; part >= 0; --part) {
+#pragma unroll
+            for (int kk = 0; kk < 2 * KT; ++kk) sc = hx_mfma32(kf[kk], s_q[part][kk][lane], sc);
+            if (part > 0) __builtin_amdgcn_sched_barrier(0);      // one part's pieces at a time in registers
+        }
+        if constexpr (TAIL) {
+            if (patch) {
+                // over what the cache held there, which gets what has been put together
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int x = 32 * t + 2 * (i & 1) + 4 * (2 * h + hl) + 16 * (i >> 1) - len;     // of elements 2 i and 2 i + 1
+                        const uint32_t take = (x >= 0 && x < wk.n ? 0xffffu : 0u) | (x >= -1 && x < wk.n - 1 ? 0xffff0000u : 0u);
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) {
+                            Piece w;
+                            w.v = vf[2 * db + h];
+                            w.u[i] = (own[2 * db + h].u[i] & take) | (w.u[i] & ~take);
+                            vf[2 * db + h] = w.v;
+                        }
+                    }
+                const int x = 32 * t + i32 - len;
+                h16_t *dst = kslab + ((size_t)(2 * t + sub) * KT * 64 + fl) * 8;
+                if (x >= 0 && x < wk.n) {
+#pragma unroll
+                    for (int kk = 0; kk < 2 * KT; ++kk) *reinterpret_cast<h16x8 *>(dst + ((kk >> 1) * 64 + 32 * (kk & 1)) * 8) = kf[kk];
+                }
+                h16_t *vdst = vslab + ((size_t)(t * DT + sub) * 64 + fl) * 8;      // whole pieces: slots that are not the rows' keep their values
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) *reinterpret_cast<h16x8 *>(vdst + (2 * db * 64 + 32 * h) * 8) = vf[2 * db + h];
+            }
+#pragma unroll
+            for (int x = 0; x < 16; ++x) sc[x] = (sees >> (8 * (x >> 2) + 4 * hl + (x & 3))) & 1u ? sc[x] : NEG_INF;
+        }
+        if (!TAIL && v + W < clean) load_k(wk.tiles.at(v + W), std::false_type{});
+        const float alpha = tree_softmax(sc, m, lsum, scale_log2e);
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) oacc[db][x] *= alpha;
+        if constexpr (TAIL) {
+            bool odd = false;
+#pragma unroll
+            for (int x = 0; x < 2 * DB; ++x) odd = odd || any_odd(vf[x]);
+            if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+                h16x8 *vt = reinterpret_cast<h16x8 *>(s_o[wave]);      // the wave's own part of the merge buffer, not in use yet
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) vt[(2 * db + sub) * 64 + fl + 32 * h] = vf[2 * db + h];
+                tree_slow_tile<DB>(reinterpret_cast<const h16_t *>(vt), sc, sees, lane, oacc);
+                return;
+            }
+        }
+        TreeP p[2], lo[2];
+        tree_pack(sc, p, lo);
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                oacc[db] = hx_mfma32(vf[2 * db + g], lo[g].v, oacc[db]);
+                oacc[db] = hx_mfma32(vf[2 * db + g], p[g].v, oacc[db]);
+            }
+    };
+    for (; v < clean; v += W) walk(wk.tiles.at(v), std::false_type{});
+    for (; v < wk.v1; v += W) walk(wk.tiles.at(v), std::true_type{});
+    const int live = min(W, wk.v1 - wk.v0);                   // waves that had a tile
+    if (wave < live) {
+        lsum = sum_halves(lsum);
+        if (hl == 0) { s_m[wave][i32] = m; s_l[wave][i32] = lsum; }
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int qd = 0; qd < 4; ++qd)
+                *reinterpret_cast<floatx4 *>(&s_o[wave][i32 * OS + 32 * db + 8 * qd + 4 * hl]) =
+                    floatx4{oacc[db][4 * qd], oacc[db][4 * qd + 1], oacc[db][4 * qd + 2], oacc[db][4 * qd + 3]};
+    }
+    __syncthreads();
+    const int nb = wk.runs(), rows = min(32, R - wk.rb * 32);
+    const size_t part_row = (size_t)wc.rows * hq_l;
+    constexpr int TP = D / 4, QUADS = 32 * TP / 512;              // threads of a row, and quads of a thread: rows threadIdx.x / TP + i 512 / TP
+    const int dd = 4 * (threadIdx.x % TP);
+    auto finish = [&](int t, int hd, const float (&o)[4], float M, float L) {
+        const float inv = 1.0f / L, x[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+        tree_store4(out, t, hd * D + dd, x);
+        if (wp.stat != nullptr && dd == 0) *reinterpret_cast<float2 *>(wp.stat + 2 * ((size_t)t * hq_l + hd)) = float2{M, inv};
+    };
+#pragma unroll
+    for (int i = 0; i < QUADS; ++i) {
+        const int row = threadIdx.x / TP + i * (512 / TP), at = wk.rb * 32 + row;
+        if (row >= rows) break;
+        float M = NEG_INF, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < W; ++w) M = fmaxf(M, s_m[min(w, live - 1)][row]);
+        const float b = M == NEG_INF ? 0.f : M;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            if (w >= live) break;
+            const float wt = __builtin_amdgcn_exp2f((s_m[w][row] - b) * scale_log2e);
+            const floatx4 x4 = *reinterpret_cast<const floatx4 *>(&s_o[w][row * OS + dd]);
+            L += s_l[w][row] * wt;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[x] += x4[x] * wt;
+        }
+        const int t = row0 + at / G, hd = wk.c * G + at % G;
+        if (nb == 1) {
+            finish(t, hd, o, M, L);
+        } else {
+            const size_t e = wk.split * part_row + (size_t)t * hq_l + hd;
+            dev_store2(wp.part_o + e * D + dd, o[0], o[1]);
+            dev_store2(wp.part_o + e * D + dd + 2, o[2], o[3]);
+            if (dd == 0) dev_store2(wp.part_ml + 2 * e, M, L);
+        }
+    }
+    if (nb == 1) return;
+    if (!tree_arrive(wp.arrived + ((size_t)wk.nth * kg.hkv_l + wk.c) * nrb + wk.rb, nb, &s_last)) return;
+    // the last block: a thread requests the (m, l) and sums of its quads of eight runs at once
+#pragma unroll
+    for (int i = 0; i < QUADS; ++i) {
+        const int row = threadIdx.x / TP + i * (512 / TP), at = wk.rb * 32 + row;
+        if (row >= rows) break;
+        const int t = row0 + at / G, hd = wk.c * G + at % G;
+        const size_t e = (size_t)t * hq_l + hd;
+        float M = NEG_INF, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int u0 = 0; u0 < nb; u0 += 8) {
+            float2 ml[8], a[8], b[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const size_t at_u = min(u0 + u, nb - 1) * part_row + e;
+                ml[u] = dev_load2(wp.part_ml + 2 * at_u);
+                a[u] = dev_load2(wp.part_o + at_u * D + dd);
+                b[u] = dev_load2(wp.part_o + at_u * D + dd + 2);
+            }
+            float M8 = M;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) M8 = fmaxf(M8, ml[u].x);
+            const float base = M8 == NEG_INF ? 0.f : M8, alpha = __builtin_amdgcn_exp2f((M - base) * scale_log2e);
+            M = M8;
+            L *= alpha;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[x] *= alpha;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                if (u0 + u >= nb) break;
+                const float wt = __builtin_amdgcn_exp2f((ml[u].x - base) * scale_log2e);
+                L += ml[u].y * wt;
+                o[0] += a[u].x * wt; o[1] += a[u].y * wt; o[2] += b[u].x * wt; o[3] += b[u].y * wt;
+            }
+        }
+        finish(t, hd, o, M, L);
+    }
+}
+
+// ---- attention, many rows ---------------------------------------------------------------------------------------------
+// A block of four waves takes 128 query rows, 32 a wave; their tiles go from HBM to LDS directly, three in flight, and are shared.  Products and softmax as
+// above.  The rows are in the cache already.
+template <int D>
+__global__ __launch_bounds__(256, 3) void win_attn_kernel(const h16_t *__restrict__ q, int64_t ldq, const h16_t *__restrict__ kc, const h16_t *__restrict__ vc, KvGeom kg,
+                                                          int hq_l, int G, int nrb, WinCall wc, const int32_t *__restrict__ lens, WinPlan wp, TreeOut out,
+                                                          float scale_log2e) {
+    constexpr int RW = 4, S = 3, ROWS = 32 * RW;
+    constexpr int KT = D / 32, DT = D / 16, DB = D / 32, TILES = 2 * KT + DT;
+    constexpr int LPT = TILES / RW;                       // 1 KB loads per wave and step
+    __shared__ h16x8 stage[S][TILES][64];
+    WinWork wk;
+    if (!wk.find(kg.hkv_l, G, nrb, ROWS, wc, lens, wp, false)) return;
+    const int len = wk.len, R = wk.R, row0 = wk.row0, steps = wk.tiles.nt;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hl = lane >> 5;
+    const int r = wk.rb * ROWS + wave * 32 + (lane & 31);
+    const int rr = min(r, R - 1), node = rr / G, head = wk.c * G + (rr - node * G);    // rows past the last repeat it and are not stored
+    const int qpos = len + node;
+    const int r0w = wk.rb * ROWS + wave * 32;             // the wave's slots; none if it has no row: it feeds the others
+    const bool idle = r0w >= R;
+    const int p_lo = len + min(r0w, R - 1) / G, p_hi = len + min(r0w + 31, R - 1) / G;
+
+    h16x8 qf[2 * KT];
+#pragma unroll
+    for (int kk = 0; kk < 2 * KT; ++kk) qf[kk] = *reinterpret_cast<const h16x8 *>(q + (size_t)(row0 + node) * ldq + (size_t)head * D + 16 * kk + 8 * hl);
+    floatx16 oacc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) oacc[db][x] = 0.f;
+    float m = NEG_INF, lsum = 0.f;
+
+    const size_t slab = (size_t)wk.seq * kg.seq_stride + (size_t)wk.c * kg.smax * D;
+    const h16x8 *ks = reinterpret_cast<const h16x8 *>(kc + slab), *vs = reinterpret_cast<const h16x8 *>(vc + slab);
+    const unsigned lane_bytes = (unsigned)lane * 16u;
+    auto issue = [&](int step) {
+        const int t = wk.tiles.at(step);
+#pragma unroll
+        for (int x = 0; x < LPT; ++x) {
+            const int tile = wave + RW * x;
+            const h16x8 *src = tile < 2 * KT ? ks + (size_t)(2 * t * KT + tile) * 64 : vs + (size_t)(t * DT + tile - 2 * KT) * 64;
+            hx_load_lds16(hx_lds_addr(&stage[step % S][tile][0]), lane_bytes, src);
+        }
+    };
+    const int sub = (lane & 31) >> 4, fl = (lane & 15) + 16 * hl;
+    HX_WAIT_VM(0);            // the query rows have landed before the first load that the compiler does not see
+    issue(0);
+    if (steps > 1) issue(1);
+    // a step whose tile every row of the block attends (TAIL false), or one that needs a mask
+    auto walk = [&](int step, auto tail) {
+        constexpr bool TAIL = decltype(tail)::value;
+        if (step + 1 < steps) HX_WAIT_VM(LPT);            // step + 1 may stay in flight
+        else HX_WAIT_VM(0);
+        HX_LDS_BARRIER();
+        if (step + S - 1 < steps) issue(step + S - 1);    // into the buffer that every wave has left
+        const int t = wk.tiles.at(step);
+        if (idle || (TAIL && !win_any(32 * t, 32, p_lo, p_hi, wc.window, wc.sinks))) return;
+        const h16x8(*st)[64] = stage[step % S];
+        floatx16 sc;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) sc[x] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < 2 * KT; ++kk) sc = hx_mfma32(st[sub * KT + (kk >> 1)][fl + 32 * (kk & 1)], qf[kk], sc);
+        uint32_t sees = 0xffffffffu;
+        if constexpr (TAIL) {
+            sees = win_sees(32 * t, qpos, wc.window, wc.sinks);
+#pragma unroll
+            for (int x = 0; x < 16; ++x) sc[x] = (sees >> (8 * (x >> 2) + 4 * hl + (x & 3))) & 1u ? sc[x] : NEG_INF;
+        }
+        const float alpha = tree_softmax(sc, m, lsum, scale_log2e);
+        if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) oacc[db][x] *= alpha;
+        }
+        if constexpr (TAIL) {
+            bool odd = false;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) odd = odd || any_odd(st[2 * KT + dt][lane]);
+            if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+                tree_slow_tile<DB>(reinterpret_cast<const h16_t *>(st[2 * KT]), sc, sees, lane, oacc);
+                return;
+            }
+        }
+        TreeP p[2], lo[2];
+        tree_pack(sc, p, lo);
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const h16x8 x = st[2 * KT + 2 * db + sub][fl + 32 * g];
+                oacc[db] = hx_mfma32(x, lo[g].v, oacc[db]);
+                oacc[db] = hx_mfma32(x, p[g].v, oacc[db]);
+            }
+    };
+    int step = 0;
+    for (; step < wk.tiles.clean; ++step) walk(step, std::false_type{});
+    for (; step < steps; ++step) walk(step, std::true_type{});
+    lsum = sum_halves(lsum);
+    if (r >= R) return;
+    const float inv = 1.0f / lsum;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int qd = 0; qd < 4; ++qd) {
+            const float x[4] = {oacc[db][4 * qd] * inv, oacc[db][4 * qd + 1] * inv, oacc[db][4 * qd + 2] * inv, oacc[db][4 * qd + 3] * inv};
+            tree_store4(out, row0 + node, head * D + 32 * db + 8 * qd + 4 * hl, x);
+        }
+    if (wp.stat != nullptr && hl == 0) *reinterpret_cast<float2 *>(wp.stat + 2 * ((size_t)(row0 + node) * hq_l + head)) = float2{m, inv};
+}
+
+void launch_win_attn(const h16_t *q, const h16_t *q_lo, int64_t ldq, const TreeIn &in, h16_t *kc, h16_t *vc, KvGeom kg, int hq_l, const WinCall &wc,
+                     const int32_t *lens, const WinPlan &wp, const TreeOut &out, hipStream_t s) {
+    const int G = hq_l / kg.hkv_l, nrb = win_row_blocks(wc.max_n, G, wp.shared ? 128 : 32);
+    const float scale_log2e = 1.4426950408889634f / sqrtf((float)kg.d);
+    const dim3 grid((unsigned)nrb * (unsigned)((wc.batch * kg.hkv_l * wp.nsplit + 7) / 8 * 8));
+#define HX_WIN_D(DD)                                                                                                                                               \
+    do {                                                                                                                                                           \
+        if (wp.shared) hipLaunchKernelGGL((win_attn_kernel<DD>), grid, dim3(256), 0, s, q, ldq, kc, vc, kg, hq_l, G, nrb, wc, lens, wp, out, scale_log2e);          \
+        else if (q_lo != nullptr) hipLaunchKernelGGL((win_few_kernel<DD, true>), grid, dim3(512), 0, s, q, q_lo, ldq, in, kc, vc, kg, hq_l, G, nrb, wc, lens, wp, out, scale_log2e); \
+        else hipLaunchKernelGGL((win_few_kernel<DD, false>), grid, dim3(512), 0, s, q, q_lo, ldq, in, kc, vc, kg, hq_l, G, nrb, wc, lens, wp, out, scale_log2e);    \
+    } while (0)
+    if (kg.d == 128) HX_WIN_D(128);
+    else HX_WIN_D(64);
+#undef HX_WIN_D
+}
+
+// ---- the weights' sums ------------------------------------------------------------------------------------------------
+// weights[j] += sum over the call's rows and a kv head's query heads of exp(s_rj - m_r) / l_r: the scores once more, now that every row's maximum and sum
+// are known.  A wave keeps the keys of one tile in registers and goes through the rows that attend it in groups of 32; the sums stay in its lanes (lane: a
+// column of every group) and meet at the end, in one order: every position belongs to one wave, nothing is added atomically.
+template <int D, bool QLO>
+__global__ __launch_bounds__(256, 4) void win_weights_kernel(const h16_t *__restrict__ q, const h16_t *__restrict__ q_lo, int64_t ldq, const h16_t *__restrict__ kc, KvGeom kg,
+                                                             int hq_l, int G, int tile_blocks, WinCall wc, const int32_t *__restrict__ lens, const float *__restrict__ stat,
+                                                             float *__restrict__ weights, float scale_log2e) {
+    constexpr int KT = D / 32;
+    const int tb = blockIdx.x % tile_blocks, c = (blockIdx.x / tile_blocks) % kg.hkv_l, nth = blockIdx.x / tile_blocks / kg.hkv_l;
+    const int seq = wc.seq0 + nth, row0 = wc.cu[nth], len = lens[seq], n = min(wc.cu[nth + 1] - row0, wc.max_seq - len), R = n * G;
+    if (n <= 0) return;
+    WinTiles tiles;
+    tiles.set(len, len + n - 1, wc.window, wc.sinks, 0);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hl = lane >> 5, i32 = lane & 31;
+    const int sub = i32 >> 4, fl = (lane & 15) + 16 * hl;
+    for (int v = 4 * tb + wave; v < tiles.nt; v += 4 * tile_blocks) {
+        const int t = tiles.at(v), p0 = 32 * t;
+        const h16_t *src = kc + (size_t)seq * kg.seq_stride + (size_t)c * kg.smax * D + ((size_t)(2 * t + sub) * KT * 64 + fl) * 8;
+        h16x8 kf[2 * KT];
+#pragma unroll
+        for (int kk = 0; kk < 2 * KT; ++kk) kf[kk] = *reinterpret_cast<const h16x8 *>(src + ((kk >> 1) * 64 + 32 * (kk & 1)) * 8);
+        // new rows that attend one of its positions: from the first at or behind the tile to the last whose window reaches it
+        const int x_lo = max(0, p0 - len), x_hi = p0 < wc.sinks ? n - 1 : min(n - 1, p0 + 31 + wc.window - 1 - len);
+        floatx16 acc;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) acc[x] = 0.f;
+        for (int g = x_lo * G / 32; g <= (x_hi * G + G - 1) / 32; ++g) {
+            const int r = 32 * g + i32, rr = min(r, R - 1), node = rr / G, head = c * G + (rr - node * G);
+            const size_t at = (size_t)(row0 + node) * ldq + (size_t)head * D + 8 * hl;
+            const float2 ml = *reinterpret_cast<const float2 *>(stat + 2 * ((size_t)(row0 + node) * hq_l + head));
+            floatx16 sc;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) sc[x] = 0.f;
+            if constexpr (QLO) {
+#pragma unroll
+                for (int kk = 0; kk < 2 * KT; ++kk) sc = hx_mfma32(kf[kk], *reinterpret_cast<const h16x8 *>(q_lo + at + 16 * kk), sc);
+            }
+#pragma unroll
+            for (int kk = 0; kk < 2 * KT; ++kk) sc = hx_mfma32(kf[kk], *reinterpret_cast<const h16x8 *>(q + at + 16 * kk), sc);
+            const float inv = r < R ? ml.y : 0.f;
+            const int first = len + 32 * g / G, last = len + min(32 * g + 31, R - 1) / G;
+            if (win_all(p0, 32, first, last, wc.window, wc.sinks) && 32 * g + 31 < R) {
+#pragma unroll
+                for (int x = 0; x < 16; ++x) acc[x] = fmaf(__builtin_amdgcn_exp2f((sc[x] - ml.x) * scale_log2e), inv, acc[x]);
+            } else {
+                const uint32_t sees = r < R ? win_sees(p0, len + node, wc.window, wc.sinks) : 0u;
+#pragma unroll
+                for (int x = 0; x < 16; ++x) {
+                    const float w = __builtin_amdgcn_exp2f((sc[x] - ml.x) * scale_log2e) * inv;
+                    acc[x] += (sees >> (8 * (x >> 2) + 4 * hl + (x & 3))) & 1u ? w : 0.f;
+                }
+            }
+        }
+        float mine = 0.f;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+            float a = acc[x];
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) a += __shfl_xor(a, o, 64);
+            mine = i32 == x ? a : mine;
+        }
+        const int pos = p0 + 8 * ((i32 & 15) >> 2) + 4 * hl + (i32 & 3);
+        if (i32 < 16 && pos < len + n) {
+            float *dst = weights + ((size_t)seq * kg.hkv_l + c) * wc.max_seq + pos;
+            *dst += mine;
+        }
+    }
+}
+void launch_win_weights(const h16_t *q, const h16_t *q_lo, int64_t ldq, const h16_t *kc, KvGeom kg, int hq_l, const WinCall &wc, const int32_t *lens,
+                        const float *stat, float *weights, int max_tiles, hipStream_t s) {
+    const int G = hq_l / kg.hkv_l, tile_blocks = (max_tiles + 3) / 4;
+    const float scale_log2e = 1.4426950408889634f / sqrtf((float)kg.d);
+    const dim3 grid((unsigned)tile_blocks * kg.hkv_l * wc.batch);
+#define HX_WIN_W(DD, LO) hipLaunchKernelGGL((win_weights_kernel<DD, LO>), grid, dim3(256), 0, s, q, q_lo, ldq, kc, kg, hq_l, G, tile_blocks, wc, lens, stat, weights, scale_log2e)
+    if (kg.d == 128) { if (q_lo != nullptr) HX_WIN_W(128, true); else HX_WIN_W(128, false); }
+    else { if (q_lo != nullptr) HX_WIN_W(64, true); else HX_WIN_W(64, false); }
+#undef HX_WIN_W
+}
+
+// ---- eviction: the move ------------------------------------------------------------------------------------------------
+// The kept rows of one (layer, sequence, kv head): row slots[j] of the source becomes row j.  A block takes chunks of 32 destination rows and
+// reads a chunk whole before it writes it.  In place there is one block for all of them, in order: rows only move to the front
+// (slots[j] >= j, both growing), so that what is written has been read.  K moves in pieces of 16 bytes, V, which lies transposed, through LDS.
+// Keys that are rotated back by their distance are rotated in fp32 and rounded to the element type once more.
+template <int D, bool ROT>
+__global__ __launch_bounds__(256) void evict_move_kernel(EvictCall ec, EvictMove mv, int blocks) {
+    constexpr int P8 = D / 8, PIECES = 32 * P8 / 256, HALF = D / 2;
+    __shared__ __align__(16) h16_t s_v[D][34];                 // [element][row of the chunk]
+    __shared__ int s_slot[32];
+    const unsigned unit = blockIdx.x / (unsigned)blocks;
+    const int chunk = (int)(blockIdx.x % (unsigned)blocks), c = unit % ec.hkv, b = (unit / ec.hkv) % ec.batch, layer = unit / ec.hkv / ec.batch;
+    const int32_t *slots = ec.slots + (size_t)unit * ec.dst_seq;
+    const size_t src = (size_t)layer * mv.src_layer + (size_t)b * mv.src.seq_stride + (size_t)c * mv.src.smax * D;
+    const size_t dst = (size_t)layer * mv.dst_layer + (size_t)b * mv.dst.seq_stride + (size_t)c * mv.dst.smax * D;
+    const h16_t *ks = static_cast<const h16_t *>(mv.ks) + src, *vs = static_cast<const h16_t *>(mv.vs) + src;
+    h16_t *kd = static_cast<h16_t *>(mv.kd) + dst, *vd = static_cast<h16_t *>(mv.vd) + dst;
+    if (blockIdx.x == 0)
+        for (int i = threadIdx.x; i < mv.dst_batch; i += 256) mv.dst_lens[i] = i < ec.batch ? min(min(mv.lens[i], ec.max_seq), ec.keep) : 0;
+    const int most = min(ec.keep, ec.dst_seq);
+    for (int j0 = 32 * chunk; j0 < most; j0 += 32 * blocks) {
+        __syncthreads();
+        if (threadIdx.x < 32) s_slot[threadIdx.x] = j0 + threadIdx.x < most ? slots[j0 + threadIdx.x] : -1;
+        __syncthreads();
+        if (s_slot[0] < 0) break;                              // the same in every thread: the kept ones come first
+        if (mv.ks == mv.kd && s_slot[31] == j0 + 31) continue;  // in place, and none of them moves
+        uint4 k[PIECES];
+        // a thread's piece i: row (threadIdx.x + 256 i) / P8 of the chunk, elements 8 ((threadIdx.x + 256 i) % P8) ..; slots that are not taken read slot 0
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int idx = threadIdx.x + 256 * i, at = max(s_slot[idx / P8], 0), dd = 8 * (idx % P8);
+            const uint4 a = *reinterpret_cast<const uint4 *>(ks + kv_k_offset(at, dd, D));
+            if constexpr (ROT) {
+                const uint4 o = *reinterpret_cast<const uint4 *>(ks + kv_k_offset(at, dd < HALF ? dd + HALF : dd - HALF, D));
+                const int moved = max(at - (j0 + idx / P8), 0), i0 = dd < HALF ? dd : dd - HALF;
+                const float *cs = mv.cos_tab + (size_t)moved * HALF + i0, *sn = mv.sin_tab + (size_t)moved * HALF + i0;
+                const uint32_t au[4] = {a.x, a.y, a.z, a.w}, ou[4] = {o.x, o.y, o.z, o.w};
+                uint32_t r[4];
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    float a0, a1, o0, o1;
+                    h16x2_to_f32(au[p], a0, a1);
+                    h16x2_to_f32(ou[p], o0, o1);
+                    const float s0 = dd < HALF ? sn[2 * p] : -sn[2 * p], s1 = dd < HALF ? sn[2 * p + 1] : -sn[2 * p + 1];
+                    r[p] = moved == 0 ? au[p] : pack_h16x2(a0 * cs[2 * p] + o0 * s0, a1 * cs[2 * p + 1] + o1 * s1);
+                }
+                k[i] = uint4{r[0], r[1], r[2], r[3]};
+            } else {
+                k[i] = a;
+            }
+        }
+        for (int idx = threadIdx.x; idx < 32 * D; idx += 256) {
+            const int row = idx & 31, dd = idx >> 5;           // a wave: two elements of the 32 rows, in slots that lie close to each other
+            s_v[dd][row] = vs[kv_v_offset(max(s_slot[row], 0), dd, D)];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int idx = threadIdx.x + 256 * i, row = idx / P8;
+            if (s_slot[row] >= 0) *reinterpret_cast<uint4 *>(kd + kv_k_offset(j0 + row, 8 * (idx % P8), D)) = k[i];
+        }
+        for (int idx = threadIdx.x; idx < 4 * D; idx += 256) {
+            const int dd = (idx & 15) + 16 * (idx >> 6), g = (idx >> 4) & 3;    // 16-byte pieces in the order in which they lie (kvlayout.h)
+            union { uint4 u; h16_t e[8]; } w;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w.e[j] = s_v[dd][4 * g + (j & 3) + 16 * (j >> 2)];
+            h16_t *at = vd + kv_v_offset(j0 + 4 * g, dd, D);
+            if (s_slot[31] >= 0) {
+                *reinterpret_cast<uint4 *>(at) = w.u;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (s_slot[4 * g + (j & 3) + 16 * (j >> 2)] >= 0) at[j] = w.e[j];
+            }
+        }
+    }
+}
+void launch_evict_move(const EvictCall &ec, const EvictMove &mv, hipStream_t s) {
+    const int blocks = evict_blocks(ec, mv);
+    const dim3 grid((unsigned)blocks * ec.layers * ec.batch * ec.hkv);
+#define HX_MOVE(DD, R) hipLaunchKernelGGL((evict_move_kernel<DD, R>), grid, dim3(256), 0, s, ec, mv, blocks)
+    if (mv.src.d == 128) { if (mv.cos_tab != nullptr) HX_MOVE(128, true); else HX_MOVE(128, false); }
+    else { if (mv.cos_tab != nullptr) HX_MOVE(64, true); else HX_MOVE(64, false); }
+#undef HX_MOVE
+}
+
+}  // namespace HX_NS

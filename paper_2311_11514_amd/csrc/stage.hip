@@ -16,6 +16,7 @@
 #include "host.h"
 #include "kernels.h"
 #include "q4.h"
+#include "window.h"
 
 namespace {
 
@@ -101,7 +102,9 @@ struct hexgen_stage {
     size_t dec_part_row = 0;         // 16 bits: most floats per row of the split decode projections' partial sums (dec_part_floats)
     int last_decode_rows = 0;        // rows of the last decode call that ran on the weight-streaming kernels
     int ws_batch_cap = 0;
-    float *tree_part = nullptr;      // from the first tree call on: partial results of contexts cut into runs (kTreePartFloats), kTreeUnits counters
+    float *tree_part = nullptr;      // from the first call on trees or windowed rows on: partial results of contexts cut into runs (kTreePartFloats), kTreeUnits counters
+    float *win_stat = nullptr;       // from the first call on that gathers attention weights: a row's and head's largest score and 1 / sum
+    size_t win_stat_floats = 0;
     int64_t weight_bytes = 0;
     Profiler prof;
 };
@@ -254,6 +257,7 @@ struct Rows {
     bool dev_rows = false;        // one new row per sequence: the prologue takes sequences and positions from the committed lengths
     RowMap rm{};
     const hexgen_tree *tree = nullptr;      // the rows are the nodes of drafted trees
+    const struct WinSpan *win = nullptr;    // the rows stand behind the committed contexts and attend a window
 };
 
 // Work that takes host-side state of this moment along (row maps, staged copies) cannot be recorded for replay.
@@ -443,6 +447,138 @@ void attn_tree(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const Rows &r, 
     }
 }
 
+// ---- windowed rows ------------------------------------------------------------------------------------------------
+// New rows of every sequence of a cache: counts[i] of sequence i (NULL: one each), packed
+struct WinSpan {
+    const int32_t *counts;
+    int batch, rows, max_n, window, sinks;
+    float *weights;               // the first layer's accumulators, or NULL
+    int count(int i) const { return counts != nullptr ? counts[i] : 1; }
+};
+constexpr size_t kWinWeights = 2;                            // floats of win_stat per row and head
+
+// the span in launches of kWinSeqs sequences; those without a row at either end of one are left out of it
+template <typename F>
+void for_each_call(const hexgen_kv_cache *kv, const WinSpan &sp, F &&fn) {
+    for (int first = 0, row = 0; first < sp.batch; first += kWinSeqs) {
+        WinCall wc;
+        wc.seq0 = first;
+        wc.batch = std::min(kWinSeqs, sp.batch - first);
+        wc.rows = sp.rows;
+        wc.window = std::min(sp.window, kWinFar);
+        wc.sinks = std::min(sp.sinks, kWinFar);
+        wc.max_seq = kv->max_seq;
+        wc.max_n = 0;
+        for (int i = 0; i < wc.batch; ++i) {
+            wc.cu[i] = row;
+            row += sp.count(first + i);
+            wc.max_n = std::max(wc.max_n, row - wc.cu[i]);
+            wc.order[i] = (uint8_t)i;
+        }
+        wc.cu[wc.batch] = row;
+        if (wc.max_n > 0) fn(wc);
+    }
+}
+
+// Rows per block, and the runs that a row's tiles are cut into.
+WinPlan pick_win_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, WinCall &wc, bool stats) {
+    const int G = st->hq_l / st->hkv_l;
+    const bool h16 = is_h16(st->dtype);
+    long blocks = 0, tiles = 0, shared_blocks = 0;
+    int longest = 1, reach[kWinSeqs];
+    const int rows = h16 ? 32 : 16;
+    for (int i = 0; i < wc.batch; ++i) {
+        const int n = wc.cu[i + 1] - wc.cu[i], len = kv->lens[wc.seq0 + i];
+        reach[i] = 0;
+        if (n == 0) continue;
+        WinTiles t;
+        t.set(len + n - 1, len + n - 1, wc.window, wc.sinks, 0);      // of the last row, which sees most
+        reach[i] = t.nt;
+        longest = std::max(longest, t.nt);
+        const long rb = (long)win_row_blocks(n, G, rows) * st->hkv_l;
+        blocks += rb;
+        tiles += rb * t.nt;
+        shared_blocks += (long)win_row_blocks(n, G, 128) * st->hkv_l;
+    }
+    WinPlan wp;
+    wp.shared = h16 && (long)wc.max_n * G > 32 && shared_blocks >= 128;
+    wp.chunk = longest;
+    wp.nsplit = 1;
+    const bool few_units = (long)wc.batch * st->hkv_l * win_row_blocks(wc.max_n, G, rows) <= kTreeUnits;
+    if (!wp.shared && blocks < 128 && few_units) {
+        const long fit = (tiles + kTreeBlocks - 1) / kTreeBlocks;
+        if (!h16) wp.chunk = (int)std::max(4L, fit);
+        else if (longest > 48) wp.chunk = (int)((std::max({16L, fit, (long)(2 * std::sqrt((double)longest))}) + 7) / 8 * 8);
+        wp.nsplit = std::min((longest + wp.chunk - 1) / wp.chunk, kWinMaxSplit);
+        wp.nsplit = (int)std::max((size_t)1, std::min((size_t)wp.nsplit, kTreePartFloats / ((size_t)wc.rows * st->hq_l * (st->d + 2))));
+    }
+    wp.part_o = st->tree_part;
+    wp.part_ml = st->tree_part + (size_t)wp.nsplit * wc.rows * st->hq_l * st->d;
+    wp.arrived = reinterpret_cast<unsigned *>(st->tree_part + kTreePartFloats);
+    wp.stat = stats ? st->win_stat : nullptr;
+    if (wp.nsplit == 1) std::stable_sort(wc.order, wc.order + wc.batch, [&](int a, int b) { return reach[a] > reach[b]; });
+    return wp;
+}
+
+// tiles of 32 positions that a call's rows reach, at most; the host's lengths say how many blocks are worth launching, no more
+int win_reach(const hexgen_kv_cache *kv, const WinCall &wc) {
+    int most = 1;
+    for (int i = 0; i < wc.batch; ++i) {
+        const int n = wc.cu[i + 1] - wc.cu[i], len = kv->lens[wc.seq0 + i];
+        if (n == 0) continue;
+        WinTiles t;
+        t.set(len, len + n - 1, wc.window, wc.sinks, 0);
+        most = std::max(most, t.nt);
+    }
+    return most;
+}
+
+// The rows' attention in one layer.  in.k given: their keys and values join the cache here, in the attention itself where a sequence's rows are one
+// block's, otherwise in front of it.
+void attn_rows(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const WinSpan &sp, const void *q, const h16_t *q_lo, int64_t ldq, const TreeIn &in, const TreeOut &out,
+               hipStream_t s) {
+    const KvGeom kg = geom(st, kv);
+    const int G = st->hq_l / st->hkv_l;
+    float *weights = sp.weights != nullptr ? sp.weights + (size_t)layer * sp.batch * st->hkv_l * kv->max_seq : nullptr;
+    for_each_call(kv, sp, [&](WinCall &wc) {
+        const WinPlan wp = pick_win_plan(st, kv, wc, weights != nullptr);
+        TreeIn here = in;
+        const bool append = in.k != nullptr && (wp.shared || (long)wc.max_n * G > (is_h16(st->dtype) ? 32 : 16));
+        if (append) here = TreeIn{nullptr, nullptr, 0, 0};
+        if (is_h16(st->dtype)) {
+            h16_t *kc = static_cast<h16_t *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<h16_t *>(kv->v) + (size_t)layer * kv->layer_stride;
+            const h16_t *q16 = static_cast<const h16_t *>(q);
+            if (append) HX_K(st->dtype, launch_win_append, in, kc, vc, kg, wc, kv->d_lens, s);
+            HX_K(st->dtype, launch_win_attn, q16, q_lo, ldq, here, kc, vc, kg, st->hq_l, wc, kv->d_lens, wp, out, s);
+            if (weights != nullptr) HX_K(st->dtype, launch_win_weights, q16, q_lo, ldq, kc, kg, st->hq_l, wc, kv->d_lens, wp.stat, weights, win_reach(kv, wc), s);
+        } else {
+            float *kc = static_cast<float *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<float *>(kv->v) + (size_t)layer * kv->layer_stride;
+            const float *q32 = static_cast<const float *>(q);
+            if (append) f32_launch_win_append(in, kc, vc, kg, wc, kv->d_lens, s);
+            f32_launch_win_attn(q32, ldq, here, kc, vc, kg, st->hq_l, wc, kv->d_lens, wp, static_cast<float *>(out.o), s);
+            if (weights != nullptr) f32_launch_win_weights(q32, ldq, kc, kg, st->hq_l, wc, kv->d_lens, wp.stat, weights, win_reach(kv, wc), s);
+        }
+    });
+}
+
+// The raw QKV projection of a stage's rows (16 bits: ws.tree_qkv, packed columns; fp32: ws.qkv32) -> rotated q, cache rows, attention
+void attn_win(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const Rows &r, const TreeOut &out, hipStream_t s) {
+    Workspace &w = st->ws;
+    const KvGeom kg = geom(st, kv);
+    const TreeIn in{nullptr, nullptr, 0, 0};       // appended by the rotation
+    h16_t *q_lo = r.decode && is_h16(st->dtype) ? w.q_lo : nullptr;      // on the decode kernels as exact as a decode step, beyond as a prefill
+    for_each_call(kv, *r.win, [&](WinCall &wc) {
+        if (is_h16(st->dtype)) {
+            h16_t *kc = static_cast<h16_t *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<h16_t *>(kv->v) + (size_t)layer * kv->layer_stride;
+            HX_K(st->dtype, launch_win_rope_append, w.tree_qkv, st->hq_l, kg, wc, kv->d_lens, kv->cos_tab, kv->sin_tab, w.q, q_lo, kc, vc, s);
+        } else {
+            float *kc = static_cast<float *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<float *>(kv->v) + (size_t)layer * kv->layer_stride;
+            f32_launch_win_rope_append(w.qkv32, st->hq_l, kg, wc, kv->d_lens, kv->cos_tab, kv->sin_tab, w.q32, kc, vc, s);
+        }
+    });
+    attn_rows(st, kv, layer, *r.win, is_h16(st->dtype) ? static_cast<const void *>(w.q) : w.q32, q_lo, st->qw, in, out, s);
+}
+
 // ---- bf16 prefill flow: five kernels per layer; RoPE / cache append, residual + next-norm operand and SwiGLU
 // run in the GEMM epilogues, RMSNorm enters as a per-token scale after the contraction ---------------------
 GemmEpi gemm_epi_base(hexgen_stage *st, int mode) {
@@ -467,13 +603,15 @@ void attn_prefill_h16(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const Ro
                        hipStream_t s) {
     Workspace &w = st->ws;
     const Layer &ly = st->layers[layer];
-    if (r.tree != nullptr) {
+    if (r.tree != nullptr || r.win != nullptr) {
         GemmEpi raw = gemm_epi_base(st, DEC_RAW);
         raw.ssq_in = ssq_in;
         raw.raw_out = w.tree_qkv;
         gemm_h16(st, r, ly.wqkv, w.n, st->nqkv, st->H, raw, PROF_QKV, s);
         st->prof.mark(PROF_ATTN, s);
-        attn_tree(st, kv, layer, r, TreeOut{TREE_OUT_FRAG, r.T, st->qw, w.o}, s);
+        const TreeOut out{TREE_OUT_FRAG, r.T, st->qw, w.o};
+        if (r.tree != nullptr) attn_tree(st, kv, layer, r, out, s);
+        else attn_win(st, kv, layer, r, out, s);
         st->prof.mark(PROF_ATTN, s);
         return;
     }
@@ -616,13 +754,15 @@ void attn_decode_h16(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const Row
                       hipStream_t s) {
     Workspace &w = *st->cur;
     const Layer &ly = st->layers[layer];
-    if (r.tree != nullptr) {
+    if (r.tree != nullptr || r.win != nullptr) {
         DecodeEpi raw = epi_base(st, DEC_RAW);
         raw.ssq_in = ssq_in;
         raw.raw_out = w.tree_qkv;
         decode_proj(st, r, ly.wqkv, w.xa_n, st->nqkv, st->H, raw, PROF_QKV, s);
         st->prof.mark(PROF_ATTN, s);
-        attn_tree(st, kv, layer, r, TreeOut{TREE_OUT_ACT, r.T, st->qw, w.xa_o}, s);
+        const TreeOut out{TREE_OUT_ACT, r.T, st->qw, w.xa_o};
+        if (r.tree != nullptr) attn_tree(st, kv, layer, r, out, s);
+        else attn_win(st, kv, layer, r, out, s);
         st->prof.mark(PROF_ATTN, s);
         return;
     }
@@ -651,7 +791,7 @@ hexgen_status_t forward_decode_h16(hexgen_stage *st, hexgen_kv_cache *kv, const 
     Workspace &w = *st->cur;
     float *ssq_a = w.ssq, *ssq_f = w.ssq + (size_t)(st->H / 16) * kDecodeMaxRows;
     HX_K(st->dtype, launch_decode_prologue, hidden_in, nullptr, 1, w.h, st->layers[0].g_attn, w.xa_n, ssq_a, r.T, st->H,
-                           r.tree != nullptr ? nullptr : kv->d_lens, w.row_pos, 1, s);
+                           r.tree != nullptr || r.win != nullptr ? nullptr : kv->d_lens, w.row_pos, 1, s);
     for (int l = 0; l < st->L; ++l) {
         const Layer &ly = st->layers[l];
         const bool last = l + 1 == st->L;
@@ -719,7 +859,7 @@ void proj_f32(hexgen_stage *st, int mode, const F32Proj &p, hipStream_t s) {
 // Does a step take attention and W_O in one launch?  By the longest context; a step that is being recorded may be replayed at any length of its
 // cache, which the host does not see, and goes by the cache's capacity.
 bool takes_attn_wo(const hexgen_stage *st, const hexgen_kv_cache *kv, const Rows &r, hipStream_t s) {
-    if (!r.decode || r.tree != nullptr) return false;
+    if (!r.decode || r.tree != nullptr || r.win != nullptr) return false;
     int positions = 0;
     for (int i = 0; i < r.batch; ++i) positions = std::max(positions, kv->lens[i] + 1);
     if (!f32_attn_wo_fits(r.T, st->hq_l, st->hkv_l, st->d, st->H, positions)) return false;
@@ -743,6 +883,10 @@ void attn_f32(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const Rows &r, c
     }
     if (r.tree != nullptr) {
         attn_tree(st, kv, layer, r, TreeOut{TREE_OUT_ROWS, r.T, st->qw, w.o32}, s);
+        return;
+    }
+    if (r.win != nullptr) {
+        attn_win(st, kv, layer, r, TreeOut{TREE_OUT_ROWS, r.T, st->qw, w.o32}, s);
         return;
     }
     if (r.max_new == 1) {          // row = sequence
@@ -859,6 +1003,48 @@ hexgen_status_t check_tree(const hexgen_kv_cache *kv, const hexgen_tree *tr) {
     if (!kv->prefilled || tr->batch == 0 || tr->batch != kv->batch) return HEXGEN_ERR_STATE;
     for (int i = 0; i < tr->batch; ++i)
         if ((long)kv->lens[i] + (tr->cu[i + 1] - tr->cu[i]) > kv->max_seq) return HEXGEN_ERR_CAPACITY;
+    return HEXGEN_OK;
+}
+
+// ---- windowed rows: storage and checks ----------------------------------------------------------------------------
+// What counts, window and sinks say, against the cache.  A launch has less than 2^32 threads (attention: 512 for 32 rows of one head, fp32 256 for 16; the
+// weights' sums 256 for four tiles; the rotation a thread for four rotary pairs, fp32 one).
+hexgen_status_t check_span(const hexgen_kv_cache *kv, const int32_t *counts, int batch, int window, int sinks, float *weights, WinSpan *out) {
+    if (batch <= 0 || window <= 0 || sinks < 0 || reinterpret_cast<uintptr_t>(weights) % sizeof(float)) return HEXGEN_ERR_INVALID_ARG;
+    if (!kv->prefilled || batch != kv->batch) return HEXGEN_ERR_STATE;
+    const hexgen_stage *st = kv->st;
+    long rows = 0;
+    int max_n = 0;
+    for (int i = 0; i < batch; ++i) {
+        const int n = counts != nullptr ? counts[i] : 1;
+        if (n < 0) return HEXGEN_ERR_INVALID_ARG;
+        if ((long)kv->lens[i] + n > kv->max_seq) return HEXGEN_ERR_CAPACITY;
+        rows += n;
+        max_n = std::max(max_n, n);
+    }
+    if (rows == 0) return HEXGEN_ERR_SHAPE;
+    const int G = st->hq_l / st->hkv_l;
+    const bool h16 = is_h16(st->dtype);
+    const uint64_t most = UINT32_MAX - 4096, seqs = std::min(batch, kWinSeqs);
+    if (rows > 0x3fffffff || (long)max_n * G > 0x3fffffff) return HEXGEN_ERR_CAPACITY;
+    const uint64_t blocks = (uint64_t)win_row_blocks(max_n, G, h16 ? 32 : 16) * (seqs * st->hkv_l + 7);
+    const uint64_t rotary = (uint64_t)rows * (st->hq_l + 2 * st->hkv_l) * (st->d / (h16 ? 8 : 2)), sums = (uint64_t)(kv->smax / 32 + 4) * 64 * (h16 ? 1 : 2) * st->hkv_l * seqs;
+    if (blocks * (h16 ? 512 : 256) > most || rotary > most || (weights != nullptr && sums > most)) return HEXGEN_ERR_CAPACITY;
+    *out = WinSpan{counts, batch, (int)rows, max_n, window, sinks, weights};
+    return HEXGEN_OK;
+}
+hexgen_status_t ensure_win_stat(hexgen_stage *st, const WinSpan &sp, hipStream_t s) {
+    const size_t want = kWinWeights * sp.rows * st->hq_l;
+    if (sp.weights == nullptr || want <= st->win_stat_floats) return HEXGEN_OK;
+    HX_TRY(refuse_capture(s));
+    float *p = nullptr;
+    HX_TRY(dmalloc(&p, want));
+    if (st->win_stat != nullptr) {
+        HX_HIP(hipDeviceSynchronize());
+        (void)hipFree(st->win_stat);
+    }
+    st->win_stat = p;
+    st->win_stat_floats = want;
     return HEXGEN_OK;
 }
 
@@ -993,6 +1179,7 @@ void hexgen_stage_destroy(hexgen_stage_t *st) {
     for (Layer &l : st->layers) free_layer(l);
     free_ws(st->ws);
     if (st->tree_part) (void)hipFree(st->tree_part);
+    if (st->win_stat) (void)hipFree(st->win_stat);
     st->prof.clear();
     delete st;
 }
@@ -1186,6 +1373,8 @@ hexgen_status_t hexgen_kv_cache_get_lengths(hexgen_kv_cache_t *kv, int32_t *lens
     for (int i = 0; i < batch; ++i) lens_out[i] = kv->lens[i];
     return HEXGEN_OK;
 }
+
+int hexgen_kv_cache_batch(const hexgen_kv_cache_t *kv) { return !kv ? -1 : kv->prefilled ? kv->batch : 0; }
 
 hexgen_status_t hexgen_kv_cache_commit(hexgen_kv_cache_t *kv, const int32_t *seq_lens, int batch) {
     if (!kv || batch <= 0) return HEXGEN_ERR_INVALID_ARG;
@@ -1543,6 +1732,91 @@ hexgen_status_t hexgen_kv_cache_keep(hexgen_kv_cache_t *kv, hexgen_tree_t *tr, c
     launch_tree_advance(kv->d_lens, d_kept, tr->batch, kv->smax, s);
     HX_HIP(hipGetLastError());
     for (int i = 0; i < tr->batch; ++i) kv->lens[i] += kept[i];
+    return HEXGEN_OK;
+}
+
+// ---- windowed rows and eviction --------------------------------------------------------------------
+hexgen_status_t hexgen_kv_window_attention(hexgen_kv_cache_t *kv, int layer, const int32_t *counts, int batch, const void *q, int64_t ldq, const void *k,
+                                           int64_t ldk, const void *v, int64_t ldv, int window, int sinks, float *weights, void *out, void *stream) {
+    if (!kv || !q || !k || !v || !out || layer < 0 || layer >= kv->st->L) return HEXGEN_ERR_INVALID_ARG;
+    hexgen_stage *st = kv->st;
+    const int64_t kw = (int64_t)st->hkv_l * st->d;
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(out);
+    if (bits % 16 || (ldq | ldk | ldv) % (16 / (int)esize(st->dtype)) || ldq < st->qw || ldk < kw || ldv < kw) return HEXGEN_ERR_INVALID_ARG;
+    WinSpan sp;
+    HX_TRY(check_span(kv, counts, batch, window, sinks, weights, &sp));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    HX_TRY(ensure_tree_part(st, s));
+    HX_TRY(ensure_win_stat(st, sp, s));
+    if (sp.weights != nullptr) sp.weights -= (size_t)layer * batch * st->hkv_l * kv->max_seq;      // this layer's own are given
+    attn_rows(st, kv, layer, sp, q, nullptr, ldq, TreeIn{k, v, ldk, ldv}, TreeOut{TREE_OUT_ROWS, sp.rows, st->qw, out}, s);
+    HX_HIP(hipGetLastError());
+    return HEXGEN_OK;
+}
+
+hexgen_status_t hexgen_stage_extend(hexgen_stage_t *st, hexgen_kv_cache_t *kv, const void *hidden_in, const int32_t *counts, int batch, int window, int sinks,
+                                    float *weights, void *out_partial, void *out_resid, void *stream) {
+    if (!st || !kv || !hidden_in || !out_partial || kv->st != st) return HEXGEN_ERR_INVALID_ARG;
+    HX_TRY(check_loaded(st));
+    WinSpan sp;
+    HX_TRY(check_span(kv, counts, batch, window, sinks, weights, &sp));
+    HX_TRY(check_rope(st, kv));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Rows r;
+    r.T = sp.rows;
+    r.batch = batch;
+    r.max_new = sp.max_n;
+    r.win = &sp;
+    r.decode = r.T <= (is_h16(st->dtype) ? kDecodeMaxRows : kF32StreamRows);
+    if (r.T > st->ws.cap_rows || r.batch > st->ws_batch_cap) HX_TRY(refuse_capture(s));
+    HX_TRY(ensure_workspace(st, r.T, r.batch));
+    HX_TRY(ensure_tree_part(st, s));
+    HX_TRY(ensure_win_stat(st, sp, s));
+    if (is_h16(st->dtype) && st->ws.tree_qkv == nullptr) {
+        HX_TRY(refuse_capture(s));
+        HX_TRY(dmalloc(&st->ws.tree_qkv, (size_t)st->ws.cap_rows * st->nqkv));
+    }
+    st->prof.mark(PROF_CALL, s);
+    if (is_h16(st->dtype)) HX_TRY(forward_h16(st, kv, r, hidden_in, out_partial, out_resid, s));
+    else HX_TRY(forward_f32(st, kv, r, hidden_in, out_partial, out_resid, nullptr, s));
+    if (r.decode && is_h16(st->dtype)) st->last_decode_rows = r.T;
+    for_each_call(kv, sp, [&](WinCall &wc) { launch_win_advance(kv->d_lens, wc, s); });
+    st->prof.mark(PROF_CALL, s);
+    HX_HIP(hipGetLastError());
+    for (int i = 0; i < batch; ++i) kv->lens[i] += sp.count(i);
+    return HEXGEN_OK;
+}
+
+hexgen_status_t hexgen_kv_cache_evict(hexgen_kv_cache_t *kv, hexgen_kv_cache_t *dst, int keep, int sinks, int recent, const float *weights, float *weights_out,
+                                      int rotate, int32_t *slots, void *stream) {
+    if (!kv || !dst || !slots || keep <= 0 || sinks < 0 || recent < 0 || (long)sinks + recent > keep || dst->st != kv->st) return HEXGEN_ERR_INVALID_ARG;
+    if ((weights == nullptr) != (weights_out == nullptr) || (dst != kv && weights != nullptr && weights == weights_out)) return HEXGEN_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(weights) | reinterpret_cast<uintptr_t>(weights_out) | reinterpret_cast<uintptr_t>(slots)) % 4) return HEXGEN_ERR_INVALID_ARG;
+    if (!kv->prefilled || kv->batch == 0) return HEXGEN_ERR_STATE;
+    hexgen_stage *st = kv->st;
+    if (rotate) {
+        HX_TRY(check_rope(st, kv));
+        HX_TRY(check_rope(st, dst));
+    }
+    if (dst->max_batch < kv->batch || dst->max_seq < std::min(keep, kv->max_seq)) return HEXGEN_ERR_CAPACITY;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    HX_TRY(refuse_capture(s));
+    const EvictCall ec{st->L, kv->batch, st->hkv_l, kv->max_seq, dst->max_seq, std::min(keep, kv->max_seq), sinks, recent, weights, weights_out, slots};
+    const EvictMove mv{kv->k, kv->v, dst->k, dst->v, kv->layer_stride, dst->layer_stride, geom(st, kv), geom(st, dst),
+                       rotate ? kv->cos_tab : nullptr, rotate ? kv->sin_tab : nullptr, kv->d_lens, dst->d_lens, dst->max_batch};
+    const uint64_t units = (uint64_t)ec.layers * ec.batch * ec.hkv;
+    if (units * 512 > UINT32_MAX || units * 256 * evict_blocks(ec, mv) > UINT32_MAX) return HEXGEN_ERR_CAPACITY;
+    launch_evict_select(ec, kv->d_lens, s);
+    if (is_h16(st->dtype)) HX_K(st->dtype, launch_evict_move, ec, mv, s);
+    else f32_launch_evict_move(ec, mv, s);
+    HX_HIP(hipGetLastError());
+    const int batch = kv->batch;
+    for (int i = 0; i < batch; ++i) dst->lens[i] = std::min(kv->lens[i], keep);
+    if (dst == kv) return HEXGEN_OK;
+    std::fill(dst->lens.begin() + batch, dst->lens.end(), 0);
+    dst->batch = batch;
+    dst->prefilled = true;
+    dst->steps = 0;
     return HEXGEN_OK;
 }
 

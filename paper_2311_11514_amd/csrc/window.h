@@ -1,0 +1,78 @@
+// New rows of ragged sequences that attend a sliding window and the first positions of their contexts: what the kernels of both storage widths share.
+#pragma once
+#include "kernels.h"
+
+// The tiles of 32 positions that rows at slots p_lo .. p_hi reach, by their index in a list: first the `clean` ones, which every row attends whole and the
+// cache holds (positions from `held` on may not be there yet) -- first positions, then the window's inside -- and behind them those that need a mask.
+struct WinTiles {
+    int full, ns, w0, c0, c1, clean, nt;       // tiles [0, full) and [c0, c1) are clean, [full, ns) and [w0, p_hi / 32] otherwise are not
+    __host__ __device__ __forceinline__ void set(int p_lo, int p_hi, int window, int sinks, int held) {
+        const int first = p_lo - window + 1;
+        w0 = first > 0 ? first >> 5 : 0;
+        ns = (sinks + 31) >> 5;
+        ns = ns < w0 ? ns : w0;
+        full = sinks >> 5;
+        full = full < ns ? full : ns;
+        const int hidden = p_hi - window;      // the last row does not see this one
+        c0 = hidden >= 0 ? (hidden >> 5) + 1 : 0;
+        c0 = c0 > w0 ? c0 : w0;
+        c1 = (p_lo < held ? p_lo + 1 : held) >> 5;
+        if (c1 <= c0) c0 = c1 = w0;
+        clean = full + c1 - c0;
+        nt = ns + (p_hi >> 5) - w0 + 1;
+    }
+    __host__ __device__ __forceinline__ int at(int v) const {
+        if (v < full) return v;
+        if (v < clean) return v - full + c0;
+        v -= c1 - c0;                          // now an index in what the clean inside of the window has been taken out of
+        if (v < ns) return v;
+        v += w0 - ns;
+        return v < c0 ? v : v + c1 - c0;
+    }
+};
+
+// bits 0 .. x - 1 of 32
+__device__ __forceinline__ uint32_t win_below(int x) { return x <= 0 ? 0u : x >= 32 ? 0xffffffffu : (1u << x) - 1; }
+// which of the 32 positions from p0 on the row at slot p attends
+__device__ __forceinline__ uint32_t win_sees(int p0, int p, int window, int sinks) {
+    return win_below(p + 1 - p0) & (~win_below(p - window + 1 - p0) | win_below(sinks - p0));
+}
+// do rows at slots p_lo .. p_hi attend all `width` positions from p0 on?
+__device__ __forceinline__ bool win_all(int p0, int width, int p_lo, int p_hi, int window, int sinks) {
+    return p0 + width - 1 <= p_lo && (p0 > p_hi - window || p0 + width <= sinks);
+}
+// does any of them attend one?
+__device__ __forceinline__ bool win_any(int p0, int width, int p_lo, int p_hi, int window, int sinks) {
+    return p0 <= p_hi && (p0 + width - 1 > p_lo - window || p0 < sinks);
+}
+
+// What a block works on: `rows` query rows of one (sequence, kv head) -- row r: new row r / G of the sequence, head r % G -- and a run of their
+// tiles.  Block id = 8 slot + xcd: the blocks of a (sequence, kv head) sit next to each other on one XCD and share its keys and values in that L2, the last
+// rows, which reach furthest, first; sequences in wc.order.
+struct WinWork {
+    int rb, split, c, seq, nth, row0, n, R, len, per, v0, v1;
+    WinTiles tiles;
+    __device__ __forceinline__ bool find(int hkv, int G, int nrb, int rows, const WinCall &wc, const int32_t *lens, const WinPlan &wp, bool fresh) {
+        const unsigned slot = blockIdx.x >> 3;
+        rb = nrb - 1 - (int)(slot % (unsigned)nrb);
+        int combo = (int)(slot / (unsigned)nrb) * 8 + (blockIdx.x & 7);
+        if (combo >= wc.batch * hkv * wp.nsplit) return false;
+        split = combo % wp.nsplit;
+        combo /= wp.nsplit;
+        c = combo % hkv;
+        nth = wc.order[combo / hkv];
+        seq = wc.seq0 + nth;
+        row0 = wc.cu[nth];
+        len = lens[seq];
+        n = min(wc.cu[nth + 1] - row0, wc.max_seq - len);     // rows that would pass the cache are left out
+        R = n * G;
+        if (rb * rows >= R) return false;
+        const int p_lo = len + rb * rows / G, p_hi = len + min(n - 1, (rb * rows + rows - 1) / G);
+        tiles.set(p_lo, p_hi, wc.window, wc.sinks, fresh ? len : p_lo + 1);
+        per = max(wp.chunk, (tiles.nt + wp.nsplit - 1) / wp.nsplit);
+        v0 = split * per;
+        v1 = min(v0 + per, tiles.nt);
+        return v0 < tiles.nt;
+    }
+    __device__ __forceinline__ int runs() const { return (tiles.nt + per - 1) / per; }
+};
