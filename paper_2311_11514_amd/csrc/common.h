@@ -57,6 +57,11 @@ __device__ __forceinline__ void hx_load_lds16(unsigned lds, unsigned off, const 
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(off), "s"(src) : "memory");
 }
 
+// the same with 4 bytes per lane, to lds + 4 * lane
+__device__ __forceinline__ void hx_load_lds4(unsigned lds, unsigned off, const void *src) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(lds), "v"(off), "s"(src) : "memory");
+}
+
 // Decode activations are hi + lo pairs (split_h16), laid out by the number of rows T of the call:
 //   T <= 2: compact token-major, per token and k-tile one 128-byte line holding the 32 hi values then the 32 lo values; a
 //           projection touches one cache line per (token, k-tile) where a 16-token tile would cost it eight;

@@ -220,6 +220,8 @@ void f32_launch_tree_keep(float *kc, float *vc, int64_t layer_stride, int layers
 // ---- windowed rows (kernels_bf16_window.hip, kernels_f32_window.hip) ---------------------------------------------
 constexpr int kWinSeqs = 256;             // sequences of one launch
 constexpr int kWinMaxSplit = 32;          // runs that a row's tiles are cut into
+constexpr size_t kWinPartFloats = (size_t)16 << 20;      // WinPlan: floats at part_o, and counters at arrived
+constexpr long kWinUnits = 1 << 14;
 // New rows of sequences seq0 .. seq0 + batch - 1, which stand behind the committed contexts: rows cu[i] .. cu[i + 1] - 1 of the call's are the ith one's.
 // The row at slot p attends slots j <= p with p - j < window or j < sinks.  Passed by value: a launch needs no copy to the device, and can be recorded.
 struct WinCall {

@@ -377,7 +377,7 @@ __global__ __launch_bounds__(512, 2) void win_few_kernel(const h16_t *__restrict
 // A block of four waves takes 128 query rows, 32 a wave; their tiles go from HBM to LDS directly, three in flight, and are shared.  Products and softmax as
 // above.  The rows are in the cache already.
 template <int D>
-__global__ __launch_bounds__(256, 3) void win_attn_kernel(const h16_t *__restrict__ q, int64_t ldq, const h16_t *__restrict__ kc, const h16_t *__restrict__ vc, KvGeom kg,
+__global__ __launch_bounds__(256, 2) void win_attn_kernel(const h16_t *__restrict__ q, int64_t ldq, const h16_t *__restrict__ kc, const h16_t *__restrict__ vc, KvGeom kg,
                                                           int hq_l, int G, int nrb, WinCall wc, const int32_t *__restrict__ lens, WinPlan wp, TreeOut out,
                                                           float scale_log2e) {
     constexpr int RW = 4, S = 3, ROWS = 32 * RW;
@@ -458,16 +458,18 @@ __global__ __launch_bounds__(256, 3) void win_attn_kernel(const h16_t *__restric
                 return;
             }
         }
-        TreeP p[2], lo[2];
-        tree_pack(sc, p, lo);
+        TreeP p[2];                                       // k-groups hl (quads 0, 2) and 2 + hl (quads 1, 3)
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int x = 4 * g + 2 * (i & 1) + 8 * (i >> 1);
+                p[g].u[i] = pack_h16x2(sc[x], sc[x + 1]);
+            }
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const h16x8 x = st[2 * KT + 2 * db + sub][fl + 32 * g];
-                oacc[db] = hx_mfma32(x, lo[g].v, oacc[db]);
-                oacc[db] = hx_mfma32(x, p[g].v, oacc[db]);
-            }
+            for (int g = 0; g < 2; ++g) oacc[db] = hx_mfma32(st[2 * KT + 2 * db + sub][fl + 32 * g], p[g].v, oacc[db]);
     };
     int step = 0;
     for (; step < wk.tiles.clean; ++step) walk(step, std::false_type{});
@@ -570,12 +572,155 @@ __global__ __launch_bounds__(256, 4) void win_weights_kernel(const h16_t *__rest
         }
     }
 }
+// groups of eight tiles in a cache's positions, each with a counter and a place for its sums
+__host__ __device__ inline int win_units(int smax) { return (smax / 32 + 7) / 8; }
+// The same for calls of many rows: a wave keeps the keys of two tiles, and the block's four waves share the rows, which go from memory to LDS directly, two
+// groups ahead, together with each row's statistics.  Where tiles are few the groups are dealt to `splits` blocks; their sums meet in the order of the
+// rows, added up by the last block to arrive.
+template <int D, bool QLO>
+__global__ __launch_bounds__(256, 2) void win_weights_shared_kernel(const h16_t *__restrict__ q, const h16_t *__restrict__ q_lo, int64_t ldq, const h16_t *__restrict__ kc,
+                                                                    KvGeom kg, int hq_l, int G, int tile_blocks, int splits, WinCall wc, const int32_t *__restrict__ lens,
+                                                                    const float *__restrict__ stat, float *__restrict__ weights, float *part, unsigned *arrived,
+                                                                    float scale_log2e) {
+    constexpr int KT = D / 32, W = 4, TW = 2, S = 3, PIECES = 2 * KT * (QLO ? 2 : 1), LPT = PIECES / W;      // 1 KB pieces of a group of 32 rows
+    __shared__ h16x8 s_q[S][PIECES][64];
+    __shared__ float s_stat[S][W][64];                        // largest score and 1 / sum of the group's rows, a copy for every wave
+    __shared__ int s_last;
+    int id = blockIdx.x;
+    const int split = id % splits;
+    id /= splits;
+    const int tb = id % tile_blocks, c = (id / tile_blocks) % kg.hkv_l, nth = id / tile_blocks / kg.hkv_l;
+    const int seq = wc.seq0 + nth, row0 = wc.cu[nth], len = lens[seq], n = min(wc.cu[nth + 1] - row0, wc.max_seq - len);
+    if (n <= 0) return;
+    WinTiles tiles;
+    tiles.set(len, len + n - 1, wc.window, wc.sinks, 0);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, hl = lane >> 5, i32 = lane & 31;
+    const int sub = i32 >> 4, fl = (lane & 15) + 16 * hl;
+    const h16_t *slab = kc + (size_t)seq * kg.seq_stride + (size_t)c * kg.smax * D;
+    const int per32 = 32 / G, rem32 = 32 % G;                 // what 32 rows on is in new rows and heads
+    for (int v0 = W * TW * tb; v0 < tiles.nt; v0 += W * TW * tile_blocks) {
+        // new rows that attend a position of the block's tiles: from the first at or behind them to the last whose window reaches them
+        const int t_first = tiles.at(v0), t_last = tiles.at(min(v0 + W * TW, tiles.nt) - 1);
+        const int x_lo = max(0, 32 * t_first - len), x_hi = 32 * t_first < wc.sinks ? n - 1 : min(n - 1, 32 * t_last + 31 + wc.window - 1 - len);
+        int g0 = x_lo * G / 32, g1 = (x_hi * G + G - 1) / 32 + 1;
+        const int share = (g1 - g0 + splits - 1) / splits;
+        g0 += split * share;
+        g1 = min(g1, g0 + share);
+        int p0[TW];
+        h16x8 kf[TW][2 * KT];
+        floatx16 acc[TW];
+#pragma unroll
+        for (int w = 0; w < TW; ++w) {
+            const int v = v0 + TW * wave + w, t = tiles.at(min(v, tiles.nt - 1));
+            p0[w] = v < tiles.nt ? 32 * t : -1;               // none: the wave feeds the others
+            const h16_t *src = slab + ((size_t)(2 * t + sub) * KT * 64 + fl) * 8;
+#pragma unroll
+            for (int kk = 0; kk < 2 * KT; ++kk) kf[w][kk] = *reinterpret_cast<const h16x8 *>(src + ((kk >> 1) * 64 + 32 * (kk & 1)) * 8);
+#pragma unroll
+            for (int x = 0; x < 16; ++x) acc[w][x] = 0.f;
+        }
+        // row r of a lane's next group to request, and of the statistics: new row and head
+        int nq = (32 * g0 + i32) / G, hq = (32 * g0 + i32) - nq * G, ns = (32 * g0 + (lane >> 1)) / G, hs = (32 * g0 + (lane >> 1)) - ns * G;
+        auto issue = [&](int g) {
+            const int base = __builtin_amdgcn_readfirstlane(min(nq, n - 1));
+            const bool past = nq >= n;                        // rows past the last repeat it
+            const unsigned row = (unsigned)((past ? n - 1 : nq) - base) * (unsigned)ldq + (unsigned)((past ? G - 1 : hq) * D + 8 * hl);
+            const size_t first = (size_t)(row0 + base) * ldq + (size_t)c * G * D;
+#pragma unroll
+            for (int x = 0; x < LPT; ++x) {
+                const int piece = wave * LPT + x, kk = piece % (2 * KT);
+                const h16_t *src = (piece < 2 * KT ? q : q_lo) + first;
+                hx_load_lds16(hx_lds_addr(&s_q[g % S][piece][0]), 2u * (row + 16u * kk), src);
+            }
+            const bool gone = ns >= n;
+            const int at = ((gone ? n - 1 : ns) - base) * hq_l + (gone ? G - 1 : hs);
+            hx_load_lds4(hx_lds_addr(&s_stat[g % S][wave][0]), (unsigned)(8 * at + 4 * (lane & 1)), stat + 2 * ((size_t)(row0 + base) * hq_l + (size_t)c * G));
+            nq += per32; hq += rem32; ns += per32; hs += rem32;
+            if (hq >= G) { hq -= G; ++nq; }
+            if (hs >= G) { hs -= G; ++ns; }
+        };
+        int node = nq, head = hq;                             // of this lane's row of the group that is worked on
+        __syncthreads();                                      // every wave has left the buffers of the tiles before
+        HX_WAIT_VM(0);
+        if (g0 < g1) issue(g0);
+        if (g0 + 1 < g1) issue(g0 + 1);
+        for (int g = g0; g < g1; ++g) {
+            if (g + 1 < g1) HX_WAIT_VM(LPT + 1);              // the next group may stay in flight
+            else HX_WAIT_VM(0);
+            HX_LDS_BARRIER();
+            if (g + 2 < g1) issue(g + 2);                     // into the buffer that every wave has left
+            const float m = s_stat[g % S][wave][2 * i32], inv = s_stat[g % S][wave][2 * i32 + 1];
+            floatx16 sc[TW];
+#pragma unroll
+            for (int w = 0; w < TW; ++w)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) sc[w][x] = 0.f;
+#pragma unroll
+            for (int piece = PIECES - 1; piece >= 0; --piece) {
+                const h16x8 row = s_q[g % S][piece][lane];
+#pragma unroll
+                for (int w = 0; w < TW; ++w) sc[w] = hx_mfma32(kf[w][piece % (2 * KT)], row, sc[w]);
+            }
+            const bool there = node < n;
+            const int first = len + __builtin_amdgcn_readfirstlane(node), last = len + __builtin_amdgcn_readlane(node, 31);
+#pragma unroll
+            for (int w = 0; w < TW; ++w) {
+                if (p0[w] < 0) continue;
+                if (last < len + n && win_all(p0[w], 32, first, last, wc.window, wc.sinks)) {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) acc[w][x] = fmaf(__builtin_amdgcn_exp2f((sc[w][x] - m) * scale_log2e), inv, acc[w][x]);
+                } else {
+                    const uint32_t sees = there ? win_sees(p0[w], len + node, wc.window, wc.sinks) : 0u;
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        const float weight = __builtin_amdgcn_exp2f((sc[w][x] - m) * scale_log2e) * inv;
+                        acc[w][x] += (sees >> (8 * (x >> 2) + 4 * hl + (x & 3))) & 1u ? weight : 0.f;
+                    }
+                }
+            }
+            node += per32; head += rem32;
+            if (head >= G) { head -= G; ++node; }
+        }
+        const size_t unit = (size_t)(nth * kg.hkv_l + c) * win_units(kg.smax) + v0 / (W * TW);
+#pragma unroll
+        for (int w = 0; w < TW; ++w) {
+            float mine = 0.f;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                float a = acc[w][x];
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) a += __shfl_xor(a, o, 64);
+                mine = i32 == x ? a : mine;
+            }
+            const int pos = 8 * ((i32 & 15) >> 2) + 4 * hl + (i32 & 3);
+            if (i32 >= 16) continue;
+            if (splits > 1) dev_store(part + ((unit * splits + split) * W + wave) * TW * 32 + 32 * w + pos, mine);
+            else if (p0[w] >= 0 && p0[w] + pos < len + n) weights[((size_t)seq * kg.hkv_l + c) * wc.max_seq + p0[w] + pos] += mine;
+        }
+        if (splits > 1 && tree_arrive(arrived + unit, splits, &s_last)) {
+            const int x = threadIdx.x, v = v0 + x / 32;       // one of the block's positions per thread
+            if (v < tiles.nt) {
+                const int pos = 32 * tiles.at(v) + x % 32;
+                float sum = 0.f;
+                for (int u = 0; u < splits; ++u) sum += dev_load(part + (unit * splits + u) * W * TW * 32 + x);
+                if (pos < len + n) weights[((size_t)seq * kg.hkv_l + c) * wc.max_seq + pos] += sum;
+            }
+        }
+    }
+}
+
 void launch_win_weights(const h16_t *q, const h16_t *q_lo, int64_t ldq, const h16_t *kc, KvGeom kg, int hq_l, const WinCall &wc, const int32_t *lens,
-                        const float *stat, float *weights, int max_tiles, hipStream_t s) {
-    const int G = hq_l / kg.hkv_l, tile_blocks = (max_tiles + 3) / 4;
+                        const WinPlan &wp, float *weights, int max_tiles, hipStream_t s) {
+    const int G = hq_l / kg.hkv_l;
     const float scale_log2e = 1.4426950408889634f / sqrtf((float)kg.d);
-    const dim3 grid((unsigned)tile_blocks * kg.hkv_l * wc.batch);
-#define HX_WIN_W(DD, LO) hipLaunchKernelGGL((win_weights_kernel<DD, LO>), grid, dim3(256), 0, s, q, q_lo, ldq, kc, kg, hq_l, G, tile_blocks, wc, lens, stat, weights, scale_log2e)
+    const bool shared = (int64_t)wc.max_n * G > 64;
+    const int tile_blocks = (max_tiles + (shared ? 7 : 3)) / (shared ? 8 : 4);
+    const int64_t blocks = (int64_t)tile_blocks * kg.hkv_l * wc.batch, groups = ((int64_t)wc.max_n * G + 31) / 32;
+    int splits = 1;
+    const int64_t units = (int64_t)wc.batch * kg.hkv_l * win_units(kg.smax);        // a length on the device may be beyond what the host knows
+    if (shared && blocks < 512 && units <= kWinUnits) splits = (int)std::max<int64_t>(1, std::min<int64_t>({(767 + blocks) / blocks, groups / 8, (int64_t)kWinPartFloats / (256 * units)}));
+    const dim3 grid((unsigned)(blocks * splits));
+#define HX_WIN_W(DD, LO)                                                                                                                                            do {                                                                                                                                                                if (shared) hipLaunchKernelGGL((win_weights_shared_kernel<DD, LO>), grid, dim3(256), 0, s, q, q_lo, ldq, kc, kg, hq_l, G, tile_blocks, splits, wc, lens, wp.stat, weights, wp.part_o, wp.arrived, scale_log2e);         else hipLaunchKernelGGL((win_weights_kernel<DD, LO>), grid, dim3(256), 0, s, q, q_lo, ldq, kc, kg, hq_l, G, tile_blocks, wc, lens, wp.stat, weights, scale_log2e);     } while (0)
     if (kg.d == 128) { if (q_lo != nullptr) HX_WIN_W(128, true); else HX_WIN_W(128, false); }
     else { if (q_lo != nullptr) HX_WIN_W(64, true); else HX_WIN_W(64, false); }
 #undef HX_WIN_W

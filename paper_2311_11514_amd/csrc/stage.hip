@@ -455,6 +455,8 @@ struct WinSpan {
     float *weights;               // the first layer's accumulators, or NULL
     int count(int i) const { return counts != nullptr ? counts[i] : 1; }
 };
+constexpr int64_t kWinRowStride = 1 << 24;                   // elements between query rows: offsets among 32 of them have 32 bits
+static_assert(kWinPartFloats == kTreePartFloats && kWinUnits == kTreeUnits, "one scratch for both");
 constexpr size_t kWinWeights = 2;                            // floats of win_stat per row and head
 
 // the span in launches of kWinSeqs sequences; those without a row at either end of one are left out of it
@@ -550,7 +552,7 @@ void attn_rows(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const WinSpan &
             const h16_t *q16 = static_cast<const h16_t *>(q);
             if (append) HX_K(st->dtype, launch_win_append, in, kc, vc, kg, wc, kv->d_lens, s);
             HX_K(st->dtype, launch_win_attn, q16, q_lo, ldq, here, kc, vc, kg, st->hq_l, wc, kv->d_lens, wp, out, s);
-            if (weights != nullptr) HX_K(st->dtype, launch_win_weights, q16, q_lo, ldq, kc, kg, st->hq_l, wc, kv->d_lens, wp.stat, weights, win_reach(kv, wc), s);
+            if (weights != nullptr) HX_K(st->dtype, launch_win_weights, q16, q_lo, ldq, kc, kg, st->hq_l, wc, kv->d_lens, wp, weights, win_reach(kv, wc), s);
         } else {
             float *kc = static_cast<float *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<float *>(kv->v) + (size_t)layer * kv->layer_stride;
             const float *q32 = static_cast<const float *>(q);
@@ -1742,7 +1744,7 @@ hexgen_status_t hexgen_kv_window_attention(hexgen_kv_cache_t *kv, int layer, con
     hexgen_stage *st = kv->st;
     const int64_t kw = (int64_t)st->hkv_l * st->d;
     const uintptr_t bits = reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(out);
-    if (bits % 16 || (ldq | ldk | ldv) % (16 / (int)esize(st->dtype)) || ldq < st->qw || ldk < kw || ldv < kw) return HEXGEN_ERR_INVALID_ARG;
+    if (bits % 16 || (ldq | ldk | ldv) % (16 / (int)esize(st->dtype)) || ldq < st->qw || ldk < kw || ldv < kw || ldq > kWinRowStride) return HEXGEN_ERR_INVALID_ARG;
     WinSpan sp;
     HX_TRY(check_span(kv, counts, batch, window, sinks, weights, &sp));
     hipStream_t s = static_cast<hipStream_t>(stream);
