@@ -239,6 +239,9 @@ struct WinPlan {
     unsigned *arrived;
     float *stat;                          // [rows][hq][2], or NULL: a row's largest score and the reciprocal of its sum, for the weights
 };
+// Tiles of 32 positions that a call's rows reach, as the host's lengths have it: of one sequence at most, and groups of eight of all sequences.  They say how many
+// blocks are worth launching, no more: the lengths on the device may be others.
+struct WinReach { int most; int64_t groups; };
 inline int win_row_blocks(int max_n, int G, int rows) { return (int)(((int64_t)max_n * G + rows - 1) / rows); }
 // Caller-owned accumulators of attention weights, [sequence of the cache's batch][kv head][max_seq]
 void f32_launch_win_rope_append(const float *qkv, int hq_l, KvGeom kg, const WinCall &wc, const int32_t *lens, const float *cos_tab, const float *sin_tab,
@@ -247,7 +250,7 @@ void f32_launch_win_append(const TreeIn &in, float *kc, float *vc, KvGeom kg, co
 void f32_launch_win_attn(const float *q, int64_t ldq, const TreeIn &in, float *kc, float *vc, KvGeom kg, int hq_l, const WinCall &wc, const int32_t *lens,
                          const WinPlan &wp, float *o, hipStream_t s);
 void f32_launch_win_weights(const float *q, int64_t ldq, const float *kc, KvGeom kg, int hq_l, const WinCall &wc, const int32_t *lens, const float *stat,
-                            float *weights, int max_tiles, hipStream_t s);
+                            float *weights, const WinReach &reach, hipStream_t s);
 void launch_win_advance(int32_t *lens, const WinCall &wc, hipStream_t s);          // lens += the call's rows, up to max_seq
 
 // ---- eviction ----------------------------------------------------------------------------------------------------------

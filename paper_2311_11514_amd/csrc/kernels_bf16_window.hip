@@ -124,6 +124,24 @@ void launch_win_append(const TreeIn &in, h16_t *kc, h16_t *vc, KvGeom kg, const 
     else hipLaunchKernelGGL(win_append_kernel<64>, grid, dim3(256), 0, s, in, kc, vc, kg, wc, lens);
 }
 
+// ---- statistics and weights ---------------------------------------------------------------------------------------------
+// What a row's softmax is relative to.  Its weights are exp2(s c - base), c = log2(e) / sqrt(d), one multiply-add a score, with base = the rounded product of c and a score
+// near the largest: the same number in the sum, in what is rescaled and in the weights' sums later, so that its rounding cancels.  From 2^20 on, where it would
+// not (a product's last bit is 1/8 there, and at 2^31 an exponent could overflow), the difference of the scores is taken first.  Statistics say which: 1 / sum
+// with its sign changed stands beside a base that is a score.
+constexpr float kWinFarBase = 1048576.0f;
+__device__ __forceinline__ float2 win_stat(float base, float inv, bool score) { return float2{base, score ? -inv : inv}; }
+// sc -> exp2 of its distance from what the lane's statistics (stat, inv) say; far: some row of the wave has a score as its base
+__device__ __forceinline__ void win_exp(floatx16 &sc, float base, float inv, bool far, float scale_log2e) {
+    if (!far) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) sc[x] = __builtin_amdgcn_exp2f(fmaf(sc[x], scale_log2e, -base));
+    } else {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) sc[x] = __builtin_amdgcn_exp2f(inv < 0.f ? (sc[x] - base) * scale_log2e : fmaf(sc[x], scale_log2e, -base));
+    }
+}
+
 // ---- attention, few rows ----------------------------------------------------------------------------------------------
 // A block of eight waves takes 32 query rows and a run of their tiles, which the waves take in turn, K and V straight to registers in the operands'
 // layout (the next unmasked tile's K is requested before this tile's softmax); the waves meet in LDS.  S^T = K . Q^T and O^T = V^T . P^T with P in
@@ -305,7 +323,7 @@ __global__ __launch_bounds__(512, 2) void win_few_kernel(const h16_t *__restrict
     auto finish = [&](int t, int hd, const float (&o)[4], float M, float L) {
         const float inv = 1.0f / L, x[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
         tree_store4(out, t, hd * D + dd, x);
-        if (wp.stat != nullptr && dd == 0) *reinterpret_cast<float2 *>(wp.stat + 2 * ((size_t)t * hq_l + hd)) = float2{M, inv};
+        if (wp.stat != nullptr && dd == 0) *reinterpret_cast<float2 *>(wp.stat + 2 * ((size_t)t * hq_l + hd)) = win_stat(M, inv, true);
     };
 #pragma unroll
     for (int i = 0; i < QUADS; ++i) {
@@ -373,6 +391,13 @@ __global__ __launch_bounds__(512, 2) void win_few_kernel(const h16_t *__restrict
     }
 }
 
+#define WIN_SCHED                                                                              \
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);                                         \
+    _Pragma("unroll") for (int i_ = 0; i_ < 2 * KT; ++i_) {                                    \
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                                     \
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                                     \
+        __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);                                     \
+    }
 // ---- attention, many rows ---------------------------------------------------------------------------------------------
 // A block of four waves takes 128 query rows, 32 a wave; their tiles go from HBM to LDS directly, three in flight, and are shared.  Products and softmax as
 // above.  The rows are in the cache already.
@@ -380,7 +405,7 @@ template <int D>
 __global__ __launch_bounds__(256, 2) void win_attn_kernel(const h16_t *__restrict__ q, int64_t ldq, const h16_t *__restrict__ kc, const h16_t *__restrict__ vc, KvGeom kg,
                                                           int hq_l, int G, int nrb, WinCall wc, const int32_t *__restrict__ lens, WinPlan wp, TreeOut out,
                                                           float scale_log2e) {
-    constexpr int RW = 4, S = 3, ROWS = 32 * RW;
+    constexpr int RW = 4, S = 4, ROWS = 32 * RW;
     constexpr int KT = D / 32, DT = D / 16, DB = D / 32, TILES = 2 * KT + DT;
     constexpr int LPT = TILES / RW;                       // 1 KB loads per wave and step
     __shared__ h16x8 stage[S][TILES][64];
@@ -393,7 +418,6 @@ __global__ __launch_bounds__(256, 2) void win_attn_kernel(const h16_t *__restric
     const int qpos = len + node;
     const int r0w = wk.rb * ROWS + wave * 32;             // the wave's slots; none if it has no row: it feeds the others
     const bool idle = r0w >= R;
-    const int p_lo = len + min(r0w, R - 1) / G, p_hi = len + min(r0w + 31, R - 1) / G;
 
     h16x8 qf[2 * KT];
 #pragma unroll
@@ -403,7 +427,9 @@ __global__ __launch_bounds__(256, 2) void win_attn_kernel(const h16_t *__restric
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int x = 0; x < 16; ++x) oacc[db][x] = 0.f;
-    float m = NEG_INF, lsum = 0.f;
+    float m = NEG_INF, base = 0.f, lsum = 0.f;            // the score that the base was taken from, and the base (win_stat)
+    bool far = false;                                     // of some row of the wave: the base is that score itself
+    const float slack = 8.0f / scale_log2e;
 
     const size_t slab = (size_t)wk.seq * kg.seq_stride + (size_t)wk.c * kg.smax * D;
     const h16x8 *ks = reinterpret_cast<const h16x8 *>(kc + slab), *vs = reinterpret_cast<const h16x8 *>(vc + slab);
@@ -421,40 +447,79 @@ __global__ __launch_bounds__(256, 2) void win_attn_kernel(const h16_t *__restric
     HX_WAIT_VM(0);            // the query rows have landed before the first load that the compiler does not see
     issue(0);
     if (steps > 1) issue(1);
-    // a step whose tile every row of the block attends (TAIL false), or one that needs a mask
-    auto walk = [&](int step, auto tail) {
-        constexpr bool TAIL = decltype(tail)::value;
-        if (step + 1 < steps) HX_WAIT_VM(LPT);            // step + 1 may stay in flight
-        else HX_WAIT_VM(0);
-        HX_LDS_BARRIER();
-        if (step + S - 1 < steps) issue(step + S - 1);    // into the buffer that every wave has left
-        const int t = wk.tiles.at(step);
-        if (idle || (TAIL && !win_any(32 * t, 32, p_lo, p_hi, wc.window, wc.sinks))) return;
+    if (steps > 2) issue(2);
+    auto scores = [&](int step, floatx16 &sc) {
         const h16x8(*st)[64] = stage[step % S];
-        floatx16 sc;
 #pragma unroll
         for (int x = 0; x < 16; ++x) sc[x] = 0.f;
 #pragma unroll
         for (int kk = 0; kk < 2 * KT; ++kk) sc = hx_mfma32(st[sub * KT + (kk >> 1)][fl + 32 * (kk & 1)], qf[kk], sc);
+    };
+    if (steps > 2) HX_WAIT_VM(2 * LPT);
+    else if (steps > 1) HX_WAIT_VM(LPT);
+    else HX_WAIT_VM(0);
+    HX_LDS_BARRIER();
+    floatx16 sc;
+    scores(0, sc);
+    // a step whose tile every row of the block attends (TAIL false), or one that needs a mask; sc holds its scores
+    auto walk = [&](int step, auto tail) {
+        constexpr bool TAIL = decltype(tail)::value;
+        if (step + 2 < steps) HX_WAIT_VM(LPT);            // step + 2 may stay in flight
+        else HX_WAIT_VM(0);
+        HX_LDS_BARRIER();
+        if (step + 3 < steps) issue(step + 3);            // into the buffer that every wave has left
+        if (idle) return;
+        const int t = wk.tiles.at(step);
+        const h16x8(*st)[64] = stage[step % S];
         uint32_t sees = 0xffffffffu;
         if constexpr (TAIL) {
             sees = win_sees(32 * t, qpos, wc.window, wc.sinks);
 #pragma unroll
             for (int x = 0; x < 16; ++x) sc[x] = (sees >> (8 * (x >> 2) + 4 * hl + (x & 3))) & 1u ? sc[x] : NEG_INF;
         }
-        const float alpha = tree_softmax(sc, m, lsum, scale_log2e);
-        if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+        float mx = NEG_INF;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) mx = fmaxf(mx, sc[x]);
+        mx = max_halves(mx);
+        // A larger score moves the base only if its weight would pass 2^8: what has been summed up is rescaled for the first tiles of a row and hardly again.
+        // (Any base is right: numerator and sum are relative to the same one, in floating point.)
+        if (__builtin_amdgcn_ballot_w64(mx > m + slack) != 0) {
+            const float m_new = fmaxf(m, mx), to = m_new == NEG_INF ? 0.f : m_new;       // a row that has seen nothing yet: weights 0, no NaN
+            const bool was = far;
+            far = far || __builtin_amdgcn_ballot_w64(fabsf(to * scale_log2e) >= kWinFarBase) != 0;
+            const float from = was ? base : m, next = far ? to : to * scale_log2e;
+            const float alpha = __builtin_amdgcn_exp2f(far ? (from - to) * scale_log2e : m == NEG_INF ? NEG_INF : base - next);
+            m = m_new;
+            base = next;
+            lsum *= alpha;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
                 for (int x = 0; x < 16; ++x) oacc[db][x] *= alpha;
         }
+        // the next tile's scores on the matrix cores while this one's weights are on the vector unit
+        floatx16 ahead;
+        float ps = 0.f;
+        if (far) {
+            scores(min(step + 1, steps - 1), ahead);
+            win_exp(sc, base, -1.f, true, scale_log2e);
+#pragma unroll
+            for (int x = 0; x < 16; ++x) ps += sc[x];
+        } else {
+            scores(min(step + 1, steps - 1), ahead);
+            win_exp(sc, base, 1.f, false, scale_log2e);
+#pragma unroll
+            for (int x = 0; x < 16; ++x) ps += sc[x];
+            WIN_SCHED
+        }
+        lsum += ps;
         if constexpr (TAIL) {
             bool odd = false;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) odd = odd || any_odd(st[2 * KT + dt][lane]);
             if (__builtin_amdgcn_ballot_w64(odd) != 0) {
                 tree_slow_tile<DB>(reinterpret_cast<const h16_t *>(st[2 * KT]), sc, sees, lane, oacc);
+                sc = ahead;
                 return;
             }
         }
@@ -467,9 +532,10 @@ __global__ __launch_bounds__(256, 2) void win_attn_kernel(const h16_t *__restric
                 p[g].u[i] = pack_h16x2(sc[x], sc[x + 1]);
             }
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
+        for (int g = 0; g < 2; ++g)
 #pragma unroll
-            for (int g = 0; g < 2; ++g) oacc[db] = hx_mfma32(st[2 * KT + 2 * db + sub][fl + 32 * g], p[g].v, oacc[db]);
+            for (int db = 0; db < DB; ++db) oacc[db] = hx_mfma32(st[2 * KT + 2 * db + sub][fl + 32 * g], p[g].v, oacc[db]);
+        sc = ahead;
     };
     int step = 0;
     for (; step < wk.tiles.clean; ++step) walk(step, std::false_type{});
@@ -484,14 +550,14 @@ __global__ __launch_bounds__(256, 2) void win_attn_kernel(const h16_t *__restric
             const float x[4] = {oacc[db][4 * qd] * inv, oacc[db][4 * qd + 1] * inv, oacc[db][4 * qd + 2] * inv, oacc[db][4 * qd + 3] * inv};
             tree_store4(out, row0 + node, head * D + 32 * db + 8 * qd + 4 * hl, x);
         }
-    if (wp.stat != nullptr && hl == 0) *reinterpret_cast<float2 *>(wp.stat + 2 * ((size_t)(row0 + node) * hq_l + head)) = float2{m, inv};
+    if (wp.stat != nullptr && hl == 0) *reinterpret_cast<float2 *>(wp.stat + 2 * ((size_t)(row0 + node) * hq_l + head)) = win_stat(base, inv, far);
 }
 
 void launch_win_attn(const h16_t *q, const h16_t *q_lo, int64_t ldq, const TreeIn &in, h16_t *kc, h16_t *vc, KvGeom kg, int hq_l, const WinCall &wc,
                      const int32_t *lens, const WinPlan &wp, const TreeOut &out, hipStream_t s) {
     const int G = hq_l / kg.hkv_l, nrb = win_row_blocks(wc.max_n, G, wp.shared ? 128 : 32);
     const float scale_log2e = 1.4426950408889634f / sqrtf((float)kg.d);
-    const dim3 grid((unsigned)nrb * (unsigned)((wc.batch * kg.hkv_l * wp.nsplit + 7) / 8 * 8));
+    const dim3 grid(win_grid(wc.batch * kg.hkv_l * wp.nsplit, nrb));
 #define HX_WIN_D(DD)                                                                                                                                               \
     do {                                                                                                                                                           \
         if (wp.shared) hipLaunchKernelGGL((win_attn_kernel<DD>), grid, dim3(256), 0, s, q, ldq, kc, vc, kg, hq_l, G, nrb, wc, lens, wp, out, scale_log2e);          \
@@ -543,19 +609,15 @@ __global__ __launch_bounds__(256, 4) void win_weights_kernel(const h16_t *__rest
             }
 #pragma unroll
             for (int kk = 0; kk < 2 * KT; ++kk) sc = hx_mfma32(kf[kk], *reinterpret_cast<const h16x8 *>(q + at + 16 * kk), sc);
-            const float inv = r < R ? ml.y : 0.f;
+            const float a = ml.y < 0.f ? ml.x : 0.f, b = ml.y < 0.f ? 0.f : ml.x, inv = fabsf(ml.y);         // (win_stat)
             const int first = len + 32 * g / G, last = len + min(32 * g + 31, R - 1) / G;
-            if (win_all(p0, 32, first, last, wc.window, wc.sinks) && 32 * g + 31 < R) {
-#pragma unroll
-                for (int x = 0; x < 16; ++x) acc[x] = fmaf(__builtin_amdgcn_exp2f((sc[x] - ml.x) * scale_log2e), inv, acc[x]);
-            } else {
+            if (32 * g + 31 >= R || !win_all(p0, 32, first, last, wc.window, wc.sinks)) {
                 const uint32_t sees = r < R ? win_sees(p0, len + node, wc.window, wc.sinks) : 0u;
 #pragma unroll
-                for (int x = 0; x < 16; ++x) {
-                    const float w = __builtin_amdgcn_exp2f((sc[x] - ml.x) * scale_log2e) * inv;
-                    acc[x] += (sees >> (8 * (x >> 2) + 4 * hl + (x & 3))) & 1u ? w : 0.f;
-                }
+                for (int x = 0; x < 16; ++x) sc[x] = (sees >> (8 * (x >> 2) + 4 * hl + (x & 3))) & 1u ? sc[x] : NEG_INF;
             }
+#pragma unroll
+            for (int x = 0; x < 16; ++x) acc[x] = fmaf(__builtin_amdgcn_exp2f(fmaf(sc[x] - a, scale_log2e, -b)), inv, acc[x]);
         }
         float mine = 0.f;
 #pragma unroll
@@ -586,10 +648,10 @@ __global__ __launch_bounds__(256, 2) void win_weights_shared_kernel(const h16_t 
     __shared__ h16x8 s_q[S][PIECES][64];
     __shared__ float s_stat[S][W][64];                        // largest score and 1 / sum of the group's rows, a copy for every wave
     __shared__ int s_last;
-    int id = blockIdx.x;
-    const int split = id % splits;
-    id /= splits;
-    const int tb = id % tile_blocks, c = (id / tile_blocks) % kg.hkv_l, nth = id / tile_blocks / kg.hkv_l;
+    int pair, id;
+    win_place(wc.batch * kg.hkv_l, tile_blocks * splits, &pair, &id);
+    if (pair >= wc.batch * kg.hkv_l) return;
+    const int split = id % splits, tb = id / splits, c = pair % kg.hkv_l, nth = wc.order[pair / kg.hkv_l];
     const int seq = wc.seq0 + nth, row0 = wc.cu[nth], len = lens[seq], n = min(wc.cu[nth + 1] - row0, wc.max_seq - len);
     if (n <= 0) return;
     WinTiles tiles;
@@ -607,12 +669,14 @@ __global__ __launch_bounds__(256, 2) void win_weights_shared_kernel(const h16_t 
         g0 += split * share;
         g1 = min(g1, g0 + share);
         int p0[TW];
+        bool live[TW];
         h16x8 kf[TW][2 * KT];
         floatx16 acc[TW];
 #pragma unroll
         for (int w = 0; w < TW; ++w) {
             const int v = v0 + TW * wave + w, t = tiles.at(min(v, tiles.nt - 1));
-            p0[w] = v < tiles.nt ? 32 * t : -1;               // none: the wave feeds the others
+            p0[w] = 32 * t;                                   // past the last tile it once more, not stored
+            live[w] = v < tiles.nt;
             const h16_t *src = slab + ((size_t)(2 * t + sub) * KT * 64 + fl) * 8;
 #pragma unroll
             for (int kk = 0; kk < 2 * KT; ++kk) kf[w][kk] = *reinterpret_cast<const h16x8 *>(src + ((kk >> 1) * 64 + 32 * (kk & 1)) * 8);
@@ -649,35 +713,41 @@ __global__ __launch_bounds__(256, 2) void win_weights_shared_kernel(const h16_t 
             else HX_WAIT_VM(0);
             HX_LDS_BARRIER();
             if (g + 2 < g1) issue(g + 2);                     // into the buffer that every wave has left
-            const float m = s_stat[g % S][wave][2 * i32], inv = s_stat[g % S][wave][2 * i32 + 1];
-            floatx16 sc[TW];
+            const float base = s_stat[g % S][wave][2 * i32], given = s_stat[g % S][wave][2 * i32 + 1];
+            const float a = given < 0.f ? base : 0.f, b = given < 0.f ? 0.f : base, inv = fabsf(given);      // (win_stat)
+            const int first = len + __builtin_amdgcn_readfirstlane(node), last = len + __builtin_amdgcn_readlane(node, 31);
+            h16x8 rows[PIECES];
 #pragma unroll
-            for (int w = 0; w < TW; ++w)
+            for (int x = 0; x < PIECES; ++x) rows[x] = s_q[g % S][x][lane];
+            floatx16 sc[TW];
+            auto scores = [&](int w) {
 #pragma unroll
                 for (int x = 0; x < 16; ++x) sc[w][x] = 0.f;
 #pragma unroll
-            for (int piece = PIECES - 1; piece >= 0; --piece) {
-                const h16x8 row = s_q[g % S][piece][lane];
+                for (int x = PIECES - 1; x >= 0; --x) sc[w] = hx_mfma32(kf[w][x % (2 * KT)], rows[x], sc[w]);
+            };
+            auto mask = [&](int w) {
+                if (last < len + n && win_all(p0[w], 32, first, last, wc.window, wc.sinks)) return;
+                const uint32_t sees = node < n ? win_sees(p0[w], len + node, wc.window, wc.sinks) : 0u;
 #pragma unroll
-                for (int w = 0; w < TW; ++w) sc[w] = hx_mfma32(kf[w][piece % (2 * KT)], row, sc[w]);
+                for (int x = 0; x < 16; ++x) sc[w][x] = (sees >> (8 * (x >> 2) + 4 * hl + (x & 3))) & 1u ? sc[w][x] : NEG_INF;
+            };
+            auto add = [&](int w) {
+#pragma unroll
+                for (int x = 0; x < 16; ++x) acc[w][x] = fmaf(__builtin_amdgcn_exp2f(fmaf(sc[w][x] - a, scale_log2e, -b)), inv, acc[w][x]);
+            };
+            static_assert(TW == 2, "the second tile's scores on the matrix cores while the first one's weights are on the vector unit");
+            scores(0);
+            mask(0);
+            scores(1);
+            add(0);
+#pragma unroll
+            for (int x = 0; x < PIECES; ++x) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);      // a matrix instruction, then what the vector unit does meanwhile
+                __builtin_amdgcn_sched_group_barrier(0x002, 64 / PIECES, 0);
             }
-            const bool there = node < n;
-            const int first = len + __builtin_amdgcn_readfirstlane(node), last = len + __builtin_amdgcn_readlane(node, 31);
-#pragma unroll
-            for (int w = 0; w < TW; ++w) {
-                if (p0[w] < 0) continue;
-                if (last < len + n && win_all(p0[w], 32, first, last, wc.window, wc.sinks)) {
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) acc[w][x] = fmaf(__builtin_amdgcn_exp2f((sc[w][x] - m) * scale_log2e), inv, acc[w][x]);
-                } else {
-                    const uint32_t sees = there ? win_sees(p0[w], len + node, wc.window, wc.sinks) : 0u;
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        const float weight = __builtin_amdgcn_exp2f((sc[w][x] - m) * scale_log2e) * inv;
-                        acc[w][x] += (sees >> (8 * (x >> 2) + 4 * hl + (x & 3))) & 1u ? weight : 0.f;
-                    }
-                }
-            }
+            mask(1);
+            add(1);
             node += per32; head += rem32;
             if (head >= G) { head -= G; ++node; }
         }
@@ -695,7 +765,7 @@ __global__ __launch_bounds__(256, 2) void win_weights_shared_kernel(const h16_t 
             const int pos = 8 * ((i32 & 15) >> 2) + 4 * hl + (i32 & 3);
             if (i32 >= 16) continue;
             if (splits > 1) dev_store(part + ((unit * splits + split) * W + wave) * TW * 32 + 32 * w + pos, mine);
-            else if (p0[w] >= 0 && p0[w] + pos < len + n) weights[((size_t)seq * kg.hkv_l + c) * wc.max_seq + p0[w] + pos] += mine;
+            else if (live[w] && p0[w] + pos < len + n) weights[((size_t)seq * kg.hkv_l + c) * wc.max_seq + p0[w] + pos] += mine;
         }
         if (splits > 1 && tree_arrive(arrived + unit, splits, &s_last)) {
             const int x = threadIdx.x, v = v0 + x / 32;       // one of the block's positions per thread
@@ -710,16 +780,24 @@ __global__ __launch_bounds__(256, 2) void win_weights_shared_kernel(const h16_t 
 }
 
 void launch_win_weights(const h16_t *q, const h16_t *q_lo, int64_t ldq, const h16_t *kc, KvGeom kg, int hq_l, const WinCall &wc, const int32_t *lens,
-                        const WinPlan &wp, float *weights, int max_tiles, hipStream_t s) {
+                        const WinPlan &wp, float *weights, const WinReach &reach, hipStream_t s) {
     const int G = hq_l / kg.hkv_l;
     const float scale_log2e = 1.4426950408889634f / sqrtf((float)kg.d);
     const bool shared = (int64_t)wc.max_n * G > 64;
-    const int tile_blocks = (max_tiles + (shared ? 7 : 3)) / (shared ? 8 : 4);
+    const int tile_blocks = (reach.most + (shared ? 7 : 3)) / (shared ? 8 : 4);
     const int64_t blocks = (int64_t)tile_blocks * kg.hkv_l * wc.batch, groups = ((int64_t)wc.max_n * G + 31) / 32;
     int splits = 1;
     const int64_t units = (int64_t)wc.batch * kg.hkv_l * win_units(kg.smax);        // a length on the device may be beyond what the host knows
-    if (shared && blocks < 512 && units <= kWinUnits) splits = (int)std::max<int64_t>(1, std::min<int64_t>({(767 + blocks) / blocks, groups / 8, (int64_t)kWinPartFloats / (256 * units)}));
-    const dim3 grid((unsigned)(blocks * splits));
+    // Two blocks a CU: so many rounds of 512, each of a block's share of the groups and of what it costs besides (keys, the first rows' way, its sums: as
+    // much as six groups)
+    if (shared && units <= kWinUnits) {
+        int64_t least = INT64_MAX;
+        for (int64_t x = 1; x <= std::min<int64_t>({16, (groups + 7) / 8, (int64_t)kWinPartFloats / (256 * units)}); ++x) {
+            const int64_t cost = (reach.groups * kg.hkv_l * x + 511) / 512 * ((groups + x - 1) / x + 6);
+            if (cost < least) { least = cost; splits = (int)x; }
+        }
+    }
+    const dim3 grid(shared ? win_grid(kg.hkv_l * wc.batch, tile_blocks * splits) : (unsigned)blocks);
 #define HX_WIN_W(DD, LO)                                                                                                                                            do {                                                                                                                                                                if (shared) hipLaunchKernelGGL((win_weights_shared_kernel<DD, LO>), grid, dim3(256), 0, s, q, q_lo, ldq, kc, kg, hq_l, G, tile_blocks, splits, wc, lens, wp.stat, weights, wp.part_o, wp.arrived, scale_log2e);         else hipLaunchKernelGGL((win_weights_kernel<DD, LO>), grid, dim3(256), 0, s, q, q_lo, ldq, kc, kg, hq_l, G, tile_blocks, wc, lens, wp.stat, weights, scale_log2e);     } while (0)
     if (kg.d == 128) { if (q_lo != nullptr) HX_WIN_W(128, true); else HX_WIN_W(128, false); }
     else { if (q_lo != nullptr) HX_WIN_W(64, true); else HX_WIN_W(64, false); }

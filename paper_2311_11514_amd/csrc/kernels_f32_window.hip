@@ -525,13 +525,13 @@ void f32_launch_win_append(const TreeIn &in, float *kc, float *vc, KvGeom kg, co
 void f32_launch_win_attn(const float *q, int64_t ldq, const TreeIn &in, float *kc, float *vc, KvGeom kg, int hq_l, const WinCall &wc, const int32_t *lens,
                          const WinPlan &wp, float *o, hipStream_t s) {
     const int G = hq_l / kg.hkv_l, nrb = win_row_blocks(wc.max_n, G, 16);
-    const dim3 grid((unsigned)nrb * (unsigned)((wc.batch * kg.hkv_l * wp.nsplit + 7) / 8 * 8));
+    const dim3 grid(win_grid(wc.batch * kg.hkv_l * wp.nsplit, nrb));
     if (kg.d == 128) hipLaunchKernelGGL((f32_win_attn_kernel<128, 4>), grid, dim3(256), 0, s, q, ldq, in, kc, vc, kg, hq_l, G, nrb, wc, lens, wp, o);
     else hipLaunchKernelGGL((f32_win_attn_kernel<64, 4>), grid, dim3(256), 0, s, q, ldq, in, kc, vc, kg, hq_l, G, nrb, wc, lens, wp, o);
 }
 void f32_launch_win_weights(const float *q, int64_t ldq, const float *kc, KvGeom kg, int hq_l, const WinCall &wc, const int32_t *lens, const float *stat,
-                            float *weights, int max_tiles, hipStream_t s) {
-    const int G = hq_l / kg.hkv_l, tile_blocks = (2 * max_tiles + 3) / 4;
+                            float *weights, const WinReach &reach, hipStream_t s) {
+    const int G = hq_l / kg.hkv_l, tile_blocks = (2 * reach.most + 3) / 4;
     const dim3 grid((unsigned)tile_blocks * kg.hkv_l * wc.batch);
     if (kg.d == 128) hipLaunchKernelGGL(f32_win_weights_kernel<128>, grid, dim3(256), 0, s, q, ldq, kc, kg, hq_l, G, tile_blocks, wc, lens, stat, weights);
     else hipLaunchKernelGGL(f32_win_weights_kernel<64>, grid, dim3(256), 0, s, q, ldq, kc, kg, hq_l, G, tile_blocks, wc, lens, stat, weights);

@@ -522,17 +522,17 @@ WinPlan pick_win_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, WinCall
     return wp;
 }
 
-// tiles of 32 positions that a call's rows reach, at most; the host's lengths say how many blocks are worth launching, no more
-int win_reach(const hexgen_kv_cache *kv, const WinCall &wc) {
-    int most = 1;
+WinReach win_reach(const hexgen_kv_cache *kv, const WinCall &wc) {
+    WinReach r{1, 0};
     for (int i = 0; i < wc.batch; ++i) {
         const int n = wc.cu[i + 1] - wc.cu[i], len = kv->lens[wc.seq0 + i];
         if (n == 0) continue;
         WinTiles t;
         t.set(len, len + n - 1, wc.window, wc.sinks, 0);
-        most = std::max(most, t.nt);
+        r.most = std::max(r.most, t.nt);
+        r.groups += (t.nt + 7) / 8;
     }
-    return most;
+    return r;
 }
 
 // The rows' attention in one layer.  in.k given: their keys and values join the cache here, in the attention itself where a sequence's rows are one

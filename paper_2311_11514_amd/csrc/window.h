@@ -46,17 +46,34 @@ __device__ __forceinline__ bool win_any(int p0, int width, int p_lo, int p_hi, i
     return p0 <= p_hi && (p0 + width - 1 > p_lo - window || p0 < sinks);
 }
 
+// Which of `units` (each `per` blocks) a block belongs to, and which of its blocks it is.  Ids go round the 8 XCDs.  Many units, or a multiple of 8: a unit's
+// blocks sit next to each other on one XCD and share what they read in that L2, and the units, which come in falling order of their work, are dealt there and back
+// so that no XCD gets the larger one every time; a few others: block by block, so that every XCD has some.
+__host__ __device__ inline bool win_grouped(int units) { return units % 8 == 0 || units >= 64; }
+__host__ __device__ inline unsigned win_grid(int units, int per) { return (unsigned)per * (unsigned)(win_grouped(units) ? (units + 7) / 8 * 8 : units); }
+__device__ __forceinline__ void win_place(int units, int per, int *unit, int *nth) {
+    const unsigned id = blockIdx.x;
+    if (win_grouped(units)) {
+        *nth = (int)((id >> 3) % (unsigned)per);
+        const int round = (int)((id >> 3) / (unsigned)per);
+        *unit = 8 * round + (int)(round & 1 ? 7 - (id & 7) : id & 7);        // at least `units`: no work
+    } else {
+        *nth = (int)(id / (unsigned)units);
+        *unit = (int)(id % (unsigned)units);
+    }
+}
+
 // What a block works on: `rows` query rows of one (sequence, kv head) -- row r: new row r / G of the sequence, head r % G -- and a run of their
-// tiles.  Block id = 8 slot + xcd: the blocks of a (sequence, kv head) sit next to each other on one XCD and share its keys and values in that L2, the last
-// rows, which reach furthest, first; sequences in wc.order.
+// tiles.  The last rows, which reach furthest, first; sequences in wc.order.
 struct WinWork {
     int rb, split, c, seq, nth, row0, n, R, len, per, v0, v1;
     WinTiles tiles;
     __device__ __forceinline__ bool find(int hkv, int G, int nrb, int rows, const WinCall &wc, const int32_t *lens, const WinPlan &wp, bool fresh) {
-        const unsigned slot = blockIdx.x >> 3;
-        rb = nrb - 1 - (int)(slot % (unsigned)nrb);
-        int combo = (int)(slot / (unsigned)nrb) * 8 + (blockIdx.x & 7);
-        if (combo >= wc.batch * hkv * wp.nsplit) return false;
+        const int units = wc.batch * hkv * wp.nsplit;
+        int combo;
+        win_place(units, nrb, &combo, &rb);
+        rb = nrb - 1 - rb;
+        if (combo >= units) return false;
         split = combo % wp.nsplit;
         combo /= wp.nsplit;
         c = combo % hkv;
