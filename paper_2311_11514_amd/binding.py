@@ -436,12 +436,21 @@ class KVCache:
         shape = (st.n_layers, max(batch, 1), st.hkv_l, dst.max_seq)
         if weights is not None:
             _device_tensor(weights, "weights", (st.n_layers, batch, st.hkv_l, self.max_seq), torch.float32)
-        with torch.cuda.stream(stream):                        # results from the memory of the stream that the call is on
-            slots = torch.empty(shape, dtype=torch.int32, device="cuda")
-            left = weights if weights is None or dst is self else torch.empty(shape, dtype=torch.float32, device="cuda")
+        if stream is None:
+            slots, left = _evicted(shape, weights, dst is self)
+        else:
+            with torch.cuda.stream(stream):                    # results from the memory of the stream that the call is on
+                slots, left = _evicted(shape, weights, dst is self)
         _check(lib.hexgen_kv_cache_evict(self.handle, dst.handle, keep, sinks, recent, None if weights is None else weights.data_ptr(),
                                          None if left is None else left.data_ptr(), int(rotate), slots.data_ptr(), _stream_handle(stream)), "hexgen_kv_cache_evict")
         return slots, left
+
+
+def _evicted(shape, weights: Optional[torch.Tensor], in_place: bool):
+    """What an eviction writes: the slots that stay, and their weights (in place: over those that were given)."""
+    if weights is None:
+        return torch.empty(shape, dtype=torch.int32, device="cuda"), None
+    return weights.new_empty(shape, dtype=torch.int32), weights if in_place else weights.new_empty(shape)
 
 
 class Tree:

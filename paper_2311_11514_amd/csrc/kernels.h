@@ -262,7 +262,7 @@ struct EvictCall {
     float *w_out;
     int32_t *slots;
 };
-void launch_evict_select(const EvictCall &ec, const int32_t *lens, hipStream_t s);
+void launch_evict_select(const EvictCall &ec, int longest, const int32_t *lens, hipStream_t s);      // longest: the longest context that the host knows of
 // the kept rows of a cache, src -> dst (the same memory: in place), keys rotated back by how far they move where cos_tab is given; then
 // dst_lens = what is left, zero behind the batch
 struct EvictMove {

@@ -811,9 +811,10 @@ void launch_win_weights(const h16_t *q, const h16_t *q_lo, int64_t ldq, const h1
 // Keys that are rotated back by their distance are rotated in fp32 and rounded to the element type once more.
 template <int D, bool ROT>
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictCall ec, EvictMove mv, int blocks) {
-    constexpr int P8 = D / 8, PIECES = 32 * P8 / 256, HALF = D / 2;
-    __shared__ __align__(16) h16_t s_v[D][34];                 // [element][row of the chunk]
+    constexpr int KT = D / 32, PIECES = ROT ? 2 : 2 * KT / 4, HALF = D / 2;
+    __shared__ h16_t s_v[32][D + 2];
     __shared__ int s_slot[32];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const unsigned unit = blockIdx.x / (unsigned)blocks;
     const int chunk = (int)(blockIdx.x % (unsigned)blocks), c = unit % ec.hkv, b = (unit / ec.hkv) % ec.batch, layer = unit / ec.hkv / ec.batch;
     const int32_t *slots = ec.slots + (size_t)unit * ec.dst_seq;
@@ -830,46 +831,52 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictCall ec, EvictMove
         __syncthreads();
         if (s_slot[0] < 0) break;                              // the same in every thread: the kept ones come first
         if (mv.ks == mv.kd && s_slot[31] == j0 + 31) continue;  // in place, and none of them moves
-        uint4 k[PIECES];
-        // a thread's piece i: row (threadIdx.x + 256 i) / P8 of the chunk, elements 8 ((threadIdx.x + 256 i) % P8) ..; slots that are not taken read slot 0
+        // a wave's piece i: one fragment tile, 16 rows x 32 elements, as it lies in the destination (rotated: and the one half a head further); rows that are not
+        // there read slot 0
+        typedef uint32_t piece __attribute__((ext_vector_type(4)));
+        piece k[PIECES];
+        constexpr int ACROSS = ROT ? KT / 2 : KT;
+        const bool has = !ROT || wave < KT;                     // a rotated head of 64 is two waves' work
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const int idx = threadIdx.x + 256 * i, at = max(s_slot[idx / P8], 0), dd = 8 * (idx % P8);
-            const uint4 a = *reinterpret_cast<const uint4 *>(ks + kv_k_offset(at, dd, D));
-            if constexpr (ROT) {
-                const uint4 o = *reinterpret_cast<const uint4 *>(ks + kv_k_offset(at, dd < HALF ? dd + HALF : dd - HALF, D));
-                const int moved = max(at - (j0 + idx / P8), 0), i0 = dd < HALF ? dd : dd - HALF;
-                const float *cs = mv.cos_tab + (size_t)moved * HALF + i0, *sn = mv.sin_tab + (size_t)moved * HALF + i0;
-                const uint32_t au[4] = {a.x, a.y, a.z, a.w}, ou[4] = {o.x, o.y, o.z, o.w};
-                uint32_t r[4];
+            const int tile = wave + (ROT ? 0 : 4 * i), row = 16 * (tile / ACROSS) + (lane & 15), dd = 32 * (tile % ACROSS) + 8 * (lane >> 4) + (ROT ? HALF * i : 0);
+            k[i] = *reinterpret_cast<const piece *>(ks + kv_k_offset(has ? max(s_slot[row], 0) : 0, dd, D));
+        }
+        if constexpr (ROT) {
+            const int row = 16 * (wave / ACROSS) + (lane & 15), dd = 32 * (wave % ACROSS) + 8 * (lane >> 4);
+            const int moved = has ? max(s_slot[row] - (j0 + row), 0) : 0;
+            if (moved != 0) {
+                const floatx4 *cs = reinterpret_cast<const floatx4 *>(mv.cos_tab + (size_t)moved * HALF + dd), *sn = reinterpret_cast<const floatx4 *>(mv.sin_tab + (size_t)moved * HALF + dd);
+                piece &lo = k[0], &hi = k[PIECES - 1];
 #pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                    float a0, a1, o0, o1;
-                    h16x2_to_f32(au[p], a0, a1);
-                    h16x2_to_f32(ou[p], o0, o1);
-                    const float s0 = dd < HALF ? sn[2 * p] : -sn[2 * p], s1 = dd < HALF ? sn[2 * p + 1] : -sn[2 * p + 1];
-                    r[p] = moved == 0 ? au[p] : pack_h16x2(a0 * cs[2 * p] + o0 * s0, a1 * cs[2 * p + 1] + o1 * s1);
+                for (int h = 0; h < 2; ++h) {
+                    const floatx4 c4 = cs[h], s4 = sn[h];
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) {
+                        float a0, a1, b0, b1;
+                        h16x2_to_f32(lo[2 * h + p], a0, a1);
+                        h16x2_to_f32(hi[2 * h + p], b0, b1);
+                        lo[2 * h + p] = pack_h16x2(a0 * c4[2 * p] + b0 * s4[2 * p], a1 * c4[2 * p + 1] + b1 * s4[2 * p + 1]);
+                        hi[2 * h + p] = pack_h16x2(b0 * c4[2 * p] - a0 * s4[2 * p], b1 * c4[2 * p + 1] - a1 * s4[2 * p + 1]);
+                    }
                 }
-                k[i] = uint4{r[0], r[1], r[2], r[3]};
-            } else {
-                k[i] = a;
             }
         }
         for (int idx = threadIdx.x; idx < 32 * D; idx += 256) {
-            const int row = idx & 31, dd = idx >> 5;           // a wave: two elements of the 32 rows, in slots that lie close to each other
-            s_v[dd][row] = vs[kv_v_offset(max(s_slot[row], 0), dd, D)];
+            const int row = idx / D, dd = idx % D;             // a wave: 64 elements of one row, two bytes of every 16 (kvlayout.h)
+            s_v[row][dd] = vs[kv_v_offset(max(s_slot[row], 0), dd, D)];
         }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const int idx = threadIdx.x + 256 * i, row = idx / P8;
-            if (s_slot[row] >= 0) *reinterpret_cast<uint4 *>(kd + kv_k_offset(j0 + row, 8 * (idx % P8), D)) = k[i];
+            const int tile = wave + (ROT ? 0 : 4 * i), row = 16 * (tile / ACROSS) + (lane & 15), dd = 32 * (tile % ACROSS) + 8 * (lane >> 4) + (ROT ? HALF * i : 0);
+            if (has && s_slot[row] >= 0) *reinterpret_cast<piece *>(kd + kv_k_offset(j0 + row, dd, D)) = k[i];
         }
         for (int idx = threadIdx.x; idx < 4 * D; idx += 256) {
             const int dd = (idx & 15) + 16 * (idx >> 6), g = (idx >> 4) & 3;    // 16-byte pieces in the order in which they lie (kvlayout.h)
             union { uint4 u; h16_t e[8]; } w;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w.e[j] = s_v[dd][4 * g + (j & 3) + 16 * (j >> 2)];
+            for (int j = 0; j < 8; ++j) w.e[j] = s_v[4 * g + (j & 3) + 16 * (j >> 2)][dd];
             h16_t *at = vd + kv_v_offset(j0 + 4 * g, dd, D);
             if (s_slot[31] >= 0) {
                 *reinterpret_cast<uint4 *>(at) = w.u;

@@ -254,12 +254,13 @@ __global__ __launch_bounds__(64 * W) void f32_win_attn_kernel(const float *__res
     }
 }
 
-// weights[j] += sum over rows and heads of exp(s_rj - m_r) / l_r, as in the 16-bit kernel: a wave keeps the keys of 16 positions and goes through the rows that
-// attend them, 16 columns at a time
-template <int D>
-__global__ __launch_bounds__(256) void f32_win_weights_kernel(const float *__restrict__ q, int64_t ldq, const float *__restrict__ kc, KvGeom kg, int hq_l, int G, int tile_blocks,
-                                                              WinCall wc, const int32_t *__restrict__ lens, const float *__restrict__ stat, float *__restrict__ weights) {
+// weights[j] += sum over rows and heads of exp(s_rj - m_r) / l_r, as in the 16-bit kernels: a block takes 16 positions, whose keys all of its waves hold; the waves
+// take the rows that attend them in turn, 16 columns at a time, the next ones' requested ahead, and meet in LDS in the order of the waves.
+template <int D, int W>
+__global__ __launch_bounds__(64 * W) void f32_win_weights_kernel(const float *__restrict__ q, int64_t ldq, const float *__restrict__ kc, KvGeom kg, int hq_l, int G, int tile_blocks,
+                                                                 WinCall wc, const int32_t *__restrict__ lens, const float *__restrict__ stat, float *__restrict__ weights) {
     constexpr int KT = D / 16;
+    __shared__ float s_sum[W][16];
     const int tb = blockIdx.x % tile_blocks, c = (blockIdx.x / tile_blocks) % kg.hkv_l, nth = blockIdx.x / tile_blocks / kg.hkv_l;
     const int seq = wc.seq0 + nth, row0 = wc.cu[nth], len = lens[seq], n = min(wc.cu[nth + 1] - row0, wc.max_seq - len), R = n * G;
     if (n <= 0) return;
@@ -268,30 +269,44 @@ __global__ __launch_bounds__(256) void f32_win_weights_kernel(const float *__res
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, i = lane & 15, g4 = lane >> 4;
     const int seen = len + n - 1;
     const float scale = 1.0f / sqrtf((float)D);
-    for (int u = 4 * tb + wave; u < 2 * tiles.nt; u += 4 * tile_blocks) {
+    for (int u = tb; u < 2 * tiles.nt; u += tile_blocks) {
         const int p0 = 32 * tiles.at(u >> 1) + 16 * (u & 1);
-        if (p0 > seen) continue;
+        if (p0 > seen) continue;                              // the same in every wave
         const float *kp = kc + (size_t)seq * kg.seq_stride + ((size_t)c * kg.smax + min(p0 + i, seen)) * D + 4 * g4;
-        floatx4 kf[KT];
-#pragma unroll
-        for (int k = 0; k < KT; ++k) kf[k] = *reinterpret_cast<const floatx4 *>(kp + 16 * k);
         const int x_lo = max(0, p0 - len), x_hi = p0 < wc.sinks ? n - 1 : min(n - 1, p0 + 15 + wc.window - 1 - len);
-        float acc[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int g = x_lo * G / 16; g <= (x_hi * G + G - 1) / 16; ++g) {
-            const int r = 16 * g + i, rr = min(r, R - 1), node = rr / G, head = c * G + (rr - node * G);
+        const int last = (x_hi * G + G - 1) / 16;
+        floatx4 kf[KT], qf[KT];
+        float2 ml;
+        auto load_q = [&](int g) {
+            const int rr = min(16 * g + i, R - 1), node = rr / G, head = c * G + (rr - node * G);
             const float *qp = q + (size_t)(row0 + node) * ldq + (size_t)head * D + 4 * g4;
-            const float2 ml = *reinterpret_cast<const float2 *>(stat + 2 * ((size_t)(row0 + node) * hq_l + head));
-            floatx4 qf[KT], s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < KT; ++k) qf[k] = *reinterpret_cast<const floatx4 *>(qp + 16 * k);
+            ml = *reinterpret_cast<const float2 *>(stat + 2 * ((size_t)(row0 + node) * hq_l + head));
+        };
+        int g = x_lo * G / 16 + wave;
+        if (g <= last) load_q(g);
 #pragma unroll
-            for (int k = 0; k < KT; ++k)
+        for (int k = 0; k < KT; ++k) kf[k] = *reinterpret_cast<const floatx4 *>(kp + 16 * k);
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+        for (; g <= last; g += W) {
+            // two chains of sums: an fp32 matrix instruction waits for the one before it
+            floatx4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int x = 0; x < 4; ++x) s = mfma_f32(kf[k][x], qf[k][x], s);
+            for (int k = 0; k < KT; ++k) {
+#pragma unroll
+                for (int x = 0; x < 4; x += 2) {
+                    s0 = mfma_f32(kf[k][x], qf[k][x], s0);
+                    s1 = mfma_f32(kf[k][x + 1], qf[k][x + 1], s1);
+                }
+            }
+            const float2 now = ml;
+            const int r = 16 * g + i, node = min(r, R - 1) / G;
+            if (g + W <= last) load_q(g + W);
             const uint32_t sees = r < R ? win_sees(p0, len + node, wc.window, wc.sinks) : 0u;
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const float w = expf(s[x] * scale - ml.x) * ml.y;
+                const float w = expf((s0[x] + s1[x]) * scale - now.x) * now.y;
                 acc[x] += (sees >> (4 * g4 + x)) & 1u ? w : 0.f;
             }
         }
@@ -303,10 +318,14 @@ __global__ __launch_bounds__(256) void f32_win_weights_kernel(const float *__res
             for (int o = 8; o > 0; o >>= 1) a += __shfl_xor(a, o, 64);
             mine = i == x ? a : mine;
         }
-        const int pos = p0 + 4 * g4 + i;
-        if (i < 4 && pos <= seen) {
-            float *dst = weights + ((size_t)seq * kg.hkv_l + c) * wc.max_seq + pos;
-            *dst += mine;
+        __syncthreads();                                      // the sums of the positions before have been read
+        if (i < 4) s_sum[wave][4 * g4 + i] = mine;
+        __syncthreads();
+        if (threadIdx.x < 16 && p0 + (int)threadIdx.x <= seen) {
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) sum += s_sum[w][threadIdx.x];
+            weights[((size_t)seq * kg.hkv_l + c) * wc.max_seq + p0 + threadIdx.x] += sum;
         }
     }
 }
@@ -326,8 +345,10 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 // A block per (layer, sequence, kv head) finds the smallest weight that stays by its digits, eight bits at a time from the top -- how many of the weights with the digits
 // found so far have each value of the next one --, then goes through the slots once in order: what is first, recent, heavier than that one, or equal to it
 // and among the first such as are still wanted.  The counts are integers: the result does not depend on the order of the LDS atomics.
-__global__ __launch_bounds__(512) void evict_select_kernel(EvictCall ec, const int32_t *__restrict__ lens) {
-    constexpr int T = 512, WAVES = T / 64, PER = 4;
+// A thread has up to PER slots next to each other, so many that all threads have some; contexts of up to T PER slots are read once and stay in registers.
+template <int T>
+__global__ __launch_bounds__(T) void evict_select_kernel(EvictCall ec, const int32_t *__restrict__ lens) {
+    constexpr int WAVES = T / 64, PER = 8;
     __shared__ unsigned s_hist[256];
     __shared__ unsigned s_prefix, s_want;
     __shared__ int s_eq[WAVES], s_take[WAVES];
@@ -345,6 +366,14 @@ __global__ __launch_bounds__(512) void evict_select_kernel(EvictCall ec, const i
         return;
     }
     const int c0 = ec.sinks, c1 = n - ec.recent, want = ec.keep - ec.sinks - ec.recent;       // the slots that are chosen from, and how many
+    const int per = min((n + T - 1) / T, PER), pass = T * per;
+    const bool once = n <= pass;
+    float x[PER];
+    auto load = [&](int i0) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) x[j] = w[min(i0 + per * thread + j, n - 1)];
+    };
+    if (once) load(0);
     uint32_t prefix = 0u;
     unsigned left = want;                                     // of those with the digits found so far: wanted
     if (want > 0) {
@@ -352,26 +381,31 @@ __global__ __launch_bounds__(512) void evict_select_kernel(EvictCall ec, const i
             for (int i = thread; i < 256; i += T) s_hist[i] = 0u;
             __syncthreads();
             const uint32_t mask = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-            for (int i0 = c0; i0 < c1; i0 += T) {
-                const int i = i0 + thread;
-                const uint32_t key = i < c1 ? weight_key(w[i]) : 0u;
-                bool mine = i < c1 && (key & mask) == prefix;
-                const unsigned digit = (key >> shift) & 255u;
-                // weights of one scale share their first digits: what has the same as the first of the wave is counted at once
-                const unsigned long long some = __builtin_amdgcn_ballot_w64(mine);
-                if (some == 0) continue;
-                const int leader = __builtin_ctzll(some);
-                const unsigned common = __shfl(digit, leader, 64);
-                const unsigned long long same = __builtin_amdgcn_ballot_w64(mine && digit == common);
-                if (lane == leader) atomicAdd(&s_hist[common], (unsigned)__builtin_popcountll(same));
-                if (mine && digit != common) atomicAdd(&s_hist[digit], 1u);
+            for (int i0 = 0; i0 < n; i0 += pass) {
+                if (!once) load(i0);
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    if (j >= per) break;
+                    const int i = i0 + per * thread + j;
+                    const uint32_t key = weight_key(x[j]);
+                    const bool mine = i >= c0 && i < c1 && (key & mask) == prefix;
+                    const unsigned digit = (key >> shift) & 255u;
+                    // weights of one scale share their first digits: what has the same as the first of the wave is counted at once
+                    const unsigned long long some = __builtin_amdgcn_ballot_w64(mine);
+                    if (some == 0) continue;
+                    const int leader = __builtin_ctzll(some);
+                    const unsigned common = __builtin_amdgcn_readlane(digit, leader);
+                    const unsigned long long same = __builtin_amdgcn_ballot_w64(mine && digit == common);
+                    if (lane == leader) atomicAdd(&s_hist[common], (unsigned)__builtin_popcountll(same));
+                    if (mine && digit != common) atomicAdd(&s_hist[digit], 1u);
+                }
             }
             __syncthreads();
             if (wave == 0) {
                 // lane l: digits 255 - 4 l down to 252 - 4 l; before: how many have larger digits
                 unsigned h[4], sum = 0u;
 #pragma unroll
-                for (int x = 0; x < 4; ++x) { h[x] = s_hist[255 - 4 * lane - x]; sum += h[x]; }
+                for (int d = 0; d < 4; ++d) { h[d] = s_hist[255 - 4 * lane - d]; sum += h[d]; }
                 unsigned before = sum;
 #pragma unroll
                 for (int o = 1; o < 64; o <<= 1) {
@@ -381,13 +415,13 @@ __global__ __launch_bounds__(512) void evict_select_kernel(EvictCall ec, const i
                 before -= sum;
                 if (before < left && before + sum >= left) {
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        if (before < left && before + h[x] >= left) {
-                            s_prefix = prefix | (unsigned)(255 - 4 * lane - x) << shift;
+                    for (int d = 0; d < 4; ++d) {
+                        if (before < left && before + h[d] >= left) {
+                            s_prefix = prefix | (unsigned)(255 - 4 * lane - d) << shift;
                             s_want = left - before;
                             before = left;                    // found
                         } else {
-                            before += h[x];
+                            before += h[d];
                         }
                     }
                 }
@@ -399,20 +433,18 @@ __global__ __launch_bounds__(512) void evict_select_kernel(EvictCall ec, const i
     }
     const int limit = (int)left;                              // of the weights equal to the last one that stays
     int eq_before = 0, out_before = 0;
-    for (int i0 = 0; i0 < n; i0 += T * PER) {
-        // a thread: PER slots next to each other
-        const int first = i0 + PER * thread;
-        float x[PER];
+    for (int i0 = 0; i0 < n; i0 += pass) {
+        const int first = i0 + per * thread;
+        if (!once) load(i0);
         bool eq[PER], take[PER];
         int eqs = 0;
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             const int i = first + j;
-            x[j] = i < n ? w[i] : 0.f;
-            const bool open = i >= c0 && i < c1 && want > 0;
+            const bool there = j < per && i < n, open = there && i >= c0 && i < c1 && want > 0;
             const uint32_t key = weight_key(x[j]);
             eq[j] = open && key == prefix;
-            take[j] = i < n && (i < c0 || i >= c1 || (open && key > prefix));
+            take[j] = there && (i < c0 || i >= c1 || (open && key > prefix));
             eqs += eq[j];
         }
         int eq_rank = eqs;
@@ -531,16 +563,19 @@ void f32_launch_win_attn(const float *q, int64_t ldq, const TreeIn &in, float *k
 }
 void f32_launch_win_weights(const float *q, int64_t ldq, const float *kc, KvGeom kg, int hq_l, const WinCall &wc, const int32_t *lens, const float *stat,
                             float *weights, const WinReach &reach, hipStream_t s) {
-    const int G = hq_l / kg.hkv_l, tile_blocks = (2 * reach.most + 3) / 4;
+    const int G = hq_l / kg.hkv_l, tile_blocks = 2 * reach.most;
     const dim3 grid((unsigned)tile_blocks * kg.hkv_l * wc.batch);
-    if (kg.d == 128) hipLaunchKernelGGL(f32_win_weights_kernel<128>, grid, dim3(256), 0, s, q, ldq, kc, kg, hq_l, G, tile_blocks, wc, lens, stat, weights);
-    else hipLaunchKernelGGL(f32_win_weights_kernel<64>, grid, dim3(256), 0, s, q, ldq, kc, kg, hq_l, G, tile_blocks, wc, lens, stat, weights);
+    if (kg.d == 128) hipLaunchKernelGGL((f32_win_weights_kernel<128, 4>), grid, dim3(256), 0, s, q, ldq, kc, kg, hq_l, G, tile_blocks, wc, lens, stat, weights);
+    else hipLaunchKernelGGL((f32_win_weights_kernel<64, 4>), grid, dim3(256), 0, s, q, ldq, kc, kg, hq_l, G, tile_blocks, wc, lens, stat, weights);
 }
 void launch_win_advance(int32_t *lens, const WinCall &wc, hipStream_t s) {
     hipLaunchKernelGGL(win_advance_kernel, dim3(1), dim3(kWinSeqs), 0, s, lens, wc);
 }
-void launch_evict_select(const EvictCall &ec, const int32_t *lens, hipStream_t s) {
-    hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)ec.layers * ec.batch * ec.hkv), dim3(512), 0, s, ec, lens);
+// Small contexts in four waves, whose barriers cost less than more lanes gain: 333 slots LOW_SMALL us in 256 threads, in 1024 10.6; 4000 slots HIGH us in 1024 and 15 in 512
+void launch_evict_select(const EvictCall &ec, int longest, const int32_t *lens, hipStream_t s) {
+    const dim3 grid((unsigned)ec.layers * ec.batch * ec.hkv);
+    if (longest <= 1024) hipLaunchKernelGGL(evict_select_kernel<256>, grid, dim3(256), 0, s, ec, lens);
+    else hipLaunchKernelGGL(evict_select_kernel<1024>, grid, dim3(1024), 0, s, ec, lens);
 }
 void f32_launch_evict_move(const EvictCall &ec, const EvictMove &mv, hipStream_t s) {
     const int blocks = evict_blocks(ec, mv);

@@ -1010,7 +1010,7 @@ hexgen_status_t check_tree(const hexgen_kv_cache *kv, const hexgen_tree *tr) {
 
 // ---- windowed rows: storage and checks ----------------------------------------------------------------------------
 // What counts, window and sinks say, against the cache.  A launch has less than 2^32 threads (attention: 512 for 32 rows of one head, fp32 256 for 16; the
-// weights' sums 256 for four tiles; the rotation a thread for four rotary pairs, fp32 one).
+// weights' sums 256 for half a tile or more; the rotation a thread for four rotary pairs, fp32 one).
 hexgen_status_t check_span(const hexgen_kv_cache *kv, const int32_t *counts, int batch, int window, int sinks, float *weights, WinSpan *out) {
     if (batch <= 0 || window <= 0 || sinks < 0 || reinterpret_cast<uintptr_t>(weights) % sizeof(float)) return HEXGEN_ERR_INVALID_ARG;
     if (!kv->prefilled || batch != kv->batch) return HEXGEN_ERR_STATE;
@@ -1030,7 +1030,7 @@ hexgen_status_t check_span(const hexgen_kv_cache *kv, const int32_t *counts, int
     const uint64_t most = UINT32_MAX - 4096, seqs = std::min(batch, kWinSeqs);
     if (rows > 0x3fffffff || (long)max_n * G > 0x3fffffff) return HEXGEN_ERR_CAPACITY;
     const uint64_t blocks = (uint64_t)win_row_blocks(max_n, G, h16 ? 32 : 16) * (seqs * st->hkv_l + 7);
-    const uint64_t rotary = (uint64_t)rows * (st->hq_l + 2 * st->hkv_l) * (st->d / (h16 ? 8 : 2)), sums = (uint64_t)(kv->smax / 32 + 4) * 64 * (h16 ? 1 : 2) * st->hkv_l * seqs;
+    const uint64_t rotary = (uint64_t)rows * (st->hq_l + 2 * st->hkv_l) * (st->d / (h16 ? 8 : 2)), sums = (uint64_t)(kv->smax / 32 + 4) * 512 * st->hkv_l * seqs;
     if (blocks * (h16 ? 512 : 256) > most || rotary > most || (weights != nullptr && sums > most)) return HEXGEN_ERR_CAPACITY;
     *out = WinSpan{counts, batch, (int)rows, max_n, window, sinks, weights};
     return HEXGEN_OK;
@@ -1807,8 +1807,8 @@ hexgen_status_t hexgen_kv_cache_evict(hexgen_kv_cache_t *kv, hexgen_kv_cache_t *
     const EvictMove mv{kv->k, kv->v, dst->k, dst->v, kv->layer_stride, dst->layer_stride, geom(st, kv), geom(st, dst),
                        rotate ? kv->cos_tab : nullptr, rotate ? kv->sin_tab : nullptr, kv->d_lens, dst->d_lens, dst->max_batch};
     const uint64_t units = (uint64_t)ec.layers * ec.batch * ec.hkv;
-    if (units * 512 > UINT32_MAX || units * 256 * evict_blocks(ec, mv) > UINT32_MAX) return HEXGEN_ERR_CAPACITY;
-    launch_evict_select(ec, kv->d_lens, s);
+    if (units * 1024 > UINT32_MAX || units * 256 * evict_blocks(ec, mv) > UINT32_MAX) return HEXGEN_ERR_CAPACITY;
+    launch_evict_select(ec, *std::max_element(kv->lens.begin(), kv->lens.begin() + kv->batch), kv->d_lens, s);
     if (is_h16(st->dtype)) HX_K(st->dtype, launch_evict_move, ec, mv, s);
     else f32_launch_evict_move(ec, mv, s);
     HX_HIP(hipGetLastError());
