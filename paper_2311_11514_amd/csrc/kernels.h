@@ -237,7 +237,10 @@ struct WinPlan {
     int nsplit, chunk;
     float *part_o, *part_ml;              // as in TreePlan
     unsigned *arrived;
-    float *stat;                          // [rows][hq][2], or NULL: a row's largest score and the reciprocal of its sum, for the weights
+    float *stat;                          // [rows][hq][2], or NULL: what a row's weights are relative to and the reciprocal of their sum, for the sums of the weights
+    // [rows][hq][32 score_tiles], or NULL: the scores of every tile in the list of a sequence's rows, which are one block's (16 bits)
+    float *scores;
+    int score_tiles;
 };
 // Tiles of 32 positions that a call's rows reach, as the host's lengths have it: of one sequence at most, and groups of eight of all sequences.  They say how many
 // blocks are worth launching, no more: the lengths on the device may be others.

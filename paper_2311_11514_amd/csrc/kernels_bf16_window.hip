@@ -273,6 +273,11 @@ __global__ __launch_bounds__(512, 2) void win_few_kernel(const h16_t *__restrict
             for (int x = 0; x < 16; ++x) sc[x] = (sees >> (8 * (x >> 2) + 4 * hl + (x & 3))) & 1u ? sc[x] : NEG_INF;
         }
         if (!TAIL && v + W < clean) load_k(wk.tiles.at(v + W), std::false_type{});
+        if (wp.scores != nullptr && wk.rb * 32 + i32 < R) {   // for the weights' sums: four positions of the lane's row a store
+            float *dst = wp.scores + ((size_t)(row0 + node) * hq_l + head) * 32 * wp.score_tiles + 32 * v + 4 * hl;
+#pragma unroll
+            for (int qd = 0; qd < 4; ++qd) *reinterpret_cast<floatx4 *>(dst + 8 * qd) = floatx4{sc[4 * qd], sc[4 * qd + 1], sc[4 * qd + 2], sc[4 * qd + 3]};
+        }
         const float alpha = tree_softmax(sc, m, lsum, scale_log2e);
 #pragma unroll
         for (int db = 0; db < DB; ++db)
@@ -634,6 +639,33 @@ __global__ __launch_bounds__(256, 4) void win_weights_kernel(const h16_t *__rest
         }
     }
 }
+// The same for few rows from the scores that the attention has left: a thread per position
+__global__ __launch_bounds__(256) void win_gather_kernel(KvGeom kg, int hq_l, int G, int tile_blocks, bool fresh, WinCall wc, const int32_t *__restrict__ lens, WinPlan wp,
+                                                         float *__restrict__ weights, float scale_log2e) {
+    const int tb = blockIdx.x % tile_blocks, c = (blockIdx.x / tile_blocks) % kg.hkv_l, nth = blockIdx.x / tile_blocks / kg.hkv_l;
+    const int seq = wc.seq0 + nth, row0 = wc.cu[nth], len = lens[seq], n = min(wc.cu[nth + 1] - row0, wc.max_seq - len);
+    if (n <= 0) return;
+    WinTiles tiles;                                           // as the attention had them: one block of rows
+    tiles.set(len, len + n - 1, wc.window, wc.sinks, fresh ? len : len + 1);
+    const size_t row_floats = (size_t)32 * wp.score_tiles;
+    for (int v = 8 * tb + threadIdx.x / 32; v < tiles.nt; v += 8 * tile_blocks) {
+        const int pos = 32 * tiles.at(v) + threadIdx.x % 32;
+        if (pos >= len + n) continue;
+        float sum = 0.f;
+        for (int x = 0; x < n; ++x) {
+            const size_t e = (size_t)(row0 + x) * hq_l + c * G;
+            const float *scores = wp.scores + e * row_floats + 32 * v + threadIdx.x % 32, *stat = wp.stat + 2 * e;
+#pragma unroll 8
+            for (int h = 0; h < G; ++h) {
+                const float base = stat[2 * h], given = stat[2 * h + 1], s = scores[h * row_floats];
+                const float a = given < 0.f ? base : 0.f, b = given < 0.f ? 0.f : base;      // (win_stat)
+                sum = fmaf(__builtin_amdgcn_exp2f(fmaf(s - a, scale_log2e, -b)), fabsf(given), sum);
+            }
+        }
+        weights[((size_t)seq * kg.hkv_l + c) * wc.max_seq + pos] += sum;
+    }
+}
+
 // groups of eight tiles in a cache's positions, each with a counter and a place for its sums
 __host__ __device__ inline int win_units(int smax) { return (smax / 32 + 7) / 8; }
 // The same for calls of many rows: a wave keeps the keys of two tiles, and the block's four waves share the rows, which go from memory to LDS directly, two
@@ -780,9 +812,14 @@ __global__ __launch_bounds__(256, 2) void win_weights_shared_kernel(const h16_t 
 }
 
 void launch_win_weights(const h16_t *q, const h16_t *q_lo, int64_t ldq, const h16_t *kc, KvGeom kg, int hq_l, const WinCall &wc, const int32_t *lens,
-                        const WinPlan &wp, float *weights, const WinReach &reach, hipStream_t s) {
+                        const WinPlan &wp, bool fresh, float *weights, const WinReach &reach, hipStream_t s) {
     const int G = hq_l / kg.hkv_l;
     const float scale_log2e = 1.4426950408889634f / sqrtf((float)kg.d);
+    if (wp.scores != nullptr) {
+        const int tile_blocks = (reach.most + 7) / 8;
+        hipLaunchKernelGGL(win_gather_kernel, dim3((unsigned)tile_blocks * kg.hkv_l * wc.batch), dim3(256), 0, s, kg, hq_l, G, tile_blocks, fresh, wc, lens, wp, weights, scale_log2e);
+        return;
+    }
     const bool shared = (int64_t)wc.max_n * G > 64;
     const int tile_blocks = (reach.most + (shared ? 7 : 3)) / (shared ? 8 : 4);
     const int64_t blocks = (int64_t)tile_blocks * kg.hkv_l * wc.batch, groups = ((int64_t)wc.max_n * G + 31) / 32;

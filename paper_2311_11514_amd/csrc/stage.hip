@@ -103,7 +103,8 @@ struct hexgen_stage {
     int last_decode_rows = 0;        // rows of the last decode call that ran on the weight-streaming kernels
     int ws_batch_cap = 0;
     float *tree_part = nullptr;      // from the first call on trees or windowed rows on: partial results of contexts cut into runs (kTreePartFloats), kTreeUnits counters
-    float *win_stat = nullptr;       // from the first call on that gathers attention weights: a row's and head's largest score and 1 / sum
+    // from the first call on that gathers attention weights: a row's and head's statistics (WinPlan), and behind them the scores of few rows
+    float *win_stat = nullptr;
     size_t win_stat_floats = 0;
     int64_t weight_bytes = 0;
     Profiler prof;
@@ -457,7 +458,8 @@ struct WinSpan {
 };
 constexpr int64_t kWinRowStride = 1 << 24;                   // elements between query rows: offsets among 32 of them have 32 bits
 static_assert(kWinPartFloats == kTreePartFloats && kWinUnits == kTreeUnits, "one scratch for both");
-constexpr size_t kWinWeights = 2;                            // floats of win_stat per row and head
+constexpr size_t kWinStatFloats = 2;                         // statistics of a row and head
+constexpr size_t kWinScoreFloats = (size_t)16 << 20;         // 64 MB of scores at most
 
 // the span in launches of kWinSeqs sequences; those without a row at either end of one are left out of it
 template <typename F>
@@ -482,8 +484,18 @@ void for_each_call(const hexgen_kv_cache *kv, const WinSpan &sp, F &&fn) {
     }
 }
 
-// Rows per block, and the runs that a row's tiles are cut into.
-WinPlan pick_win_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, WinCall &wc, bool stats) {
+// Tiles that a sequence's rows reach, whatever its length: what the scores of few rows have room for.  0 where they are not kept (32-bit stages, rows of several
+// blocks, more than kWinScoreFloats): the weights' sums then multiply the keys once more.
+int win_score_tiles(const hexgen_stage *st, const hexgen_kv_cache *kv, const WinSpan &sp) {
+    if (!is_h16(st->dtype) || (long)sp.max_n * (st->hq_l / st->hkv_l) > 32) return 0;
+    const long reach = ((long)sp.window + sp.max_n + 61) / 32 + 1 + ((long)sp.sinks + 31) / 32;
+    const long tiles = std::min<long>(reach, kv->smax / 32);
+    return (size_t)sp.rows * st->hq_l * 32 * tiles <= kWinScoreFloats ? (int)tiles : 0;
+}
+
+// Rows per block, and the runs that a row's tiles are cut into.  One kv head, one row each, 8 heads, d 128: runs of 16 tiles where there are more than 24 (a
+// window of 1024: one sequence 13.4 us whole, 10.7 in three runs, 10.4 in five), whole rounds of the eight waves; otherwise as for trees (pick_tree_plan).
+WinPlan pick_win_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, WinCall &wc, bool stats, int score_tiles) {
     const int G = st->hq_l / st->hkv_l;
     const bool h16 = is_h16(st->dtype);
     long blocks = 0, tiles = 0, shared_blocks = 0;
@@ -510,7 +522,7 @@ WinPlan pick_win_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, WinCall
     if (!wp.shared && blocks < 128 && few_units) {
         const long fit = (tiles + kTreeBlocks - 1) / kTreeBlocks;
         if (!h16) wp.chunk = (int)std::max(4L, fit);
-        else if (longest > 48) wp.chunk = (int)((std::max({16L, fit, (long)(2 * std::sqrt((double)longest))}) + 7) / 8 * 8);
+        else if (longest > 24) wp.chunk = (int)((std::max({16L, fit, (long)(2 * std::sqrt((double)longest))}) + 7) / 8 * 8);
         wp.nsplit = std::min((longest + wp.chunk - 1) / wp.chunk, kWinMaxSplit);
         wp.nsplit = (int)std::max((size_t)1, std::min((size_t)wp.nsplit, kTreePartFloats / ((size_t)wc.rows * st->hq_l * (st->d + 2))));
     }
@@ -518,6 +530,8 @@ WinPlan pick_win_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, WinCall
     wp.part_ml = st->tree_part + (size_t)wp.nsplit * wc.rows * st->hq_l * st->d;
     wp.arrived = reinterpret_cast<unsigned *>(st->tree_part + kTreePartFloats);
     wp.stat = stats ? st->win_stat : nullptr;
+    wp.scores = stats && score_tiles > 0 ? st->win_stat + kWinStatFloats * wc.rows * st->hq_l : nullptr;
+    wp.score_tiles = score_tiles;
     if (wp.nsplit == 1) std::stable_sort(wc.order, wc.order + wc.batch, [&](int a, int b) { return reach[a] > reach[b]; });
     return wp;
 }
@@ -542,8 +556,9 @@ void attn_rows(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const WinSpan &
     const KvGeom kg = geom(st, kv);
     const int G = st->hq_l / st->hkv_l;
     float *weights = sp.weights != nullptr ? sp.weights + (size_t)layer * sp.batch * st->hkv_l * kv->max_seq : nullptr;
+    const int score_tiles = win_score_tiles(st, kv, sp);
     for_each_call(kv, sp, [&](WinCall &wc) {
-        const WinPlan wp = pick_win_plan(st, kv, wc, weights != nullptr);
+        const WinPlan wp = pick_win_plan(st, kv, wc, weights != nullptr, score_tiles);
         TreeIn here = in;
         const bool append = in.k != nullptr && (wp.shared || (long)wc.max_n * G > (is_h16(st->dtype) ? 32 : 16));
         if (append) here = TreeIn{nullptr, nullptr, 0, 0};
@@ -552,7 +567,7 @@ void attn_rows(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const WinSpan &
             const h16_t *q16 = static_cast<const h16_t *>(q);
             if (append) HX_K(st->dtype, launch_win_append, in, kc, vc, kg, wc, kv->d_lens, s);
             HX_K(st->dtype, launch_win_attn, q16, q_lo, ldq, here, kc, vc, kg, st->hq_l, wc, kv->d_lens, wp, out, s);
-            if (weights != nullptr) HX_K(st->dtype, launch_win_weights, q16, q_lo, ldq, kc, kg, st->hq_l, wc, kv->d_lens, wp, weights, win_reach(kv, wc), s);
+            if (weights != nullptr) HX_K(st->dtype, launch_win_weights, q16, q_lo, ldq, kc, kg, st->hq_l, wc, kv->d_lens, wp, here.k != nullptr, weights, win_reach(kv, wc), s);
         } else {
             float *kc = static_cast<float *>(kv->k) + (size_t)layer * kv->layer_stride, *vc = static_cast<float *>(kv->v) + (size_t)layer * kv->layer_stride;
             const float *q32 = static_cast<const float *>(q);
@@ -1035,8 +1050,8 @@ hexgen_status_t check_span(const hexgen_kv_cache *kv, const int32_t *counts, int
     *out = WinSpan{counts, batch, (int)rows, max_n, window, sinks, weights};
     return HEXGEN_OK;
 }
-hexgen_status_t ensure_win_stat(hexgen_stage *st, const WinSpan &sp, hipStream_t s) {
-    const size_t want = kWinWeights * sp.rows * st->hq_l;
+hexgen_status_t ensure_win_stat(hexgen_stage *st, const hexgen_kv_cache *kv, const WinSpan &sp, hipStream_t s) {
+    const size_t want = (kWinStatFloats + (size_t)32 * win_score_tiles(st, kv, sp)) * sp.rows * st->hq_l;
     if (sp.weights == nullptr || want <= st->win_stat_floats) return HEXGEN_OK;
     HX_TRY(refuse_capture(s));
     float *p = nullptr;
@@ -1749,7 +1764,7 @@ hexgen_status_t hexgen_kv_window_attention(hexgen_kv_cache_t *kv, int layer, con
     HX_TRY(check_span(kv, counts, batch, window, sinks, weights, &sp));
     hipStream_t s = static_cast<hipStream_t>(stream);
     HX_TRY(ensure_tree_part(st, s));
-    HX_TRY(ensure_win_stat(st, sp, s));
+    HX_TRY(ensure_win_stat(st, kv, sp, s));
     if (sp.weights != nullptr) sp.weights -= (size_t)layer * batch * st->hkv_l * kv->max_seq;      // this layer's own are given
     attn_rows(st, kv, layer, sp, q, nullptr, ldq, TreeIn{k, v, ldk, ldv}, TreeOut{TREE_OUT_ROWS, sp.rows, st->qw, out}, s);
     HX_HIP(hipGetLastError());
@@ -1773,7 +1788,7 @@ hexgen_status_t hexgen_stage_extend(hexgen_stage_t *st, hexgen_kv_cache_t *kv, c
     if (r.T > st->ws.cap_rows || r.batch > st->ws_batch_cap) HX_TRY(refuse_capture(s));
     HX_TRY(ensure_workspace(st, r.T, r.batch));
     HX_TRY(ensure_tree_part(st, s));
-    HX_TRY(ensure_win_stat(st, sp, s));
+    HX_TRY(ensure_win_stat(st, kv, sp, s));
     if (is_h16(st->dtype) && st->ws.tree_qkv == nullptr) {
         HX_TRY(refuse_capture(s));
         HX_TRY(dmalloc(&st->ws.tree_qkv, (size_t)st->ws.cap_rows * st->nqkv));
