@@ -58,7 +58,7 @@ __global__ __launch_bounds__(256) void f32_win_append_kernel(TreeIn in, float *_
 // and positions 4 (l / 16) + r, P stays in registers).  Rows that are not in the cache yet (in.k != NULL: a sequence's rows are one block's columns then) are
 // read from the caller's and appended by the run that holds their tile.
 template <int D, int W>
-__global__ __launch_bounds__(64 * W) void f32_win_attn_kernel(const float *__restrict__ q, int64_t ldq, TreeIn in, float *kc, float *vc, KvGeom kg, int hq_l, int G, int nrb,
+__global__ __launch_bounds__(64 * W, 3) void f32_win_attn_kernel(const float *__restrict__ q, int64_t ldq, TreeIn in, float *kc, float *vc, KvGeom kg, int hq_l, int G, int nrb,
                                                               WinCall wc, const int32_t *__restrict__ lens, WinPlan wp, float *__restrict__ o) {
     constexpr int KT = D / 16, VH = D / 64;
     __shared__ float s_m[W][16], s_l[W][16];
