@@ -124,23 +124,25 @@ void launch_win_append(const TreeIn &in, h16_t *kc, h16_t *vc, KvGeom kg, const 
     else hipLaunchKernelGGL(win_append_kernel<64>, grid, dim3(256), 0, s, in, kc, vc, kg, wc, lens);
 }
 
-// ---- statistics and weights ---------------------------------------------------------------------------------------------
-// What a row's softmax is relative to.  Its weights are exp2(s c - base), c = log2(e) / sqrt(d), one multiply-add a score, with base = the rounded product of c and a score
-// near the largest: the same number in the sum, in what is rescaled and in the weights' sums later, so that its rounding cancels.  From 2^20 on, where it would
-// not (a product's last bit is 1/8 there, and at 2^31 an exponent could overflow), the difference of the scores is taken first.  Statistics say which: 1 / sum
-// with its sign changed stands beside a base that is a score.
+// ---- statistics -------------------------------------------------------------------------------------------------------
+// What a row's softmax is relative to.  In blocks that share tiles its weights are exp2(s c - base), c = log2(e) / sqrt(d), one multiply-add a score, with base = the
+// rounded product of c and a score near the largest: the same number in the sum, in what is rescaled and in the weights' sums later, so that its rounding
+// cancels.  From 2^20 on, where it would not (a product's last bit is 1/8 there, and from 2^31 on an exponent could overflow), and in blocks of few rows the
+// difference of the scores is taken first.  Statistics say which: 1 / sum with its sign changed stands beside a base that is a score.
 constexpr float kWinFarBase = 1048576.0f;
 __device__ __forceinline__ float2 win_stat(float base, float inv, bool score) { return float2{base, score ? -inv : inv}; }
-// sc -> exp2 of its distance from what the lane's statistics (stat, inv) say; far: some row of the wave has a score as its base
-__device__ __forceinline__ void win_exp(floatx16 &sc, float base, float inv, bool far, float scale_log2e) {
-    if (!far) {
-#pragma unroll
-        for (int x = 0; x < 16; ++x) sc[x] = __builtin_amdgcn_exp2f(fmaf(sc[x], scale_log2e, -base));
-    } else {
-#pragma unroll
-        for (int x = 0; x < 16; ++x) sc[x] = __builtin_amdgcn_exp2f(inv < 0.f ? (sc[x] - base) * scale_log2e : fmaf(sc[x], scale_log2e, -base));
+// a weight from a score: exp2((s - a) c - b) / sum
+struct WinBase {
+    float a, b, inv;
+    __device__ __forceinline__ WinBase(float base, float given) : a(given < 0.f ? base : 0.f), b(given < 0.f ? 0.f : base), inv(fabsf(given)) {}
+    __device__ __forceinline__ float exp(float s, float scale_log2e) const { return __builtin_amdgcn_exp2f(fmaf(s - a, scale_log2e, -b)); }
+    // its sum is an infinity or a NaN: what the row does not attend (a score of -infinity) must not take part, not even as zero times that
+    __device__ __forceinline__ bool odd() const { return !(inv < INFINITY); }
+    __device__ __forceinline__ float add(float sum, float s, float scale_log2e, bool careful) const {
+        const float e = exp(s, scale_log2e);
+        return !careful ? fmaf(e, inv, sum) : s == NEG_INF ? sum : sum + e * inv;
     }
-}
+};
 
 // ---- attention, few rows ----------------------------------------------------------------------------------------------
 // A block of eight waves takes 32 query rows and a run of their tiles, which the waves take in turn, K and V straight to registers in the operands'
@@ -396,13 +398,6 @@ __global__ __launch_bounds__(512, 2) void win_few_kernel(const h16_t *__restrict
     }
 }
 
-#define WIN_SCHED                                                                              \
-    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);                                         \
-    _Pragma("unroll") for (int i_ = 0; i_ < 2 * KT; ++i_) {                                    \
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                                     \
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);                                     \
-        __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);                                     \
-    }
 // ---- attention, many rows ---------------------------------------------------------------------------------------------
 // A block of four waves takes 128 query rows, 32 a wave; their tiles go from HBM to LDS directly, three in flight, and are shared.  Products and softmax as
 // above.  The rows are in the cache already.
@@ -507,15 +502,19 @@ __global__ __launch_bounds__(256, 2) void win_attn_kernel(const h16_t *__restric
         float ps = 0.f;
         if (far) {
             scores(min(step + 1, steps - 1), ahead);
-            win_exp(sc, base, -1.f, true, scale_log2e);
 #pragma unroll
-            for (int x = 0; x < 16; ++x) ps += sc[x];
+            for (int x = 0; x < 16; ++x) { sc[x] = __builtin_amdgcn_exp2f((sc[x] - base) * scale_log2e); ps += sc[x]; }
         } else {
             scores(min(step + 1, steps - 1), ahead);
-            win_exp(sc, base, 1.f, false, scale_log2e);
 #pragma unroll
-            for (int x = 0; x < 16; ++x) ps += sc[x];
-            WIN_SCHED
+            for (int x = 0; x < 16; ++x) { sc[x] = __builtin_amdgcn_exp2f(fmaf(sc[x], scale_log2e, -base)); ps += sc[x]; }
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);          // reads of LDS; then a matrix instruction, a read, and what the vector unit does meanwhile
+#pragma unroll
+            for (int x = 0; x < 2 * KT; ++x) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
+            }
         }
         lsum += ps;
         if constexpr (TAIL) {
@@ -614,7 +613,8 @@ __global__ __launch_bounds__(256, 4) void win_weights_kernel(const h16_t *__rest
             }
 #pragma unroll
             for (int kk = 0; kk < 2 * KT; ++kk) sc = hx_mfma32(kf[kk], *reinterpret_cast<const h16x8 *>(q + at + 16 * kk), sc);
-            const float a = ml.y < 0.f ? ml.x : 0.f, b = ml.y < 0.f ? 0.f : ml.x, inv = fabsf(ml.y);         // (win_stat)
+            const WinBase base(ml.x, ml.y);
+            const bool careful = __builtin_amdgcn_ballot_w64(base.odd()) != 0;
             const int first = len + 32 * g / G, last = len + min(32 * g + 31, R - 1) / G;
             if (32 * g + 31 >= R || !win_all(p0, 32, first, last, wc.window, wc.sinks)) {
                 const uint32_t sees = r < R ? win_sees(p0, len + node, wc.window, wc.sinks) : 0u;
@@ -622,7 +622,7 @@ __global__ __launch_bounds__(256, 4) void win_weights_kernel(const h16_t *__rest
                 for (int x = 0; x < 16; ++x) sc[x] = (sees >> (8 * (x >> 2) + 4 * hl + (x & 3))) & 1u ? sc[x] : NEG_INF;
             }
 #pragma unroll
-            for (int x = 0; x < 16; ++x) acc[x] = fmaf(__builtin_amdgcn_exp2f(fmaf(sc[x] - a, scale_log2e, -b)), inv, acc[x]);
+            for (int x = 0; x < 16; ++x) acc[x] = base.add(acc[x], sc[x], scale_log2e, careful);
         }
         float mine = 0.f;
 #pragma unroll
@@ -657,9 +657,8 @@ __global__ __launch_bounds__(256) void win_gather_kernel(KvGeom kg, int hq_l, in
             const float *scores = wp.scores + e * row_floats + 32 * v + threadIdx.x % 32, *stat = wp.stat + 2 * e;
 #pragma unroll 8
             for (int h = 0; h < G; ++h) {
-                const float base = stat[2 * h], given = stat[2 * h + 1], s = scores[h * row_floats];
-                const float a = given < 0.f ? base : 0.f, b = given < 0.f ? 0.f : base;      // (win_stat)
-                sum = fmaf(__builtin_amdgcn_exp2f(fmaf(s - a, scale_log2e, -b)), fabsf(given), sum);
+                const WinBase base(stat[2 * h], stat[2 * h + 1]);
+                sum = base.add(sum, scores[h * row_floats], scale_log2e, true);
             }
         }
         weights[((size_t)seq * kg.hkv_l + c) * wc.max_seq + pos] += sum;
@@ -745,8 +744,8 @@ __global__ __launch_bounds__(256, 2) void win_weights_shared_kernel(const h16_t 
             else HX_WAIT_VM(0);
             HX_LDS_BARRIER();
             if (g + 2 < g1) issue(g + 2);                     // into the buffer that every wave has left
-            const float base = s_stat[g % S][wave][2 * i32], given = s_stat[g % S][wave][2 * i32 + 1];
-            const float a = given < 0.f ? base : 0.f, b = given < 0.f ? 0.f : base, inv = fabsf(given);      // (win_stat)
+            const WinBase base(s_stat[g % S][wave][2 * i32], s_stat[g % S][wave][2 * i32 + 1]);
+            const bool careful = __builtin_amdgcn_ballot_w64(base.odd()) != 0;
             const int first = len + __builtin_amdgcn_readfirstlane(node), last = len + __builtin_amdgcn_readlane(node, 31);
             h16x8 rows[PIECES];
 #pragma unroll
@@ -765,8 +764,13 @@ __global__ __launch_bounds__(256, 2) void win_weights_shared_kernel(const h16_t 
                 for (int x = 0; x < 16; ++x) sc[w][x] = (sees >> (8 * (x >> 2) + 4 * hl + (x & 3))) & 1u ? sc[w][x] : NEG_INF;
             };
             auto add = [&](int w) {
+                if (careful) {
 #pragma unroll
-                for (int x = 0; x < 16; ++x) acc[w][x] = fmaf(__builtin_amdgcn_exp2f(fmaf(sc[w][x] - a, scale_log2e, -b)), inv, acc[w][x]);
+                    for (int x = 0; x < 16; ++x) acc[w][x] = base.add(acc[w][x], sc[w][x], scale_log2e, true);
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) acc[w][x] = base.add(acc[w][x], sc[w][x], scale_log2e, false);
+                }
             };
             static_assert(TW == 2, "the second tile's scores on the matrix cores while the first one's weights are on the vector unit");
             scores(0);

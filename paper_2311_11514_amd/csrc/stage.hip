@@ -459,6 +459,7 @@ struct WinSpan {
 constexpr int64_t kWinRowStride = 1 << 24;                   // elements between query rows: offsets among 32 of them have 32 bits
 static_assert(kWinPartFloats == kTreePartFloats && kWinUnits == kTreeUnits, "one scratch for both");
 constexpr size_t kWinStatFloats = 2;                         // statistics of a row and head
+size_t win_stat_floats(const hexgen_stage *st, int rows) { return (kWinStatFloats * rows * st->hq_l + 3) / 4 * 4; }       // the scores behind them are written 16 bytes at a time
 constexpr size_t kWinScoreFloats = (size_t)16 << 20;         // 64 MB of scores at most
 
 // the span in launches of kWinSeqs sequences; those without a row at either end of one are left out of it
@@ -530,7 +531,7 @@ WinPlan pick_win_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, WinCall
     wp.part_ml = st->tree_part + (size_t)wp.nsplit * wc.rows * st->hq_l * st->d;
     wp.arrived = reinterpret_cast<unsigned *>(st->tree_part + kTreePartFloats);
     wp.stat = stats ? st->win_stat : nullptr;
-    wp.scores = stats && score_tiles > 0 ? st->win_stat + kWinStatFloats * wc.rows * st->hq_l : nullptr;
+    wp.scores = stats && score_tiles > 0 ? st->win_stat + win_stat_floats(st, wc.rows) : nullptr;
     wp.score_tiles = score_tiles;
     if (wp.nsplit == 1) std::stable_sort(wc.order, wc.order + wc.batch, [&](int a, int b) { return reach[a] > reach[b]; });
     return wp;
@@ -1051,7 +1052,7 @@ hexgen_status_t check_span(const hexgen_kv_cache *kv, const int32_t *counts, int
     return HEXGEN_OK;
 }
 hexgen_status_t ensure_win_stat(hexgen_stage *st, const hexgen_kv_cache *kv, const WinSpan &sp, hipStream_t s) {
-    const size_t want = (kWinStatFloats + (size_t)32 * win_score_tiles(st, kv, sp)) * sp.rows * st->hq_l;
+    const size_t want = win_stat_floats(st, sp.rows) + (size_t)32 * win_score_tiles(st, kv, sp) * sp.rows * st->hq_l;
     if (sp.weights == nullptr || want <= st->win_stat_floats) return HEXGEN_OK;
     HX_TRY(refuse_capture(s));
     float *p = nullptr;

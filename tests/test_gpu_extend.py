@@ -54,6 +54,30 @@ def test_extend_matches_the_stage_in_64_bits(dtype, chunks, tp, window, sinks):
             assert abs(got.sum() - done[b] * cfg.n_heads // tp) < 1e-3 * done[b] * cfg.n_heads        # every row's weights are one in all
 
 
+def test_more_sequences_than_a_launch_takes():
+    """Some of them without a row, some beyond the first launch: against the same sequences in a call of their own."""
+    cfg, st, _ = _stage("bf16", 12, 1, heads=4, kv=2, hidden=256, ffn=512, batch=300)
+    counts = [(i * 7) % 4 for i in range(300)]
+    x = generate.hidden_rows(cfg, sum(counts))
+    kv = st.kv_cache_create(300, 16)
+    kv.set_lengths([i % 5 for i in range(300)])              # contexts of zeros
+    p, r = _extend(st, kv, cfg, x, counts, window=12, sinks=1)
+    assert kv.get_lengths(300) == [i % 5 + n for i, n in enumerate(counts)]
+    few = [2, 130, 255, 256, 257, 298]
+    at = np.concatenate([[0], np.cumsum(counts)])
+    rows = np.concatenate([np.arange(at[i], at[i + 1]) for i in few])
+    other = st.kv_cache_create(6, 16)
+    other.set_lengths([i % 5 for i in few])
+    q, s = _extend(st, other, cfg, x[torch.tensor(rows)], [counts[i] for i in few], window=12, sinks=1)
+    check("partial", p[rows], q, TOL["bf16"])
+    check("residual", r[rows], s, TOL["bf16"])
+    for j, i in enumerate(few):
+        n = i % 5 + counts[i]
+        if n:
+            for a, b in zip(kv.read(0, i, 0, n), other.read(0, j, 0, n)):
+                assert torch.allclose(a, b, rtol=0, atol=0.05 * float(b.abs().max()))
+
+
 @pytest.mark.parametrize("dtype,lens", [("bf16", [50, 33]), ("f16", [9, 14]), ("f32", [40, 21])])
 def test_without_a_window_it_is_prefill_and_decode(dtype, lens):
     cfg, st, _ = _stage(dtype, None, 0)

@@ -80,6 +80,7 @@ FEW = [
     (4, 1, 64, [20, 3], [100, 256], 50, 70),
     (2, 1, 64, [700, 650], [1, 1], 1, 1),                  # the first and itself
     (1, 1, 128, [64, 95, 96], [1, 31, 33], 64, 64),
+    (1, 1, 128, [64, 95, 100], [1, 1, 1], 40, 2),          # an odd number of rows and heads
     (10, 5, 64, [200, 10], [2, 3], (1 << 31) - 1, (1 << 31) - 1),      # a window and sinks beyond everything
 ]
 
@@ -87,8 +88,6 @@ FEW = [
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("hq,hkv,d,lens,counts,window,sinks", FEW)
 def test_attention_and_weights_match_64_bits(dtype, hq, hkv, d, lens, counts, window, sinks):
-    if hq * d % 128:
-        pytest.skip("no such stage")
     c = Case(dtype, hq, hkv, d, lens, counts, window, sinks)
     alone = c.attend()
     out, weights = c.attend_both()
@@ -167,6 +166,47 @@ def test_what_a_row_does_not_attend_has_no_influence(dtype, hq, hkv, d, lens, co
     assert np.all((np.abs(got.double().cpu().numpy() - o) <= bound)[touched.numpy()])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("hq,hkv,d,lens,counts,window,sinks", [(4, 1, 64, [100], [3], 10, 2), (8, 1, 128, [70, 3], [20, 9], 33, 1), (64, 8, 64, [130, 0], [200, 70], 45, 7)])
+def test_a_row_of_nan_spoils_the_weights_of_what_it_attends_alone(dtype, hq, hkv, d, lens, counts, window, sinks):
+    c = Case(dtype, hq, hkv, d, lens, counts, window, sinks, seed=6)
+    out, weights = c.attend_both()
+    at = counts[0] - 2
+    c.q[at, 0] = float("nan")                              # the first query head of one row of the first sequence
+    got, spoiled = c.attend_both()
+    seen = wr.visible(lens[0] + at, window, sinks)
+    rest = torch.ones_like(weights, dtype=torch.bool)
+    rest[0, 0, seen] = False
+    assert torch.isnan(spoiled[0, 0, seen]).all() and torch.equal(spoiled[rest], weights[rest])
+    same = torch.ones_like(out, dtype=torch.bool)
+    same[at, 0] = False
+    assert torch.equal(got[same], out[same]) and torch.isnan(got[at, 0]).all()
+
+
+@pytest.mark.parametrize("dtype,power", [(t, p) for t, most in (("bf16", 14), ("f16", 11), ("f32", 14)) for p in (5, 10, most)])
+@pytest.mark.parametrize("hq,hkv,lens,counts", [(8, 1, [90], [2]), (64, 8, [70, 0], [200, 70])])
+def test_scores_far_from_zero(dtype, hq, hkv, lens, counts, power):
+    """Scores of 2^10 and more, the largest of a row far in front of its others: the row is that position's value.  The position's key is the row's query times 2^power in every
+    group's first head; whatever comes after it in the tiles, and the bases that the largest scores need, change nothing."""
+    c = Case(dtype, hq, hkv, 64, lens, counts, 64, 3, seed=12)
+    group = hq // hkv
+    unit = torch.sign(c.q[:, ::group].float())
+    c.q[:, :] = (unit * 2.0 ** power).repeat_interleave(group, 1).to(c.q.dtype)
+    c.k[:, :] = (unit * 2.0 ** 4).to(c.k.dtype)              # a row's own key is the one that fits: score 2^(power + 4) 64 / 8; any other's is smaller by 2^(power + 5) / 8 a sign
+    for b in range(len(lens)):
+        c.ctx[0][b][0] = torch.zeros_like(c.ctx[0][b][0])
+        if lens[b]:
+            c.kv.fill(0, b, *c.ctx[0][b])
+    c.kv.set_lengths(lens)
+    out, weights = c.attend_both()
+    assert torch.equal(out.cpu(), c.v.repeat_interleave(group, 1))
+    row = 0
+    for b, (n, m) in enumerate(zip(lens, counts)):
+        gathered = (weights[b].cpu() - c.before[b])[:, :n + m]
+        assert torch.allclose(gathered[:, n:], torch.full((hkv, m), float(group)), rtol=0, atol=1e-4) and torch.allclose(gathered[:, :n], torch.zeros(hkv, n), rtol=0, atol=1e-6)
+        row += m
+
+
 def test_infinite_values_that_are_attended_stay():
     c = Case("f32", 4, 2, 64, [40], [3], 16, 0)
     c.v[1, 0, 5] = float("inf")
@@ -223,6 +263,14 @@ def test_more_sequences_than_a_launch_takes(dtype):
     c = Case(dtype, 2, 1, 64, lens, counts, 24, 2, seed=11)
     out, weights = c.attend_both()
     c.check(out, weights)
+
+
+def test_a_launch_of_sequences_without_rows():
+    counts = [0] * 256 + [2, 0, 1]
+    c = Case("bf16", 2, 1, 64, [30] * 259, counts, 8, 1, seed=13)
+    out, weights = c.attend_both()
+    c.check(out, weights)
+    assert torch.equal(weights[:256].cpu(), c.before[:256])
 
 
 def test_another_stream_and_the_order_that_the_caller_makes():
