@@ -494,29 +494,40 @@ int win_score_tiles(const hexgen_stage *st, const hexgen_kv_cache *kv, const Win
     return (size_t)sp.rows * st->hq_l * 32 * tiles <= kWinScoreFloats ? (int)tiles : 0;
 }
 
-// Rows per block, and the runs that a row's tiles are cut into.  One kv head, one row each, 8 heads, d 128: runs of 16 tiles where there are more than 24 (a
-// window of 1024: one sequence 13.4 us whole, 10.7 in three runs, 10.4 in five), whole rounds of the eight waves; otherwise as for trees (pick_tree_plan).
+// Rows per block, and the runs that a row's tiles are cut into.
+// Blocks of 32 rows ("few") or, where that is expected to be faster, of 128 that share tiles.  A block of 32 has a CU and takes about 5 us and 0.45 a tile, one of 128
+// half a CU, 8 us and 0.85 a tile, so that few blocks of 128 with long walks leave most of the chip waiting.  (us; 16 bits, d 128, 8 heads a kv head, no window,
+// few / shared.  Eight kv heads: one sequence, 256 rows from the start 17.6 / 16.7, 512 rows 35.6 / 24.6, 128 rows at 2048 23.8 / 59.8; at 2000 four sequences of 32 rows
+// 25.0 / 56.9, sixteen of 8 35.0 / 54.5, thirty-two of 8 65.6 / 57.4.  One kv head: one sequence, 1024 rows from the start 16.6 / 33.5, 2048 rows 29.7 / 57.1; four of 256
+// rows at 1000 18.8 / 40.5, sixteen of 32 at 4000 33.4 / 102.8)
+// Runs: one kv head, one row each, 8 heads, d 128: of 16 tiles where there are more than 24 (a window of 1024: one sequence 13.4 us whole, 10.7 in three runs, 10.4
+// in five; sixteen of 2048 without one: a step of two layers in runs of 8 1.3 us more than in runs of 16), whole rounds of the eight waves; otherwise as for trees
+// (pick_tree_plan).
 WinPlan pick_win_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, WinCall &wc, bool stats, int score_tiles) {
     const int G = st->hq_l / st->hkv_l;
     const bool h16 = is_h16(st->dtype);
-    long blocks = 0, tiles = 0, shared_blocks = 0;
+    long blocks = 0, tiles = 0;
+    double few = 0, shared = 0;                                      // us
     int longest = 1, reach[kWinSeqs];
     const int rows = h16 ? 32 : 16;
     for (int i = 0; i < wc.batch; ++i) {
         const int n = wc.cu[i + 1] - wc.cu[i], len = kv->lens[wc.seq0 + i];
         reach[i] = 0;
         if (n == 0) continue;
-        WinTiles t;
-        t.set(len + n - 1, len + n - 1, wc.window, wc.sinks, 0);      // of the last row, which sees most
-        reach[i] = t.nt;
-        longest = std::max(longest, t.nt);
+        WinTiles first, last;
+        first.set(len, len, wc.window, wc.sinks, 0);
+        last.set(len + n - 1, len + n - 1, wc.window, wc.sinks, 0);
+        reach[i] = last.nt;
+        longest = std::max(longest, last.nt);
         const long rb = (long)win_row_blocks(n, G, rows) * st->hkv_l;
+        const double walk = 0.5 * (first.nt + last.nt);
         blocks += rb;
-        tiles += rb * t.nt;
-        shared_blocks += (long)win_row_blocks(n, G, 128) * st->hkv_l;
+        tiles += rb * last.nt;
+        few += rb * (5 + 0.45 * walk) / 256;
+        shared += (double)win_row_blocks(n, G, 128) * st->hkv_l * (8 + 0.85 * walk) / 512;
     }
     WinPlan wp;
-    wp.shared = h16 && (long)wc.max_n * G > 32 && shared_blocks >= 128;
+    wp.shared = h16 && (long)wc.max_n * G > 32 && std::max(shared, 8 + 0.85 * longest) < std::max(few, 5 + 0.45 * longest);
     wp.chunk = longest;
     wp.nsplit = 1;
     const bool few_units = (long)wc.batch * st->hkv_l * win_row_blocks(wc.max_n, G, rows) <= kTreeUnits;

@@ -112,10 +112,10 @@ def test_long_contexts_in_runs_match_64_bits(dtype, hq, hkv, d, lens, counts, wi
 
 WIDE = [                                                   # enough rows that blocks share tiles
     (64, 8, 128, [0, 31, 300, 503], [64, 65, 70, 130], 100, 33),
-    (64, 8, 64, [0, 31, 300, 503], [64, 65, 70, 130], None, 0),
+    (64, 8, 64, [0, 31, 300, 203], [96, 65, 120, 130], None, 0),
     (64, 8, 64, [64, 1, 0, 0], [96, 65, 33, 200], 1, 0),
-    (16, 16, 64, [0, 77], [500, 300], 128, 5),
-    (24, 8, 128, [5, 260, 0], [300, 0, 301], 32, 64),
+    (16, 16, 64, [0, 77], [900, 600], 128, 5),
+    (24, 8, 128, [5, 260, 0], [701, 0, 600], 32, 64),
 ]
 
 
@@ -284,7 +284,7 @@ def test_another_stream_and_the_order_that_the_caller_makes():
     assert torch.equal(got, want) and torch.equal(more, weights)
 
 
-@pytest.mark.parametrize("dtype,hq,hkv,lens,counts", [("bf16", 8, 1, [1000, 40], [1, 1]), ("f16", 64, 8, [40, 0], [64, 70]), ("f32", 8, 2, [300, 17], [2, 1])])
+@pytest.mark.parametrize("dtype,hq,hkv,lens,counts", [("bf16", 8, 1, [1000, 40], [1, 1]), ("f16", 64, 8, [40, 0], [164, 170]), ("f32", 8, 2, [300, 17], [2, 1])])
 def test_recorded_and_replayed(dtype, hq, hkv, lens, counts):
     """A replay appends, attends and gathers at the lengths that hold then."""
     c = Case(dtype, hq, hkv, 64, lens, counts, 50, 4, max_seq=1200 + max(counts))

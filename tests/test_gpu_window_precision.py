@@ -35,7 +35,7 @@ def rounded(o, dtype):
 
 FEW = [(8, 2, 64, [40], [1], 24, 4), (6, 2, 64, [129], [5], None, 0), (8, 1, 128, [300, 31, 5], [3, 2, 4], 100, 3), (4, 1, 64, [20, 3], [100, 256], 50, 70),
        (2, 1, 128, [2900], [2], None, 0), (8, 1, 128, [2500, 0, 700], [26, 20, 30], 2000, 33)]
-SHARED = [(64, 8, 128, [0, 31, 300, 503], [64, 65, 70, 130], 100, 33), (64, 8, 64, [0, 31, 300, 503], [64, 65, 70, 130], None, 0), (16, 16, 64, [0, 77], [500, 300], 128, 5)]
+SHARED = [(64, 8, 128, [0, 31, 300, 503], [64, 65, 70, 130], 100, 33), (64, 8, 64, [0, 31, 300, 203], [96, 65, 120, 130], None, 0), (16, 16, 64, [0, 77], [900, 600], 128, 5)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
