@@ -824,6 +824,8 @@ void launch_win_weights(const h16_t *q, const h16_t *q_lo, int64_t ldq, const h1
         hipLaunchKernelGGL(win_gather_kernel, dim3((unsigned)tile_blocks * kg.hkv_l * wc.batch), dim3(256), 0, s, kg, hq_l, G, tile_blocks, fresh, wc, lens, wp, weights, scale_log2e);
         return;
     }
+    // shared from 65 rows on (a whole call at 2000 positions, eight kv heads of eight, us, tiles alone / shared: one sequence of 8 rows 28.3 / 29.2, of 16 32.1 / 31.9, of
+    // 64 58.6 / 40.7; sixteen of 5 rows 62.3 / 61.5, of 8 66.0 / 62.6, of 16 104 / 90)
     const bool shared = (int64_t)wc.max_n * G > 64;
     const int tile_blocks = (reach.most + (shared ? 7 : 3)) / (shared ? 8 : 4);
     const int64_t blocks = (int64_t)tile_blocks * kg.hkv_l * wc.batch, groups = ((int64_t)wc.max_n * G + 31) / 32;
@@ -846,16 +848,18 @@ void launch_win_weights(const h16_t *q, const h16_t *q_lo, int64_t ldq, const h1
 }
 
 // ---- eviction: the move ------------------------------------------------------------------------------------------------
-// The kept rows of one (layer, sequence, kv head): row slots[j] of the source becomes row j.  A block takes chunks of 32 destination rows and
-// reads a chunk whole before it writes it.  In place there is one block for all of them, in order: rows only move to the front
+// The kept rows of one (layer, sequence, kv head): row slots[j] of the source becomes row j.  A group of 256 threads takes chunks of 32 destination rows and
+// reads a chunk whole before it writes it.  In place there is one block for all of them, four chunks at a time, in order: rows only move to the front
 // (slots[j] >= j, both growing), so that what is written has been read.  K moves in pieces of 16 bytes, V, which lies transposed, through LDS.
 // Keys that are rotated back by their distance are rotated in fp32 and rounded to the element type once more.
-template <int D, bool ROT>
-__global__ __launch_bounds__(256) void evict_move_kernel(EvictCall ec, EvictMove mv, int blocks) {
+template <int D, bool ROT, int GROUPS>
+__global__ __launch_bounds__(256 * GROUPS) void evict_move_kernel(EvictCall ec, EvictMove mv, int blocks) {
     constexpr int KT = D / 32, PIECES = ROT ? 2 : 2 * KT / 4, HALF = D / 2;
-    __shared__ h16_t s_v[32][D + 2];
-    __shared__ int s_slot[32];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    __shared__ h16_t s_rows[GROUPS][32][D + 2];
+    __shared__ int s_slots[GROUPS][32];
+    const int group = threadIdx.x / 256, thread = threadIdx.x % 256, wave = thread >> 6, lane = thread & 63;
+    h16_t(*s_v)[D + 2] = s_rows[group];
+    int *s_slot = s_slots[group];
     const unsigned unit = blockIdx.x / (unsigned)blocks;
     const int chunk = (int)(blockIdx.x % (unsigned)blocks), c = unit % ec.hkv, b = (unit / ec.hkv) % ec.batch, layer = unit / ec.hkv / ec.batch;
     const int32_t *slots = ec.slots + (size_t)unit * ec.dst_seq;
@@ -864,14 +868,15 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictCall ec, EvictMove
     const h16_t *ks = static_cast<const h16_t *>(mv.ks) + src, *vs = static_cast<const h16_t *>(mv.vs) + src;
     h16_t *kd = static_cast<h16_t *>(mv.kd) + dst, *vd = static_cast<h16_t *>(mv.vd) + dst;
     if (blockIdx.x == 0)
-        for (int i = threadIdx.x; i < mv.dst_batch; i += 256) mv.dst_lens[i] = i < ec.batch ? min(min(mv.lens[i], ec.max_seq), ec.keep) : 0;
+        for (int i = threadIdx.x; i < mv.dst_batch; i += 256 * GROUPS) mv.dst_lens[i] = i < ec.batch ? min(min(mv.lens[i], ec.max_seq), ec.keep) : 0;
     const int most = min(ec.keep, ec.dst_seq);
-    for (int j0 = 32 * chunk; j0 < most; j0 += 32 * blocks) {
+    for (int first = 32 * GROUPS * chunk; first < most; first += 32 * GROUPS * blocks) {
+        const int j0 = first + 32 * group;
         __syncthreads();
-        if (threadIdx.x < 32) s_slot[threadIdx.x] = j0 + threadIdx.x < most ? slots[j0 + threadIdx.x] : -1;
+        if (thread < 32) s_slot[thread] = j0 + thread < most ? slots[j0 + thread] : -1;
         __syncthreads();
-        if (s_slot[0] < 0) break;                              // the same in every thread: the kept ones come first
-        if (mv.ks == mv.kd && s_slot[31] == j0 + 31) continue;  // in place, and none of them moves
+        // nothing to move: the kept ones come first; or in place, and every row is where it belongs
+        const bool moves = s_slot[0] >= 0 && !(mv.ks == mv.kd && s_slot[31] == j0 + 31);
         // a wave's piece i: one fragment tile, 16 rows x 32 elements, as it lies in the destination (rotated: and the one half a head further); rows that are not
         // there read slot 0
         typedef uint32_t piece __attribute__((ext_vector_type(4)));
@@ -903,7 +908,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictCall ec, EvictMove
                 }
             }
         }
-        for (int idx = threadIdx.x; idx < 32 * D; idx += 256) {
+        for (int idx = moves ? thread : 32 * D; idx < 32 * D; idx += 256) {
             const int row = idx / D, dd = idx % D;             // a wave: 64 elements of one row, two bytes of every 16 (kvlayout.h)
             s_v[row][dd] = vs[kv_v_offset(max(s_slot[row], 0), dd, D)];
         }
@@ -911,9 +916,9 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictCall ec, EvictMove
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const int tile = wave + (ROT ? 0 : 4 * i), row = 16 * (tile / ACROSS) + (lane & 15), dd = 32 * (tile % ACROSS) + 8 * (lane >> 4) + (ROT ? HALF * i : 0);
-            if (has && s_slot[row] >= 0) *reinterpret_cast<piece *>(kd + kv_k_offset(j0 + row, dd, D)) = k[i];
+            if (has && moves && s_slot[row] >= 0) *reinterpret_cast<piece *>(kd + kv_k_offset(j0 + row, dd, D)) = k[i];
         }
-        for (int idx = threadIdx.x; idx < 4 * D; idx += 256) {
+        for (int idx = moves ? thread : 4 * D; idx < 4 * D; idx += 256) {
             const int dd = (idx & 15) + 16 * (idx >> 6), g = (idx >> 4) & 3;    // 16-byte pieces in the order in which they lie (kvlayout.h)
             union { uint4 u; h16_t e[8]; } w;
 #pragma unroll
@@ -932,7 +937,11 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictCall ec, EvictMove
 void launch_evict_move(const EvictCall &ec, const EvictMove &mv, hipStream_t s) {
     const int blocks = evict_blocks(ec, mv);
     const dim3 grid((unsigned)blocks * ec.layers * ec.batch * ec.hkv);
-#define HX_MOVE(DD, R) hipLaunchKernelGGL((evict_move_kernel<DD, R>), grid, dim3(256), 0, s, ec, mv, blocks)
+#define HX_MOVE(DD, R)                                                                                                                     \
+    do {                                                                                                                                   \
+        if (mv.ks == mv.kd) hipLaunchKernelGGL((evict_move_kernel<DD, R, 4>), grid, dim3(1024), 0, s, ec, mv, blocks);                      \
+        else hipLaunchKernelGGL((evict_move_kernel<DD, R, 1>), grid, dim3(256), 0, s, ec, mv, blocks);                                      \
+    } while (0)
     if (mv.src.d == 128) { if (mv.cos_tab != nullptr) HX_MOVE(128, true); else HX_MOVE(128, false); }
     else { if (mv.cos_tab != nullptr) HX_MOVE(64, true); else HX_MOVE(64, false); }
 #undef HX_MOVE

@@ -496,11 +496,13 @@ __global__ __launch_bounds__(T) void evict_select_kernel(EvictCall ec, const int
     }
 }
 
-// The kept rows, as in the 16-bit kernel: chunks of 32 rows, read whole before they are written; one block for all chunks in place
-template <int D, bool ROT>
-__global__ __launch_bounds__(256) void f32_evict_move_kernel(EvictCall ec, EvictMove mv, int blocks) {
+// The kept rows, as in the 16-bit kernel: chunks of 32 rows, read whole before they are written; one block for all chunks in place, four at a time
+template <int D, bool ROT, int GROUPS>
+__global__ __launch_bounds__(256 * GROUPS) void f32_evict_move_kernel(EvictCall ec, EvictMove mv, int blocks) {
     constexpr int P4 = D / 4, PIECES = 32 * P4 / 256, HALF = D / 2;
-    __shared__ int s_slot[32];
+    __shared__ int s_slots[GROUPS][32];
+    const int group = threadIdx.x / 256, thread = threadIdx.x % 256;
+    int *s_slot = s_slots[group];
     const unsigned unit = blockIdx.x / (unsigned)blocks;
     const int chunk = (int)(blockIdx.x % (unsigned)blocks), c = unit % ec.hkv, b = (unit / ec.hkv) % ec.batch, layer = unit / ec.hkv / ec.batch;
     const int32_t *slots = ec.slots + (size_t)unit * ec.dst_seq;
@@ -509,18 +511,18 @@ __global__ __launch_bounds__(256) void f32_evict_move_kernel(EvictCall ec, Evict
     const float *ks = static_cast<const float *>(mv.ks) + src, *vs = static_cast<const float *>(mv.vs) + src;
     float *kd = static_cast<float *>(mv.kd) + dst, *vd = static_cast<float *>(mv.vd) + dst;
     if (blockIdx.x == 0)
-        for (int i = threadIdx.x; i < mv.dst_batch; i += 256) mv.dst_lens[i] = i < ec.batch ? min(min(mv.lens[i], ec.max_seq), ec.keep) : 0;
+        for (int i = threadIdx.x; i < mv.dst_batch; i += 256 * GROUPS) mv.dst_lens[i] = i < ec.batch ? min(min(mv.lens[i], ec.max_seq), ec.keep) : 0;
     const int most = min(ec.keep, ec.dst_seq);
-    for (int j0 = 32 * chunk; j0 < most; j0 += 32 * blocks) {
+    for (int first = 32 * GROUPS * chunk; first < most; first += 32 * GROUPS * blocks) {
+        const int j0 = first + 32 * group;
         __syncthreads();
-        if (threadIdx.x < 32) s_slot[threadIdx.x] = j0 + threadIdx.x < most ? slots[j0 + threadIdx.x] : -1;
+        if (thread < 32) s_slot[thread] = j0 + thread < most ? slots[j0 + thread] : -1;
         __syncthreads();
-        if (s_slot[0] < 0) break;
-        if (mv.ks == mv.kd && s_slot[31] == j0 + 31) continue;  // in place, and none of them moves
+        const bool moves = s_slot[0] >= 0 && !(mv.ks == mv.kd && s_slot[31] == j0 + 31);
         floatx4 k[PIECES], v[PIECES];
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const int idx = threadIdx.x + 256 * i, at = max(s_slot[idx / P4], 0), dd = 4 * (idx % P4);
+            const int idx = thread + 256 * i, at = max(s_slot[idx / P4], 0), dd = 4 * (idx % P4);
             k[i] = *reinterpret_cast<const floatx4 *>(ks + (size_t)at * D + dd);
             v[i] = *reinterpret_cast<const floatx4 *>(vs + (size_t)at * D + dd);
             if constexpr (ROT) {
@@ -534,8 +536,8 @@ __global__ __launch_bounds__(256) void f32_evict_move_kernel(EvictCall ec, Evict
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const int idx = threadIdx.x + 256 * i, row = idx / P4, dd = 4 * (idx % P4);
-            if (s_slot[row] < 0) continue;
+            const int idx = thread + 256 * i, row = idx / P4, dd = 4 * (idx % P4);
+            if (!moves || s_slot[row] < 0) continue;
             *reinterpret_cast<floatx4 *>(kd + (size_t)(j0 + row) * D + dd) = k[i];
             *reinterpret_cast<floatx4 *>(vd + (size_t)(j0 + row) * D + dd) = v[i];
         }
@@ -580,7 +582,11 @@ void launch_evict_select(const EvictCall &ec, int longest, const int32_t *lens, 
 void f32_launch_evict_move(const EvictCall &ec, const EvictMove &mv, hipStream_t s) {
     const int blocks = evict_blocks(ec, mv);
     const dim3 grid((unsigned)blocks * ec.layers * ec.batch * ec.hkv);
-#define HX_MOVE(DD, R) hipLaunchKernelGGL((f32_evict_move_kernel<DD, R>), grid, dim3(256), 0, s, ec, mv, blocks)
+#define HX_MOVE(DD, R)                                                                                                                     \
+    do {                                                                                                                                   \
+        if (mv.ks == mv.kd) hipLaunchKernelGGL((f32_evict_move_kernel<DD, R, 4>), grid, dim3(1024), 0, s, ec, mv, blocks);                  \
+        else hipLaunchKernelGGL((f32_evict_move_kernel<DD, R, 1>), grid, dim3(256), 0, s, ec, mv, blocks);                                  \
+    } while (0)
     if (mv.src.d == 128) { if (mv.cos_tab != nullptr) HX_MOVE(128, true); else HX_MOVE(128, false); }
     else { if (mv.cos_tab != nullptr) HX_MOVE(64, true); else HX_MOVE(64, false); }
 #undef HX_MOVE

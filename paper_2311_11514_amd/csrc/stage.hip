@@ -1834,7 +1834,7 @@ hexgen_status_t hexgen_kv_cache_evict(hexgen_kv_cache_t *kv, hexgen_kv_cache_t *
     const EvictMove mv{kv->k, kv->v, dst->k, dst->v, kv->layer_stride, dst->layer_stride, geom(st, kv), geom(st, dst),
                        rotate ? kv->cos_tab : nullptr, rotate ? kv->sin_tab : nullptr, kv->d_lens, dst->d_lens, dst->max_batch};
     const uint64_t units = (uint64_t)ec.layers * ec.batch * ec.hkv;
-    if (units * 1024 > UINT32_MAX || units * 256 * evict_blocks(ec, mv) > UINT32_MAX) return HEXGEN_ERR_CAPACITY;
+    if (units * 1024 > UINT32_MAX || units * (dst == kv ? 1024 : 256 * (uint64_t)evict_blocks(ec, mv)) > UINT32_MAX) return HEXGEN_ERR_CAPACITY;
     launch_evict_select(ec, *std::max_element(kv->lens.begin(), kv->lens.begin() + kv->batch), kv->d_lens, s);
     if (is_h16(st->dtype)) HX_K(st->dtype, launch_evict_move, ec, mv, s);
     else f32_launch_evict_move(ec, mv, s);

@@ -120,6 +120,14 @@ def test_first_and_newest_without_weights(dtype):
     c.check(64, 4, 10, weights=False)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("d,rotate", [(64, True), (128, False), (128, True)])
+def test_many_rows_in_place(dtype, d, rotate):
+    """Rows that one block moves in several steps, some of which move nothing."""
+    c = Case(dtype, 1, 4, 2, d, [900, 611, 450], 900, seed=13)
+    c.check(610, 200, 100, rotate=rotate)
+
+
 def test_twice_in_place():
     """What an eviction leaves is a context like any other: it can be evicted from again."""
     c = Case("bf16", 1, 2, 2, 64, [220, 90], 256, seed=7)
