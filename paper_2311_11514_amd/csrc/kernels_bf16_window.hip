@@ -73,7 +73,8 @@ void launch_win_rope_append(const float *qkv, int hq_l, KvGeom kg, const WinCall
     hipLaunchKernelGGL(win_rope_append_kernel, dim3((n + 255) / 256), dim3(256), 0, s, qkv, hq_l, kg, wc, lens, cos_tab, sin_tab, q, q_lo, kc, vc);
 }
 
-// Plain rows into the cache, a block per tile of 32 slots: K in pieces of 16 bytes, V through LDS, so that the tile's transposed pieces are written whole
+// Plain rows into the cache, a block per tile of 32 slots: K in pieces of 16 bytes, V through LDS, so that the tile's transposed pieces are written whole.
+// Bound by HBM: 4096 rows of 8 kv heads, d 128, 8.9 us (3.8 TB/s read and written).
 template <int D>
 __global__ __launch_bounds__(256) void win_append_kernel(TreeIn in, h16_t *__restrict__ kc, h16_t *__restrict__ vc, KvGeom kg, WinCall wc, const int32_t *__restrict__ lens) {
     constexpr int P8 = D / 8, PIECES = 32 * P8 / 256;
@@ -150,6 +151,10 @@ struct WinBase {
 // two parts (tree_pack2).  Rows that are not in the cache yet (in.k != NULL: a sequence's rows are one block's then) are put over the tile and appended by
 // the run that holds their tile.  Runs leave (m, l, o) with device-scope stores; the last to arrive joins them in the order of the context.
 // A weight of zero times an infinity would be a NaN: a masked tile with a value that is not finite is multiplied out over what each row attends.
+// Unmasked tiles come first (WinTiles), in a loop of their own: with masked and unmasked ones in one the compiler spilled 126 registers.
+// Bound by HBM where there are many sequences, by the chain launch, rows, tiles, joining where there are few: d 128, one row each, 8 heads a kv head: 32 contexts of
+// 240 .. 4027 under a window of 2048, 8 kv heads, 38.6 us (5.5 TB/s), 43.2 with the scores for the weights' sums (14 MB); one sequence, one kv head, window 1024 10.8;
+// sixteen of 2048, one kv head, 10.9.
 template <int D, bool QLO>
 __global__ __launch_bounds__(512, 2) void win_few_kernel(const h16_t *__restrict__ q, const h16_t *__restrict__ q_lo, int64_t ldq, TreeIn in, h16_t *kc, h16_t *vc,
                                                          KvGeom kg, int hq_l, int G, int nrb, WinCall wc, const int32_t *__restrict__ lens, WinPlan wp, TreeOut out,
@@ -399,8 +404,13 @@ __global__ __launch_bounds__(512, 2) void win_few_kernel(const h16_t *__restrict
 }
 
 // ---- attention, many rows ---------------------------------------------------------------------------------------------
-// A block of four waves takes 128 query rows, 32 a wave; their tiles go from HBM to LDS directly, three in flight, and are shared.  Products and softmax as
-// above.  The rows are in the cache already.
+// A block of four waves takes 128 query rows, 32 a wave; their tiles go from HBM to LDS directly, four buffers deep, and are shared.  The rows are in the cache
+// already.  S^T = K . Q^T, O^T = V^T . P^T on the 32 x 32 x 16 MFMA, P in registers, rounded to the element type once as in the prefill attention: with two parts, as few rows
+// have them, results are a quarter more exact (RMS against 64 bits 1.6e-3 instead of 2.1e-3, bf16) and a call of 4096 rows under a window of 1024 took 207 us instead of
+// 166, one of 8 x 512 rows that gathers weights 418 instead of 358.
+// While the vector unit works on a tile's weights the matrix cores have the next tile's scores.  Bound by each wave's chain of LDS reads, products and softmax, 1.7 waves
+// a SIMD (240 registers): matrix cores 34 % busy, vector units 48 %; three waves spill (358 us).  d 128, 64 query and 8 kv heads: 4096 rows under a window of 1024 155 us (780 TFLOP/s
+// over the pairs that are attended); 8 x 512 rows at 1000 .. 3500, 32 / 4 heads, 210 (820).
 template <int D>
 __global__ __launch_bounds__(256, 2) void win_attn_kernel(const h16_t *__restrict__ q, int64_t ldq, const h16_t *__restrict__ kc, const h16_t *__restrict__ vc, KvGeom kg,
                                                           int hq_l, int G, int nrb, WinCall wc, const int32_t *__restrict__ lens, WinPlan wp, TreeOut out,
@@ -574,9 +584,10 @@ void launch_win_attn(const h16_t *q, const h16_t *q_lo, int64_t ldq, const TreeI
 }
 
 // ---- the weights' sums ------------------------------------------------------------------------------------------------
-// weights[j] += sum over the call's rows and a kv head's query heads of exp(s_rj - m_r) / l_r: the scores once more, now that every row's maximum and sum
-// are known.  A wave keeps the keys of one tile in registers and goes through the rows that attend it in groups of 32; the sums stay in its lanes (lane: a
-// column of every group) and meet at the end, in one order: every position belongs to one wave, nothing is added atomically.
+// weights[j] += sum over the call's rows and a kv head's query heads of exp(s_rj - m_r) / l_r, once every row's maximum and sum are known.  Every position belongs to
+// one wave, or its partial sums are joined in one order; nothing is added atomically, so that the same call gives the same bits.
+// Here: the scores once more.  A wave keeps the keys of one tile in registers and goes through the rows that attend it in groups of 32; the sums stay in its
+// lanes (lane: a column of every group) and meet at the end.  For 33 to 64 rows a kv head, and for fewer where the scores have no room.
 template <int D, bool QLO>
 __global__ __launch_bounds__(256, 4) void win_weights_kernel(const h16_t *__restrict__ q, const h16_t *__restrict__ q_lo, int64_t ldq, const h16_t *__restrict__ kc, KvGeom kg,
                                                              int hq_l, int G, int tile_blocks, WinCall wc, const int32_t *__restrict__ lens, const float *__restrict__ stat,
@@ -639,7 +650,8 @@ __global__ __launch_bounds__(256, 4) void win_weights_kernel(const h16_t *__rest
         }
     }
 }
-// The same for few rows from the scores that the attention has left: a thread per position
+// The same for up to 32 rows a kv head from the scores that the attention has left (WinPlan), a thread per position: 32 ragged contexts, 8 heads a kv head, 6.2 us
+// where the keys once more took 23 to 28
 __global__ __launch_bounds__(256) void win_gather_kernel(KvGeom kg, int hq_l, int G, int tile_blocks, bool fresh, WinCall wc, const int32_t *__restrict__ lens, WinPlan wp,
                                                          float *__restrict__ weights, float scale_log2e) {
     const int tb = blockIdx.x % tile_blocks, c = (blockIdx.x / tile_blocks) % kg.hkv_l, nth = blockIdx.x / tile_blocks / kg.hkv_l;
@@ -852,6 +864,8 @@ void launch_win_weights(const h16_t *q, const h16_t *q_lo, int64_t ldq, const h1
 // reads a chunk whole before it writes it.  In place there is one block for all of them, four chunks at a time, in order: rows only move to the front
 // (slots[j] >= j, both growing), so that what is written has been read.  K moves in pieces of 16 bytes, V, which lies transposed, through LDS.
 // Keys that are rotated back by their distance are rotated in fp32 and rounded to the element type once more.
+// Bound by HBM: where slots stay here and there, nearly every 64 bytes of the context hold one of them (K four, V eight positions each), so that a fetch takes most of it:
+// 2 layers x 8 x 8 heads, 1500 .. 4000 to 1024 slots by weight 50 us (134 MB of rows moved, 230 MB over HBM at 4.6 TB/s); 2 x 16 x 1 heads, 2048 newest of 4000, rotated 22 us (67 MB).
 template <int D, bool ROT, int GROUPS>
 __global__ __launch_bounds__(256 * GROUPS) void evict_move_kernel(EvictCall ec, EvictMove mv, int blocks) {
     constexpr int KT = D / 32, PIECES = ROT ? 2 : 2 * KT / 4, HALF = D / 2;

@@ -56,7 +56,9 @@ __global__ __launch_bounds__(256) void f32_win_append_kernel(TreeIn in, float *_
 // A block takes 16 query columns of one (sequence, kv head) -- column j: new row j / G, head j % G -- and a run of their tiles, over whose halves of 16 positions
 // its W waves interleave; products and register layouts are those of the stage's fp32 attention (v_mfma_f32_16x16x4_f32, a lane owns column l % 16
 // and positions 4 (l / 16) + r, P stays in registers).  Rows that are not in the cache yet (in.k != NULL: a sequence's rows are one block's columns then) are
-// read from the caller's and appended by the run that holds their tile.
+// read from the caller's and appended by the run that holds their tile.  Three waves a SIMD instead of two: 30.7 -> 25.8 us.
+// Bound by each wave's chain of loads and fp32 matrix instructions (32 cycles each, 64 for 16 positions): d 128, 16 / 4 heads, three prompts of 90 .. 301 rows under a window
+// of 128 25.8 us; one row at 40 positions, d 64, 5.3, half of that the launch.
 template <int D, int W>
 __global__ __launch_bounds__(64 * W, 3) void f32_win_attn_kernel(const float *__restrict__ q, int64_t ldq, TreeIn in, float *kc, float *vc, KvGeom kg, int hq_l, int G, int nrb,
                                                               WinCall wc, const int32_t *__restrict__ lens, WinPlan wp, float *__restrict__ o) {
@@ -255,7 +257,8 @@ __global__ __launch_bounds__(64 * W, 3) void f32_win_attn_kernel(const float *__
 }
 
 // weights[j] += sum over rows and heads of exp(s_rj - m_r) / l_r, as in the 16-bit kernels: a block takes 16 positions, whose keys all of its waves hold; the waves
-// take the rows that attend them in turn, 16 columns at a time, the next ones' requested ahead, and meet in LDS in the order of the waves.
+// take the rows that attend them in turn, 16 columns at a time, the next ones' requested ahead, and meet in LDS in the order of the waves.  Three prompts as above 21.5 us
+// (one wave a tile of all rows 91, eight waves a block 23): the first positions, which every row attends, are the longest chain.
 template <int D, int W>
 __global__ __launch_bounds__(64 * W) void f32_win_weights_kernel(const float *__restrict__ q, int64_t ldq, const float *__restrict__ kc, KvGeom kg, int hq_l, int G, int tile_blocks,
                                                                  WinCall wc, const int32_t *__restrict__ lens, const float *__restrict__ stat, float *__restrict__ weights) {
@@ -345,7 +348,7 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 // A block per (layer, sequence, kv head) finds the smallest weight that stays by its digits, eight bits at a time from the top -- how many of the weights with the digits
 // found so far have each value of the next one --, then goes through the slots once in order: what is first, recent, heavier than that one, or equal to it
 // and among the first such as are still wanted.  The counts are integers: the result does not depend on the order of the LDS atomics.
-// A thread has up to PER slots next to each other, so many that all threads have some; contexts of up to T PER slots are read once and stay in registers.
+// Bound by latency: four digits of three barriers each.  A thread has up to PER slots next to each other, so many that all threads have some; contexts of up to T PER slots are read once and stay in registers.
 template <int T>
 __global__ __launch_bounds__(T) void evict_select_kernel(EvictCall ec, const int32_t *__restrict__ lens) {
     constexpr int WAVES = T / 64, PER = 8;
@@ -573,7 +576,8 @@ void f32_launch_win_weights(const float *q, int64_t ldq, const float *kc, KvGeom
 void launch_win_advance(int32_t *lens, const WinCall &wc, hipStream_t s) {
     hipLaunchKernelGGL(win_advance_kernel, dim3(1), dim3(kWinSeqs), 0, s, lens, wc);
 }
-// Small contexts in four waves, whose barriers cost less than more lanes gain: 333 slots LOW_SMALL us in 256 threads, in 1024 10.6; 4000 slots HIGH us in 1024 and 15 in 512
+// Small contexts in four waves, whose barriers cost less than more lanes gain: 333 slots 8.8 us in 256 threads, in 1024 10.6; 4000 slots 13.5 us in
+// 1024 and 15 in 512
 void launch_evict_select(const EvictCall &ec, int longest, const int32_t *lens, hipStream_t s) {
     const dim3 grid((unsigned)ec.layers * ec.batch * ec.hkv);
     if (longest <= 1024) hipLaunchKernelGGL(evict_select_kernel<256>, grid, dim3(256), 0, s, ec, lens);
