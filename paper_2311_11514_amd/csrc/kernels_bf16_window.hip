@@ -409,8 +409,8 @@ __global__ __launch_bounds__(512, 2) void win_few_kernel(const h16_t *__restrict
 // have them, results are a quarter more exact (RMS against 64 bits 1.6e-3 instead of 2.1e-3, bf16) and a call of 4096 rows under a window of 1024 took 207 us instead of
 // 166, one of 8 x 512 rows that gathers weights 418 instead of 358.
 // While the vector unit works on a tile's weights the matrix cores have the next tile's scores.  Bound by each wave's chain of LDS reads, products and softmax, 1.7 waves
-// a SIMD (240 registers): matrix cores 34 % busy, vector units 48 %; three waves spill (358 us).  d 128, 64 query and 8 kv heads: 4096 rows under a window of 1024 155 us (780 TFLOP/s
-// over the pairs that are attended); 8 x 512 rows at 1000 .. 3500, 32 / 4 heads, 210 (820).
+// a SIMD (240 registers): matrix cores 34 % busy, vector units 48 %; three waves spill (358 us).  d 128, 64 query and 8 kv heads: 4096 rows under a window of 1024 157 of a call's 166 us
+// (770 TFLOP/s over the pairs that are attended); 8 x 512 rows at 1000 .. 3500, 32 / 4 heads, 210 (820).
 template <int D>
 __global__ __launch_bounds__(256, 2) void win_attn_kernel(const h16_t *__restrict__ q, int64_t ldq, const h16_t *__restrict__ kc, const h16_t *__restrict__ vc, KvGeom kg,
                                                           int hq_l, int G, int nrb, WinCall wc, const int32_t *__restrict__ lens, WinPlan wp, TreeOut out,
