@@ -853,7 +853,14 @@ void launch_win_weights(const h16_t *q, const h16_t *q_lo, int64_t ldq, const h1
         }
     }
     const dim3 grid(shared ? win_grid(kg.hkv_l * wc.batch, tile_blocks * splits) : (unsigned)blocks);
-#define HX_WIN_W(DD, LO)                                                                                                                                            do {                                                                                                                                                                if (shared) hipLaunchKernelGGL((win_weights_shared_kernel<DD, LO>), grid, dim3(256), 0, s, q, q_lo, ldq, kc, kg, hq_l, G, tile_blocks, splits, wc, lens, wp.stat, weights, wp.part_o, wp.arrived, scale_log2e);         else hipLaunchKernelGGL((win_weights_kernel<DD, LO>), grid, dim3(256), 0, s, q, q_lo, ldq, kc, kg, hq_l, G, tile_blocks, wc, lens, wp.stat, weights, scale_log2e);     } while (0)
+#define HX_WIN_W(DD, LO)                                                                                                                                                   \
+    do {                                                                                                                                                                   \
+        if (shared)                                                                                                                                                        \
+            hipLaunchKernelGGL((win_weights_shared_kernel<DD, LO>), grid, dim3(256), 0, s, q, q_lo, ldq, kc, kg, hq_l, G, tile_blocks, splits, wc, lens, wp.stat, weights, \
+                               wp.part_o, wp.arrived, scale_log2e);                                                                                                        \
+        else                                                                                                                                                               \
+            hipLaunchKernelGGL((win_weights_kernel<DD, LO>), grid, dim3(256), 0, s, q, q_lo, ldq, kc, kg, hq_l, G, tile_blocks, wc, lens, wp.stat, weights, scale_log2e);  \
+    } while (0)
     if (kg.d == 128) { if (q_lo != nullptr) HX_WIN_W(128, true); else HX_WIN_W(128, false); }
     else { if (q_lo != nullptr) HX_WIN_W(64, true); else HX_WIN_W(64, false); }
 #undef HX_WIN_W

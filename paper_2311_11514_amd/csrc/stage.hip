@@ -453,7 +453,7 @@ void attn_tree(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const Rows &r, 
 struct WinSpan {
     const int32_t *counts;
     int batch, rows, max_n, window, sinks;
-    float *weights;               // the first layer's accumulators, or NULL
+    float *weights;               // the accumulators that the caller gave: of every layer, or of the one layer that is asked for; or NULL
     int count(int i) const { return counts != nullptr ? counts[i] : 1; }
 };
 constexpr int64_t kWinRowStride = 1 << 24;                   // elements between query rows: offsets among 32 of them have 32 bits
@@ -462,7 +462,7 @@ constexpr size_t kWinStatFloats = 2;                         // statistics of a 
 size_t win_stat_floats(const hexgen_stage *st, int rows) { return (kWinStatFloats * rows * st->hq_l + 3) / 4 * 4; }       // the scores behind them are written 16 bytes at a time
 constexpr size_t kWinScoreFloats = (size_t)16 << 20;         // 64 MB of scores at most
 
-// the span in launches of kWinSeqs sequences; those without a row at either end of one are left out of it
+// the span in launches of kWinSeqs sequences; one whose sequences have no row is left out
 template <typename F>
 void for_each_call(const hexgen_kv_cache *kv, const WinSpan &sp, F &&fn) {
     for (int first = 0, row = 0; first < sp.batch; first += kWinSeqs) {
@@ -502,8 +502,8 @@ int win_score_tiles(const hexgen_stage *st, const hexgen_kv_cache *kv, const Win
 // rows at 1000 18.8 / 40.5, sixteen of 32 at 4000 33.4 / 102.8)
 // Runs: one kv head, one row each, 8 heads, d 128: of 16 tiles where there are more than 24 (a window of 1024: one sequence 13.4 us whole, 10.7 in three runs, 10.4
 // in five; sixteen of 2048 without one: a step of two layers in runs of 8 1.3 us more than in runs of 16), whole rounds of the eight waves; otherwise as for trees
-// (pick_tree_plan).
-WinPlan pick_win_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, WinCall &wc, bool stats, int score_tiles) {
+// (pick_tree_plan).  two_parts: the query rows come in two parts, which only blocks of 32 take.
+WinPlan pick_win_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, WinCall &wc, bool two_parts, bool stats, int score_tiles) {
     const int G = st->hq_l / st->hkv_l;
     const bool h16 = is_h16(st->dtype);
     long blocks = 0, tiles = 0;
@@ -527,7 +527,7 @@ WinPlan pick_win_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, WinCall
         shared += (double)win_row_blocks(n, G, 128) * st->hkv_l * (8 + 0.85 * walk) / 512;
     }
     WinPlan wp;
-    wp.shared = h16 && (long)wc.max_n * G > 32 && std::max(shared, 8 + 0.85 * longest) < std::max(few, 5 + 0.45 * longest);
+    wp.shared = h16 && !two_parts && (long)wc.max_n * G > 32 && std::max(shared, 8 + 0.85 * longest) < std::max(few, 5 + 0.45 * longest);
     wp.chunk = longest;
     wp.nsplit = 1;
     const bool few_units = (long)wc.batch * st->hkv_l * win_row_blocks(wc.max_n, G, rows) <= kTreeUnits;
@@ -562,15 +562,14 @@ WinReach win_reach(const hexgen_kv_cache *kv, const WinCall &wc) {
 }
 
 // The rows' attention in one layer.  in.k given: their keys and values join the cache here, in the attention itself where a sequence's rows are one
-// block's, otherwise in front of it.
-void attn_rows(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const WinSpan &sp, const void *q, const h16_t *q_lo, int64_t ldq, const TreeIn &in, const TreeOut &out,
-               hipStream_t s) {
+// block's, otherwise in front of it.  weights: this layer's, or NULL.
+void attn_rows(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const WinSpan &sp, float *weights, const void *q, const h16_t *q_lo, int64_t ldq, const TreeIn &in,
+               const TreeOut &out, hipStream_t s) {
     const KvGeom kg = geom(st, kv);
     const int G = st->hq_l / st->hkv_l;
-    float *weights = sp.weights != nullptr ? sp.weights + (size_t)layer * sp.batch * st->hkv_l * kv->max_seq : nullptr;
     const int score_tiles = win_score_tiles(st, kv, sp);
     for_each_call(kv, sp, [&](WinCall &wc) {
-        const WinPlan wp = pick_win_plan(st, kv, wc, weights != nullptr, score_tiles);
+        const WinPlan wp = pick_win_plan(st, kv, wc, q_lo != nullptr, weights != nullptr, score_tiles);
         TreeIn here = in;
         const bool append = in.k != nullptr && (wp.shared || (long)wc.max_n * G > (is_h16(st->dtype) ? 32 : 16));
         if (append) here = TreeIn{nullptr, nullptr, 0, 0};
@@ -605,7 +604,8 @@ void attn_win(hexgen_stage *st, hexgen_kv_cache *kv, int layer, const Rows &r, c
             f32_launch_win_rope_append(w.qkv32, st->hq_l, kg, wc, kv->d_lens, kv->cos_tab, kv->sin_tab, w.q32, kc, vc, s);
         }
     });
-    attn_rows(st, kv, layer, *r.win, is_h16(st->dtype) ? static_cast<const void *>(w.q) : w.q32, q_lo, st->qw, in, out, s);
+    float *weights = r.win->weights != nullptr ? r.win->weights + (size_t)layer * r.win->batch * st->hkv_l * kv->max_seq : nullptr;
+    attn_rows(st, kv, layer, *r.win, weights, is_h16(st->dtype) ? static_cast<const void *>(w.q) : w.q32, q_lo, st->qw, in, out, s);
 }
 
 // ---- bf16 prefill flow: five kernels per layer; RoPE / cache append, residual + next-norm operand and SwiGLU
@@ -1777,8 +1777,7 @@ hexgen_status_t hexgen_kv_window_attention(hexgen_kv_cache_t *kv, int layer, con
     hipStream_t s = static_cast<hipStream_t>(stream);
     HX_TRY(ensure_tree_part(st, s));
     HX_TRY(ensure_win_stat(st, kv, sp, s));
-    if (sp.weights != nullptr) sp.weights -= (size_t)layer * batch * st->hkv_l * kv->max_seq;      // this layer's own are given
-    attn_rows(st, kv, layer, sp, q, nullptr, ldq, TreeIn{k, v, ldk, ldv}, TreeOut{TREE_OUT_ROWS, sp.rows, st->qw, out}, s);
+    attn_rows(st, kv, layer, sp, sp.weights, q, nullptr, ldq, TreeIn{k, v, ldk, ldv}, TreeOut{TREE_OUT_ROWS, sp.rows, st->qw, out}, s);
     HX_HIP(hipGetLastError());
     return HEXGEN_OK;
 }
