@@ -244,10 +244,12 @@ hexgen_status_t hexgen_kv_cache_keep(hexgen_kv_cache_t *kv, hexgen_tree_t *tr, c
  * each of which the call adds the softmax weights that its slot got, over the call's rows and the query heads of the kv head; slots that no row
  * attends, and those behind the rows, stay as they are.  May be NULL.  The sums have one order: the same call gives the same bits.
  *
- *   hexgen_kv_window_attention: one layer's attention alone, for callers with projections of their own.  q, k, v, out and their row strides as for
- *     hexgen_kv_tree_attention, q and k rotated at the rows' positions (slots; or, behind evictions, whatever positions the caller's keys carry).  k and v join
- *     `layer`'s cache at the rows' slots, uncommitted: hexgen_kv_cache_commit once all layers have processed the rows.  What a row
- *     does not attend has no influence on it, infinities and NaN included.
+ *   hexgen_kv_window_attention: one layer's attention alone, for callers with projections of their own.  q, k, v, out and their row strides
+ *     (q's at most 2^24 elements: HEXGEN_ERR_INVALID_ARG beyond) as for hexgen_kv_tree_attention, q and k rotated at the rows' positions (slots;
+ *     or, behind evictions, whatever positions the caller's keys carry).  k and v join `layer`'s cache at the rows' slots, uncommitted:
+ *     hexgen_kv_cache_commit once all layers have processed the rows.  What a row does not attend has no influence on it, infinities and NaN
+ *     included.  16-bit types: softmax weights enter the sums in two parts (16 bits or more of them), or may be rounded to the type once, as a prefill's,
+ *     where a sequence has more than 32 rows x heads per kv head; an attended infinite value whose weight rounds to zero gives NaN.
  *   hexgen_stage_extend: the rows through every layer of the stage, rotated at their slots; buffers as for hexgen_stage_prefill.  The committed
  *     lengths grow by counts; the decode steps' count does not change.  Up to 32 rows are computed as decode steps are, more as a prefill is.
  *   hexgen_kv_cache_evict: of every sequence's len_i slots min(len_i, keep) stay, in their order: the first `sinks`, the last `recent`, and of the others those
@@ -258,7 +260,7 @@ hexgen_status_t hexgen_kv_cache_keep(hexgen_kv_cache_t *kv, hexgen_tree_t *tr, c
  *     Device outputs, rows of dst's max_seq: slots int32 [n_layers][batch][hkv_local][dst max_seq], the slots that stayed, filled up with -1; weights_out fp32 of the same
  *     shape (NULL when weights is), their weights, filled up with 0 (in place: may be weights itself).  dst's committed lengths become min(len_i, keep); a dst that is not kv starts
  *     its decode steps at 0.  HEXGEN_ERR_INVALID_ARG when sinks + recent > keep; HEXGEN_ERR_CAPACITY unless dst takes the batch and min(keep, max_seq) slots;
- *     HEXGEN_ERR_DEVICE when it would be recorded.  Drafted rows that are not committed are dropped.
+ *     HEXGEN_ERR_DEVICE when it would be recorded.  Rows that are not committed are dropped.
  * All three enqueue on `stream`; HEXGEN_ERR_STATE unless the cache holds a batch (prefill, set_lengths, commit), of just `batch` sequences; HEXGEN_ERR_SHAPE when
  * there is no row at all; HEXGEN_ERR_CAPACITY when a context and its rows exceed max_seq, or for more than a launch takes.  The attention and
  * hexgen_stage_extend can be recorded once a call of that size has run outside a graph (with weights, if it is to gather them); a recording is for its counts, window and sinks,

@@ -171,6 +171,24 @@ def test_attention_reads_what_is_left(dtype, rotate):
             assert torch.equal(small.read(layer, b, 0, keep)[1][:, 0], want)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_drafted_trees_over_what_is_left(dtype):
+    """The other attention over the cache takes the lengths and rows of an eviction as well: a tree of one node is a row."""
+    c = Case(dtype, 1, 8, 2, 64, [180, 64, 300], 330, seed=15)
+    c.kv.evict(70, sinks=3, recent=8, weights=c.w.cuda())
+    g = torch.Generator().manual_seed(2)
+    td = tr.TORCH[dtype]
+    q, k, v = [torch.randn(3, x, 64, generator=g).to(td) for x in (8, 2, 2)]
+    tree = hx.Tree(3, 3)
+    tree.set([1, 1, 1], [-1, -1, -1])
+    outs = [c.kv.tree_attention(0, tree, q.cuda(), k.cuda(), v.cuda()), c.kv.window_attention(0, q.cuda(), k.cuda(), v.cuda())]
+    for b, n in enumerate((70, 64, 70)):
+        ctx = [x.double().numpy() for x in c.kv.read(0, b, 0, n)]
+        o, a, s, _, _ = wr.attention(q[b:b + 1].double().numpy(), *ctx, k[b:b + 1].double().numpy(), v[b:b + 1].double().numpy(), None, 0)
+        for out in outs:
+            assert np.all(np.abs(out[b:b + 1].double().cpu().numpy() - o) <= tr.attention_bound(o, a, s, dtype, 64, n + 1))
+
+
 def test_more_layers_and_heads_than_a_grid_dimension():
     """66 layers x 63 sequences x 16 heads: 66528 units."""
     stage = hx.Stage(16 * 64, 16, 16, 256, 66, 1, 0, "bf16")

@@ -179,6 +179,28 @@ def test_extend_recorded_and_replayed(dtype, counts):
                 assert torch.equal(a, c)
 
 
+@pytest.mark.parametrize("dtype,counts", [("bf16", [3, 1]), ("f16", [40, 9]), ("f32", [2, 5])])
+def test_extend_on_another_stream(dtype, counts):
+    """Behind an event, and an eviction and another step behind it on the same stream."""
+    cfg, st, _ = _stage(dtype, 16, 2)
+    x = to_dev(generate.hidden_rows(cfg, sum(counts)), cfg)
+    found = []
+    for stream in (None, torch.cuda.Stream()):
+        kv = st.kv_cache_create(2, 90)
+        kv.set_lengths([20, 12])                             # contexts of zeros
+        weights = torch.zeros(2, 2, st.hkv_l, 90, device="cuda")
+        p, r, last = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())
+        st.extend(kv, x, p, r, counts=counts, window=16, sinks=2, weights=weights, stream=stream)
+        slots, left = kv.evict(11, sinks=1, recent=4, weights=weights, rotate=True, stream=stream)
+        st.extend(kv, x, last, counts=counts, window=16, sinks=2, weights=weights, stream=stream)
+        torch.cuda.synchronize()
+        assert left is weights and kv.get_lengths(2) == [min(n + c, 11) + c for n, c in zip([20, 12], counts)]
+        found.append((p, r, last, slots, weights))
+    assert all(torch.equal(a, b) for a, b in zip(*found))
+
+
 def test_extend_refusals():
     cfg, st, _ = _stage("bf16", None, 0)
     kv = st.kv_cache_create(2, 40)

@@ -393,6 +393,16 @@ def test_refusals():
     with pytest.raises(hx.HexgenError) as e:
         call(0, unaligned, k, v, [2, 1])
     assert e.value.status == 1
+    far = torch.zeros((1 << 24) + 8 + 256, dtype=torch.bfloat16, device="cuda")
+    for apart, ok in ((1 << 24, True), ((1 << 24) + 8, False)):  # of 2 rows, elements
+        rows = far.as_strided((2, 4, 64), (apart, 64, 1))
+        if ok:
+            rows.copy_(q[:2])
+            assert torch.equal(call(0, rows, k[:2], v[:2], [1, 1], window=8), call(0, q[:2], k[:2], v[:2], [1, 1], window=8))
+            continue
+        with pytest.raises(hx.HexgenError) as e:
+            call(0, rows, k[:2], v[:2], [1, 1])
+        assert e.value.status == 1
     assert c.kv.get_lengths(2) == [10, 20]
     fresh = c.stage.kv_cache_create(2, 24)
     with pytest.raises(hx.HexgenError) as e:
