@@ -498,7 +498,8 @@ __global__ __launch_bounds__(256, 2) void win_attn_kernel(const h16_t *__restric
             const bool was = far;
             far = far || __builtin_amdgcn_ballot_w64(fabsf(to * scale_log2e) >= kWinFarBase) != 0;
             const float from = was ? base : m, next = far ? to : to * scale_log2e;
-            const float alpha = __builtin_amdgcn_exp2f(far ? (from - to) * scale_log2e : m == NEG_INF ? NEG_INF : base - next);
+            // (nothing summed up yet: 0, whatever base a row without a score stands at)
+            const float alpha = __builtin_amdgcn_exp2f(m == NEG_INF ? NEG_INF : far ? (from - to) * scale_log2e : base - next);
             m = m_new;
             base = next;
             lsum *= alpha;
