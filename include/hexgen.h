@@ -265,7 +265,8 @@ hexgen_status_t hexgen_kv_cache_keep(hexgen_kv_cache_t *kv, hexgen_tree_t *tr, c
  * there is no row at all; HEXGEN_ERR_CAPACITY when a context and its rows exceed max_seq, or for more than a launch takes.  The attention and
  * hexgen_stage_extend can be recorded once a call of that size has run outside a graph (with weights, if it is to gather them); a recording is for its counts, window and sinks,
  * a replay reads the lengths that hold then, leaves out what would pass max_seq, and advances (extend) the lengths on the device.  Calls on one stage, replays among them, may not
- * overlap in time (they share its workspace).  A call with more rows or sequences than any before it replaces that workspace: what was recorded
+ * overlap in time (they share its workspace).  A recorded hexgen_kv_window_attention stays valid whatever calls follow it.  The calls through a stage's layers (prefill, decode,
+ * decode_tree, extend, run_sublayer) share one more workspace, which such a call with more rows or sequences than any of them before replaces: a hexgen_stage_extend that was recorded
  * earlier has to be recorded again.
  */
 hexgen_status_t hexgen_kv_window_attention(hexgen_kv_cache_t *kv, int layer, const int32_t *counts, int batch, const void *q, int64_t ldq,

@@ -104,8 +104,13 @@ struct hexgen_stage {
     int ws_batch_cap = 0;
     float *tree_part = nullptr;      // from the first call on trees or windowed rows on: partial results of contexts cut into runs (kTreePartFloats), kTreeUnits counters
     // from the first call on that gathers attention weights: a row's and head's statistics (WinPlan), and behind them the scores of few rows
-    float *win_stat = nullptr;
+    // From the first call that gathers attention weights on: a row's and head's statistics (WinPlan); 16 bits: the scores of few rows (kWinScoreFloats).  A
+    // recorded step holds these addresses for good, whatever is called between its replays: scores have all their room at once, and statistics that a call
+    // with more rows outgrows stay allocated (together less than what replaces them, which has twice their size or more).
+    float *win_stat = nullptr, *win_scores = nullptr;
     size_t win_stat_floats = 0;
+    float *win_stat_old[64] = {};
+    int win_stat_olds = 0;
     int64_t weight_bytes = 0;
     Profiler prof;
 };
@@ -459,7 +464,6 @@ struct WinSpan {
 constexpr int64_t kWinRowStride = 1 << 24;                   // elements between query rows: offsets among 32 of them have 32 bits
 static_assert(kWinPartFloats == kTreePartFloats && kWinUnits == kTreeUnits, "one scratch for both");
 constexpr size_t kWinStatFloats = 2;                         // statistics of a row and head
-size_t win_stat_floats(const hexgen_stage *st, int rows) { return (kWinStatFloats * rows * st->hq_l + 3) / 4 * 4; }       // the scores behind them are written 16 bytes at a time
 constexpr size_t kWinScoreFloats = (size_t)16 << 20;         // 64 MB of scores at most
 
 // the span in launches of kWinSeqs sequences; one whose sequences have no row is left out
@@ -542,7 +546,7 @@ WinPlan pick_win_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, WinCall
     wp.part_ml = st->tree_part + (size_t)wp.nsplit * wc.rows * st->hq_l * st->d;
     wp.arrived = reinterpret_cast<unsigned *>(st->tree_part + kTreePartFloats);
     wp.stat = stats ? st->win_stat : nullptr;
-    wp.scores = stats && score_tiles > 0 ? st->win_stat + win_stat_floats(st, wc.rows) : nullptr;
+    wp.scores = stats && score_tiles > 0 ? st->win_scores : nullptr;
     wp.score_tiles = score_tiles;
     if (wp.nsplit == 1) std::stable_sort(wc.order, wc.order + wc.batch, [&](int a, int b) { return reach[a] > reach[b]; });
     return wp;
@@ -1062,18 +1066,22 @@ hexgen_status_t check_span(const hexgen_kv_cache *kv, const int32_t *counts, int
     *out = WinSpan{counts, batch, (int)rows, max_n, window, sinks, weights};
     return HEXGEN_OK;
 }
-hexgen_status_t ensure_win_stat(hexgen_stage *st, const hexgen_kv_cache *kv, const WinSpan &sp, hipStream_t s) {
-    const size_t want = win_stat_floats(st, sp.rows) + (size_t)32 * win_score_tiles(st, kv, sp) * sp.rows * st->hq_l;
-    if (sp.weights == nullptr || want <= st->win_stat_floats) return HEXGEN_OK;
-    HX_TRY(refuse_capture(s));
-    float *p = nullptr;
-    HX_TRY(dmalloc(&p, want));
-    if (st->win_stat != nullptr) {
-        HX_HIP(hipDeviceSynchronize());
-        (void)hipFree(st->win_stat);
+hexgen_status_t ensure_win_stat(hexgen_stage *st, const WinSpan &sp, hipStream_t s) {
+    if (sp.weights == nullptr) return HEXGEN_OK;
+    const size_t want = kWinStatFloats * sp.rows * st->hq_l;
+    if (want > st->win_stat_floats) {
+        HX_TRY(refuse_capture(s));
+        const size_t size = std::max(want, 2 * st->win_stat_floats);
+        float *p = nullptr;
+        HX_TRY(dmalloc(&p, size));
+        if (st->win_stat != nullptr) st->win_stat_old[st->win_stat_olds++] = st->win_stat;      // doubled each time: never 64 of them
+        st->win_stat = p;
+        st->win_stat_floats = size;
     }
-    st->win_stat = p;
-    st->win_stat_floats = want;
+    if (is_h16(st->dtype) && st->win_scores == nullptr) {
+        HX_TRY(refuse_capture(s));
+        HX_TRY(dmalloc(&st->win_scores, kWinScoreFloats));
+    }
     return HEXGEN_OK;
 }
 
@@ -1209,6 +1217,8 @@ void hexgen_stage_destroy(hexgen_stage_t *st) {
     free_ws(st->ws);
     if (st->tree_part) (void)hipFree(st->tree_part);
     if (st->win_stat) (void)hipFree(st->win_stat);
+    if (st->win_scores) (void)hipFree(st->win_scores);
+    for (float *p : st->win_stat_old) (void)hipFree(p);
     st->prof.clear();
     delete st;
 }
@@ -1776,7 +1786,7 @@ hexgen_status_t hexgen_kv_window_attention(hexgen_kv_cache_t *kv, int layer, con
     HX_TRY(check_span(kv, counts, batch, window, sinks, weights, &sp));
     hipStream_t s = static_cast<hipStream_t>(stream);
     HX_TRY(ensure_tree_part(st, s));
-    HX_TRY(ensure_win_stat(st, kv, sp, s));
+    HX_TRY(ensure_win_stat(st, sp, s));
     attn_rows(st, kv, layer, sp, sp.weights, q, nullptr, ldq, TreeIn{k, v, ldk, ldv}, TreeOut{TREE_OUT_ROWS, sp.rows, st->qw, out}, s);
     HX_HIP(hipGetLastError());
     return HEXGEN_OK;
@@ -1799,7 +1809,7 @@ hexgen_status_t hexgen_stage_extend(hexgen_stage_t *st, hexgen_kv_cache_t *kv, c
     if (r.T > st->ws.cap_rows || r.batch > st->ws_batch_cap) HX_TRY(refuse_capture(s));
     HX_TRY(ensure_workspace(st, r.T, r.batch));
     HX_TRY(ensure_tree_part(st, s));
-    HX_TRY(ensure_win_stat(st, kv, sp, s));
+    HX_TRY(ensure_win_stat(st, sp, s));
     if (is_h16(st->dtype) && st->ws.tree_qkv == nullptr) {
         HX_TRY(refuse_capture(s));
         HX_TRY(dmalloc(&st->ws.tree_qkv, (size_t)st->ws.cap_rows * st->nqkv));
