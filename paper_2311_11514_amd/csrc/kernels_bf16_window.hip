@@ -405,12 +405,13 @@ __global__ __launch_bounds__(512, 2) void win_few_kernel(const h16_t *__restrict
 
 // ---- attention, many rows ---------------------------------------------------------------------------------------------
 // A block of four waves takes 128 query rows, 32 a wave; their tiles go from HBM to LDS directly, four buffers deep, and are shared.  The rows are in the cache
-// already.  S^T = K . Q^T, O^T = V^T . P^T on the 32 x 32 x 16 MFMA, P in registers, rounded to the element type once as in the prefill attention: with two parts, as few rows
-// have them, results are a quarter more exact (RMS against 64 bits 1.6e-3 instead of 2.1e-3, bf16) and a call of 4096 rows under a window of 1024 took 207 us instead of
-// 166, one of 8 x 512 rows that gathers weights 418 instead of 358.
+// already.  S^T = K . Q^T, O^T = V^T . P^T on the 32 x 32 x 16 MFMA, P in registers, in two parts as in blocks of few rows, so that a row is as exact whatever rows its
+// call has besides.  (Rounded once, as in the prefill attention, results are a third less exact, RMS against 64 bits 2.1e-3 instead of 1.6e-3 in bf16, and a call of 4096 rows
+// under a window of 1024 takes 166 us instead of 211, one of 8 x 512 rows that gathers weights 360 instead of 425.)
 // While the vector unit works on a tile's weights the matrix cores have the next tile's scores.  Bound by each wave's chain of LDS reads, products and softmax, 1.7 waves
-// a SIMD (240 registers): matrix cores 34 % busy, vector units 48 %; three waves spill (358 us).  d 128, 64 query and 8 kv heads: 4096 rows under a window of 1024 157 of a call's 166 us
-// (770 TFLOP/s over the pairs that are attended); 8 x 512 rows at 1000 .. 3500, 32 / 4 heads, 210 (820).
+// a SIMD (240 registers): matrix cores 42 % busy, vector units 47 %.  A wave's second product beside the packing of its other half, by order or by scheduling groups, is no faster.
+// d 128, 64 query and 8 kv heads, 4096 rows under a window of 1024: of launches on their own, as a profiler has them, 237 us, the smallest 217 (556 TFLOP/s over the pairs that are
+// attended; calls one behind another 211 with the append); 8 x 512 rows at 1000 .. 3500, 32 / 4 heads, 284 and 268 (647).
 template <int D>
 __global__ __launch_bounds__(256, 2) void win_attn_kernel(const h16_t *__restrict__ q, int64_t ldq, const h16_t *__restrict__ kc, const h16_t *__restrict__ vc, KvGeom kg,
                                                           int hq_l, int G, int nrb, WinCall wc, const int32_t *__restrict__ lens, WinPlan wp, TreeOut out,
@@ -538,18 +539,16 @@ __global__ __launch_bounds__(256, 2) void win_attn_kernel(const h16_t *__restric
                 return;
             }
         }
-        TreeP p[2];                                       // k-groups hl (quads 0, 2) and 2 + hl (quads 1, 3)
+        TreeP p[2], lo[2];
+        tree_pack(sc, p, lo);
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int x = 4 * g + 2 * (i & 1) + 8 * (i >> 1);
-                p[g].u[i] = pack_h16x2(sc[x], sc[x + 1]);
+            for (int db = 0; db < DB; ++db) {
+                const h16x8 v = st[2 * KT + 2 * db + sub][fl + 32 * g];
+                oacc[db] = hx_mfma32(v, lo[g].v, oacc[db]);
+                oacc[db] = hx_mfma32(v, p[g].v, oacc[db]);
             }
-#pragma unroll
-        for (int g = 0; g < 2; ++g)
-#pragma unroll
-            for (int db = 0; db < DB; ++db) oacc[db] = hx_mfma32(st[2 * KT + 2 * db + sub][fl + 32 * g], p[g].v, oacc[db]);
         sc = ahead;
     };
     int step = 0;

@@ -500,10 +500,10 @@ int win_score_tiles(const hexgen_stage *st, const hexgen_kv_cache *kv, const Win
 
 // Rows per block, and the runs that a row's tiles are cut into.
 // Blocks of 32 rows ("few") or, where that is expected to be faster, of 128 that share tiles.  A block of 32 has a CU and takes about 5 us and 0.45 a tile, one of 128
-// half a CU, 8 us and 0.85 a tile, so that few blocks of 128 with long walks leave most of the chip waiting.  (us; 16 bits, d 128, 8 heads a kv head, no window,
-// few / shared.  Eight kv heads: one sequence, 256 rows from the start 17.6 / 16.7, 512 rows 35.6 / 24.6, 128 rows at 2048 23.8 / 59.8; at 2000 four sequences of 32 rows
-// 25.0 / 56.9, sixteen of 8 35.0 / 54.5, thirty-two of 8 65.6 / 57.4.  One kv head: one sequence, 1024 rows from the start 16.6 / 33.5, 2048 rows 29.7 / 57.1; four of 256
-// rows at 1000 18.8 / 40.5, sixteen of 32 at 4000 33.4 / 102.8)
+// half a CU, 8 us and 0.95 a tile, so that few blocks of 128 with long walks leave most of the chip waiting.  (us; bf16, d 128, 8 heads a kv head, no window,
+// few / shared.  Eight kv heads: one sequence, 256 rows from the start 18.9 / 18.8, 512 rows 36.3 / 27.2, 128 rows at 2048 25.6 / 69.8; at 2000 four sequences of 32 rows
+// 27.2 / 67.1, sixteen of 8 30.7 / 63.1, thirty-two of 8 58.0 / 66.2.  One kv head: one sequence, 1024 rows from the start 17.9 / 38.3, 2048 rows 32.7 / 67.8; four of 256
+// rows at 1000 20.3 / 47.6, sixteen of 32 at 4000 36.8 / 121.6)
 // Runs: one kv head, one row each, 8 heads, d 128: of 16 tiles where there are more than 24 (a window of 1024: one sequence 13.4 us whole, 10.7 in three runs, 10.4
 // in five; sixteen of 2048 without one: a step of two layers in runs of 8 1.3 us more than in runs of 16), whole rounds of the eight waves; otherwise as for trees
 // (pick_tree_plan).  two_parts: the query rows come in two parts, which only blocks of 32 take.
@@ -528,10 +528,10 @@ WinPlan pick_win_plan(const hexgen_stage *st, const hexgen_kv_cache *kv, WinCall
         blocks += rb;
         tiles += rb * last.nt;
         few += rb * (5 + 0.45 * walk) / 256;
-        shared += (double)win_row_blocks(n, G, 128) * st->hkv_l * (8 + 0.85 * walk) / 512;
+        shared += (double)win_row_blocks(n, G, 128) * st->hkv_l * (8 + 0.95 * walk) / 512;
     }
     WinPlan wp;
-    wp.shared = h16 && !two_parts && (long)wc.max_n * G > 32 && std::max(shared, 8 + 0.85 * longest) < std::max(few, 5 + 0.45 * longest);
+    wp.shared = h16 && !two_parts && (long)wc.max_n * G > 32 && std::max(shared, 8 + 0.95 * longest) < std::max(few, 5 + 0.45 * longest);
     wp.chunk = longest;
     wp.nsplit = 1;
     const bool few_units = (long)wc.batch * st->hkv_l * win_row_blocks(wc.max_n, G, rows) <= kTreeUnits;
