@@ -248,8 +248,8 @@ hexgen_status_t hexgen_kv_cache_keep(hexgen_kv_cache_t *kv, hexgen_tree_t *tr, c
  *     (q's at most 2^24 elements: HEXGEN_ERR_INVALID_ARG beyond) as for hexgen_kv_tree_attention, q and k rotated at the rows' positions (slots;
  *     or, behind evictions, whatever positions the caller's keys carry).  k and v join `layer`'s cache at the rows' slots, uncommitted:
  *     hexgen_kv_cache_commit once all layers have processed the rows.  What a row does not attend has no influence on it, infinities and NaN
- *     included.  16-bit types: softmax weights enter the sums in two parts (bf16: 16 bits of them), whatever rows a call has; an attended infinite value
- *     whose weight rounds to zero gives NaN.
+ *     included.  16-bit types: softmax weights enter the sums in two parts (bf16: 16 bits of each; fp16: 21, or to 2^-37 of the row's largest one),
+ *     whatever rows a call has; an attended infinite value whose weight rounds to zero gives NaN.
  *   hexgen_stage_extend: the rows through every layer of the stage, rotated at their slots; buffers as for hexgen_stage_prefill.  The committed
  *     lengths grow by counts; the decode steps' count does not change.  Up to 32 rows are computed as decode steps are, more as a prefill is.
  *   hexgen_kv_cache_evict: of every sequence's len_i slots min(len_i, keep) stay, in their order: the first `sinks`, the last `recent`, and of the others those

@@ -40,7 +40,14 @@ __device__ __forceinline__ bool any_odd(h16x8 v) {
     return odd;
 }
 
-// The running softmax over one tile's scores (sc becomes the weights): m, l and the factor for what was summed up before
+// fp16 has no numbers below 2^-24, which both parts of a weight would be cut off at, so that many positions of 2^-20 beside a heavy one lost a tenth and more of their sum.
+// Its weights are carried times 2^14, sums and results with them: a weight is exact to 2^-38 of the row's largest one.  bf16 has fp32's exponents.
+#ifdef HX_ELEM_F16
+constexpr float kWeightShift = 14.f, kWeightUnit = 16384.f;
+#else
+constexpr float kWeightShift = 0.f, kWeightUnit = 1.f;
+#endif
+// The running softmax over one tile's scores (sc becomes the weights, times kWeightUnit): m, l and the factor for what was summed up before
 __device__ __forceinline__ float tree_softmax(floatx16 &sc, float &m, float &lsum, float scale_log2e) {
     float mx = NEG_INF;
 #pragma unroll
@@ -53,7 +60,7 @@ __device__ __forceinline__ float tree_softmax(floatx16 &sc, float &m, float &lsu
 #pragma unroll
     for (int x = 0; x < 16; ++x) {
         // (the difference first: scores near the type's lowest value would not cancel in a multiply-add with -base * scale)
-        sc[x] = __builtin_amdgcn_exp2f((sc[x] - base) * scale_log2e);
+        sc[x] = __builtin_amdgcn_exp2f(fmaf(sc[x] - base, scale_log2e, kWeightShift));
         ps += sc[x];
     }
     lsum = lsum * alpha + ps;

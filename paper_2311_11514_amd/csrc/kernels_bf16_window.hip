@@ -335,7 +335,7 @@ __global__ __launch_bounds__(512, 2) void win_few_kernel(const h16_t *__restrict
     auto finish = [&](int t, int hd, const float (&o)[4], float M, float L) {
         const float inv = 1.0f / L, x[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
         tree_store4(out, t, hd * D + dd, x);
-        if (wp.stat != nullptr && dd == 0) *reinterpret_cast<float2 *>(wp.stat + 2 * ((size_t)t * hq_l + hd)) = win_stat(M, inv, true);
+        if (wp.stat != nullptr && dd == 0) *reinterpret_cast<float2 *>(wp.stat + 2 * ((size_t)t * hq_l + hd)) = win_stat(M, inv * kWeightUnit, true);
     };
 #pragma unroll
     for (int i = 0; i < QUADS; ++i) {
@@ -440,7 +440,9 @@ __global__ __launch_bounds__(256, 2) void win_attn_kernel(const h16_t *__restric
         for (int x = 0; x < 16; ++x) oacc[db][x] = 0.f;
     float m = NEG_INF, base = 0.f, lsum = 0.f;            // the score that the base was taken from, and the base (win_stat)
     bool far = false;                                     // of some row of the wave: the base is that score itself
-    const float slack = 8.0f / scale_log2e;
+    // Weights are carried times 2^SHIFT (kWeightShift), up to 2^SLACK of that above the base: fp16's largest number is just below 2^16
+    constexpr float SHIFT = kWeightShift > 0.f ? kWeightShift - 1.f : 0.f, UNIT = kWeightShift > 0.f ? 0.5f * kWeightUnit : 1.f, SLACK = kWeightShift > 0.f ? 2.f : 8.f;
+    const float slack = SLACK / scale_log2e;
 
     const size_t slab = (size_t)wk.seq * kg.seq_stride + (size_t)wk.c * kg.smax * D;
     const h16x8 *ks = reinterpret_cast<const h16x8 *>(kc + slab), *vs = reinterpret_cast<const h16x8 *>(vc + slab);
@@ -492,13 +494,13 @@ __global__ __launch_bounds__(256, 2) void win_attn_kernel(const h16_t *__restric
 #pragma unroll
         for (int x = 0; x < 16; ++x) mx = fmaxf(mx, sc[x]);
         mx = max_halves(mx);
-        // A larger score moves the base only if its weight would pass 2^8: what has been summed up is rescaled for the first tiles of a row and hardly again.
+        // A larger score moves the base only if its weight would pass 2^SLACK: what has been summed up is rescaled for the first tiles of a row and hardly again.
         // (Any base is right: numerator and sum are relative to the same one, in floating point.)
         if (__builtin_amdgcn_ballot_w64(mx > m + slack) != 0) {
             const float m_new = fmaxf(m, mx), to = m_new == NEG_INF ? 0.f : m_new;       // a row that has seen nothing yet: weights 0, no NaN
             const bool was = far;
             far = far || __builtin_amdgcn_ballot_w64(fabsf(to * scale_log2e) >= kWinFarBase) != 0;
-            const float from = was ? base : m, next = far ? to : to * scale_log2e;
+            const float from = was ? base : m, next = far ? to : to * scale_log2e - SHIFT;
             // (nothing summed up yet: 0, whatever base a row without a score stands at)
             const float alpha = __builtin_amdgcn_exp2f(m == NEG_INF ? NEG_INF : far ? (from - to) * scale_log2e : base - next);
             m = m_new;
@@ -515,7 +517,7 @@ __global__ __launch_bounds__(256, 2) void win_attn_kernel(const h16_t *__restric
         if (far) {
             scores(min(step + 1, steps - 1), ahead);
 #pragma unroll
-            for (int x = 0; x < 16; ++x) { sc[x] = __builtin_amdgcn_exp2f((sc[x] - base) * scale_log2e); ps += sc[x]; }
+            for (int x = 0; x < 16; ++x) { sc[x] = __builtin_amdgcn_exp2f(fmaf(sc[x] - base, scale_log2e, SHIFT)); ps += sc[x]; }
         } else {
             scores(min(step + 1, steps - 1), ahead);
 #pragma unroll
@@ -564,7 +566,7 @@ __global__ __launch_bounds__(256, 2) void win_attn_kernel(const h16_t *__restric
             const float x[4] = {oacc[db][4 * qd] * inv, oacc[db][4 * qd + 1] * inv, oacc[db][4 * qd + 2] * inv, oacc[db][4 * qd + 3] * inv};
             tree_store4(out, row0 + node, head * D + 32 * db + 8 * qd + 4 * hl, x);
         }
-    if (wp.stat != nullptr && hl == 0) *reinterpret_cast<float2 *>(wp.stat + 2 * ((size_t)(row0 + node) * hq_l + head)) = win_stat(base, inv, far);
+    if (wp.stat != nullptr && hl == 0) *reinterpret_cast<float2 *>(wp.stat + 2 * ((size_t)(row0 + node) * hq_l + head)) = win_stat(base, far ? inv * UNIT : inv, far);
 }
 
 void launch_win_attn(const h16_t *q, const h16_t *q_lo, int64_t ldq, const TreeIn &in, h16_t *kc, h16_t *vc, KvGeom kg, int hq_l, const WinCall &wc,
