@@ -260,7 +260,8 @@ hexgen_status_t hexgen_kv_cache_keep(hexgen_kv_cache_t *kv, hexgen_tree_t *tr, c
  *     Device outputs, rows of dst's max_seq: slots int32 [n_layers][batch][hkv_local][dst max_seq], the slots that stayed, filled up with -1; weights_out fp32 of the same
  *     shape (NULL when weights is), their weights, filled up with 0 (in place: may be weights itself).  dst's committed lengths become min(len_i, keep); a dst that is not kv starts
  *     its decode steps at 0.  HEXGEN_ERR_INVALID_ARG when sinks + recent > keep; HEXGEN_ERR_CAPACITY unless dst takes the batch and min(keep, max_seq) slots;
- *     HEXGEN_ERR_DEVICE when it would be recorded.  Rows that are not committed are dropped.
+ *     HEXGEN_ERR_DEVICE when it would be recorded.  Rows that are not committed are dropped.  len_i are the lengths on the device; where steps of kv have been recorded, whose
+ *     replays take these further than the host counts, the call waits for `stream` and the lengths that the host knows become them.
  * All three enqueue on `stream`; HEXGEN_ERR_STATE unless the cache holds a batch (prefill, set_lengths, commit), of just `batch` sequences; HEXGEN_ERR_SHAPE when
  * there is no row at all; HEXGEN_ERR_CAPACITY when a context and its rows exceed max_seq, or for more than a launch takes.  The attention and
  * hexgen_stage_extend can be recorded once a call of that size has run outside a graph (with weights, if it is to gather them); a recording is for its counts, window and sinks,

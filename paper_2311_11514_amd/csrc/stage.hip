@@ -127,6 +127,7 @@ struct hexgen_kv_cache {
     int batch = 0;
     bool prefilled = false;
     int steps = 0;
+    bool recorded = false;                 // a step that advances the lengths has been recorded: on the device they may be others than the host counted
 };
 
 struct hexgen_tree {
@@ -271,6 +272,14 @@ hexgen_status_t refuse_capture(hipStream_t s) {
     hipStreamCaptureStatus c = hipStreamCaptureStatusNone;
     HX_HIP(hipStreamIsCapturing(s, &c));
     return c == hipStreamCaptureStatusNone ? HEXGEN_OK : HEXGEN_ERR_DEVICE;
+}
+
+// Behind a step that advances a cache's lengths: has it been recorded rather than run?
+void note_capture(hexgen_kv_cache *kv, hipStream_t s) {
+    if (kv->recorded) return;
+    hipStreamCaptureStatus c = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(s, &c) == hipSuccess) kv->recorded = c != hipStreamCaptureStatusNone;
+    else (void)hipGetLastError();
 }
 
 // Validate the new rows against the cache and build the device row maps.  A prefill (allow_decode false) starts a new batch:
@@ -1545,6 +1554,7 @@ hexgen_status_t hexgen_stage_decode(hexgen_stage_t *st, hexgen_kv_cache_t *kv, i
     if (r.decode && is_h16(st->dtype)) st->last_decode_rows = r.T;
     if (!r.dev_rows) launch_advance_lens(kv->d_lens, kv->batch, s);   // else: the prologue (fp32: the last projection) did
     st->prof.mark(PROF_CALL, s);
+    note_capture(kv, s);
     for (int i = 0; i < kv->batch; ++i) kv->lens[i] += 1;
     kv->steps += 1;
     return HEXGEN_OK;
@@ -1586,6 +1596,7 @@ hexgen_status_t hexgen_stage_decode_static(hexgen_stage_t *st, hexgen_kv_cache_t
     st->prof.mask = saved_mask;
     HX_TRY(rc);
     HX_HIP(hipGetLastError());
+    note_capture(kv, s);
     for (int i = 0; i < batch; ++i) kv->lens[i] += 1;
     kv->steps += 1;
     return HEXGEN_OK;
@@ -1821,6 +1832,7 @@ hexgen_status_t hexgen_stage_extend(hexgen_stage_t *st, hexgen_kv_cache_t *kv, c
     for_each_call(kv, sp, [&](WinCall &wc) { launch_win_advance(kv->d_lens, wc, s); });
     st->prof.mark(PROF_CALL, s);
     HX_HIP(hipGetLastError());
+    note_capture(kv, s);
     for (int i = 0; i < batch; ++i) kv->lens[i] += sp.count(i);
     return HEXGEN_OK;
 }
@@ -1844,6 +1856,10 @@ hexgen_status_t hexgen_kv_cache_evict(hexgen_kv_cache_t *kv, hexgen_kv_cache_t *
                        rotate ? kv->cos_tab : nullptr, rotate ? kv->sin_tab : nullptr, kv->d_lens, dst->d_lens, dst->max_batch};
     const uint64_t units = (uint64_t)ec.layers * ec.batch * ec.hkv;
     if (units * 1024 > UINT32_MAX || units * (dst == kv ? 1024 : 256 * (uint64_t)evict_blocks(ec, mv)) > UINT32_MAX) return HEXGEN_ERR_CAPACITY;
+    if (kv->recorded) {                    // replays go on where the device's lengths stand: the host's become those again
+        HX_HIP(hipMemcpyAsync(kv->lens.data(), kv->d_lens, sizeof(int32_t) * kv->batch, hipMemcpyDeviceToHost, s));
+        HX_HIP(hipStreamSynchronize(s));
+    }
     launch_evict_select(ec, *std::max_element(kv->lens.begin(), kv->lens.begin() + kv->batch), kv->d_lens, s);
     if (is_h16(st->dtype)) HX_K(st->dtype, launch_evict_move, ec, mv, s);
     else f32_launch_evict_move(ec, mv, s);
