@@ -245,7 +245,7 @@ class Stage:
 
     def load_layer(self, layer: int, g_attn, wq, wk, wv, wo, g_ffn, w1, w3, w2):
         """Global [in, out] tensors (host or device); converted to the stage's dtype if needed."""
-        td = _torch_dtype(self.dtype)
+        layer, td = _int32(layer, "layer"), _torch_dtype(self.dtype)
         ts = [t.to(td).contiguous() for t in (g_attn, wq, wk, wv, wo, g_ffn, w1, w3, w2)]
         _check(lib.hexgen_stage_load_layer(self.handle, layer, *[t.data_ptr() for t in ts]),
                "hexgen_stage_load_layer")
@@ -299,11 +299,12 @@ class Stage:
 
     def run_sublayer(self, kv: "KVCache", layer: int, which: int, h_in: torch.Tensor,
                      seq_lens: Optional[Sequence[int]], batch: int, partial_out: torch.Tensor, stream=None):
-        _check(lib.hexgen_stage_run_sublayer(self.handle, kv.handle, layer, which, _ptr(h_in), _i32(seq_lens),
+        _check(lib.hexgen_stage_run_sublayer(self.handle, kv.handle, _int32(layer, "layer"), which, _ptr(h_in), _i32(seq_lens),
                                              batch, _ptr(partial_out), _stream_handle(stream)),
                "hexgen_stage_run_sublayer")
 
     def set_tap(self, layer: int, h_dump: Optional[torch.Tensor]):
+        layer = _int32(layer, "layer")
         self._taps[layer] = h_dump          # keep the buffer alive
         _check(lib.hexgen_stage_set_tap(self.handle, layer, _ptr(h_dump)), "hexgen_stage_set_tap")
 
@@ -363,13 +364,14 @@ class KVCache:
 
     def fill(self, layer: int, seq: int, k: torch.Tensor, v: torch.Tensor):
         """k, v: [n, hkv_local, head_dim], host or device, taken as fp32."""
+        layer, seq = _int32(layer, "layer"), _int32(seq, "seq")
         k = k.to(torch.float32).contiguous()
         v = v.to(torch.float32).contiguous()
         _check(lib.hexgen_kv_cache_fill(self.handle, layer, seq, k.shape[0],
                                         C.cast(k.data_ptr(), _fp), C.cast(v.data_ptr(), _fp)), "hexgen_kv_cache_fill")
 
     def read(self, layer: int, seq: int, pos0: int, n: int):
-        st = self.stage
+        st, layer, seq, pos0 = self.stage, _int32(layer, "layer"), _int32(seq, "seq"), _int32(pos0, "pos0")
         k = torch.empty(n, st.hkv_l, st.head_dim, dtype=torch.float32)
         v = torch.empty_like(k)
         _check(lib.hexgen_kv_cache_read(self.handle, layer, seq, pos0, n, C.cast(k.data_ptr(), _fp),
@@ -381,7 +383,7 @@ class KVCache:
                        out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """hexgen_kv_tree_attention: q [rows, hq_local, head_dim], k, v [rows, hkv_local, head_dim] of the trees' nodes, rotated; rows may
         be apart (parts of a fused projection).  Returns [rows, hq_local, head_dim]."""
-        st, rows, here = self.stage, tree.rows, _here(q)
+        st, rows, here, layer = self.stage, tree.rows, _here(q), _int32(layer, "layer")
         td, hq, hkv, d = _TORCH_DTYPE[st.dtype], st.hq_l, st.hkv_l, st.head_dim
         ldq = _rows_of_heads(q, "q", rows, hq, d, td, here)
         ldk = _rows_of_heads(k, "k", rows, hkv, d, td, here)
@@ -407,7 +409,7 @@ class KVCache:
         """hexgen_kv_window_attention: counts[i] new rows of every sequence (None: one each), q [rows, hq_local, head_dim], k, v [rows, hkv_local,
         head_dim], rotated; rows may be apart (parts of a fused projection).  A row attends the last `window` slots (None: all), its own among them, and the first
         `sinks`.  weights float32 [batch, hkv_local, max_seq]: the attention weights' sums are added to it.  Returns [rows, hq_local, head_dim]."""
-        st, here = self.stage, _here(q)
+        st, here, layer = self.stage, _here(q), _int32(layer, "layer")
         c, batch, rows, window = _span(counts, q.shape[0], window)
         td, hq, hkv, d = _TORCH_DTYPE[st.dtype], st.hq_l, st.hkv_l, st.head_dim
         ldq = _rows_of_heads(q, "q", rows, hq, d, td, here)
