@@ -246,12 +246,12 @@ struct WinPlan {
 // blocks are worth launching, no more: the lengths on the device may be others.
 struct WinReach { int most; int64_t groups; };
 inline int win_row_blocks(int max_n, int G, int rows) { return (int)(((int64_t)max_n * G + rows - 1) / rows); }
-// Caller-owned accumulators of attention weights, [sequence of the cache's batch][kv head][max_seq]
 void f32_launch_win_rope_append(const float *qkv, int hq_l, KvGeom kg, const WinCall &wc, const int32_t *lens, const float *cos_tab, const float *sin_tab,
                                 float *q, float *kc, float *vc, hipStream_t s);
 void f32_launch_win_append(const TreeIn &in, float *kc, float *vc, KvGeom kg, const WinCall &wc, const int32_t *lens, hipStream_t s);
 void f32_launch_win_attn(const float *q, int64_t ldq, const TreeIn &in, float *kc, float *vc, KvGeom kg, int hq_l, const WinCall &wc, const int32_t *lens,
                          const WinPlan &wp, float *o, hipStream_t s);
+// weights: caller-owned accumulators, [sequence of the cache's batch][kv head][max_seq]
 void f32_launch_win_weights(const float *q, int64_t ldq, const float *kc, KvGeom kg, int hq_l, const WinCall &wc, const int32_t *lens, const float *stat,
                             float *weights, const WinReach &reach, hipStream_t s);
 void launch_win_advance(int32_t *lens, const WinCall &wc, hipStream_t s);          // lens += the call's rows, up to max_seq
