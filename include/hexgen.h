@@ -155,7 +155,8 @@ int64_t hexgen_stage_decode_static_bytes(const hexgen_stage_t *st, int batch);
  *               positions len_i .. len_i + n_i - 1 where len_i is the committed length.
  *   partial_out device fp32 [n_rows, hidden]: this rank's partial (no residual)
  * The attention sub-layer writes K, V of the new rows into `layer`'s cache but does not change
- * the committed lengths; call hexgen_kv_cache_commit once all layers have processed the rows.
+ * the committed lengths; call hexgen_kv_cache_commit once all layers have processed the rows (behind replays of recorded steps it adds to the lengths that
+ * these have left on the device).
  */
 hexgen_status_t hexgen_stage_run_sublayer(hexgen_stage_t *st, hexgen_kv_cache_t *kv, int layer,
                                           int which, const void *h_in, const int32_t *seq_lens,
@@ -266,7 +267,8 @@ hexgen_status_t hexgen_kv_cache_keep(hexgen_kv_cache_t *kv, hexgen_tree_t *tr, c
  * there is no row at all; HEXGEN_ERR_CAPACITY when a context and its rows exceed max_seq, or for more than a launch takes.  The attention and
  * hexgen_stage_extend can be recorded once a call of that size has run outside a graph (with weights, if it is to gather them); a recording is for its counts, window and sinks,
  * a replay reads the lengths that hold then, leaves out what would pass max_seq, and advances (extend) the lengths on the device.  Calls on one stage, replays among them, may not
- * overlap in time (they share its workspace).  A recorded hexgen_kv_window_attention stays valid whatever calls follow it.  The calls through a stage's layers (prefill, decode,
+ * overlap in time (they share its workspace).  The host does not count replays (hexgen_kv_cache_commit and _evict read the lengths back): an eager call behind them is held to the
+ * lengths that the host knows, and leaves out what would pass max_seq on the device.  A recorded hexgen_kv_window_attention stays valid whatever calls follow it.  The calls through a stage's layers (prefill, decode,
  * decode_tree, extend, run_sublayer) share one more workspace, which such a call with more rows or sequences than any of them before replaces: a hexgen_stage_extend that was recorded
  * earlier has to be recorded again.
  */

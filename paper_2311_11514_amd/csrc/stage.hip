@@ -282,6 +282,14 @@ void note_capture(hexgen_kv_cache *kv, hipStream_t s) {
     else (void)hipGetLastError();
 }
 
+// Replays go on where the device's lengths stand: behind what is on `s`, the host's become those again.
+hexgen_status_t read_lens(hexgen_kv_cache *kv, hipStream_t s) {
+    if (!kv->recorded || kv->batch == 0) return HEXGEN_OK;
+    HX_HIP(hipMemcpyAsync(kv->lens.data(), kv->d_lens, sizeof(int32_t) * kv->batch, hipMemcpyDeviceToHost, s));
+    HX_HIP(hipStreamSynchronize(s));
+    return HEXGEN_OK;
+}
+
 // Validate the new rows against the cache and build the device row maps.  A prefill (allow_decode false) starts a new batch:
 // whatever still uses the cache, the workspace or the caller's buffers may sit on any stream, also on one that this stage has
 // never seen (a recorded step that is being replayed, the producer of hidden_in), so it waits for the device, as the cache's
@@ -1427,12 +1435,12 @@ int hexgen_kv_cache_batch(const hexgen_kv_cache_t *kv) { return !kv ? -1 : kv->p
 hexgen_status_t hexgen_kv_cache_commit(hexgen_kv_cache_t *kv, const int32_t *seq_lens, int batch) {
     if (!kv || batch <= 0) return HEXGEN_ERR_INVALID_ARG;
     if (batch > kv->max_batch) return HEXGEN_ERR_CAPACITY;
-    for (int i = 0; i < batch; ++i) {
-        const int n = seq_lens ? seq_lens[i] : 1;
-        if (n < 0) return HEXGEN_ERR_INVALID_ARG;
-        if ((long)kv->lens[i] + n > kv->max_seq) return HEXGEN_ERR_CAPACITY;
-    }
+    for (int i = 0; i < batch; ++i)
+        if (seq_lens && seq_lens[i] < 0) return HEXGEN_ERR_INVALID_ARG;
     HX_HIP(hipDeviceSynchronize());
+    HX_TRY(read_lens(kv, nullptr));
+    for (int i = 0; i < batch; ++i)
+        if ((long)kv->lens[i] + (seq_lens ? seq_lens[i] : 1) > kv->max_seq) return HEXGEN_ERR_CAPACITY;
     for (int i = 0; i < batch; ++i) kv->lens[i] += seq_lens ? seq_lens[i] : 1;
     kv->batch = std::max(kv->batch, batch);
     kv->prefilled = true;
@@ -1856,10 +1864,7 @@ hexgen_status_t hexgen_kv_cache_evict(hexgen_kv_cache_t *kv, hexgen_kv_cache_t *
                        rotate ? kv->cos_tab : nullptr, rotate ? kv->sin_tab : nullptr, kv->d_lens, dst->d_lens, dst->max_batch};
     const uint64_t units = (uint64_t)ec.layers * ec.batch * ec.hkv;
     if (units * 1024 > UINT32_MAX || units * (dst == kv ? 1024 : 256 * (uint64_t)evict_blocks(ec, mv)) > UINT32_MAX) return HEXGEN_ERR_CAPACITY;
-    if (kv->recorded) {                    // replays go on where the device's lengths stand: the host's become those again
-        HX_HIP(hipMemcpyAsync(kv->lens.data(), kv->d_lens, sizeof(int32_t) * kv->batch, hipMemcpyDeviceToHost, s));
-        HX_HIP(hipStreamSynchronize(s));
-    }
+    HX_TRY(read_lens(kv, s));
     launch_evict_select(ec, *std::max_element(kv->lens.begin(), kv->lens.begin() + kv->batch), kv->d_lens, s);
     if (is_h16(st->dtype)) HX_K(st->dtype, launch_evict_move, ec, mv, s);
     else f32_launch_evict_move(ec, mv, s);
